@@ -310,6 +310,78 @@ int tv2d_prox_bwd_bf16(const uint16_t *g_up, uint16_t *grad_y, float *grad_lam, 
                        int64_t H, int64_t W, tv_lambda lam, int sweeps, void *ws, size_t ws_bytes,
                        hipStream_t stream);
 
+/*
+ * Channel products: what a network does between its TV passes, with the activations that its backward pass
+ * needs held in 8 bits where the caller asks for it.
+ *
+ *   z = x W^T + b,  y = act(z) + r        x [m, k], W [n, k], b [n] or NULL, r [m, n] or NULL, y [m, n]
+ *   dz = g act'(z), dx = dz W, dW = dz^T x, db[j] = sum_i dz[i, j]      (dr = g: nothing to compute)
+ *
+ * Arrays are dense rows with the last index contiguous; ld* are row strides in ELEMENTS (at least the row's
+ * length, below 2^31), any alignment that suits the type.  W's rows are ldw apart, b is packed.  One dtype for
+ * all of x, W, b, r, y, g and the gradients; sums and activations are fp32, each output is rounded once.  In
+ * bf16, dz is rounded to bf16 before the products that give dx and dW (db sums it unrounded).
+ * Activations: gelu is z Phi(z) (with erf), silu z / (1 + exp(-z)); ReLU is 0 where z <= 0, with slope 0 there.
+ *
+ * m = 0: the forward call does nothing, the backward call sets dw and db to zero.  Results do not depend on the
+ * stream, on timing or on what the workspace holds; how the contraction is split (and so the last bits of the
+ * fp32 sums) depends on the sizes alone.
+ */
+typedef enum { TV_F32 = 0, TV_BF16 = 1 } tv_dtype;
+typedef enum { TV_ACT_NONE = 0, TV_ACT_RELU = 1, TV_ACT_GELU = 2, TV_ACT_SILU = 3 } tv_act;
+
+typedef struct {
+    int64_t m, k, n;
+    int64_t ldx, ldw, ldr, ldy;    /* ldr: read where r is given; ldy: of y in the forward call, of g in the backward */
+    int32_t dtype, act;            /* tv_dtype, tv_act */
+} tv_linear_desc;
+
+/*
+ * What the forward call writes of z for the backward call, device memory of the caller:
+ *   TV_HELD_NONE   nothing (inference; the backward call of TV_ACT_NONE)
+ *   TV_HELD_PLAIN  data [m, n] packed, of the call's dtype                       (gelu, silu)
+ *   TV_HELD_BITS   data int32 [m, ceil(n / 32)], bit j % 32 of word j / 32 set where not z <= 0     (ReLU)
+ *   TV_HELD_8BIT   data int8 [m, n] packed and exps [m, ceil(n / 32)]: an 8-bit checkpoint of fp32 z (gelu, silu)
+ * Any other pairing is TV_ERR_UNSUPPORTED; data not aligned to its type TV_ERR_STRIDE.
+ */
+typedef enum { TV_HELD_NONE = 0, TV_HELD_PLAIN = 1, TV_HELD_BITS = 2, TV_HELD_8BIT = 3 } tv_held_kind;
+typedef struct {
+    void *data;
+    uint8_t *exps;
+    int32_t kind;                  /* tv_held_kind */
+} tv_held;
+
+/*
+ * y may be r exactly (same pointer and stride); no other output may overlap an input.  ws: device scratch of at
+ * least tv_linear_fwd_workspace_bytes() bytes, 16-byte aligned (may be NULL where that is 0), contents undefined
+ * afterwards.
+ */
+size_t tv_linear_fwd_workspace_bytes(tv_linear_desc desc);
+int tv_linear_fwd(const void *x, const void *w, const void *bias, const void *res, void *y, tv_held held,
+                  tv_linear_desc desc, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * x: the forward call's input, or (x_exps given) the codes of its 8-bit checkpoint, packed [m, k]; held: as the
+ * forward call wrote it; g: rows of desc.ldy elements.  dx [m, k], dw [n, k] and db [n] are packed; each may be
+ * NULL where it is not wanted (w is not read without dx, x not without dw).
+ */
+size_t tv_linear_bwd_workspace_bytes(tv_linear_desc desc, int x_is_8bit);
+int tv_linear_bwd(const void *g, const void *x, const uint8_t *x_exps, tv_held held, const void *w, void *dx,
+                  void *dw, void *db, tv_linear_desc desc, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * 8-bit checkpoints of a [rows, n] tensor (rows of ldx elements): codes int8 [rows, n] packed, exps
+ * [rows, ceil(n / 32)].  A block of 32 consecutive samples of a row (the last may be shorter) has the step
+ * s = 2^(floor(log2 M) - 6), M its largest finite magnitude (2^-120 at least), kept as the byte log2(s) + 127;
+ * a sample's code is x / s rounded to nearest even and clamped to -127 .. 127, -128 for one that is not finite.
+ * It stands for code * s (exact in fp32 and in bf16), -128 for a NaN: off by at most s / 2, or s where the clamp
+ * acts, and s <= M / 64 (M at least 2^-120).
+ */
+int tv_ckpt8_save(const void *x, int8_t *codes, uint8_t *exps, int64_t rows, int64_t n, int64_t ldx, int dtype,
+                  hipStream_t stream);
+int tv_ckpt8_load(const int8_t *codes, const uint8_t *exps, void *x, int64_t rows, int64_t n, int64_t ldx, int dtype,
+                  hipStream_t stream);
+
 const char *tv_status_str(int status);
 
 /*

@@ -23,6 +23,20 @@ class tv_fwd_extra(ctypes.Structure):
                 ("flags", ctypes.c_uint32)]
 
 
+class tv_linear_desc(ctypes.Structure):
+    _fields_ = [("m", _i64), ("k", _i64), ("n", _i64), ("ldx", _i64), ("ldw", _i64), ("ldr", _i64), ("ldy", _i64),
+                ("dtype", ctypes.c_int32), ("act", ctypes.c_int32)]
+
+
+class tv_held(ctypes.Structure):
+    _fields_ = [("data", _vp), ("exps", _vp), ("kind", ctypes.c_int32)]
+
+
+TV_F32, TV_BF16 = 0, 1
+TV_ACT_NONE, TV_ACT_RELU, TV_ACT_GELU, TV_ACT_SILU = 0, 1, 2, 3
+TV_HELD_NONE, TV_HELD_PLAIN, TV_HELD_BITS, TV_HELD_8BIT = 0, 1, 2, 3
+TV_CKPT8_BLOCK = 32
+
 TV_FWD_ORDER_READY = 1
 TV_FWD_PARALLEL_SEARCH = 2
 
@@ -110,6 +124,18 @@ def lib() -> ctypes.CDLL:
         L.tv2d_prox_fwd_bf16.restype = ctypes.c_int
         L.tv2d_prox_bwd_bf16.argtypes = L.tv2d_prox_bwd.argtypes
         L.tv2d_prox_bwd_bf16.restype = ctypes.c_int
+        L.tv_linear_fwd_workspace_bytes.argtypes = [tv_linear_desc]
+        L.tv_linear_fwd_workspace_bytes.restype = ctypes.c_size_t
+        L.tv_linear_fwd.argtypes = [_vp, _vp, _vp, _vp, _vp, tv_held, tv_linear_desc, _vp, ctypes.c_size_t, _vp]
+        L.tv_linear_fwd.restype = ctypes.c_int
+        L.tv_linear_bwd_workspace_bytes.argtypes = [tv_linear_desc, ctypes.c_int]
+        L.tv_linear_bwd_workspace_bytes.restype = ctypes.c_size_t
+        L.tv_linear_bwd.argtypes = [_vp, _vp, _vp, tv_held, _vp, _vp, _vp, _vp, tv_linear_desc, _vp, ctypes.c_size_t, _vp]
+        L.tv_linear_bwd.restype = ctypes.c_int
+        L.tv_ckpt8_save.argtypes = [_vp, _vp, _vp, _i64, _i64, _i64, ctypes.c_int, _vp]
+        L.tv_ckpt8_save.restype = ctypes.c_int
+        L.tv_ckpt8_load.argtypes = [_vp, _vp, _vp, _i64, _i64, _i64, ctypes.c_int, _vp]
+        L.tv_ckpt8_load.restype = ctypes.c_int
         _current_stream = _stream_lookup(torch)
         _lib = L
     return _lib
@@ -262,3 +288,30 @@ def tv2d_prox_bwd_bf16(g_up, grad_y, grad_lam, planes, H, W, lam: tv_lambda, swe
                        stream=None):
     _check(lib().tv2d_prox_bwd_bf16(_ptr(g_up), _ptr(grad_y), _ptr(grad_lam), planes, H, W, lam,
                                     int(sweeps), _ptr(ws), int(ws_bytes), _stream(stream)))
+
+
+def tv_linear_fwd_workspace_bytes(desc: tv_linear_desc) -> int:
+    return int(lib().tv_linear_fwd_workspace_bytes(desc))
+
+
+def tv_linear_fwd(x, w, bias, res, y, held: tv_held, desc: tv_linear_desc, ws=None, ws_bytes: int = 0, stream=None):
+    _check(lib().tv_linear_fwd(_ptr(x), _ptr(w), _ptr(bias), _ptr(res), _ptr(y), held, desc, _ptr(ws), int(ws_bytes),
+                               _stream(stream)))
+
+
+def tv_linear_bwd_workspace_bytes(desc: tv_linear_desc, x_is_8bit: bool) -> int:
+    return int(lib().tv_linear_bwd_workspace_bytes(desc, int(bool(x_is_8bit))))
+
+
+def tv_linear_bwd(g, x, x_exps, held: tv_held, w, dx, dw, db, desc: tv_linear_desc, ws=None, ws_bytes: int = 0,
+                  stream=None):
+    _check(lib().tv_linear_bwd(_ptr(g), _ptr(x), _ptr(x_exps), held, _ptr(w), _ptr(dx), _ptr(dw), _ptr(db), desc,
+                               _ptr(ws), int(ws_bytes), _stream(stream)))
+
+
+def tv_ckpt8_save(x, codes, exps, rows: int, n: int, ldx: int, dtype: int, stream=None):
+    _check(lib().tv_ckpt8_save(_ptr(x), _ptr(codes), _ptr(exps), int(rows), int(n), int(ldx), int(dtype), _stream(stream)))
+
+
+def tv_ckpt8_load(codes, exps, x, rows: int, n: int, ldx: int, dtype: int, stream=None):
+    _check(lib().tv_ckpt8_load(_ptr(codes), _ptr(exps), _ptr(x), int(rows), int(n), int(ldx), int(dtype), _stream(stream)))

@@ -1,0 +1,193 @@
+// Matrix products of channel mixing: D[m, n] = sum_k A(m, k) B(n, k), either operand stored with k contiguous or with
+// its other index contiguous (the gradients read their operands that way round), sums in 32 bits.
+#pragma once
+#include "tv_linear.hpp"
+
+namespace tvl {
+
+struct Product {
+    const void *a, *b;       // A(m, k) = a[m * lda + k], or a[k * lda + m] where A is transposed; B alike
+    int64_t  lda, ldb;
+    int32_t  M, N, K;
+    int32_t  k_per;          // contraction indices of one split, a multiple of 64
+    int32_t  splits;
+    float   *partial;        // [splits, M, ceil(N / 4) * 4] sums, where splits > 1
+    uint32_t tiles_m, tiles_n;
+};
+
+// One 16 x 16 tile step on 16 bytes a lane of either operand: lane l holds row l % 16 of its operand and the bytes
+// 16 * (l / 16) .. of 64 contraction bytes.  D's rows run over the first operand, its columns over the second: lane l
+// has column l % 16, rows 4 * (l / 16) ...  In f32 four steps of four contraction indices each take one element of
+// every lane's four, the same one on both sides.
+template <class T> __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c)
+{
+    if constexpr (sizeof(T) == 2)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0, 0, 0);
+        return c;
+    }
+}
+
+typedef uint32_t u32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));
+
+// 16 bytes from any address that suits T, or the first `have` elements and zeros.
+template <class T> __device__ __forceinline__ u32x4 load16(const T *p, int have)
+{
+    constexpr int E = Elems<T>::kPer16;
+    if (have >= E) {
+        if constexpr (sizeof(T) == 4) return *(const u32x4_at4 *)p;
+        else return *(const u32x4_at2 *)p;
+    }
+    u32x4 v = {0, 0, 0, 0};
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (i < have) v[i] = __float_as_uint(p[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (i < have) v[i >> 1] |= (uint32_t)((const uint16_t *)p)[i] << (16 * (i & 1));
+    }
+    return v;
+}
+
+// A wave's outputs, NT x MT tiles of 16 x 16 from (m0, n0) on, into the epilogue or, of one split of several, as sums.
+template <class T, int NT, int MT>
+__device__ __forceinline__ void store_tile(f32x4 (&acc)[NT][MT], const Product &g, const Epilogue &e, int m0, int n0, int lane)
+{
+    const int64_t pitch = (g.N + 3) & ~3;
+#pragma unroll
+    for (int j = 0; j < MT; ++j) {
+        const int64_t m = m0 + 16 * j + (lane & 15);
+#pragma unroll
+        for (int i = 0; i < NT; i += 2) {
+            const int n = n0 + 16 * i + (lane >> 4) * 4;
+            if (g.splits > 1) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (m < g.M && n + 16 * h < g.N)
+                        *(f32x4 *)(g.partial + ((int64_t)blockIdx.y * g.M + m) * pitch + n + 16 * h) = acc[i + h][j];
+            } else {
+                f32x4 p[2] = {acc[i][j], acc[i + 1][j]};
+                finish_block<T, 2, 16, 32, 0>(p, m, n, g.N, m < g.M, e);
+            }
+        }
+    }
+}
+
+// The sums of all splits, in order, through the epilogue: four columns a thread, eight threads a block of 32.
+template <class T>
+__global__ __launch_bounds__(256) void join_kernel(Product g, Epilogue e)
+{
+    const int per_row = (g.N + 31) / 32 * 8;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t m = at / per_row;
+    const int n = (int)(at - m * per_row) * 4;
+    const int64_t pitch = (g.N + 3) & ~3;
+    f32x4 p[1] = {{0.0f, 0.0f, 0.0f, 0.0f}};
+    if (m < g.M && n < g.N)
+        for (int s = 0; s < g.splits; ++s) p[0] += *(const f32x4 *)(g.partial + ((int64_t)s * g.M + m) * pitch + n);
+    finish_block<T, 1, 1, 2, 4>(p, m, n, g.N, m < g.M, e);
+}
+
+// ---- any shape, stride and alignment: 128 x 128 outputs a workgroup of four waves, 128 contraction bytes at a time
+// through registers into two LDS buffers, always with k contiguous there.  Row r's 16-byte piece c lies in slot
+// c ^ ((r / 2) % 8): sixteen rows that a wave reads at one c then touch all 64 banks once.
+template <class T, bool TRANSPOSED> struct Stage {
+    static constexpr int E = Elems<T>::kPer16;
+    static constexpr int kDepth = 8 * E;              // contraction indices of a tile
+    u32x4 r[4];
+
+    __device__ __forceinline__ void load(const T *p, int64_t ld, int rows, int k_end, int row0, int k0, int t)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int q = t + 256 * i;
+            if constexpr (!TRANSPOSED) {
+                const int row = row0 + q / 8, k = k0 + q % 8 * E;
+                r[i] = row < rows && k < k_end ? load16(p + row * ld + k, k_end - k) : u32x4{0, 0, 0, 0};
+            } else {
+                const int row = row0 + q % (128 / E) * E, k = k0 + q / (128 / E);
+                r[i] = row < rows && k < k_end ? load16(p + k * ld + row, rows - row) : u32x4{0, 0, 0, 0};
+            }
+        }
+    }
+    __device__ __forceinline__ static int place(int row, int piece) { return row * 128 + ((piece ^ ((row >> 1) & 7)) << 4); }
+    __device__ __forceinline__ void put(char *lds, int t) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int q = t + 256 * i;
+            if constexpr (!TRANSPOSED) {
+                *(u32x4 *)(lds + place(q / 8, q % 8)) = r[i];
+            } else {
+                const int row = q % (128 / E) * E, k = q / (128 / E);
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    char *to = lds + place(row + j, k / E) + k % E * (int)sizeof(T);
+                    if constexpr (sizeof(T) == 4) *(uint32_t *)to = r[i][j];
+                    else *(uint16_t *)to = (uint16_t)(r[i][j >> 1] >> (16 * (j & 1)));
+                }
+            }
+        }
+    }
+};
+
+template <class T, bool AT, bool BT>
+__global__ __launch_bounds__(256) void gemm_any_kernel(Product g, Epilogue e)
+{
+    constexpr int kDepth = Stage<T, AT>::kDepth;
+    __shared__ __attribute__((aligned(16))) char lds[2][2][128 * 128];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int m0 = (int)(blockIdx.x % g.tiles_m) * 128, n0 = (int)(blockIdx.x / g.tiles_m) * 128;
+    const int k0 = (int)blockIdx.y * g.k_per, k_end = min(g.K, k0 + g.k_per);
+    const int steps = (k_end - k0 + kDepth - 1) / kDepth;
+    const int wm = (wave & 1) * 64, wn = (wave >> 1) * 64;
+
+    f32x4 acc[4][4];                                  // [n tile][m tile]
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    Stage<T, AT> sa;
+    Stage<T, BT> sb;
+    sa.load((const T *)g.a, g.lda, g.M, k_end, m0, k0, t);
+    sb.load((const T *)g.b, g.ldb, g.N, k_end, n0, k0, t);
+    sa.put(lds[0][0], t);
+    sb.put(lds[0][1], t);
+    __syncthreads();
+    for (int s = 0; s < steps; ++s) {
+        const bool more = s + 1 < steps;
+        if (more) {
+            sa.load((const T *)g.a, g.lda, g.M, k_end, m0, k0 + (s + 1) * kDepth, t);
+            sb.load((const T *)g.b, g.ldb, g.N, k_end, n0, k0 + (s + 1) * kDepth, t);
+        }
+        const char *la = lds[s & 1][0], *lb = lds[s & 1][1];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            u32x4 fa[4], fb[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                fa[i] = *(const u32x4 *)(la + Stage<T, AT>::place(wm + 16 * i + (lane & 15), h * 4 + (lane >> 4)));
+                fb[i] = *(const u32x4 *)(lb + Stage<T, BT>::place(wn + 16 * i + (lane & 15), h * 4 + (lane >> 4)));
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = mma<T>(fb[i], fa[j], acc[i][j]);
+        }
+        if (more) {
+            sa.put(lds[(s + 1) & 1][0], t);
+            sb.put(lds[(s + 1) & 1][1], t);
+        }
+        __syncthreads();
+    }
+    store_tile<T, 4, 4>(acc, g, e, m0 + wm, n0 + wn, lane);
+}
+
+}  // namespace tvl

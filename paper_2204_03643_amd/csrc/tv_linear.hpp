@@ -1,0 +1,217 @@
+// Channel products (y = act(x W^T + b) + r and its gradients): types, activations, the 8-bit blocks and the
+// epilogue that the product kernels share.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace tvl {
+
+using bf16 = __bf16;
+typedef bf16     bf16x4 __attribute__((ext_vector_type(4)));
+typedef bf16     bf16x8 __attribute__((ext_vector_type(8)));
+typedef float    f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int16_t  s16x4 __attribute__((ext_vector_type(4)));
+
+enum Act : int { kNone = 0, kRelu = 1, kGelu = 2, kSilu = 3 };
+// how z is held for the backward call
+enum Held : int { kHeldNone = 0, kHeldPlain = 1, kHeldBits = 2, kHeld8 = 3 };
+
+constexpr int kBlock = 32;            // samples that share a step in an 8-bit checkpoint
+
+template <class T> struct Elems { static constexpr int kPer16 = 16 / (int)sizeof(T); };
+
+__device__ __forceinline__ float widen(float v) { return v; }
+__device__ __forceinline__ float widen(bf16 v) { return (float)v; }
+template <class T> __device__ __forceinline__ T narrow(float v) { return (T)v; }      // to nearest even
+
+// Activations and their slopes.  A NaN goes through all of them (ReLU is zero where z <= 0, which a NaN is not);
+// at -infinity gelu and silu are infinity times zero, a NaN.  Results that are kept in 32 bits take erff and expf
+// of the device library.  Results that are rounded to bf16 (2^-8) take the normal distribution's tail as
+// Q(|z|) = p(t) exp(-z^2/2) / 2, t = 1 / (1 + 0.3275911 |z| / sqrt 2), p the polynomial 7.1.26 of Abramowitz and
+// Stegun (off by at most 1.5e-7), and the hardware's exp2 and reciprocal: 16 instructions in place of about 50.
+struct Gauss { float cdf, bell; };          // Phi(z), exp(-z^2/2)
+template <bool FAST> __device__ __forceinline__ Gauss gauss(float z)
+{
+    if constexpr (FAST) {
+        const float bell = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
+        const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.23164190f, 1.0f));
+        const float p = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+        const float q = 0.5f * p * bell;
+        return {z < 0.0f ? q : 1.0f - q, bell};
+    } else {
+        return {0.5f * (1.0f + erff(z * 0.70710678f)), expf(-0.5f * z * z)};
+    }
+}
+template <bool FAST> __device__ __forceinline__ float logistic(float z)
+{
+    if constexpr (FAST) return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
+    else return 1.0f / (1.0f + expf(-z));
+}
+
+template <bool FAST> __device__ __forceinline__ float act_of(float z, int act)
+{
+    if (act == kRelu) return z <= 0.0f ? 0.0f : z;
+    if (act == kGelu) return z * gauss<FAST>(z).cdf;
+    if (act == kSilu) return z * logistic<FAST>(z);
+    return z;
+}
+
+template <bool FAST> __device__ __forceinline__ float slope_of(float z, int act)
+{
+    if (act == kRelu) return z <= 0.0f ? 0.0f : 1.0f;
+    if (act == kGelu) {
+        const Gauss g = gauss<FAST>(z);
+        return g.cdf + z * g.bell * 0.39894228f;
+    }
+    if (act == kSilu) {
+        const float s = logistic<FAST>(z);
+        return s * (1.0f + z * (1.0f - s));
+    }
+    return 1.0f;
+}
+
+// ---- 8-bit blocks.  The step is 2^(e - 6), 2^e the power of two at or below the block's largest finite magnitude
+// (2^-120 at least, so that the step is a normal number): the exponent field of that magnitude, less six, is the byte
+// that is kept, and everything is exact but the one rounding of x / step to a whole number.
+constexpr uint32_t kLeastMagnitude = 7u << 23;      // 2^-120
+
+__device__ __forceinline__ uint32_t finite_magnitude(float v)
+{
+    const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
+    return b < 0x7f800000u ? b : 0u;
+}
+__device__ __forceinline__ uint32_t step_byte(uint32_t magnitude)
+{
+    return (max(magnitude, kLeastMagnitude) >> 23) - 6u;
+}
+// the code of v for the step 2^(byte - 127); v / step < 128, so the product below cannot overflow
+__device__ __forceinline__ int code_of(float v, uint32_t byte)
+{
+    const float inverse = __uint_as_float((254u - byte) << 23);
+    const float q = fminf(fmaxf(rintf(v * inverse), -127.0f), 127.0f);
+    return finite_magnitude(v) == 0u && (__float_as_uint(v) & 0x7fffffffu) != 0u ? -128 : (int)q;
+}
+__device__ __forceinline__ float value_of(int code, uint32_t byte)
+{
+    return code == -128 ? __uint_as_float(0x7fc00000u) : (float)code * __uint_as_float(byte << 23);
+}
+
+// ---- the epilogue of y = act(x W^T + b) + r
+struct Epilogue {
+    const void *bias;        // [n] or null
+    const void *res;         // [m, n] rows of ldr elements, or null
+    void       *y;           // [m, n] rows of ldy elements
+    void       *held;        // z as it is, packed [m, n]; a bit a sample, 32 to a word; or codes, packed [m, n]
+    uint8_t    *exps;        // [m, ceil(n / 32)] step bytes (kHeld8)
+    int64_t     ldr, ldy;
+    int32_t     act, kind;
+    uint32_t    vec;         // rows of y, res, held and the bias start on multiples of four elements
+};
+
+// Four consecutive outputs of row m from column n on (n a multiple of four): p = their products' sums.
+// FOUR elements exist (n + 3 < N) or only some.  Returns z.
+template <class T> __device__ __forceinline__ f32x4 load4(const T *p, int have, bool vec)
+{
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (have == 4 && vec) {
+        if constexpr (sizeof(T) == 4) v = *(const f32x4 *)p;
+        else {
+            const bf16x4 h = *(const bf16x4 *)p;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = widen(h[i]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < have) v[i] = widen(p[i]);
+    }
+    return v;
+}
+template <class T> __device__ __forceinline__ void store4(T *p, f32x4 v, int have, bool vec)
+{
+    if (have == 4 && vec) {
+        if constexpr (sizeof(T) == 4) *(f32x4 *)p = v;
+        else {
+            bf16x4 h;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) h[i] = narrow<bf16>(v[i]);
+            *(bf16x4 *)p = h;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < have) p[i] = narrow<T>(v[i]);
+    }
+}
+
+// p: sums of products for outputs (m, n .. n+3).  have: how many of them exist (0 for a lane without work).
+// The lanes that share a block of 32 columns of one row are this lane xor the masks of `Lanes`; each of them holds
+// PER groups of four columns, group i sixteen columns after group i - 1.
+template <class T, int PER, int LANE0, int LANE1, int LANE2>
+__device__ __forceinline__ void finish_block(f32x4 (&p)[PER], int64_t m, int n, int N, bool row, const Epilogue &e)
+{
+    constexpr bool kFast = sizeof(T) == 2;
+    constexpr int kStep = PER == 2 ? 16 : 4;
+    const bool vec = e.vec != 0;
+    int have[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) have[i] = row ? max(0, min(4, N - (n + kStep * i))) : 0;
+    if (e.bias) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (have[i]) p[i] += load4((const T *)e.bias + n + kStep * i, have[i], vec);
+    }
+    if (e.kind == kHeldPlain) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (have[i]) store4((T *)e.held + m * N + n + kStep * i, p[i], have[i], vec);
+    } else if (e.kind == kHeldBits) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j < have[i] && !(p[i][j] <= 0.0f)) w |= 1u << (((n + kStep * i) & 31) + j);
+        if constexpr (LANE0) w |= __shfl_xor(w, LANE0);
+        if constexpr (LANE1) w |= __shfl_xor(w, LANE1);
+        if constexpr (LANE2) w |= __shfl_xor(w, LANE2);
+        if (have[0] && (n & 31) == 0) ((uint32_t *)e.held)[m * ((N + 31) / 32) + n / 32] = w;
+    } else if (e.kind == kHeld8) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j < have[i]) top = max(top, finite_magnitude(p[i][j]));
+        if constexpr (LANE0) top = max(top, (uint32_t)__shfl_xor(top, LANE0));
+        if constexpr (LANE1) top = max(top, (uint32_t)__shfl_xor(top, LANE1));
+        if constexpr (LANE2) top = max(top, (uint32_t)__shfl_xor(top, LANE2));
+        const uint32_t byte = step_byte(top);
+        if (have[0] && (n & 31) == 0) e.exps[m * ((N + 31) / 32) + n / 32] = (uint8_t)byte;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            uint32_t c = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) c |= ((uint32_t)code_of(p[i][j], byte) & 255u) << (8 * j);
+            int8_t *to = (int8_t *)e.held + m * N + n + kStep * i;
+            if (have[i] == 4 && vec) *(uint32_t *)to = c;
+            else
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < have[i]) to[j] = (int8_t)(c >> (8 * j));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if (!have[i]) continue;
+        if (e.act != kNone)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) p[i][j] = act_of<kFast>(p[i][j], e.act);
+        if (e.res) p[i] += load4((const T *)e.res + m * e.ldr + n + kStep * i, have[i], vec);
+        store4((T *)e.y + m * e.ldy + n + kStep * i, p[i], have[i], vec);
+    }
+}
+
+}  // namespace tvl

@@ -1,0 +1,290 @@
+// C-ABI entry points of the channel products and the 8-bit checkpoints: argument validation, choice of kernels,
+// workspace layout and launches.
+#include "../../include/tvprox.h"
+#include "tv_ckpt8.hpp"
+#include "tv_gemm.hpp"
+#include "tv_slope.hpp"
+
+namespace {
+
+using namespace tvl;
+
+constexpr int64_t kMostIndex = (int64_t)1 << 31;      // sizes and strides stay below
+constexpr int64_t kMostTiles = (int64_t)1 << 23;      // workgroups of a launch
+
+int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+int64_t tiles(int64_t v, int64_t of) { return (v + of - 1) / of; }
+size_t elem_bytes(int dtype) { return dtype == TV_BF16 ? 2 : 4; }
+bool aligned(const void *p, size_t to) { return (uintptr_t)p % to == 0; }
+int launched() { return hipGetLastError() == hipSuccess ? TV_OK : TV_ERR_HIP; }
+
+// ---- products
+struct Split { int splits, k_per; };
+
+// One workgroup a compute unit at least where the contraction is long enough: each split keeps 512 indices or more.
+Split split_of(int64_t M, int64_t N, int64_t K)
+{
+    const int64_t t = tiles(M, 128) * tiles(N, 128);
+    int64_t s = t >= 256 || t < 1 ? 1 : (512 + t - 1) / t;
+    if (s > K / 512) s = K / 512;
+    if (s < 1) s = 1;
+    const int64_t per = up(tiles(K, s), 64);
+    return {(int)(K > 0 ? tiles(K, per) : 1), (int)(per > 0 ? per : 64)};
+}
+
+size_t product_bytes(int64_t M, int64_t N, int64_t K)
+{
+    const Split s = split_of(M, N, K);
+    return s.splits > 1 ? (size_t)up((int64_t)s.splits * M * up(N, 4) * 4, 256) : 0;
+}
+
+bool product_fits(int64_t M, int64_t N) { return tiles(M, 128) * tiles(N, 128) <= kMostTiles; }
+
+template <class T, bool AT, bool BT>
+int run_product(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t M, int64_t N, int64_t K,
+                const Epilogue &e, void *ws, hipStream_t stream)
+{
+    const Split sp = split_of(M, N, K);
+    Product g{a, b, lda, ldb, (int32_t)M, (int32_t)N, (int32_t)K, sp.k_per, sp.splits, (float *)ws,
+              (uint32_t)tiles(M, 128), (uint32_t)tiles(N, 128)};
+    hipLaunchKernelGGL((gemm_any_kernel<T, AT, BT>), dim3(g.tiles_m * g.tiles_n, sp.splits), dim3(256), 0, stream, g, e);
+    if (sp.splits > 1) {
+        if (launched() != TV_OK) return TV_ERR_HIP;
+        hipLaunchKernelGGL((join_kernel<T>), dim3((uint32_t)tiles(M * tiles(N, 32) * 8, 256)), dim3(256), 0, stream, g, e);
+    }
+    return launched();
+}
+
+// Rows of four elements at once where every row of every array the epilogue touches starts on such a boundary.
+uint32_t epilogue_vec(const Epilogue &e, size_t size, int64_t N)
+{
+    if (N % 4 || e.ldy % 4 || !aligned(e.y, 4 * size)) return 0;
+    if (e.res && (e.ldr % 4 || !aligned(e.res, 4 * size))) return 0;
+    if (e.bias && !aligned(e.bias, 4 * size)) return 0;
+    if (e.held && !aligned(e.held, e.kind == kHeldPlain ? 4 * size : 4)) return 0;
+    return 1;
+}
+
+Epilogue plain_output(void *y, int64_t ldy, size_t size, int64_t N)
+{
+    Epilogue e{};
+    e.y = y; e.ldy = ldy;
+    e.vec = epilogue_vec(e, size, N);
+    return e;
+}
+
+// ---- validation
+int check_sizes(const tv_linear_desc &d)
+{
+    if (d.m < 0 || d.k < 1 || d.n < 1 || d.m >= kMostIndex || d.k >= kMostIndex - 128 || d.n >= kMostIndex - 128) return TV_ERR_SHAPE;
+    if (!product_fits(d.m, d.n) || !product_fits(d.m, d.k) || !product_fits(d.n, d.k)) return TV_ERR_SHAPE;
+    if ((d.dtype != TV_F32 && d.dtype != TV_BF16) || d.act < TV_ACT_NONE || d.act > TV_ACT_SILU) return TV_ERR_UNSUPPORTED;
+    if (d.ldx < d.k || d.ldw < d.k || d.ldy < d.n || d.ldx >= kMostIndex || d.ldw >= kMostIndex || d.ldy >= kMostIndex) return TV_ERR_STRIDE;
+    return TV_OK;
+}
+
+int check_held(const tv_linear_desc &d, const tv_held &h, bool needed)
+{
+    const bool smooth = d.act == TV_ACT_GELU || d.act == TV_ACT_SILU;
+    switch (h.kind) {
+    case TV_HELD_NONE: return needed && d.act != TV_ACT_NONE ? TV_ERR_UNSUPPORTED : TV_OK;
+    case TV_HELD_BITS:
+        if (d.act != TV_ACT_RELU) return TV_ERR_UNSUPPORTED;
+        break;
+    case TV_HELD_PLAIN:
+    case TV_HELD_8BIT:
+        if (!smooth) return TV_ERR_UNSUPPORTED;
+        break;
+    default: return TV_ERR_UNSUPPORTED;
+    }
+    if (d.m == 0) return TV_OK;
+    if (!h.data || (h.kind == TV_HELD_8BIT && !h.exps)) return TV_ERR_NULL;
+    const size_t to = h.kind == TV_HELD_BITS ? 4 : h.kind == TV_HELD_PLAIN ? elem_bytes(d.dtype) : 1;
+    return aligned(h.data, to) ? TV_OK : TV_ERR_STRIDE;
+}
+
+int check_workspace(const void *ws, size_t have, size_t need)
+{
+    return need && (!ws || !aligned(ws, 16) || have < need) ? TV_ERR_WORKSPACE : TV_OK;
+}
+
+template <class T>
+int linear_fwd(const void *x, const void *w, const void *bias, const void *res, void *y, const tv_held &h,
+               const tv_linear_desc &d, void *ws, hipStream_t stream)
+{
+    Epilogue e{};
+    e.bias = bias; e.res = res; e.y = y;
+    e.held = h.kind == TV_HELD_NONE ? nullptr : h.data; e.exps = h.exps;
+    e.ldr = d.ldr; e.ldy = d.ldy; e.act = d.act; e.kind = h.kind;
+    e.vec = epilogue_vec(e, sizeof(T), d.n);
+    return run_product<T, false, false>(x, d.ldx, w, d.ldw, d.m, d.n, d.k, e, ws, stream);
+}
+
+// ---- the backward call's workspace: dz, x out of its checkpoint, the column sums of groups of rows, split sums
+struct BwdPlan {
+    size_t dz, x, sums, split, bytes;
+    int64_t ldz, ldx;
+    int rows_per, groups;
+};
+
+BwdPlan bwd_plan(const tv_linear_desc &d, bool x8)
+{
+    BwdPlan p{};
+    const size_t size = elem_bytes(d.dtype);
+    size_t at = 0;
+    p.ldz = up(d.n, 8);
+    p.dz = at;
+    if (d.act != TV_ACT_NONE) at += up(d.m * p.ldz * (int64_t)size, 256);
+    p.ldx = up(d.k, 8);
+    p.x = at;
+    if (x8) at += up(d.m * p.ldx * (int64_t)size, 256);
+    // about 1024 workgroups of 256 columns each, of sixteen rows at least
+    const int64_t want = 1024 / tiles(d.n, 256) + 1;
+    p.rows_per = (int)(d.m > 0 ? up(tiles(d.m, want < 256 ? want : 256), 16) : 16);
+    p.groups = (int)tiles(d.m, p.rows_per);
+    p.sums = at;
+    at += up((int64_t)p.groups * d.n * 4, 256);
+    p.split = at;
+    const size_t s1 = product_bytes(d.m, d.k, d.n), s2 = product_bytes(d.n, d.k, d.m);
+    p.bytes = at + (s1 > s2 ? s1 : s2);
+    return p;
+}
+
+template <class T>
+int linear_bwd(const void *g, const void *x, const uint8_t *x_exps, const tv_held &h, const void *w, void *dx, void *dw,
+               void *db, const tv_linear_desc &d, char *ws, hipStream_t stream)
+{
+    const BwdPlan p = bwd_plan(d, x_exps != nullptr);
+    const void *dz = g;
+    int64_t ldz = d.ldy;
+    if (d.m > 0 && (d.act != TV_ACT_NONE || db)) {
+        SlopeArgs a{};
+        a.g = g; a.held = h.data; a.exps = h.exps;
+        a.dz = d.act != TV_ACT_NONE ? ws + p.dz : nullptr;
+        a.sums = db ? (float *)(ws + p.sums) : nullptr;
+        a.ldg = d.ldy; a.ldz = p.ldz;
+        a.M = (int32_t)d.m; a.N = (int32_t)d.n; a.rows_per = p.rows_per;
+        a.act = d.act; a.kind = d.act == TV_ACT_NONE ? TV_HELD_NONE : h.kind;
+        a.vec = d.n % 4 == 0 && d.ldy % 4 == 0 && aligned(g, 4 * sizeof(T)) &&
+                aligned(h.data, a.kind == kHeldPlain ? 4 * sizeof(T) : 4);
+        hipLaunchKernelGGL((slope_kernel<T>), dim3((uint32_t)tiles(d.n, 256), p.groups), dim3(256), 0, stream, a);
+        if (launched() != TV_OK) return TV_ERR_HIP;
+        if (a.dz) { dz = a.dz; ldz = p.ldz; }
+    }
+    if (db) {
+        hipLaunchKernelGGL((column_sum_kernel<T>), dim3((uint32_t)tiles(d.n, 256)), dim3(256), 0, stream,
+                           (const float *)(ws + p.sums), (T *)db, d.m > 0 ? p.groups : 0, (int)d.n);
+        if (launched() != TV_OK) return TV_ERR_HIP;
+    }
+    if (dx && d.m > 0) {
+        const int st = run_product<T, false, true>(dz, ldz, w, d.ldw, d.m, d.k, d.n, plain_output(dx, d.k, sizeof(T), d.k),
+                                                   ws + p.split, stream);
+        if (st != TV_OK) return st;
+    }
+    if (dw) {
+        const void *xs = x;
+        int64_t ldx = d.ldx;
+        if (x_exps && d.m > 0) {
+            const int st = tv_ckpt8_load((const int8_t *)x, x_exps, ws + p.x, d.m, d.k, p.ldx, d.dtype, stream);
+            if (st != TV_OK) return st;
+            xs = ws + p.x; ldx = p.ldx;
+        }
+        return run_product<T, true, true>(dz, ldz, xs, ldx, d.n, d.k, d.m, plain_output(dw, d.k, sizeof(T), d.k),
+                                          ws + p.split, stream);
+    }
+    return TV_OK;
+}
+
+int check_ckpt8(int64_t rows, int64_t n, int64_t ld, int dtype)
+{
+    if (rows < 0 || n < 1 || rows >= kMostIndex || n >= kMostIndex - 128) return TV_ERR_SHAPE;
+    if (rows > ((int64_t)1 << 40) / n) return TV_ERR_SHAPE;
+    if (dtype != TV_F32 && dtype != TV_BF16) return TV_ERR_UNSUPPORTED;
+    if (ld < n || ld >= kMostIndex) return TV_ERR_STRIDE;
+    return TV_OK;
+}
+
+dim3 ckpt8_grid(int64_t rows, int64_t n)
+{
+    const int64_t groups = tiles(rows * tiles(n, kBlock), 64), wide = (int64_t)1 << 22;
+    return groups <= wide ? dim3((uint32_t)groups) : dim3((uint32_t)wide, (uint32_t)tiles(groups, wide));
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t tv_linear_fwd_workspace_bytes(tv_linear_desc d)
+{
+    return check_sizes(d) == TV_OK ? product_bytes(d.m, d.n, d.k) : 0;
+}
+
+int tv_linear_fwd(const void *x, const void *w, const void *bias, const void *res, void *y, tv_held held,
+                  tv_linear_desc d, void *ws, size_t ws_bytes, hipStream_t stream)
+{
+    int st = check_sizes(d);
+    if (st != TV_OK) return st;
+    if (res && (d.ldr < d.n || d.ldr >= kMostIndex)) return TV_ERR_STRIDE;
+    if ((st = check_held(d, held, false)) != TV_OK) return st;
+    if (d.m == 0) return TV_OK;
+    if (!x || !w || !y) return TV_ERR_NULL;
+    const size_t size = elem_bytes(d.dtype);
+    if (!aligned(x, size) || !aligned(w, size) || !aligned(bias, size) || !aligned(res, size) || !aligned(y, size)) return TV_ERR_STRIDE;
+    if ((st = check_workspace(ws, ws_bytes, product_bytes(d.m, d.n, d.k))) != TV_OK) return st;
+    return d.dtype == TV_BF16 ? linear_fwd<bf16>(x, w, bias, res, y, held, d, ws, stream)
+                              : linear_fwd<float>(x, w, bias, res, y, held, d, ws, stream);
+}
+
+size_t tv_linear_bwd_workspace_bytes(tv_linear_desc d, int x_is_8bit)
+{
+    return check_sizes(d) == TV_OK ? bwd_plan(d, x_is_8bit != 0).bytes : 0;
+}
+
+int tv_linear_bwd(const void *g, const void *x, const uint8_t *x_exps, tv_held held, const void *w, void *dx, void *dw,
+                  void *db, tv_linear_desc d, void *ws, size_t ws_bytes, hipStream_t stream)
+{
+    int st = check_sizes(d);
+    if (st != TV_OK) return st;
+    if ((st = check_held(d, held, true)) != TV_OK) return st;
+    if ((d.m > 0 && (!g || (dx && !w) || (dw && !x)))) return TV_ERR_NULL;
+    const size_t size = elem_bytes(d.dtype);
+    if (!aligned(g, size) || (!x_exps && !aligned(x, size)) || !aligned(w, size) || !aligned(dx, size) || !aligned(dw, size) ||
+        !aligned(db, size)) return TV_ERR_STRIDE;
+    if ((st = check_workspace(ws, ws_bytes, bwd_plan(d, x_exps != nullptr).bytes)) != TV_OK) return st;
+    return d.dtype == TV_BF16 ? linear_bwd<bf16>(g, x, x_exps, held, w, dx, dw, db, d, (char *)ws, stream)
+                              : linear_bwd<float>(g, x, x_exps, held, w, dx, dw, db, d, (char *)ws, stream);
+}
+
+int tv_ckpt8_save(const void *x, int8_t *codes, uint8_t *exps, int64_t rows, int64_t n, int64_t ldx, int dtype, hipStream_t stream)
+{
+    const int st = check_ckpt8(rows, n, ldx, dtype);
+    if (st != TV_OK || rows == 0) return st;
+    if (!x || !codes || !exps) return TV_ERR_NULL;
+    const size_t size = elem_bytes(dtype);
+    if (!aligned(x, size)) return TV_ERR_STRIDE;
+    const int blocks = (int)tiles(n, kBlock);
+    const uint32_t vec = n % 8 == 0 && ldx % 4 == 0 && aligned(x, 4 * size) && aligned(codes, 8);
+    if (dtype == TV_BF16)
+        hipLaunchKernelGGL((ckpt8_save_kernel<bf16>), ckpt8_grid(rows, n), dim3(256), 0, stream, (const bf16 *)x, ldx, codes, exps, rows, (int)n, blocks, vec);
+    else
+        hipLaunchKernelGGL((ckpt8_save_kernel<float>), ckpt8_grid(rows, n), dim3(256), 0, stream, (const float *)x, ldx, codes, exps, rows, (int)n, blocks, vec);
+    return launched();
+}
+
+int tv_ckpt8_load(const int8_t *codes, const uint8_t *exps, void *x, int64_t rows, int64_t n, int64_t ldx, int dtype, hipStream_t stream)
+{
+    const int st = check_ckpt8(rows, n, ldx, dtype);
+    if (st != TV_OK || rows == 0) return st;
+    if (!x || !codes || !exps) return TV_ERR_NULL;
+    const size_t size = elem_bytes(dtype);
+    if (!aligned(x, size)) return TV_ERR_STRIDE;
+    const int blocks = (int)tiles(n, kBlock);
+    const uint32_t vec = n % 8 == 0 && ldx % 4 == 0 && aligned(x, 4 * size) && aligned(codes, 8);
+    if (dtype == TV_BF16)
+        hipLaunchKernelGGL((ckpt8_load_kernel<bf16>), ckpt8_grid(rows, n), dim3(256), 0, stream, codes, exps, (bf16 *)x, ldx, rows, (int)n, blocks, vec);
+    else
+        hipLaunchKernelGGL((ckpt8_load_kernel<float>), ckpt8_grid(rows, n), dim3(256), 0, stream, codes, exps, (float *)x, ldx, rows, (int)n, blocks, vec);
+    return launched();
+}
+
+}  // extern "C"
