@@ -11,7 +11,7 @@ struct Product {
     int32_t  M, N, K;
     int32_t  k_per;          // contraction indices of one split, a multiple of 64
     int32_t  splits;
-    float   *partial;        // [splits, M, ceil(N / 4) * 4] sums, where splits > 1
+    float   *partial;        // [splits, M, ceil(N / 8) * 8] sums, where splits > 1
     uint32_t tiles_m, tiles_n;
 };
 
@@ -55,43 +55,59 @@ template <class T> __device__ __forceinline__ u32x4 load16(const T *p, int have)
     return v;
 }
 
-// A wave's outputs, NT x MT tiles of 16 x 16 from (m0, n0) on, into the epilogue or, of one split of several, as sums.
-template <class T, int NT, int MT>
-__device__ __forceinline__ void store_tile(f32x4 (&acc)[NT][MT], const Product &g, const Epilogue &e, int m0, int n0, int lane)
+// A wave's outputs leave through its own piece of LDS, R rows of 64 columns at a time, so that eight lanes write a
+// row's 64 columns side by side (straight from the accumulators every store would touch 16 or 32 rows).  The piece's
+// rows are 68 floats apart: sixteen rows of one column group then lie in different banks.
+constexpr int kOutPitch = 68;
+
+__device__ __forceinline__ void wave_sync()
 {
-    const int64_t pitch = (g.N + 3) & ~3;
-#pragma unroll
-    for (int j = 0; j < MT; ++j) {
-        const int64_t m = m0 + 16 * j + (lane & 15);
-#pragma unroll
-        for (int i = 0; i < NT; i += 2) {
-            const int n = n0 + 16 * i + (lane >> 4) * 4;
-            if (g.splits > 1) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    if (m < g.M && n + 16 * h < g.N)
-                        *(f32x4 *)(g.partial + ((int64_t)blockIdx.y * g.M + m) * pitch + n + 16 * h) = acc[i + h][j];
-            } else {
-                f32x4 p[2] = {acc[i][j], acc[i + 1][j]};
-                finish_block<T, 2, 16, 32, 0>(p, m, n, g.N, m < g.M, e);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+template <class T, int R>
+__device__ __forceinline__ void store_rows(const float *piece, const Product &g, const Epilogue &e, int m0, int n0, int lane)
+{
+    const int64_t pitch = (g.N + 7) & ~7;
+    const int n = n0 + (lane & 7) * 8;
+#pragma unroll 1
+    for (int i = 0; i < R / 8; ++i) {
+        const int r = i * 8 + (lane >> 3);
+        const int64_t m = m0 + r;
+        const f32x4 a = *(const f32x4 *)(piece + r * kOutPitch + (lane & 7) * 8);
+        const f32x4 b = *(const f32x4 *)(piece + r * kOutPitch + (lane & 7) * 8 + 4);
+        if (g.splits > 1) {
+            if (m < g.M && n < g.N) {
+                float *to = g.partial + ((int64_t)blockIdx.y * g.M + m) * pitch + n;
+                *(f32x4 *)to = a;
+                *(f32x4 *)(to + 4) = b;
             }
+        } else {
+            float p[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+            finish8<T>(p, m, n, g.N, m < g.M, e);
         }
     }
 }
 
-// The sums of all splits, in order, through the epilogue: four columns a thread, eight threads a block of 32.
+// The sums of all splits, in order, through the epilogue: eight columns a thread, four threads a block of 32.
 template <class T>
 __global__ __launch_bounds__(256) void join_kernel(Product g, Epilogue e)
 {
-    const int per_row = (g.N + 31) / 32 * 8;
+    const int per_row = (g.N + 31) / 32 * 4;
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t m = at / per_row;
-    const int n = (int)(at - m * per_row) * 4;
-    const int64_t pitch = (g.N + 3) & ~3;
-    f32x4 p[1] = {{0.0f, 0.0f, 0.0f, 0.0f}};
+    const int n = (int)(at - m * per_row) * 8;
+    const int64_t pitch = (g.N + 7) & ~7;
+    f32x4 a = {0.0f, 0.0f, 0.0f, 0.0f}, b = a;
     if (m < g.M && n < g.N)
-        for (int s = 0; s < g.splits; ++s) p[0] += *(const f32x4 *)(g.partial + ((int64_t)s * g.M + m) * pitch + n);
-    finish_block<T, 1, 1, 2, 4>(p, m, n, g.N, m < g.M, e);
+        for (int s = 0; s < g.splits; ++s) {
+            const float *from = g.partial + ((int64_t)s * g.M + m) * pitch + n;
+            a += *(const f32x4 *)from;
+            b += *(const f32x4 *)(from + 4);
+        }
+    float p[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    finish8<T>(p, m, n, g.N, m < g.M, e);
 }
 
 // ---- any shape, stride and alignment: 128 x 128 outputs a workgroup of four waves, 128 contraction bytes at a time
@@ -187,7 +203,18 @@ __global__ __launch_bounds__(256) void gemm_any_kernel(Product g, Epilogue e)
         }
         __syncthreads();
     }
-    store_tile<T, 4, 4>(acc, g, e, m0 + wm, n0 + wn, lane);
+    float *piece = (float *)&lds[0][0][0] + wave * 16 * kOutPitch;      // the last barrier has ended every read of LDS
+#pragma unroll 1
+    for (int j = 0; j < 4; ++j) {                     // one copy of the epilogue's code, and of its registers
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj)
+            if (j == jj)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) *(f32x4 *)(piece + (lane & 15) * kOutPitch + 16 * i + (lane >> 4) * 4) = acc[i][jj];
+        wave_sync();
+        store_rows<T, 16>(piece, g, e, m0 + wm + 16 * j, n0 + wn, lane);
+        wave_sync();
+    }
 }
 
 }  // namespace tvl

@@ -107,11 +107,9 @@ struct Epilogue {
     uint8_t    *exps;        // [m, ceil(n / 32)] step bytes (kHeld8)
     int64_t     ldr, ldy;
     int32_t     act, kind;
-    uint32_t    vec;         // rows of y, res, held and the bias start on multiples of four elements
+    uint32_t    vec;         // rows of y, res, z and the bias start on 16-byte boundaries, of codes on 8-byte ones
 };
 
-// Four consecutive outputs of row m from column n on (n a multiple of four): p = their products' sums.
-// FOUR elements exist (n + 3 < N) or only some.  Returns z.
 template <class T> __device__ __forceinline__ f32x4 load4(const T *p, int have, bool vec)
 {
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -146,72 +144,97 @@ template <class T> __device__ __forceinline__ void store4(T *p, f32x4 v, int hav
     }
 }
 
-// p: sums of products for outputs (m, n .. n+3).  have: how many of them exist (0 for a lane without work).
-// The lanes that share a block of 32 columns of one row are this lane xor the masks of `Lanes`; each of them holds
-// PER groups of four columns, group i sixteen columns after group i - 1.
-template <class T, int PER, int LANE0, int LANE1, int LANE2>
-__device__ __forceinline__ void finish_block(f32x4 (&p)[PER], int64_t m, int n, int N, bool row, const Epilogue &e)
+// Eight consecutive values from p on, the first `have` of them; vec: p lies on a 16-byte boundary.
+template <class T> __device__ __forceinline__ void load8(float (&v)[8], const T *p, int have, bool vec)
+{
+    if (have == 8 && vec) {
+        if constexpr (sizeof(T) == 2) {
+            const bf16x8 h = *(const bf16x8 *)p;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = widen(h[i]);
+        } else {
+            const f32x4 a = *(const f32x4 *)p, b = *(const f32x4 *)(p + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < have ? widen(p[i]) : 0.0f;
+    }
+}
+template <class T> __device__ __forceinline__ void store8(T *p, const float (&v)[8], int have, bool vec)
+{
+    if (have == 8 && vec) {
+        if constexpr (sizeof(T) == 2) {
+            bf16x8 h;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] = narrow<bf16>(v[i]);
+            *(bf16x8 *)p = h;
+        } else {
+            *(f32x4 *)p = f32x4{v[0], v[1], v[2], v[3]};
+            *(f32x4 *)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < have) p[i] = narrow<T>(v[i]);
+    }
+}
+
+// p: the sums of products for outputs (m, n .. n + 7), n a multiple of eight; four neighbouring lanes hold a block of
+// 32 columns of one row.  row: whether this lane has a row at all (it takes part in the block's exchanges either way).
+template <class T>
+__device__ __forceinline__ void finish8(float (&p)[8], int64_t m, int n, int N, bool row, const Epilogue &e)
 {
     constexpr bool kFast = sizeof(T) == 2;
-    constexpr int kStep = PER == 2 ? 16 : 4;
     const bool vec = e.vec != 0;
-    int have[PER];
-#pragma unroll
-    for (int i = 0; i < PER; ++i) have[i] = row ? max(0, min(4, N - (n + kStep * i))) : 0;
+    const int have = row ? max(0, min(8, N - n)) : 0;
+    float v[8];
     if (e.bias) {
+        load8(v, (const T *)e.bias + n, have, vec);
 #pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (have[i]) p[i] += load4((const T *)e.bias + n + kStep * i, have[i], vec);
+        for (int i = 0; i < 8; ++i) p[i] += v[i];
     }
     if (e.kind == kHeldPlain) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (have[i]) store4((T *)e.held + m * N + n + kStep * i, p[i], have[i], vec);
+        if (have) store8((T *)e.held + m * N + n, p, have, vec);
     } else if (e.kind == kHeldBits) {
         uint32_t w = 0;
 #pragma unroll
-        for (int i = 0; i < PER; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j < have[i] && !(p[i][j] <= 0.0f)) w |= 1u << (((n + kStep * i) & 31) + j);
-        if constexpr (LANE0) w |= __shfl_xor(w, LANE0);
-        if constexpr (LANE1) w |= __shfl_xor(w, LANE1);
-        if constexpr (LANE2) w |= __shfl_xor(w, LANE2);
-        if (have[0] && (n & 31) == 0) ((uint32_t *)e.held)[m * ((N + 31) / 32) + n / 32] = w;
+        for (int i = 0; i < 8; ++i)
+            if (i < have && !(p[i] <= 0.0f)) w |= 1u << ((n & 31) + i);
+        w |= __shfl_xor(w, 1);
+        w |= __shfl_xor(w, 2);
+        if (have && (n & 31) == 0) ((uint32_t *)e.held)[m * ((N + 31) / 32) + n / 32] = w;
     } else if (e.kind == kHeld8) {
         uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < PER; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j < have[i]) top = max(top, finite_magnitude(p[i][j]));
-        if constexpr (LANE0) top = max(top, (uint32_t)__shfl_xor(top, LANE0));
-        if constexpr (LANE1) top = max(top, (uint32_t)__shfl_xor(top, LANE1));
-        if constexpr (LANE2) top = max(top, (uint32_t)__shfl_xor(top, LANE2));
+        for (int i = 0; i < 8; ++i)
+            if (i < have) top = max(top, finite_magnitude(p[i]));
+        top = max(top, (uint32_t)__shfl_xor(top, 1));
+        top = max(top, (uint32_t)__shfl_xor(top, 2));
         const uint32_t byte = step_byte(top);
-        if (have[0] && (n & 31) == 0) e.exps[m * ((N + 31) / 32) + n / 32] = (uint8_t)byte;
+        uint32_t c[2] = {0, 0};
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            uint32_t c = 0;
+        for (int i = 0; i < 8; ++i) c[i >> 2] |= ((uint32_t)code_of(p[i], byte) & 255u) << (8 * (i & 3));
+        if (have && (n & 31) == 0) e.exps[m * ((N + 31) / 32) + n / 32] = (uint8_t)byte;
+        int8_t *to = (int8_t *)e.held + m * N + n;
+        if (have == 8 && vec) {
+            *(u32x2 *)to = u32x2{c[0], c[1]};
+        } else
 #pragma unroll
-            for (int j = 0; j < 4; ++j) c |= ((uint32_t)code_of(p[i][j], byte) & 255u) << (8 * j);
-            int8_t *to = (int8_t *)e.held + m * N + n + kStep * i;
-            if (have[i] == 4 && vec) *(uint32_t *)to = c;
-            else
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j < have[i]) to[j] = (int8_t)(c >> (8 * j));
-        }
+            for (int i = 0; i < 8; ++i)
+                if (i < have) to[i] = (int8_t)(c[i >> 2] >> (8 * (i & 3)));
     }
+    if (!have) return;
+    if (e.act != kNone)
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        if (!have[i]) continue;
-        if (e.act != kNone)
+        for (int i = 0; i < 8; ++i) p[i] = act_of<kFast>(p[i], e.act);
+    if (e.res) {
+        load8(v, (const T *)e.res + m * e.ldr + n, have, vec);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) p[i][j] = act_of<kFast>(p[i][j], e.act);
-        if (e.res) p[i] += load4((const T *)e.res + m * e.ldr + n + kStep * i, have[i], vec);
-        store4((T *)e.y + m * e.ldy + n + kStep * i, p[i], have[i], vec);
+        for (int i = 0; i < 8; ++i) p[i] += v[i];
     }
+    store8((T *)e.y + m * e.ldy + n, p, have, vec);
 }
 
 }  // namespace tvl

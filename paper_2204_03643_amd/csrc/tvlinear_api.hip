@@ -2,7 +2,7 @@
 // workspace layout and launches.
 #include "../../include/tvprox.h"
 #include "tv_ckpt8.hpp"
-#include "tv_gemm.hpp"
+#include "tv_gemm16.hpp"
 #include "tv_slope.hpp"
 
 namespace {
@@ -19,50 +19,87 @@ bool aligned(const void *p, size_t to) { return (uintptr_t)p % to == 0; }
 int launched() { return hipGetLastError() == hipSuccess ? TV_OK : TV_ERR_HIP; }
 
 // ---- products
-struct Split { int splits, k_per; };
+// One operand: rows of `cols` elements, ld apart; padded: readable, and zero, up to a multiple of eight columns.
+struct Operand {
+    const void *p;
+    int64_t ld, cols;
+    bool padded;
+};
 
-// One workgroup a compute unit at least where the contraction is long enough: each split keeps 512 indices or more.
-Split split_of(int64_t M, int64_t N, int64_t K)
+// Which kernel a product takes and how its contraction is split, from sizes and alignment alone.
+enum Kind { kAny, kTile256, kTile128 };
+struct Choice {
+    Kind kind;
+    int splits, k_per;
+};
+
+int tile_side(Kind k) { return k == kTile256 ? 256 : 128; }
+
+Choice split_for(Kind kind, int64_t M, int64_t N, int64_t K, int64_t slots, int64_t least)
 {
-    const int64_t t = tiles(M, 128) * tiles(N, 128);
-    int64_t s = t >= 256 || t < 1 ? 1 : (512 + t - 1) / t;
-    if (s > K / 512) s = K / 512;
+    const int64_t side = tile_side(kind), t = tiles(M, side) * tiles(N, side);
+    int64_t s = t >= slots || t < 1 ? 1 : (2 * slots + t - 1) / t / 2;
+    if (s > K / least) s = K / least;
     if (s < 1) s = 1;
-    const int64_t per = up(tiles(K, s), 64);
-    return {(int)(K > 0 ? tiles(K, per) : 1), (int)(per > 0 ? per : 64)};
+    const int64_t per = up(tiles(K, s), 128);
+    return {kind, (int)(K > 0 ? tiles(K, per) : 1), (int)(per > 0 ? per : 128)};
 }
 
-size_t product_bytes(int64_t M, int64_t N, int64_t K)
+Choice choose(int dtype, bool direct, int64_t M, int64_t N, int64_t K)
 {
-    const Split s = split_of(M, N, K);
-    return s.splits > 1 ? (size_t)up((int64_t)s.splits * M * up(N, 4) * 4, 256) : 0;
+    if (dtype != TV_BF16 || !direct || M < 1 || K < 1) return split_for(kAny, M, N, K, 256, 512);
+    if (tiles(M, 256) * tiles(N, 256) >= 192) return split_for(kTile256, M, N, K, 1, 512);
+    return split_for(kTile128, M, N, K, 512, 512);
+}
+
+size_t split_bytes(const Choice &c, int64_t M, int64_t N)
+{
+    return c.splits > 1 ? (size_t)up((int64_t)c.splits * M * up(N, 8) * 4, 256) : 0;
 }
 
 bool product_fits(int64_t M, int64_t N) { return tiles(M, 128) * tiles(N, 128) <= kMostTiles; }
 
-template <class T, bool AT, bool BT>
-int run_product(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t M, int64_t N, int64_t K,
-                const Epilogue &e, void *ws, hipStream_t stream)
+// Rows on 16-byte boundaries, whole 16-byte pieces, and offsets within a tile of 256 rows that 32 bits hold.
+bool direct(const Operand &o)
 {
-    const Split sp = split_of(M, N, K);
-    Product g{a, b, lda, ldb, (int32_t)M, (int32_t)N, (int32_t)K, sp.k_per, sp.splits, (float *)ws,
+    return aligned(o.p, 16) && o.ld % 8 == 0 && (o.cols % 8 == 0 || o.padded) && o.ld <= ((int64_t)1 << 22);
+}
+
+template <int SIDE, int WM, int WN, bool AT, bool BT>
+void launch16(Product g, const Epilogue &e, hipStream_t stream)
+{
+    g.tiles_m = (uint32_t)tiles(g.M, SIDE);
+    g.tiles_n = (uint32_t)tiles(g.N, SIDE);
+    hipLaunchKernelGGL((gemm16_kernel<SIDE, SIDE, WM, WN, AT, BT>), dim3(g.tiles_m * g.tiles_n, g.splits), dim3(WM * WN * 64), 0, stream, g, e);
+}
+
+template <class T, bool AT, bool BT>
+int run_product(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const Choice &c, const Epilogue &e,
+                void *ws, hipStream_t stream)
+{
+    Product g{a.p, b.p, a.ld, b.ld, (int32_t)M, (int32_t)N, (int32_t)K, c.k_per, c.splits, (float *)ws,
               (uint32_t)tiles(M, 128), (uint32_t)tiles(N, 128)};
-    hipLaunchKernelGGL((gemm_any_kernel<T, AT, BT>), dim3(g.tiles_m * g.tiles_n, sp.splits), dim3(256), 0, stream, g, e);
-    if (sp.splits > 1) {
+    if constexpr (sizeof(T) == 2) {
+        if (c.kind == kTile256) launch16<256, 2, 4, AT, BT>(g, e, stream);
+        if (c.kind == kTile128) launch16<128, 2, 2, AT, BT>(g, e, stream);
+    }
+    if (c.kind == kAny)
+        hipLaunchKernelGGL((gemm_any_kernel<T, AT, BT>), dim3(g.tiles_m * g.tiles_n, c.splits), dim3(256), 0, stream, g, e);
+    if (c.splits > 1) {
         if (launched() != TV_OK) return TV_ERR_HIP;
-        hipLaunchKernelGGL((join_kernel<T>), dim3((uint32_t)tiles(M * tiles(N, 32) * 8, 256)), dim3(256), 0, stream, g, e);
+        hipLaunchKernelGGL((join_kernel<T>), dim3((uint32_t)tiles(M * tiles(N, 32) * 4, 256)), dim3(256), 0, stream, g, e);
     }
     return launched();
 }
 
-// Rows of four elements at once where every row of every array the epilogue touches starts on such a boundary.
+// Eight columns at once where every row of every array that the epilogue touches starts on such a boundary.
 uint32_t epilogue_vec(const Epilogue &e, size_t size, int64_t N)
 {
-    if (N % 4 || e.ldy % 4 || !aligned(e.y, 4 * size)) return 0;
-    if (e.res && (e.ldr % 4 || !aligned(e.res, 4 * size))) return 0;
-    if (e.bias && !aligned(e.bias, 4 * size)) return 0;
-    if (e.held && !aligned(e.held, e.kind == kHeldPlain ? 4 * size : 4)) return 0;
-    return 1;
+    const int64_t per = 16 / (int64_t)size;
+    if (N % 8 || e.ldy % per || !aligned(e.y, 16)) return 0;
+    if (e.res && (e.ldr % per || !aligned(e.res, 16))) return 0;
+    if (!aligned(e.bias, 16)) return 0;
+    return aligned(e.held, e.kind == kHeldPlain ? 16 : 8) || e.kind == kHeldBits;
 }
 
 Epilogue plain_output(void *y, int64_t ldy, size_t size, int64_t N)
@@ -108,6 +145,19 @@ int check_workspace(const void *ws, size_t have, size_t need)
     return need && (!ws || !aligned(ws, 16) || have < need) ? TV_ERR_WORKSPACE : TV_OK;
 }
 
+Choice fwd_choice(const tv_linear_desc &d, const void *x, const void *w)
+{
+    return choose(d.dtype, direct({x, d.ldx, d.k, false}) && direct({w, d.ldw, d.k, false}), d.m, d.n, d.k);
+}
+
+// (The workspace is asked for before there are pointers, and has to do for either choice.)
+size_t fwd_bytes(const tv_linear_desc &d)
+{
+    const size_t a = split_bytes(choose(d.dtype, true, d.m, d.n, d.k), d.m, d.n);
+    const size_t b = split_bytes(choose(d.dtype, false, d.m, d.n, d.k), d.m, d.n);
+    return a > b ? a : b;
+}
+
 template <class T>
 int linear_fwd(const void *x, const void *w, const void *bias, const void *res, void *y, const tv_held &h,
                const tv_linear_desc &d, void *ws, hipStream_t stream)
@@ -117,7 +167,7 @@ int linear_fwd(const void *x, const void *w, const void *bias, const void *res, 
     e.held = h.kind == TV_HELD_NONE ? nullptr : h.data; e.exps = h.exps;
     e.ldr = d.ldr; e.ldy = d.ldy; e.act = d.act; e.kind = h.kind;
     e.vec = epilogue_vec(e, sizeof(T), d.n);
-    return run_product<T, false, false>(x, d.ldx, w, d.ldw, d.m, d.n, d.k, e, ws, stream);
+    return run_product<T, false, false>({x, d.ldx, d.k, false}, {w, d.ldw, d.k, false}, d.m, d.n, d.k, fwd_choice(d, x, w), e, ws, stream);
 }
 
 // ---- the backward call's workspace: dz, x out of its checkpoint, the column sums of groups of rows, split sums
@@ -145,8 +195,14 @@ BwdPlan bwd_plan(const tv_linear_desc &d, bool x8)
     p.sums = at;
     at += up((int64_t)p.groups * d.n * 4, 256);
     p.split = at;
-    const size_t s1 = product_bytes(d.m, d.k, d.n), s2 = product_bytes(d.n, d.k, d.m);
-    p.bytes = at + (s1 > s2 ? s1 : s2);
+    size_t most = 0;
+    for (bool dir : {false, true}) {
+        const size_t s1 = split_bytes(choose(d.dtype, dir, d.m, d.k, d.n), d.m, d.k);
+        const size_t s2 = split_bytes(choose(d.dtype, dir, d.n, d.k, d.m), d.n, d.k);
+        most = most > s1 ? most : s1;
+        most = most > s2 ? most : s2;
+    }
+    p.bytes = at + most;
     return p;
 }
 
@@ -155,8 +211,7 @@ int linear_bwd(const void *g, const void *x, const uint8_t *x_exps, const tv_hel
                void *db, const tv_linear_desc &d, char *ws, hipStream_t stream)
 {
     const BwdPlan p = bwd_plan(d, x_exps != nullptr);
-    const void *dz = g;
-    int64_t ldz = d.ldy;
+    Operand dz{g, d.ldy, d.n, false};
     if (d.m > 0 && (d.act != TV_ACT_NONE || db)) {
         SlopeArgs a{};
         a.g = g; a.held = h.data; a.exps = h.exps;
@@ -169,7 +224,7 @@ int linear_bwd(const void *g, const void *x, const uint8_t *x_exps, const tv_hel
                 aligned(h.data, a.kind == kHeldPlain ? 4 * sizeof(T) : 4);
         hipLaunchKernelGGL((slope_kernel<T>), dim3((uint32_t)tiles(d.n, 256), p.groups), dim3(256), 0, stream, a);
         if (launched() != TV_OK) return TV_ERR_HIP;
-        if (a.dz) { dz = a.dz; ldz = p.ldz; }
+        if (a.dz) dz = {a.dz, p.ldz, d.n, false};
     }
     if (db) {
         hipLaunchKernelGGL((column_sum_kernel<T>), dim3((uint32_t)tiles(d.n, 256)), dim3(256), 0, stream,
@@ -177,20 +232,20 @@ int linear_bwd(const void *g, const void *x, const uint8_t *x_exps, const tv_hel
         if (launched() != TV_OK) return TV_ERR_HIP;
     }
     if (dx && d.m > 0) {
-        const int st = run_product<T, false, true>(dz, ldz, w, d.ldw, d.m, d.k, d.n, plain_output(dx, d.k, sizeof(T), d.k),
-                                                   ws + p.split, stream);
+        const Operand ow{w, d.ldw, d.k, false};
+        const int st = run_product<T, false, true>(dz, ow, d.m, d.k, d.n, choose(d.dtype, direct(dz) && direct(ow), d.m, d.k, d.n),
+                                                   plain_output(dx, d.k, sizeof(T), d.k), ws + p.split, stream);
         if (st != TV_OK) return st;
     }
     if (dw) {
-        const void *xs = x;
-        int64_t ldx = d.ldx;
+        Operand xs{x, d.ldx, d.k, false};
         if (x_exps && d.m > 0) {
             const int st = tv_ckpt8_load((const int8_t *)x, x_exps, ws + p.x, d.m, d.k, p.ldx, d.dtype, stream);
             if (st != TV_OK) return st;
-            xs = ws + p.x; ldx = p.ldx;
+            xs = {ws + p.x, p.ldx, d.k, false};
         }
-        return run_product<T, true, true>(dz, ldz, xs, ldx, d.n, d.k, d.m, plain_output(dw, d.k, sizeof(T), d.k),
-                                          ws + p.split, stream);
+        return run_product<T, true, true>(dz, xs, d.n, d.k, d.m, choose(d.dtype, direct(dz) && direct(xs), d.n, d.k, d.m),
+                                          plain_output(dw, d.k, sizeof(T), d.k), ws + p.split, stream);
     }
     return TV_OK;
 }
@@ -216,7 +271,7 @@ extern "C" {
 
 size_t tv_linear_fwd_workspace_bytes(tv_linear_desc d)
 {
-    return check_sizes(d) == TV_OK ? product_bytes(d.m, d.n, d.k) : 0;
+    return check_sizes(d) == TV_OK ? fwd_bytes(d) : 0;
 }
 
 int tv_linear_fwd(const void *x, const void *w, const void *bias, const void *res, void *y, tv_held held,
@@ -230,7 +285,7 @@ int tv_linear_fwd(const void *x, const void *w, const void *bias, const void *re
     if (!x || !w || !y) return TV_ERR_NULL;
     const size_t size = elem_bytes(d.dtype);
     if (!aligned(x, size) || !aligned(w, size) || !aligned(bias, size) || !aligned(res, size) || !aligned(y, size)) return TV_ERR_STRIDE;
-    if ((st = check_workspace(ws, ws_bytes, product_bytes(d.m, d.n, d.k))) != TV_OK) return st;
+    if ((st = check_workspace(ws, ws_bytes, fwd_bytes(d))) != TV_OK) return st;
     return d.dtype == TV_BF16 ? linear_fwd<bf16>(x, w, bias, res, y, held, d, ws, stream)
                               : linear_fwd<float>(x, w, bias, res, y, held, d, ws, stream);
 }
