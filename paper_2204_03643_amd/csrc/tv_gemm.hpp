@@ -43,14 +43,20 @@ template <class T> __device__ __forceinline__ u32x4 load16(const T *p, int have)
         else return *(const u32x4_at2 *)p;
     }
     u32x4 v = {0, 0, 0, 0};
+    if (have <= 0) return v;
+    // (every load from an element that exists, so that none of them waits for a branch)
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int i = 0; i < E; ++i)
-            if (i < have) v[i] = __float_as_uint(p[i]);
+        for (int i = 0; i < E; ++i) {
+            const uint32_t w = __float_as_uint(p[min(i, have - 1)]);
+            v[i] = i < have ? w : 0u;
+        }
     } else {
 #pragma unroll
-        for (int i = 0; i < E; ++i)
-            if (i < have) v[i >> 1] |= (uint32_t)((const uint16_t *)p)[i] << (16 * (i & 1));
+        for (int i = 0; i < E; ++i) {
+            const uint32_t w = ((const uint16_t *)p)[min(i, have - 1)];
+            v[i >> 1] |= (i < have ? w : 0u) << (16 * (i & 1));
+        }
     }
     return v;
 }
@@ -66,27 +72,39 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_wave_barrier();
 }
 
-template <class T, int R>
+// PLAIN: the epilogue only rounds (the gradients' products).
+template <class T, int R, bool PLAIN>
 __device__ __forceinline__ void store_rows(const float *piece, const Product &g, const Epilogue &e, int m0, int n0, int lane)
 {
-    const int64_t pitch = (g.N + 7) & ~7;
     const int n = n0 + (lane & 7) * 8;
+    const float *from = piece + (lane >> 3) * kOutPitch + (lane & 7) * 8;
+    if (g.splits > 1) {
+        const int64_t pitch = (g.N + 7) & ~7;
+        float *to = g.partial + ((int64_t)blockIdx.y * g.M + m0 + (lane >> 3)) * pitch + n;
+#pragma unroll
+        for (int i = 0; i < R / 8; ++i)
+            if (m0 + i * 8 + (lane >> 3) < g.M && n < g.N) {
+                *(f32x4 *)(to + i * 8 * pitch) = *(const f32x4 *)(from + i * 8 * kOutPitch);
+                *(f32x4 *)(to + i * 8 * pitch + 4) = *(const f32x4 *)(from + i * 8 * kOutPitch + 4);
+            }
+        return;
+    }
+    if (PLAIN && e.vec && m0 + R <= g.M && n0 + 64 <= g.N) {
+        T *to = (T *)e.y + (int64_t)(m0 + (lane >> 3)) * e.ldy + n;
+#pragma unroll
+        for (int i = 0; i < R / 8; ++i) {
+            const f32x4 a = *(const f32x4 *)(from + i * 8 * kOutPitch), b = *(const f32x4 *)(from + i * 8 * kOutPitch + 4);
+            const float p[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+            store8(to + i * 8 * e.ldy, p, 8, true);
+        }
+        return;
+    }
 #pragma unroll 1
     for (int i = 0; i < R / 8; ++i) {
-        const int r = i * 8 + (lane >> 3);
-        const int64_t m = m0 + r;
-        const f32x4 a = *(const f32x4 *)(piece + r * kOutPitch + (lane & 7) * 8);
-        const f32x4 b = *(const f32x4 *)(piece + r * kOutPitch + (lane & 7) * 8 + 4);
-        if (g.splits > 1) {
-            if (m < g.M && n < g.N) {
-                float *to = g.partial + ((int64_t)blockIdx.y * g.M + m) * pitch + n;
-                *(f32x4 *)to = a;
-                *(f32x4 *)(to + 4) = b;
-            }
-        } else {
-            float p[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-            finish8<T>(p, m, n, g.N, m < g.M, e);
-        }
+        const int64_t m = m0 + i * 8 + (lane >> 3);
+        const f32x4 a = *(const f32x4 *)(from + i * 8 * kOutPitch), b = *(const f32x4 *)(from + i * 8 * kOutPitch + 4);
+        float p[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        finish8<T>(p, m, n, g.N, m < g.M, e);
     }
 }
 
@@ -212,7 +230,7 @@ __global__ __launch_bounds__(256) void gemm_any_kernel(Product g, Epilogue e)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) *(f32x4 *)(piece + (lane & 15) * kOutPitch + 16 * i + (lane >> 4) * 4) = acc[i][jj];
         wave_sync();
-        store_rows<T, 16>(piece, g, e, m0 + wm + 16 * j, n0 + wn, lane);
+        store_rows<T, 16, AT || BT>(piece, g, e, m0 + wm + 16 * j, n0 + wn, lane);
         wave_sync();
     }
 }

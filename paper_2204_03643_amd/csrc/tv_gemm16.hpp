@@ -2,6 +2,7 @@
 // through registers, two buffers in turn, 32 x 32 x 16 matrix instructions.
 #pragma once
 #include "tv_gemm.hpp"
+#include <type_traits>
 
 namespace tvl {
 
@@ -16,12 +17,15 @@ __device__ __attribute__((aligned(16))) uint32_t zeros16[4];       // what a lan
 //
 // transposed (the output index contiguous): LDS holds ROWS values of one k after those of the next, as in memory; the
 // transposing LDS read hands each lane four k of its column.  A read takes 64 bytes of four rows k % 4 (and of four more,
-// eight further on, in the second half of the wave): 64-byte piece p of row k lies in slot p ^ (k % 4).
+// eight further on, in the second half of the wave): 64-byte piece p of row k lies in slot p ^ (k % 4), so that the four lie
+// in different banks.  (Rows of 64 values have two pieces, and two rows fill the banks: p ^ (k / 2 % 2).)
 template <int ROWS, int WAVES, bool TRANSPOSED> struct Tile16 {
     static constexpr int kLoads = ROWS * 128 / 1024 / WAVES;       // 1024 bytes a load of a wave
     static constexpr int kPieces = ROWS / 8;                       // 16-byte pieces of one k (transposed)
     uint32_t off[kLoads];        // bytes from the tile's origin in memory
     int32_t  k[kLoads];          // contraction index of the lane's piece within a tile
+
+    __device__ __forceinline__ static int swizzle(int kk) { return ROWS >= 128 ? (kk & 3) << 2 : (kk & 2) << 1; }
 
     // rows: how many output indices there are from the tile's origin on (at least one)
     __device__ __forceinline__ void setup(uint32_t ld, int rows, int wave, int lane)
@@ -34,7 +38,7 @@ template <int ROWS, int WAVES, bool TRANSPOSED> struct Tile16 {
                 k[j] = c * 8;
                 off[j] = ((uint32_t)min(r, rows - 1) * ld + (uint32_t)c * 8) * 2;
             } else {
-                const int kk = at / kPieces, c = (at % kPieces) ^ ((kk & 3) << 2);
+                const int kk = at / kPieces, c = (at % kPieces) ^ swizzle(kk);
                 k[j] = kk;
                 off[j] = ((uint32_t)kk * ld + (c * 8 < rows ? (uint32_t)c * 8 : 0u)) * 2;
             }
@@ -62,7 +66,7 @@ template <int ROWS, int WAVES, bool TRANSPOSED> struct Tile16 {
         } else {
             const int kk = q * 16 + (lane >> 5) * 8 + ((lane >> 2) & 3);
             const int col = row + (lane & 16) + (lane & 3) * 4;    // this lane's four columns of row kk
-            const char *p = lds + kk * (ROWS * 2) + (((col >> 3) ^ ((kk & 3) << 2)) << 4) + (col & 4) * 2;
+            const char *p = lds + kk * (ROWS * 2) + (((col >> 3) ^ swizzle(kk)) << 4) + (col & 4) * 2;
             typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p);
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 4 * ROWS * 2));
@@ -84,26 +88,43 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tm, uint32_t tn, u
     n = in / rows;
 }
 
-// BM x BN outputs a workgroup of WM x WN waves.
-template <int BM, int BN, int WM, int WN, bool AT, bool BT>
+// Waits until at most N of this wave's loads are on their way and its LDS reads have ended, then for all waves.
+template <int N> __device__ __forceinline__ void turn()
+{
+    static_assert(N < 64, "");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4) << 14);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// BM x BN outputs a workgroup of WM x WN waves, BUF buffers of 64 contraction indices.
+//
+// The contraction goes in steps of 64, each four times 16.  While the matrix instructions of one sixteen run, the LDS
+// reads of the next are on their way; the barrier that hands a step's buffer over stands in the middle of the
+// matrix instructions of its last sixteen, whose operands are in registers by then, so that the first reads of the next step
+// and the loads into the freed buffer start behind running matrix instructions too.
+template <int BM, int BN, int WM, int WN, int BUF, bool AT, bool BT>
 __global__ __launch_bounds__(WM * WN * 64) void gemm16_kernel(Product g, Epilogue e)
 {
     constexpr int W = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
-    constexpr int kA = BM * 128, kB = BN * 128, kOut = W / 2 * 32 * kOutPitch * 4;
-    static_assert(TN == 2, "a wave's outputs are 64 columns wide");
-    static_assert(kOut <= kA + kB, "the outputs' pieces fit a buffer");
-    __shared__ __attribute__((aligned(1024))) char even[kA + kB];
-    __shared__ __attribute__((aligned(1024))) char odd[kA + kB];
+    constexpr int kA = BM * 128, kB = BN * 128, kOut = W * 32 * kOutPitch * 4;
+    static_assert(TN % 2 == 0, "a wave's outputs leave 64 columns at a time");
+    static_assert(kOut <= BUF * (kA + kB), "the outputs' pieces fit");
+    __shared__ __attribute__((aligned(1024))) char lds[BUF][kA + kB];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t tm, tn;
     tile_of(blockIdx.x, g.tiles_m, g.tiles_n, tm, tn);
     const int m0 = (int)tm * BM, n0 = (int)tn * BN;
     const int k0 = (int)blockIdx.y * g.k_per, k_end = min(g.K, k0 + g.k_per);
-    const int steps = (k_end - k0 + 63) / 64;
+    const int steps = (k_end - k0 + 63) / 64, whole = (k_end - k0) / 64;
     const int wm = wave % WM * (BM / WM), wn = wave / WM * (BN / WN);
 
-    Tile16<BM, W, AT> ta;
-    Tile16<BN, W, BT> tb;
+    using TileA = Tile16<BM, W, AT>;
+    using TileB = Tile16<BN, W, BT>;
+    constexpr int kLoads = TileA::kLoads + TileB::kLoads;
+    TileA ta;
+    TileB tb;
     ta.setup((uint32_t)g.lda, g.M - m0, wave, lane);
     tb.setup((uint32_t)g.ldb, g.N - n0, wave, lane);
     const char *pa = (const char *)g.a + (AT ? (int64_t)k0 * g.lda + m0 : (int64_t)m0 * g.lda + k0) * 2;
@@ -117,65 +138,104 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm16_kernel(Product g, Epilogu
         for (int j = 0; j < TM; ++j)
 #pragma unroll
             for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.0f;
+    bf16x8 fa[2][TM], fb[2][TN];
+#pragma unroll
+    for (int j = 0; j < TM; ++j) fa[1][j] = bf16x8{};
+#pragma unroll
+    for (int i = 0; i < TN; ++i) fb[1][i] = bf16x8{};
 
-    auto issue = [&](int s, char *to) {
+    // loads of one step, in order of steps; all of it is there (WHOLE) or zeros stand for what is not
+    auto issue = [&](auto all, int s, char *to) {
+        constexpr bool WHOLE = decltype(all)::value;
         const int left = k_end - k0 - s * 64;
-        if (left >= 64) {
-            ta.template load<true>(pa, to, left, wave);
-            tb.template load<true>(pb, to + kA, left, wave);
-        } else {
-            ta.template load<false>(pa, to, left, wave);
-            tb.template load<false>(pb, to + kA, left, wave);
-        }
+        ta.template load<WHOLE>(pa, to, left, wave);
+        tb.template load<WHOLE>(pb, to + kA, left, wave);
         pa += step_a;
         pb += step_b;
     };
-    auto compute = [&](const char *from) {
+    auto read = [&](const char *from, int q, int set) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            bf16x8 fa[TM], fb[TN];
+        for (int i = 0; i < TN; ++i) fb[set][i] = TileB::read(from + kA, wn + 32 * i, q, lane);
 #pragma unroll
-            for (int i = 0; i < TN; ++i) fb[i] = Tile16<BN, W, BT>::read(from + kA, wn + 32 * i, q, lane);
+        for (int j = 0; j < TM; ++j) fa[set][j] = TileA::read(from, wm + 32 * j, q, lane);
+    };
+    auto multiply = [&](int set, int first, int last) {          // the set's matrix instructions first .. last - 1
 #pragma unroll
-            for (int j = 0; j < TM; ++j) fa[j] = Tile16<BM, W, AT>::read(from, wm + 32 * j, q, lane);
+        for (int x = 0; x < TM * TN; ++x)
+            if (x >= first && x < last)
+                acc[x % TN][x / TN] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[set][x % TN], fa[set][x / TN], acc[x % TN][x / TN], 0, 0, 0);
+    };
+    constexpr int kAll = TM * TN, kHalf = kAll / 2;
+    // the order of a run of matrix instructions and of what goes behind them: the LDS reads, two after each at least, and
+    // the next loads, spread over the step's first one and a half sixteens
+    auto order = [&](auto count, auto with_loads) {
+        constexpr int kReads = TM * (AT ? 2 : 1) + TN * (BT ? 2 : 1);
+        constexpr int n = decltype(count)::value, kEach = (kReads + n - 1) / n > 2 ? (kReads + n - 1) / n : 2;
+        constexpr int kLoadsEach = (kLoads + kAll + kHalf - 1) / (kAll + kHalf);
 #pragma unroll
-            for (int j = 0; j < TM; ++j)
-#pragma unroll
-                for (int i = 0; i < TN; ++i)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[i], fa[j], acc[i][j], 0, 0, 0);
+        for (int x = 0; x < n; ++x) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (x * kEach < kReads) __builtin_amdgcn_sched_group_barrier(0x100, kEach, 0);
+            if constexpr (decltype(with_loads)::value) __builtin_amdgcn_sched_group_barrier(0x010, kLoadsEach, 0);
         }
     };
-    // a buffer's loads have landed, and nobody reads the other buffer any more
-    auto turn = [&] {
-        __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0)
-        __syncthreads();
+    // (`to` and `from` are told apart by __restrict: otherwise the compiler takes every LDS read for one of what is still
+    // being loaded, and waits for all loads)
+    auto step = [&](auto all, char *__restrict to, const char *__restrict from, int s) {
+        read(from, 0, 0);
+        multiply(1, kHalf, kAll);
+        if (decltype(all)::value || s - 1 + BUF < steps) issue(all, s - 1 + BUF, to);
+        order(std::integral_constant<int, kAll - kHalf>{}, all);
+        read(from, 1, 1);
+        multiply(0, 0, kAll);
+        order(std::integral_constant<int, kAll>{}, all);
+#pragma unroll
+        for (int q = 1; q < 3; ++q) {
+            read(from, q + 1, (q + 1) & 1);
+            multiply(q & 1, 0, kAll);
+            order(std::integral_constant<int, kAll>{}, std::false_type{});
+        }
+        multiply(1, 0, kHalf);
     };
-
-    // two steps a turn of the loop, one a buffer; past the end a step of zeros
-    issue(0, even);
-    for (int s = 0; s < steps; s += 2) {
-        turn();
-        issue(s + 1, odd);
-        compute(even);
-        turn();
-        if (s + 2 < steps) issue(s + 2, even);
-        compute(odd);
+#pragma unroll
+    for (int s = 0; s < BUF - 1; ++s)
+        if (s < whole) issue(std::true_type{}, s, lds[s]);
+        else if (s < steps) issue(std::false_type{}, s, lds[s]);
+    if (steps >= BUF - 1) turn<(BUF - 2) * kLoads>();
+    else turn<0>();
+    // step s's loads are this wave's oldest: they have landed when no more than those of the steps after it are on their
+    // way; behind the barrier everybody's have, and nobody reads the buffer of step s - 1 any more
+    int fill = BUF - 1, from = 0, s = 0;
+    for (; s - 1 + BUF < whole; ++s) {
+        step(std::true_type{}, lds[fill], lds[from], s);
+        turn<(BUF - 2) * kLoads>();
+        fill = from;
+        from = from + 1 == BUF ? 0 : from + 1;
     }
-    __syncthreads();
-    float *piece = (float *)(wave & 1 ? odd : even) + (wave >> 1) * 32 * kOutPitch;
+    for (; s < steps; ++s) {
+        step(std::false_type{}, lds[fill], lds[from], s);
+        turn<0>();
+        fill = from;
+        from = from + 1 == BUF ? 0 : from + 1;
+    }
+    multiply(1, kHalf, kAll);
+
+    float *piece = (float *)lds + wave * 32 * kOutPitch;
 #pragma unroll 1
-    for (int j = 0; j < TM; ++j) {                    // one copy of the epilogue's code, and of its registers
+    for (int x = 0; x < TM * TN / 2; ++x) {           // one copy of the epilogue's code, and of its registers
 #pragma unroll
-        for (int jj = 0; jj < TM; ++jj)
-            if (j == jj)
+        for (int y = 0; y < TM * TN / 2; ++y)
+            if (x == y)
 #pragma unroll
-                for (int i = 0; i < TN; ++i)
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x16 &a = acc[y / TM * 2 + i][y % TM];
                         *(f32x4 *)(piece + (lane & 31) * kOutPitch + 32 * i + q * 8 + (lane >> 5) * 4) =
-                            f32x4{acc[i][jj][4 * q], acc[i][jj][4 * q + 1], acc[i][jj][4 * q + 2], acc[i][jj][4 * q + 3]};
+                            f32x4{a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
+                    }
         wave_sync();
-        store_rows<bf16, 32>(piece, g, e, m0 + wm + 32 * j, n0 + wn, lane);
+        store_rows<bf16, 32, AT || BT>(piece, g, e, m0 + wm + x % TM * 32, n0 + wn + x / TM * 64, lane);
         wave_sync();
     }
 }

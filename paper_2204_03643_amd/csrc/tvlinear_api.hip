@@ -3,6 +3,7 @@
 #include "../../include/tvprox.h"
 #include "tv_ckpt8.hpp"
 #include "tv_gemm16.hpp"
+#include "tv_gemv.hpp"
 #include "tv_slope.hpp"
 
 namespace {
@@ -26,30 +27,72 @@ struct Operand {
     bool padded;
 };
 
+constexpr int64_t kFewRows = 64;
+
 // Which kernel a product takes and how its contraction is split, from sizes and alignment alone.
-enum Kind { kAny, kTile256, kTile128 };
+enum Kind { kAny, kFew, kTile256, kTile128, kTile128Deep, kTile64 };
 struct Choice {
     Kind kind;
     int splits, k_per;
 };
 
-int tile_side(Kind k) { return k == kTile256 ? 256 : 128; }
+struct Tile { int m, n; };
+Tile tile_of_kind(Kind k)
+{
+    if (k == kTile256) return {256, 256};
+    if (k == kTile64) return {64, 128};
+    return {128, 128};
+}
+
+int64_t few_columns(int64_t) { return 32; }
+
+// `s` splits of a contraction of K, each a multiple of `unit`
+Choice cut(Kind kind, int64_t s, int64_t K, int64_t unit)
+{
+    if (s < 1) s = 1;
+    const int64_t per = up(K > 0 ? tiles(K, s) : 1, unit);
+    return {kind, (int)(K > 0 ? tiles(K, per) : 1), (int)per};
+}
 
 Choice split_for(Kind kind, int64_t M, int64_t N, int64_t K, int64_t slots, int64_t least)
 {
-    const int64_t side = tile_side(kind), t = tiles(M, side) * tiles(N, side);
-    int64_t s = t >= slots || t < 1 ? 1 : (2 * slots + t - 1) / t / 2;
-    if (s > K / least) s = K / least;
-    if (s < 1) s = 1;
-    const int64_t per = up(tiles(K, s), 128);
-    return {kind, (int)(K > 0 ? tiles(K, per) : 1), (int)(per > 0 ? per : 128)};
+    const Tile side = tile_of_kind(kind);
+    const int64_t t = tiles(M, side.m) * tiles(N, side.n);
+    int64_t s = t >= slots || t < 1 ? 1 : slots / t;
+    return cut(kind, s < K / least ? s : K / least, K, 64);
 }
 
-Choice choose(int dtype, bool direct, int64_t M, int64_t N, int64_t K)
+Choice choose(int dtype, bool direct, bool transposed, int64_t M, int64_t N, int64_t K)
 {
-    if (dtype != TV_BF16 || !direct || M < 1 || K < 1) return split_for(kAny, M, N, K, 256, 512);
-    if (tiles(M, 256) * tiles(N, 256) >= 192) return split_for(kTile256, M, N, K, 1, 512);
-    return split_for(kTile128, M, N, K, 512, 512);
+    if (!transposed && M >= 1 && M <= (direct && dtype == TV_BF16 ? kFewRows / 2 : kFewRows)) {
+        const int64_t turn = 8 * 64 / (int64_t)elem_bytes(dtype);            // a turn of all eight waves
+        const int64_t t = tiles(N, few_columns(M));
+        const int64_t s = t >= 256 ? 1 : 256 / t;
+        return cut(kFew, s < K / (8 * turn) ? s : K / (8 * turn), K, turn);
+    }
+    if (dtype != TV_BF16) return split_for(kAny, M, N, K, 512, 128);
+    if (!direct || M < 1 || K < 1) return split_for(kAny, M, N, K, 256, 512);
+    /*SWEEP*/
+    // The cheapest by a model of the time in microseconds, fitted to sweeps of tiles and splits over outputs of
+    // 128 x 128 to 8192 x 8192 and contractions of 64 to 8192: a launch, rounds of workgroups over 256 compute units (of
+    // two 128 x 128 workgroups each where there are more tiles than units), in each a start and an end and so much a step
+    // of 64, and for split contractions the second launch and the sums' trip through memory.
+    struct Cost { Kind kind; int64_t slots; double round, step; };
+    constexpr Cost costs[] = {{kTile64, 256, 1.0, 0.30}, {kTile128Deep, 256, 2.0, 0.47}, {kTile128, 512, 3.0, 0.88}, {kTile256, 256, 6.5, 1.50}};
+    Choice best{};
+    double least = 1e30;
+    for (const Cost &c : costs) {
+        const Tile side = tile_of_kind(c.kind);
+        const int64_t t = tiles(M, side.m) * tiles(N, side.n);
+        for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+            if (s > 1 && (K < 128 * s || t * s > 1024)) break;
+            const Choice x = cut(c.kind, s, K, 64);
+            double us = 3.0 + (double)tiles(t * x.splits, c.slots) * (c.round + c.step * (double)tiles(x.k_per < K ? x.k_per : K, 64));
+            if (x.splits > 1) us += 5.0 + (double)M * (double)N * x.splits * 8 / 4e6;
+            if (us < least) { least = us; best = x; }
+        }
+    }
+    return best;
 }
 
 size_t split_bytes(const Choice &c, int64_t M, int64_t N)
@@ -65,12 +108,12 @@ bool direct(const Operand &o)
     return aligned(o.p, 16) && o.ld % 8 == 0 && (o.cols % 8 == 0 || o.padded) && o.ld <= ((int64_t)1 << 22);
 }
 
-template <int SIDE, int WM, int WN, bool AT, bool BT>
+template <int BM, int BN, int WM, int WN, int BUF, bool AT, bool BT>
 void launch16(Product g, const Epilogue &e, hipStream_t stream)
 {
-    g.tiles_m = (uint32_t)tiles(g.M, SIDE);
-    g.tiles_n = (uint32_t)tiles(g.N, SIDE);
-    hipLaunchKernelGGL((gemm16_kernel<SIDE, SIDE, WM, WN, AT, BT>), dim3(g.tiles_m * g.tiles_n, g.splits), dim3(WM * WN * 64), 0, stream, g, e);
+    g.tiles_m = (uint32_t)tiles(g.M, BM);
+    g.tiles_n = (uint32_t)tiles(g.N, BN);
+    hipLaunchKernelGGL((gemm16_kernel<BM, BN, WM, WN, BUF, AT, BT>), dim3(g.tiles_m * g.tiles_n, g.splits), dim3(WM * WN * 64), 0, stream, g, e);
 }
 
 template <class T, bool AT, bool BT>
@@ -80,9 +123,18 @@ int run_product(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_
     Product g{a.p, b.p, a.ld, b.ld, (int32_t)M, (int32_t)N, (int32_t)K, c.k_per, c.splits, (float *)ws,
               (uint32_t)tiles(M, 128), (uint32_t)tiles(N, 128)};
     if constexpr (sizeof(T) == 2) {
-        if (c.kind == kTile256) launch16<256, 2, 4, AT, BT>(g, e, stream);
-        if (c.kind == kTile128) launch16<128, 2, 2, AT, BT>(g, e, stream);
+        if (c.kind == kTile256) launch16<256, 256, 2, 4, 2, AT, BT>(g, e, stream);
+        if (c.kind == kTile128) launch16<128, 128, 2, 2, 2, AT, BT>(g, e, stream);
+        if (c.kind == kTile128Deep) launch16<128, 128, 2, 2, 4, AT, BT>(g, e, stream);
+        if (c.kind == kTile64) launch16<64, 128, 2, 2, 4, AT, BT>(g, e, stream);
     }
+    if constexpr (!AT && !BT)
+        if (c.kind == kFew) {
+            const dim3 grid((uint32_t)tiles(N, few_columns(M)), c.splits), block(512);
+            if (M <= 16) hipLaunchKernelGGL((gemv_kernel<T, 1, 2, 8>), grid, block, 0, stream, g, e);
+            else if (M <= 32) hipLaunchKernelGGL((gemv_kernel<T, 2, 2, 8>), grid, block, 0, stream, g, e);
+            else hipLaunchKernelGGL((gemv_kernel<T, 4, 2, 4>), grid, block, 0, stream, g, e);
+        }
     if (c.kind == kAny)
         hipLaunchKernelGGL((gemm_any_kernel<T, AT, BT>), dim3(g.tiles_m * g.tiles_n, c.splits), dim3(256), 0, stream, g, e);
     if (c.splits > 1) {
@@ -147,14 +199,14 @@ int check_workspace(const void *ws, size_t have, size_t need)
 
 Choice fwd_choice(const tv_linear_desc &d, const void *x, const void *w)
 {
-    return choose(d.dtype, direct({x, d.ldx, d.k, false}) && direct({w, d.ldw, d.k, false}), d.m, d.n, d.k);
+    return choose(d.dtype, direct({x, d.ldx, d.k, false}) && direct({w, d.ldw, d.k, false}), false, d.m, d.n, d.k);
 }
 
 // (The workspace is asked for before there are pointers, and has to do for either choice.)
 size_t fwd_bytes(const tv_linear_desc &d)
 {
-    const size_t a = split_bytes(choose(d.dtype, true, d.m, d.n, d.k), d.m, d.n);
-    const size_t b = split_bytes(choose(d.dtype, false, d.m, d.n, d.k), d.m, d.n);
+    const size_t a = split_bytes(choose(d.dtype, true, false, d.m, d.n, d.k), d.m, d.n);
+    const size_t b = split_bytes(choose(d.dtype, false, false, d.m, d.n, d.k), d.m, d.n);
     return a > b ? a : b;
 }
 
@@ -197,8 +249,8 @@ BwdPlan bwd_plan(const tv_linear_desc &d, bool x8)
     p.split = at;
     size_t most = 0;
     for (bool dir : {false, true}) {
-        const size_t s1 = split_bytes(choose(d.dtype, dir, d.m, d.k, d.n), d.m, d.k);
-        const size_t s2 = split_bytes(choose(d.dtype, dir, d.n, d.k, d.m), d.n, d.k);
+        const size_t s1 = split_bytes(choose(d.dtype, dir, true, d.m, d.k, d.n), d.m, d.k);
+        const size_t s2 = split_bytes(choose(d.dtype, dir, true, d.n, d.k, d.m), d.n, d.k);
         most = most > s1 ? most : s1;
         most = most > s2 ? most : s2;
     }
@@ -233,7 +285,7 @@ int linear_bwd(const void *g, const void *x, const uint8_t *x_exps, const tv_hel
     }
     if (dx && d.m > 0) {
         const Operand ow{w, d.ldw, d.k, false};
-        const int st = run_product<T, false, true>(dz, ow, d.m, d.k, d.n, choose(d.dtype, direct(dz) && direct(ow), d.m, d.k, d.n),
+        const int st = run_product<T, false, true>(dz, ow, d.m, d.k, d.n, choose(d.dtype, direct(dz) && direct(ow), true, d.m, d.k, d.n),
                                                    plain_output(dx, d.k, sizeof(T), d.k), ws + p.split, stream);
         if (st != TV_OK) return st;
     }
@@ -244,7 +296,7 @@ int linear_bwd(const void *g, const void *x, const uint8_t *x_exps, const tv_hel
             if (st != TV_OK) return st;
             xs = {ws + p.x, p.ldx, d.k, false};
         }
-        return run_product<T, true, true>(dz, xs, d.n, d.k, d.m, choose(d.dtype, direct(dz) && direct(xs), d.n, d.k, d.m),
+        return run_product<T, true, true>(dz, xs, d.n, d.k, d.m, choose(d.dtype, direct(dz) && direct(xs), true, d.n, d.k, d.m),
                                           plain_output(dw, d.k, sizeof(T), d.k), ws + p.split, stream);
     }
     return TV_OK;
