@@ -128,111 +128,4 @@ __global__ __launch_bounds__(256) void join_kernel(Product g, Epilogue e)
     finish8<T>(p, m, n, g.N, m < g.M, e);
 }
 
-// ---- any shape, stride and alignment: 128 x 128 outputs a workgroup of four waves, 128 contraction bytes at a time
-// through registers into two LDS buffers, always with k contiguous there.  Row r's 16-byte piece c lies in slot
-// c ^ ((r / 2) % 8): sixteen rows that a wave reads at one c then touch all 64 banks once.
-template <class T, bool TRANSPOSED> struct Stage {
-    static constexpr int E = Elems<T>::kPer16;
-    static constexpr int kDepth = 8 * E;              // contraction indices of a tile
-    u32x4 r[4];
-
-    __device__ __forceinline__ void load(const T *p, int64_t ld, int rows, int k_end, int row0, int k0, int t)
-    {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int q = t + 256 * i;
-            if constexpr (!TRANSPOSED) {
-                const int row = row0 + q / 8, k = k0 + q % 8 * E;
-                r[i] = row < rows && k < k_end ? load16(p + row * ld + k, k_end - k) : u32x4{0, 0, 0, 0};
-            } else {
-                const int row = row0 + q % (128 / E) * E, k = k0 + q / (128 / E);
-                r[i] = row < rows && k < k_end ? load16(p + k * ld + row, rows - row) : u32x4{0, 0, 0, 0};
-            }
-        }
-    }
-    __device__ __forceinline__ static int place(int row, int piece) { return row * 128 + ((piece ^ ((row >> 1) & 7)) << 4); }
-    __device__ __forceinline__ void put(char *lds, int t) const
-    {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int q = t + 256 * i;
-            if constexpr (!TRANSPOSED) {
-                *(u32x4 *)(lds + place(q / 8, q % 8)) = r[i];
-            } else {
-                const int row = q % (128 / E) * E, k = q / (128 / E);
-#pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    char *to = lds + place(row + j, k / E) + k % E * (int)sizeof(T);
-                    if constexpr (sizeof(T) == 4) *(uint32_t *)to = r[i][j];
-                    else *(uint16_t *)to = (uint16_t)(r[i][j >> 1] >> (16 * (j & 1)));
-                }
-            }
-        }
-    }
-};
-
-template <class T, bool AT, bool BT>
-__global__ __launch_bounds__(256) void gemm_any_kernel(Product g, Epilogue e)
-{
-    constexpr int kDepth = Stage<T, AT>::kDepth;
-    __shared__ __attribute__((aligned(16))) char lds[2][2][128 * 128];
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    const int m0 = (int)(blockIdx.x % g.tiles_m) * 128, n0 = (int)(blockIdx.x / g.tiles_m) * 128;
-    const int k0 = (int)blockIdx.y * g.k_per, k_end = min(g.K, k0 + g.k_per);
-    const int steps = (k_end - k0 + kDepth - 1) / kDepth;
-    const int wm = (wave & 1) * 64, wn = (wave >> 1) * 64;
-
-    f32x4 acc[4][4];                                  // [n tile][m tile]
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-    Stage<T, AT> sa;
-    Stage<T, BT> sb;
-    sa.load((const T *)g.a, g.lda, g.M, k_end, m0, k0, t);
-    sb.load((const T *)g.b, g.ldb, g.N, k_end, n0, k0, t);
-    sa.put(lds[0][0], t);
-    sb.put(lds[0][1], t);
-    __syncthreads();
-    for (int s = 0; s < steps; ++s) {
-        const bool more = s + 1 < steps;
-        if (more) {
-            sa.load((const T *)g.a, g.lda, g.M, k_end, m0, k0 + (s + 1) * kDepth, t);
-            sb.load((const T *)g.b, g.ldb, g.N, k_end, n0, k0 + (s + 1) * kDepth, t);
-        }
-        const char *la = lds[s & 1][0], *lb = lds[s & 1][1];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            u32x4 fa[4], fb[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                fa[i] = *(const u32x4 *)(la + Stage<T, AT>::place(wm + 16 * i + (lane & 15), h * 4 + (lane >> 4)));
-                fb[i] = *(const u32x4 *)(lb + Stage<T, BT>::place(wn + 16 * i + (lane & 15), h * 4 + (lane >> 4)));
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = mma<T>(fb[i], fa[j], acc[i][j]);
-        }
-        if (more) {
-            sa.put(lds[(s + 1) & 1][0], t);
-            sb.put(lds[(s + 1) & 1][1], t);
-        }
-        __syncthreads();
-    }
-    float *piece = (float *)&lds[0][0][0] + wave * 16 * kOutPitch;      // the last barrier has ended every read of LDS
-#pragma unroll 1
-    for (int j = 0; j < 4; ++j) {                     // one copy of the epilogue's code, and of its registers
-#pragma unroll
-        for (int jj = 0; jj < 4; ++jj)
-            if (j == jj)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) *(f32x4 *)(piece + (lane & 15) * kOutPitch + 16 * i + (lane >> 4) * 4) = acc[i][jj];
-        wave_sync();
-        store_rows<T, 16, AT || BT>(piece, g, e, m0 + wm + 16 * j, n0 + wn, lane);
-        wave_sync();
-    }
-}
-
 }  // namespace tvl

@@ -2,7 +2,7 @@
 // workspace layout and launches.
 #include "../../include/tvprox.h"
 #include "tv_ckpt8.hpp"
-#include "tv_gemm16.hpp"
+#include "tv_gemm_split.hpp"
 #include "tv_gemv.hpp"
 #include "tv_slope.hpp"
 
@@ -11,7 +11,7 @@ namespace {
 using namespace tvl;
 
 constexpr int64_t kMostIndex = (int64_t)1 << 31;      // sizes and strides stay below
-constexpr int64_t kMostTiles = (int64_t)1 << 23;      // workgroups of a launch
+constexpr int64_t kMostTiles = (int64_t)1 << 22;      // workgroups of a launch
 
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 int64_t tiles(int64_t v, int64_t of) { return (v + of - 1) / of; }
@@ -30,7 +30,7 @@ struct Operand {
 constexpr int64_t kFewRows = 64;
 
 // Which kernel a product takes and how its contraction is split, from sizes and alignment alone.
-enum Kind { kAny, kFew, kTile256, kTile128, kTile128Deep, kTile64 };
+enum Kind { kFew, kTile256, kTile128, kTile128Deep, kTile64, kSplit256, kSplit128, kSplit64 };
 struct Choice {
     Kind kind;
     int splits, k_per;
@@ -39,8 +39,8 @@ struct Choice {
 struct Tile { int m, n; };
 Tile tile_of_kind(Kind k)
 {
-    if (k == kTile256) return {256, 256};
-    if (k == kTile64) return {64, 128};
+    if (k == kTile256 || k == kSplit256) return {256, 256};
+    if (k == kTile64 || k == kSplit64) return {64, 128};
     return {128, 128};
 }
 
@@ -54,14 +54,6 @@ Choice cut(Kind kind, int64_t s, int64_t K, int64_t unit)
     return {kind, (int)(K > 0 ? tiles(K, per) : 1), (int)per};
 }
 
-Choice split_for(Kind kind, int64_t M, int64_t N, int64_t K, int64_t slots, int64_t least)
-{
-    const Tile side = tile_of_kind(kind);
-    const int64_t t = tiles(M, side.m) * tiles(N, side.n);
-    int64_t s = t >= slots || t < 1 ? 1 : slots / t;
-    return cut(kind, s < K / least ? s : K / least, K, 64);
-}
-
 Choice choose(int dtype, bool direct, bool transposed, int64_t M, int64_t N, int64_t K)
 {
     if (!transposed && M >= 1 && M <= (direct && dtype == TV_BF16 ? kFewRows / 2 : kFewRows)) {
@@ -70,18 +62,21 @@ Choice choose(int dtype, bool direct, bool transposed, int64_t M, int64_t N, int
         const int64_t s = t >= 256 ? 1 : 256 / t;
         return cut(kFew, s < K / (8 * turn) ? s : K / (8 * turn), K, turn);
     }
-    if (dtype != TV_BF16) return split_for(kAny, M, N, K, 512, 128);
-    if (!direct || M < 1 || K < 1) return split_for(kAny, M, N, K, 256, 512);
     /*SWEEP*/
     // The cheapest by a model of the time in microseconds, fitted to sweeps of tiles and splits over outputs of
     // 128 x 128 to 8192 x 8192 and contractions of 64 to 8192: a launch, rounds of workgroups over 256 compute units (of
-    // two 128 x 128 workgroups each where there are more tiles than units), in each a start and an end and so much a step
-    // of 64, and for split contractions the second launch and the sums' trip through memory.
+    // two workgroups each where there are more than 256 of a kernel that leaves room for two), in each a start and an end
+    // and so much a step of 64, and for split contractions the second launch and the sums' trip through memory.
     struct Cost { Kind kind; int64_t slots; double round, step; };
-    constexpr Cost costs[] = {{kTile64, 256, 1.0, 0.30}, {kTile128Deep, 256, 2.0, 0.47}, {kTile128, 512, 3.0, 0.88}, {kTile256, 256, 6.5, 1.50}};
-    Choice best{};
+    constexpr Cost direct16[] = {{kTile64, 256, 1.0, 0.30}, {kTile128Deep, 256, 2.0, 0.47}, {kTile128, 512, 3.0, 0.88}, {kTile256, 256, 6.5, 1.50}};
+    constexpr Cost any16[] = {{kSplit64, 256, 1.5, 0.62}, {kSplit64, 512, 2.0, 0.85}, {kSplit128, 256, 3.0, 0.95}};
+    constexpr Cost any32[] = {{kSplit64, 256, 2.0, 1.6}, {kSplit64, 512, 2.5, 3.2}, {kSplit128, 256, 3.0, 2.9}, {kSplit128, 512, 4.0, 5.4}, {kSplit256, 256, 8.0, 9.4}};
+    const Cost *costs = dtype != TV_BF16 ? any32 : direct ? direct16 : any16;
+    const int kinds = dtype != TV_BF16 ? 5 : direct ? 4 : 3;
+    Choice best = cut(costs[0].kind, 1, K, 64);
     double least = 1e30;
-    for (const Cost &c : costs) {
+    for (int i = 0; i < kinds; ++i) {
+        const Cost &c = costs[i];
         const Tile side = tile_of_kind(c.kind);
         const int64_t t = tiles(M, side.m) * tiles(N, side.n);
         for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
@@ -108,25 +103,30 @@ bool direct(const Operand &o)
     return aligned(o.p, 16) && o.ld % 8 == 0 && (o.cols % 8 == 0 || o.padded) && o.ld <= ((int64_t)1 << 22);
 }
 
-template <int BM, int BN, int WM, int WN, int BUF, bool AT, bool BT>
-void launch16(Product g, const Epilogue &e, hipStream_t stream)
+template <int BM, int BN, int THREADS>
+void launch_tiles(void (*kernel)(Product, Epilogue), Product g, const Epilogue &e, hipStream_t stream)
 {
     g.tiles_m = (uint32_t)tiles(g.M, BM);
     g.tiles_n = (uint32_t)tiles(g.N, BN);
-    hipLaunchKernelGGL((gemm16_kernel<BM, BN, WM, WN, BUF, AT, BT>), dim3(g.tiles_m * g.tiles_n, g.splits), dim3(WM * WN * 64), 0, stream, g, e);
+    hipLaunchKernelGGL(kernel, dim3(g.tiles_m * g.tiles_n, g.splits), dim3(THREADS), 0, stream, g, e);
 }
 
 template <class T, bool AT, bool BT>
 int run_product(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const Choice &c, const Epilogue &e,
                 void *ws, hipStream_t stream)
 {
-    Product g{a.p, b.p, a.ld, b.ld, (int32_t)M, (int32_t)N, (int32_t)K, c.k_per, c.splits, (float *)ws,
-              (uint32_t)tiles(M, 128), (uint32_t)tiles(N, 128)};
+    Product g{a.p, b.p, a.ld, b.ld, (int32_t)M, (int32_t)N, (int32_t)K, c.k_per, c.splits, (float *)ws, 0, 0};
     if constexpr (sizeof(T) == 2) {
-        if (c.kind == kTile256) launch16<256, 256, 2, 4, 2, AT, BT>(g, e, stream);
-        if (c.kind == kTile128) launch16<128, 128, 2, 2, 2, AT, BT>(g, e, stream);
-        if (c.kind == kTile128Deep) launch16<128, 128, 2, 2, 4, AT, BT>(g, e, stream);
-        if (c.kind == kTile64) launch16<64, 128, 2, 2, 4, AT, BT>(g, e, stream);
+        if (c.kind == kTile256) launch_tiles<256, 256, 512>(gemm16_kernel<256, 256, 2, 4, 2, AT, BT>, g, e, stream);
+        if (c.kind == kTile128) launch_tiles<128, 128, 256>(gemm16_kernel<128, 128, 2, 2, 2, AT, BT>, g, e, stream);
+        if (c.kind == kTile128Deep) launch_tiles<128, 128, 256>(gemm16_kernel<128, 128, 2, 2, 4, AT, BT>, g, e, stream);
+        if (c.kind == kTile64) launch_tiles<64, 128, 256>(gemm16_kernel<64, 128, 2, 2, 4, AT, BT>, g, e, stream);
+        if (c.kind == kSplit128) launch_tiles<128, 128, 256>(gemm_split_kernel<T, 128, 128, 2, 2, 4, 2, AT, BT>, g, e, stream);
+        if (c.kind == kSplit64) launch_tiles<64, 128, 256>(gemm_split_kernel<T, 64, 128, 2, 2, 4, 2, AT, BT>, g, e, stream);
+    } else {
+        if (c.kind == kSplit256) launch_tiles<256, 256, 512>(gemm_split_kernel<T, 256, 256, 2, 4, 1, 1, AT, BT>, g, e, stream);
+        if (c.kind == kSplit128) launch_tiles<128, 128, 256>(gemm_split_kernel<T, 128, 128, 2, 2, 1, 2, AT, BT>, g, e, stream);
+        if (c.kind == kSplit64) launch_tiles<64, 128, 256>(gemm_split_kernel<T, 64, 128, 2, 2, 2, 2, AT, BT>, g, e, stream);
     }
     if constexpr (!AT && !BT)
         if (c.kind == kFew) {
@@ -135,8 +135,6 @@ int run_product(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_
             else if (M <= 32) hipLaunchKernelGGL((gemv_kernel<T, 2, 2, 8>), grid, block, 0, stream, g, e);
             else hipLaunchKernelGGL((gemv_kernel<T, 4, 2, 4>), grid, block, 0, stream, g, e);
         }
-    if (c.kind == kAny)
-        hipLaunchKernelGGL((gemm_any_kernel<T, AT, BT>), dim3(g.tiles_m * g.tiles_n, c.splits), dim3(256), 0, stream, g, e);
     if (c.splits > 1) {
         if (launched() != TV_OK) return TV_ERR_HIP;
         hipLaunchKernelGGL((join_kernel<T>), dim3((uint32_t)tiles(M * tiles(N, 32) * 4, 256)), dim3(256), 0, stream, g, e);
