@@ -2,8 +2,18 @@
 // its other index contiguous (the gradients read their operands that way round), sums in 32 bits.
 #pragma once
 #include "tv_linear.hpp"
+#include <type_traits>
 
 namespace tvl {
+
+// f(0) .. f(N - 1), each with a constant of its own.
+template <int N, int I = 0, class F> __device__ __forceinline__ void each(F f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        each<N, I + 1>(f);
+    }
+}
 
 struct Product {
     const void *a, *b;       // A(m, k) = a[m * lda + k], or a[k * lda + m] where A is transposed; B alike
@@ -72,39 +82,92 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_wave_barrier();
 }
 
-// PLAIN: the epilogue only rounds (the gradients' products).
-template <class T, int R, bool PLAIN>
-__device__ __forceinline__ void store_rows(const float *piece, const Product &g, const Epilogue &e, int m0, int n0, int lane)
+// A wave's outputs, PIECES pieces of R rows by 64 columns: `place(x, piece)` writes piece x there, `at(x)` says where it
+// belongs.  PLAIN: the epilogue only rounds (the gradients' products).  Where the residual is read, the next piece's
+// is on its way while one is worked on.
+template <class T, int R, int PIECES, bool PLAIN, class Place, class At>
+__device__ __forceinline__ void store_wave(float *piece, const Product &g, const Epilogue &e, int lane, Place place, At at)
 {
-    const int n = n0 + (lane & 7) * 8;
-    const float *from = piece + (lane >> 3) * kOutPitch + (lane & 7) * 8;
+    const int row = lane >> 3, col = (lane & 7) * 8;
+    const float *from = piece + row * kOutPitch + col;
+    const bool whole = e.vec && at(PIECES - 1).x + R <= g.M && at(PIECES - 1).y + 64 <= g.N;      // (the last piece lies furthest)
     if (g.splits > 1) {
         const int64_t pitch = (g.N + 7) & ~7;
-        float *to = g.partial + ((int64_t)blockIdx.y * g.M + m0 + (lane >> 3)) * pitch + n;
+#pragma unroll 1
+        for (int x = 0; x < PIECES; ++x) {
+            place(x);
+            wave_sync();
+            const int2 o = at(x);
+            float *to = g.partial + ((int64_t)blockIdx.y * g.M + o.x + row) * pitch + o.y + col;
 #pragma unroll
-        for (int i = 0; i < R / 8; ++i)
-            if (m0 + i * 8 + (lane >> 3) < g.M && n < g.N) {
-                *(f32x4 *)(to + i * 8 * pitch) = *(const f32x4 *)(from + i * 8 * kOutPitch);
-                *(f32x4 *)(to + i * 8 * pitch + 4) = *(const f32x4 *)(from + i * 8 * kOutPitch + 4);
-            }
-        return;
-    }
-    if (PLAIN && e.vec && m0 + R <= g.M && n0 + 64 <= g.N) {
-        T *to = (T *)e.y + (int64_t)(m0 + (lane >> 3)) * e.ldy + n;
-#pragma unroll
-        for (int i = 0; i < R / 8; ++i) {
-            const f32x4 a = *(const f32x4 *)(from + i * 8 * kOutPitch), b = *(const f32x4 *)(from + i * 8 * kOutPitch + 4);
-            const float p[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-            store8(to + i * 8 * e.ldy, p, 8, true);
+            for (int i = 0; i < R / 8; ++i)
+                if (o.x + i * 8 + row < g.M && o.y + col < g.N) {
+                    *(f32x4 *)(to + i * 8 * pitch) = *(const f32x4 *)(from + i * 8 * kOutPitch);
+                    *(f32x4 *)(to + i * 8 * pitch + 4) = *(const f32x4 *)(from + i * 8 * kOutPitch + 4);
+                }
+            wave_sync();
         }
         return;
     }
+    if (!whole) {
 #pragma unroll 1
-    for (int i = 0; i < R / 8; ++i) {
-        const int64_t m = m0 + i * 8 + (lane >> 3);
-        const f32x4 a = *(const f32x4 *)(from + i * 8 * kOutPitch), b = *(const f32x4 *)(from + i * 8 * kOutPitch + 4);
-        float p[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-        finish8<T>(p, m, n, g.N, m < g.M, e);
+        for (int x = 0; x < PIECES; ++x) {
+            place(x);
+            wave_sync();
+            const int2 o = at(x);
+#pragma unroll 1
+            for (int i = 0; i < R / 8; ++i) {
+                const f32x4 a = *(const f32x4 *)(from + i * 8 * kOutPitch), b = *(const f32x4 *)(from + i * 8 * kOutPitch + 4);
+                float p[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+                finish8<T>(p, o.x + i * 8 + row, o.y + col, g.N, o.x + i * 8 + row < g.M, e);
+            }
+            wave_sync();
+        }
+        return;
+    }
+    constexpr int kRaw = sizeof(T) / 2;
+    u32x4 res[R / 8][kRaw], next[R / 8][kRaw], bias[kRaw];
+    auto ask = [&](int x) __attribute__((always_inline)) {
+        const int2 o = at(x);
+        const T *p = (const T *)e.res + (int64_t)(o.x + row) * e.ldr + o.y + col;
+#pragma unroll
+        for (int i = 0; i < R / 8; ++i)
+#pragma unroll
+            for (int j = 0; j < kRaw; ++j) next[i][j] = *((const u32x4 *)(p + i * 8 * e.ldr) + j);
+    };
+    if (!PLAIN && e.res) ask(0);
+    int column = -1;
+#pragma unroll 1
+    for (int x = 0; x < PIECES; ++x) {
+        const int2 o = at(x);
+        if (!PLAIN && e.bias && o.y != column) {
+            column = o.y;
+#pragma unroll
+            for (int j = 0; j < kRaw; ++j) bias[j] = *((const u32x4 *)((const T *)e.bias + o.y + col) + j);
+        }
+        if (!PLAIN && e.res) {
+#pragma unroll
+            for (int i = 0; i < R / 8; ++i)
+#pragma unroll
+                for (int j = 0; j < kRaw; ++j) res[i][j] = next[i][j];
+            if (x + 1 < PIECES) ask(x + 1);
+        }
+        place(x);
+        wave_sync();
+        T *to = (T *)e.y + (int64_t)(o.x + row) * e.ldy + o.y + col;
+#pragma unroll
+        for (int i = 0; i < R / 8; ++i) {
+            const f32x4 a = *(const f32x4 *)(from + i * 8 * kOutPitch), b = *(const f32x4 *)(from + i * 8 * kOutPitch + 4);
+            float p[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+            if (!PLAIN) {
+                if (e.bias) add8<T>(p, bias);
+                hold8<T>(p, o.x + i * 8 + row, o.y + col, g.N, 8, true, e);
+                act8<sizeof(T) == 2>(p, e.act);
+                if (e.res) add8<T>(p, res[i]);
+            }
+            store8(to + i * 8 * e.ldy, p, 8, true);
+        }
+        wave_sync();
     }
 }
 

@@ -2,7 +2,6 @@
 // through registers, two buffers in turn, 32 x 32 x 16 matrix instructions.
 #pragma once
 #include "tv_gemm.hpp"
-#include <type_traits>
 
 namespace tvl {
 
@@ -132,12 +131,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm16_kernel(Product g, Epilogu
     const int64_t step_a = AT ? g.lda * 128 : 128, step_b = BT ? g.ldb * 128 : 128;
 
     f32x16 acc[TN][TM];
-#pragma unroll
-    for (int i = 0; i < TN; ++i)
-#pragma unroll
-        for (int j = 0; j < TM; ++j)
-#pragma unroll
-            for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.0f;
+    each<TN * TM>([&](auto x) __attribute__((always_inline)) { acc[x % TN][x / TN] = f32x16{}; });
     bf16x8 fa[2][TM], fb[2][TN];
 #pragma unroll
     for (int j = 0; j < TM; ++j) fa[1][j] = bf16x8{};
@@ -159,13 +153,17 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm16_kernel(Product g, Epilogu
 #pragma unroll
         for (int j = 0; j < TM; ++j) fa[set][j] = TileA::read(from, wm + 32 * j, q, lane);
     };
-    auto multiply = [&](int set, int first, int last) {          // the set's matrix instructions first .. last - 1
-#pragma unroll
-        for (int x = 0; x < TM * TN; ++x)
-            if (x >= first && x < last)
-                acc[x % TN][x / TN] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[set][x % TN], fa[set][x / TN], acc[x % TN][x / TN], 0, 0, 0);
+    auto multiply = [&](auto set, auto first, auto last) __attribute__((always_inline)) {     // the set's matrix instructions first .. last - 1
+        each<last - first>([&](auto y) __attribute__((always_inline)) {
+            constexpr int x = first + y, i = x % TN, j = x / TN;
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[set][i], fa[set][j], acc[i][j], 0, 0, 0);
+        });
     };
     constexpr int kAll = TM * TN, kHalf = kAll / 2;
+    constexpr std::integral_constant<int, 0> c0{};
+    constexpr std::integral_constant<int, 1> c1{};
+    constexpr std::integral_constant<int, kHalf> cHalf{};
+    constexpr std::integral_constant<int, kAll> cAll{};
     // the order of a run of matrix instructions and of what goes behind them: the LDS reads, two after each at least, and
     // the next loads, spread over the step's first one and a half sixteens
     auto order = [&](auto count, auto with_loads) {
@@ -183,19 +181,19 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm16_kernel(Product g, Epilogu
     // being loaded, and waits for all loads)
     auto step = [&](auto all, char *__restrict to, const char *__restrict from, int s) {
         read(from, 0, 0);
-        multiply(1, kHalf, kAll);
+        multiply(c1, cHalf, cAll);
         if (decltype(all)::value || s - 1 + BUF < steps) issue(all, s - 1 + BUF, to);
         order(std::integral_constant<int, kAll - kHalf>{}, all);
         read(from, 1, 1);
-        multiply(0, 0, kAll);
-        order(std::integral_constant<int, kAll>{}, all);
-#pragma unroll
-        for (int q = 1; q < 3; ++q) {
-            read(from, q + 1, (q + 1) & 1);
-            multiply(q & 1, 0, kAll);
-            order(std::integral_constant<int, kAll>{}, std::false_type{});
-        }
-        multiply(1, 0, kHalf);
+        multiply(c0, c0, cAll);
+        order(cAll, all);
+        read(from, 2, 0);
+        multiply(c1, c0, cAll);
+        order(cAll, std::false_type{});
+        read(from, 3, 1);
+        multiply(c0, c0, cAll);
+        order(cAll, std::false_type{});
+        multiply(c1, c0, cHalf);
     };
 #pragma unroll
     for (int s = 0; s < BUF - 1; ++s)
@@ -218,26 +216,25 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm16_kernel(Product g, Epilogu
         fill = from;
         from = from + 1 == BUF ? 0 : from + 1;
     }
-    multiply(1, kHalf, kAll);
+    multiply(c1, cHalf, cAll);
 
     float *piece = (float *)lds + wave * 32 * kOutPitch;
-#pragma unroll 1
-    for (int x = 0; x < TM * TN / 2; ++x) {           // one copy of the epilogue's code, and of its registers
-#pragma unroll
-        for (int y = 0; y < TM * TN / 2; ++y)
-            if (x == y)
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const f32x16 &a = acc[y / TM * 2 + i][y % TM];
-                        *(f32x4 *)(piece + (lane & 31) * kOutPitch + 32 * i + q * 8 + (lane >> 5) * 4) =
-                            f32x4{a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
-                    }
-        wave_sync();
-        store_rows<bf16, 32, AT || BT>(piece, g, e, m0 + wm + x % TM * 32, n0 + wn + x / TM * 64, lane);
-        wave_sync();
-    }
+    store_wave<bf16, 32, TM * TN / 2, AT || BT>(piece, g, e, lane,
+        [&](int x) __attribute__((always_inline)) {  // (one copy of the epilogue's code, whichever the accumulators)
+            each<TM * TN / 2>([&](auto y) __attribute__((always_inline)) {
+                if (x == y)
+                    each<2>([&](auto i) __attribute__((always_inline)) {
+                        f32x16 a = acc[y / TM * 2 + i][y % TM];
+                        asm volatile("" : "+v"(a));   // (or the compiler joins the branches by the accumulators' addresses)
+                        each<4>([&](auto z) __attribute__((always_inline)) {
+                            constexpr int q = 4 * z;
+                            *(f32x4 *)(piece + (lane & 31) * kOutPitch + 32 * i + 2 * q + (lane >> 5) * 4) =
+                                f32x4{a[q], a[q + 1], a[q + 2], a[q + 3]};
+                        });
+                    });
+            });
+        },
+        [&](int x) __attribute__((always_inline)) { return int2{m0 + wm + x % TM * 32, n0 + wn + x / TM * 64}; });
 }
 
 }  // namespace tvl

@@ -106,8 +106,8 @@ template <class T, int ROWS, int THREADS, int KQ, bool TRANSPOSED> struct Staged
 
 // A 32 x 32 tile of outputs from (m0, n0) on with f32 matrix instructions, two contraction indices at a time, straight
 // from memory: what is left for tiles that hold NaNs.
-template <bool AT, bool BT>
-__device__ __attribute__((noinline)) f32x16 tile_in_f32(const float *a, const float *b, int64_t lda, int64_t ldb, int M, int N, int k0, int k_end, int m0, int n0, int lane)
+template <class TA, class TB, bool AT, bool BT>
+__device__ __attribute__((noinline)) f32x16 tile_in_f32(const TA *a, const TB *b, int64_t lda, int64_t ldb, int M, int N, int k0, int k_end, int m0, int n0, int lane)
 {
     const int64_t m = min(m0 + (lane & 31), M - 1), n = min(n0 + (lane & 31), N - 1);
     f32x16 acc;
@@ -116,19 +116,21 @@ __device__ __attribute__((noinline)) f32x16 tile_in_f32(const float *a, const fl
     for (int k = k0; k < k_end; k += 2) {
         const int64_t kk = min(k + (lane >> 5), k_end - 1);
         const bool there = k + (lane >> 5) < k_end;
-        const float x = a[AT ? kk * lda + m : m * lda + kk], y = b[BT ? kk * ldb + n : n * ldb + kk];
+        const float x = widen(a[AT ? kk * lda + m : m * lda + kk]), y = widen(b[BT ? kk * ldb + n : n * ldb + kk]);
         acc = __builtin_amdgcn_mfma_f32_32x32x2f32(there ? y : 0.0f, there ? x : 0.0f, acc, 0, 0, 0);
     }
     return acc;
 }
 
-template <class T, int BM, int BN, int WM, int WN, int KQ, int AHEAD, bool AT, bool BT>
+// T: A's type and the outputs'; TB: B's.
+template <class T, class TB, int BM, int BN, int WM, int WN, int KQ, int AHEAD, bool AT, bool BT>
 __global__ __launch_bounds__(WM * WN * 64) void gemm_split_kernel(Product g, Epilogue e)
 {
-    constexpr int W = WM * WN, THREADS = W * 64, TM = BM / WM / 32, TN = BN / WN / 32, P = Parts<T>::kCount;
+    constexpr int W = WM * WN, THREADS = W * 64, TM = BM / WM / 32, TN = BN / WN / 32, P = Parts<T>::kCount, PB = Parts<TB>::kCount;
+    constexpr int kOrders = P > PB ? P : PB;
     using TileA = Staged<T, BM, THREADS, KQ, AT>;
-    using TileB = Staged<T, BN, THREADS, KQ, BT>;
-    constexpr int kA = P * TileA::kBytes, kB = P * TileB::kBytes, kOut = W * 32 * kOutPitch * 4;
+    using TileB = Staged<TB, BN, THREADS, KQ, BT>;
+    constexpr int kA = P * TileA::kBytes, kB = PB * TileB::kBytes, kOut = W * 32 * kOutPitch * 4;
     static_assert(TN % 2 == 0, "a wave's outputs leave 64 columns at a time");
     __shared__ __attribute__((aligned(1024))) char lds[2 * (kA + kB) > kOut ? 2 * (kA + kB) : kOut];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -140,18 +142,13 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_split_kernel(Product g, Epi
     const int wm = wave % WM * (BM / WM), wn = wave / WM * (BN / WN);
 
     f32x16 acc[TN][TM];
-#pragma unroll
-    for (int i = 0; i < TN; ++i)
-#pragma unroll
-        for (int j = 0; j < TM; ++j)
-#pragma unroll
-            for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.0f;
+    each<TN * TM>([&](auto x) __attribute__((always_inline)) { acc[x % TN][x / TN] = f32x16{}; });
 
     // AHEAD steps' values are in registers or on their way besides the two in LDS; past the contraction's end there are zeros
     TileA ta;
     TileB tb;
     ta.setup((const T *)g.a, g.lda, g.M, m0, k0, t);
-    tb.setup((const T *)g.b, g.ldb, g.N, n0, k0, t);
+    tb.setup((const TB *)g.b, g.ldb, g.N, n0, k0, t);
     struct Both { typename TileA::Raw a; typename TileB::Raw b; } raw[AHEAD];
     auto load = [&](auto all, Both &r, int s) {
         constexpr bool WHOLE = decltype(all)::value;
@@ -165,30 +162,33 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_split_kernel(Product g, Epi
     auto step = [&](auto all, Both &r, const char *from, char *to, int s) {
 #pragma unroll
         for (int q = 0; q < KQ; ++q) {
-            bf16x8 fa[P][TM], fb[P][TN];
+            bf16x8 fa[P][TM], fb[PB][TN];
 #pragma unroll
-            for (int o = 0; o < P; ++o) {
+            for (int o = 0; o < PB; ++o)
 #pragma unroll
                 for (int i = 0; i < TN; ++i) fb[o][i] = TileB::read(from + kA + o * TileB::kBytes, wn + 32 * i, q, lane);
 #pragma unroll
+            for (int o = 0; o < P; ++o)
+#pragma unroll
                 for (int j = 0; j < TM; ++j) fa[o][j] = TileA::read(from + o * TileA::kBytes, wm + 32 * j, q, lane);
-            }
             // by their order's size, the smallest first
-#pragma unroll
-            for (int order = P - 1; order >= 0; --order)
-#pragma unroll
-                for (int oa = 0; oa <= order; ++oa)
-#pragma unroll
-                    for (int j = 0; j < TM; ++j)
-#pragma unroll
-                        for (int i = 0; i < TN; ++i)
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[order - oa][i], fa[oa][j], acc[i][j], 0, 0, 0);
+            each<kOrders>([&](auto z) __attribute__((always_inline)) {
+                constexpr int order = kOrders - 1 - z, first = order < PB ? 0 : order - PB + 1, last = order < P ? order : P - 1;
+                each<last - first + 1>([&](auto y) __attribute__((always_inline)) {
+                    constexpr int oa = first + y, ob = order - oa;
+                    each<TM * TN>([&](auto x) __attribute__((always_inline)) {
+                        constexpr int i = x % TN, j = x / TN;
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[ob][i], fa[oa][j], acc[i][j], 0, 0, 0);
+                    });
+                });
+            });
         }
         put(r, to);
         load(all, r, s + 1 + AHEAD);
         if constexpr (AHEAD > 1) {
-            constexpr int kReads = P * KQ * (TM * (AT ? 2 : 1) + TN * (BT ? 2 : 1)), kMfma = P * (P + 1) / 2 * KQ * TM * TN;
-            constexpr int kSplit = (TileA::kUnits + TileB::kUnits) * (P > 1 ? 60 : 8), kEach = (kSplit + kMfma - 1) / kMfma;
+            constexpr int kReads = KQ * (P * TM * (AT ? 2 : 1) + PB * TN * (BT ? 2 : 1));
+            constexpr int kMfma = (P * PB > 3 ? 6 : P * PB) * KQ * TM * TN;
+            constexpr int kSplit = TileA::kUnits * (P > 1 ? 60 : 8) + TileB::kUnits * (PB > 1 ? 60 : 8), kEach = (kSplit + kMfma - 1) / kMfma;
             __builtin_amdgcn_sched_group_barrier(0x100, kReads / KQ, 0);
 #pragma unroll
             for (int x = 0; x < kMfma; ++x) {
@@ -217,43 +217,38 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_split_kernel(Product g, Epi
         step(some, raw[1 % AHEAD], even, odd, s);
         step(some, raw[0], odd, even, s + 1);
     }
-    if constexpr (P > 1) {
-        bool nan = false;
-#pragma unroll
-        for (int i = 0; i < TN; ++i)
-#pragma unroll
-            for (int j = 0; j < TM; ++j)
-#pragma unroll
-                for (int q = 0; q < 16; ++q) nan |= acc[i][j][q] != acc[i][j][q];
-        if (__any(nan))
-#pragma unroll
-            for (int i = 0; i < TN; ++i)
-#pragma unroll
-                for (int j = 0; j < TM; ++j) {
-                    const f32x16 again = tile_in_f32<AT, BT>((const float *)g.a, (const float *)g.b, g.lda, g.ldb, g.M, g.N, k0, k_end,
-                                                             m0 + wm + 32 * j, n0 + wn + 32 * i, lane);
-#pragma unroll
-                    for (int q = 0; q < 16; ++q) acc[i][j][q] = acc[i][j][q] != acc[i][j][q] ? again[q] : acc[i][j][q];
-                }
+    if constexpr (P * PB > 1) {
+        uint32_t most = 0;                            // of all sums, a NaN's bits being above infinity's
+        each<TM * TN>([&](auto x) __attribute__((always_inline)) {
+            each<16>([&](auto q) __attribute__((always_inline)) {
+                most = max(most, __float_as_uint(acc[x % TN][x / TN][decltype(q)::value]) & 0x7fffffffu);
+            });
+        });
+        if (__any(most > 0x7f800000u))
+            each<TM * TN>([&](auto x) __attribute__((always_inline)) {
+                constexpr int i = x % TN, j = x / TN;
+                const f32x16 again = tile_in_f32<T, TB, AT, BT>((const T *)g.a, (const TB *)g.b, g.lda, g.ldb, g.M, g.N, k0, k_end,
+                                                                m0 + wm + 32 * j, n0 + wn + 32 * i, lane);
+                each<16>([&](auto y) __attribute__((always_inline)) { constexpr int q = y; acc[i][j][q] = acc[i][j][q] != acc[i][j][q] ? again[q] : acc[i][j][q]; });
+            });
     }
     float *piece = (float *)lds + wave * 32 * kOutPitch;
-#pragma unroll 1
-    for (int x = 0; x < TM * TN / 2; ++x) {           // one copy of the epilogue's code, and of its registers
-#pragma unroll
-        for (int y = 0; y < TM * TN / 2; ++y)
-            if (x == y)
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const f32x16 &a = acc[y / TM * 2 + i][y % TM];
-                        *(f32x4 *)(piece + (lane & 31) * kOutPitch + 32 * i + q * 8 + (lane >> 5) * 4) =
-                            f32x4{a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
-                    }
-        wave_sync();
-        store_rows<T, 32, AT || BT>(piece, g, e, m0 + wm + x % TM * 32, n0 + wn + x / TM * 64, lane);
-        wave_sync();
-    }
+    store_wave<T, 32, TM * TN / 2, AT || BT>(piece, g, e, lane,
+        [&](int x) __attribute__((always_inline)) {  // (one copy of the epilogue's code, whichever the accumulators)
+            each<TM * TN / 2>([&](auto y) __attribute__((always_inline)) {
+                if (x == y)
+                    each<2>([&](auto i) __attribute__((always_inline)) {
+                        f32x16 a = acc[y / TM * 2 + i][y % TM];
+                        asm volatile("" : "+v"(a));   // (or the compiler joins the branches by the accumulators' addresses)
+                        each<4>([&](auto z) __attribute__((always_inline)) {
+                            constexpr int q = 4 * z;
+                            *(f32x4 *)(piece + (lane & 31) * kOutPitch + 32 * i + 2 * q + (lane >> 5) * 4) =
+                                f32x4{a[q], a[q + 1], a[q + 2], a[q + 3]};
+                        });
+                    });
+            });
+        },
+        [&](int x) __attribute__((always_inline)) { return int2{m0 + wm + x % TM * 32, n0 + wn + x / TM * 64}; });
 }
 
 }  // namespace tvl

@@ -181,20 +181,36 @@ template <class T> __device__ __forceinline__ void store8(T *p, const float (&v)
     }
 }
 
-// p: the sums of products for outputs (m, n .. n + 7), n a multiple of eight; four neighbouring lanes hold a block of
-// 32 columns of one row.  row: whether this lane has a row at all (it takes part in the block's exchanges either way).
-template <class T>
-__device__ __forceinline__ void finish8(float (&p)[8], int64_t m, int n, int N, bool row, const Epilogue &e)
+// Adds the eight values of T that lie in v.
+template <class T> __device__ __forceinline__ void add8(float (&p)[8], const u32x4 (&v)[sizeof(T) / 2])
 {
-    constexpr bool kFast = sizeof(T) == 2;
-    const bool vec = e.vec != 0;
-    const int have = row ? max(0, min(8, N - n)) : 0;
-    float v[8];
-    if (e.bias) {
-        load8(v, (const T *)e.bias + n, have, vec);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] += v[i];
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (sizeof(T) == 2)       // a bf16 is the upper half of the f32
+            p[i] += __uint_as_float(i & 1 ? v[0][i >> 1] & 0xffff0000u : v[0][i >> 1] << 16);
+        else
+            p[i] += __uint_as_float(v[i >> 2][i & 3]);
     }
+}
+
+template <bool FAST> __device__ __forceinline__ void act8(float (&p)[8], int act)
+{
+    if (act == kRelu)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = act_of<FAST>(p[i], kRelu);
+    else if (act == kGelu)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = act_of<FAST>(p[i], kGelu);
+    else if (act == kSilu)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = act_of<FAST>(p[i], kSilu);
+}
+
+// Writes down z of (m, n .. n + 7), of which `have` exist, as e.kind says; four neighbouring lanes hold a block of 32
+// columns of one row, and all lanes take part in the exchanges.
+template <class T>
+__device__ __forceinline__ void hold8(const float (&p)[8], int64_t m, int n, int N, int have, bool vec, const Epilogue &e)
+{
     if (e.kind == kHeldPlain) {
         if (have) store8((T *)e.held + m * N + n, p, have, vec);
     } else if (e.kind == kHeldBits) {
@@ -218,17 +234,30 @@ __device__ __forceinline__ void finish8(float (&p)[8], int64_t m, int n, int N, 
         for (int i = 0; i < 8; ++i) c[i >> 2] |= ((uint32_t)code_of(p[i], byte) & 255u) << (8 * (i & 3));
         if (have && (n & 31) == 0) e.exps[m * ((N + 31) / 32) + n / 32] = (uint8_t)byte;
         int8_t *to = (int8_t *)e.held + m * N + n;
-        if (have == 8 && vec) {
-            *(u32x2 *)to = u32x2{c[0], c[1]};
-        } else
+        if (have == 8 && vec) *(u32x2 *)to = u32x2{c[0], c[1]};
+        else
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (i < have) to[i] = (int8_t)(c[i >> 2] >> (8 * (i & 3)));
     }
-    if (!have) return;
-    if (e.act != kNone)
+}
+
+// p: the sums of products for outputs (m, n .. n + 7), n a multiple of eight.  row: whether this lane has a row at all (it
+// takes part in its block's exchanges either way).
+template <class T>
+__device__ __forceinline__ void finish8(float (&p)[8], int64_t m, int n, int N, bool row, const Epilogue &e)
+{
+    const bool vec = e.vec != 0;
+    const int have = row ? max(0, min(8, N - n)) : 0;
+    float v[8];
+    if (e.bias) {
+        load8(v, (const T *)e.bias + n, have, vec);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = act_of<kFast>(p[i], e.act);
+        for (int i = 0; i < 8; ++i) p[i] += v[i];
+    }
+    hold8<T>(p, m, n, N, have, vec, e);
+    if (!have) return;
+    act8<sizeof(T) == 2>(p, e.act);
     if (e.res) {
         load8(v, (const T *)e.res + m * e.ldr + n, have, vec);
 #pragma unroll

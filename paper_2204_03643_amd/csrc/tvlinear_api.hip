@@ -111,7 +111,7 @@ void launch_tiles(void (*kernel)(Product, Epilogue), Product g, const Epilogue &
     hipLaunchKernelGGL(kernel, dim3(g.tiles_m * g.tiles_n, g.splits), dim3(THREADS), 0, stream, g, e);
 }
 
-template <class T, bool AT, bool BT>
+template <class T, class TB, bool AT, bool BT>
 int run_product(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const Choice &c, const Epilogue &e,
                 void *ws, hipStream_t stream)
 {
@@ -121,12 +121,12 @@ int run_product(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_
         if (c.kind == kTile128) launch_tiles<128, 128, 256>(gemm16_kernel<128, 128, 2, 2, 2, AT, BT>, g, e, stream);
         if (c.kind == kTile128Deep) launch_tiles<128, 128, 256>(gemm16_kernel<128, 128, 2, 2, 4, AT, BT>, g, e, stream);
         if (c.kind == kTile64) launch_tiles<64, 128, 256>(gemm16_kernel<64, 128, 2, 2, 4, AT, BT>, g, e, stream);
-        if (c.kind == kSplit128) launch_tiles<128, 128, 256>(gemm_split_kernel<T, 128, 128, 2, 2, 4, 2, AT, BT>, g, e, stream);
-        if (c.kind == kSplit64) launch_tiles<64, 128, 256>(gemm_split_kernel<T, 64, 128, 2, 2, 4, 2, AT, BT>, g, e, stream);
+        if (c.kind == kSplit128) launch_tiles<128, 128, 256>(gemm_split_kernel<T, TB, 128, 128, 2, 2, 4, 2, AT, BT>, g, e, stream);
+        if (c.kind == kSplit64) launch_tiles<64, 128, 256>(gemm_split_kernel<T, TB, 64, 128, 2, 2, 4, 2, AT, BT>, g, e, stream);
     } else {
-        if (c.kind == kSplit256) launch_tiles<256, 256, 512>(gemm_split_kernel<T, 256, 256, 2, 4, 1, 1, AT, BT>, g, e, stream);
-        if (c.kind == kSplit128) launch_tiles<128, 128, 256>(gemm_split_kernel<T, 128, 128, 2, 2, 1, 2, AT, BT>, g, e, stream);
-        if (c.kind == kSplit64) launch_tiles<64, 128, 256>(gemm_split_kernel<T, 64, 128, 2, 2, 2, 2, AT, BT>, g, e, stream);
+        if (c.kind == kSplit256) launch_tiles<256, 256, 512>(gemm_split_kernel<T, TB, 256, 256, 2, 4, 1, 1, AT, BT>, g, e, stream);
+        if (c.kind == kSplit128) launch_tiles<128, 128, 256>(gemm_split_kernel<T, TB, 128, 128, 2, 2, 1, 2, AT, BT>, g, e, stream);
+        if (c.kind == kSplit64) launch_tiles<64, 128, 256>(gemm_split_kernel<T, TB, 64, 128, 2, 2, 2, 2, AT, BT>, g, e, stream);
     }
     if constexpr (!AT && !BT)
         if (c.kind == kFew) {
@@ -217,7 +217,7 @@ int linear_fwd(const void *x, const void *w, const void *bias, const void *res, 
     e.held = h.kind == TV_HELD_NONE ? nullptr : h.data; e.exps = h.exps;
     e.ldr = d.ldr; e.ldy = d.ldy; e.act = d.act; e.kind = h.kind;
     e.vec = epilogue_vec(e, sizeof(T), d.n);
-    return run_product<T, false, false>({x, d.ldx, d.k, false}, {w, d.ldw, d.k, false}, d.m, d.n, d.k, fwd_choice(d, x, w), e, ws, stream);
+    return run_product<T, T, false, false>({x, d.ldx, d.k, false}, {w, d.ldw, d.k, false}, d.m, d.n, d.k, fwd_choice(d, x, w), e, ws, stream);
 }
 
 // ---- the backward call's workspace: dz, x out of its checkpoint, the column sums of groups of rows, split sums
@@ -237,7 +237,7 @@ BwdPlan bwd_plan(const tv_linear_desc &d, bool x8)
     if (d.act != TV_ACT_NONE) at += up(d.m * p.ldz * (int64_t)size, 256);
     p.ldx = up(d.k, 8);
     p.x = at;
-    if (x8) at += up(d.m * p.ldx * (int64_t)size, 256);
+    if (x8) at += up(d.m * p.ldx * 2, 256);
     // about 1024 workgroups of 256 columns each, of sixteen rows at least
     const int64_t want = 1024 / tiles(d.n, 256) + 1;
     p.rows_per = (int)(d.m > 0 ? up(tiles(d.m, want < 256 ? want : 256), 16) : 16);
@@ -277,25 +277,27 @@ int linear_bwd(const void *g, const void *x, const uint8_t *x_exps, const tv_hel
         if (a.dz) dz = {a.dz, p.ldz, d.n, false};
     }
     if (db) {
-        hipLaunchKernelGGL((column_sum_kernel<T>), dim3((uint32_t)tiles(d.n, 256)), dim3(256), 0, stream,
+        hipLaunchKernelGGL((column_sum_kernel<T>), dim3((uint32_t)tiles(d.n, 32)), dim3(256), 0, stream,
                            (const float *)(ws + p.sums), (T *)db, d.m > 0 ? p.groups : 0, (int)d.n);
         if (launched() != TV_OK) return TV_ERR_HIP;
     }
     if (dx && d.m > 0) {
         const Operand ow{w, d.ldw, d.k, false};
-        const int st = run_product<T, false, true>(dz, ow, d.m, d.k, d.n, choose(d.dtype, direct(dz) && direct(ow), true, d.m, d.k, d.n),
+        const int st = run_product<T, T, false, true>(dz, ow, d.m, d.k, d.n, choose(d.dtype, direct(dz) && direct(ow), true, d.m, d.k, d.n),
                                                    plain_output(dx, d.k, sizeof(T), d.k), ws + p.split, stream);
         if (st != TV_OK) return st;
     }
     if (dw) {
         Operand xs{x, d.ldx, d.k, false};
-        if (x_exps && d.m > 0) {
-            const int st = tv_ckpt8_load((const int8_t *)x, x_exps, ws + p.x, d.m, d.k, p.ldx, d.dtype, stream);
+        if (x_exps && d.m > 0) {                      // what codes stand for is exact in bf16
+            const int st = tv_ckpt8_load((const int8_t *)x, x_exps, ws + p.x, d.m, d.k, p.ldx, TV_BF16, stream);
             if (st != TV_OK) return st;
             xs = {ws + p.x, p.ldx, d.k, false};
         }
-        return run_product<T, true, true>(dz, xs, d.n, d.k, d.m, choose(d.dtype, direct(dz) && direct(xs), true, d.n, d.k, d.m),
-                                          plain_output(dw, d.k, sizeof(T), d.k), ws + p.split, stream);
+        const Choice c = choose(d.dtype, direct(dz) && direct(xs), true, d.n, d.k, d.m);
+        const Epilogue e = plain_output(dw, d.k, sizeof(T), d.k);
+        return x_exps ? run_product<T, bf16, true, true>(dz, xs, d.n, d.k, d.m, c, e, ws + p.split, stream)
+                      : run_product<T, T, true, true>(dz, xs, d.n, d.k, d.m, c, e, ws + p.split, stream);
     }
     return TV_OK;
 }
