@@ -270,8 +270,8 @@ int linear_bwd(const void *g, const void *x, const uint8_t *x_exps, const tv_hel
         a.ldg = d.ldy; a.ldz = p.ldz;
         a.M = (int32_t)d.m; a.N = (int32_t)d.n; a.rows_per = p.rows_per;
         a.act = d.act; a.kind = d.act == TV_ACT_NONE ? TV_HELD_NONE : h.kind;
-        a.vec = d.n % 4 == 0 && d.ldy % 4 == 0 && aligned(g, 4 * sizeof(T)) &&
-                aligned(h.data, a.kind == kHeldPlain ? 4 * sizeof(T) : 4);
+        // (dz's rows start on 16-byte boundaries by themselves)
+        a.vec = d.n % 8 == 0 && d.ldy % (16 / (int64_t)sizeof(T)) == 0 && aligned(g, 16) && aligned(h.data, a.kind == kHeldPlain ? 16 : 8);
         hipLaunchKernelGGL((slope_kernel<T>), dim3((uint32_t)tiles(d.n, 256), p.groups), dim3(256), 0, stream, a);
         if (launched() != TV_OK) return TV_ERR_HIP;
         if (a.dz) dz = {a.dz, p.ldz, d.n, false};
