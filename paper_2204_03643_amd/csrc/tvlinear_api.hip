@@ -210,14 +210,14 @@ size_t fwd_bytes(const tv_linear_desc &d)
 
 template <class T>
 int linear_fwd(const void *x, const void *w, const void *bias, const void *res, void *y, const tv_held &h,
-               const tv_linear_desc &d, void *ws, hipStream_t stream)
+               const tv_linear_desc &d, const Choice &c, void *ws, hipStream_t stream)
 {
     Epilogue e{};
     e.bias = bias; e.res = res; e.y = y;
     e.held = h.kind == TV_HELD_NONE ? nullptr : h.data; e.exps = h.exps;
     e.ldr = d.ldr; e.ldy = d.ldy; e.act = d.act; e.kind = h.kind;
     e.vec = epilogue_vec(e, sizeof(T), d.n);
-    return run_product<T, T, false, false>({x, d.ldx, d.k, false}, {w, d.ldw, d.k, false}, d.m, d.n, d.k, fwd_choice(d, x, w), e, ws, stream);
+    return run_product<T, T, false, false>({x, d.ldx, d.k, false}, {w, d.ldw, d.k, false}, d.m, d.n, d.k, c, e, ws, stream);
 }
 
 // ---- the backward call's workspace: dz, x out of its checkpoint, the column sums of groups of rows, split sums
@@ -337,9 +337,10 @@ int tv_linear_fwd(const void *x, const void *w, const void *bias, const void *re
     if (!x || !w || !y) return TV_ERR_NULL;
     const size_t size = elem_bytes(d.dtype);
     if (!aligned(x, size) || !aligned(w, size) || !aligned(bias, size) || !aligned(res, size) || !aligned(y, size)) return TV_ERR_STRIDE;
-    if ((st = check_workspace(ws, ws_bytes, fwd_bytes(d))) != TV_OK) return st;
-    return d.dtype == TV_BF16 ? linear_fwd<bf16>(x, w, bias, res, y, held, d, ws, stream)
-                              : linear_fwd<float>(x, w, bias, res, y, held, d, ws, stream);
+    const Choice c = fwd_choice(d, x, w);
+    if (c.splits > 1 && (st = check_workspace(ws, ws_bytes, fwd_bytes(d))) != TV_OK) return st;
+    return d.dtype == TV_BF16 ? linear_fwd<bf16>(x, w, bias, res, y, held, d, c, ws, stream)
+                              : linear_fwd<float>(x, w, bias, res, y, held, d, c, ws, stream);
 }
 
 size_t tv_linear_bwd_workspace_bytes(tv_linear_desc d, int x_is_8bit)

@@ -9,6 +9,7 @@ a TV pass along the tokens and two channel products.  float32 and bfloat16, CUDA
 """
 from __future__ import annotations
 
+import functools
 import math
 
 import torch
@@ -19,6 +20,7 @@ from .layer import tv_prox_1d
 _DTYPES = {torch.float32: _b.TV_F32, torch.bfloat16: _b.TV_BF16}
 _ACTS = {"none": _b.TV_ACT_NONE, "relu": _b.TV_ACT_RELU, "gelu": _b.TV_ACT_GELU, "silu": _b.TV_ACT_SILU}
 _CHECKPOINTS = ("full", "8bit")
+_HELD_BY_DTYPE = {torch.int32: _b.TV_HELD_BITS, torch.int8: _b.TV_HELD_8BIT}
 _NOTHING_HELD = _b.tv_held(None, None, _b.TV_HELD_NONE)
 
 
@@ -36,6 +38,8 @@ def _as_rows(t: torch.Tensor):
     """(tensor, row stride) of t as rows of its last axis: a matrix whose rows are dense stays where it is, anything
     else is made contiguous."""
     n = t.shape[-1]
+    if t.is_contiguous():
+        return t, n
     if t.dim() == 2 and (t.stride(1) == 1 or n == 1) and (t.stride(0) >= n or t.shape[0] == 1):
         return t, (t.stride(0) if t.shape[0] > 1 else n)
     return t.contiguous(), n
@@ -45,8 +49,24 @@ def _blocks(n: int) -> int:
     return -(-n // _b.TV_CKPT8_BLOCK)
 
 
-def _scratch(nbytes: int, device):
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+@functools.lru_cache(maxsize=4096)
+def _fwd_bytes(m, k, n, dtype):
+    """The forward call's workspace: the sizes and the dtype say it all."""
+    return _b.tv_linear_fwd_workspace_bytes(_b.tv_linear_desc(m, k, n, k, k, n, n, dtype, 0))
+
+
+@functools.lru_cache(maxsize=4096)
+def _bwd_bytes(m, k, n, dtype, act, x_is_8bit):
+    return _b.tv_linear_bwd_workspace_bytes(_b.tv_linear_desc(m, k, n, k, k, n, n, dtype, act), x_is_8bit)
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
+
+
+def _check(status):
+    if status:
+        raise _b.TVError(status)
 
 
 class Checkpoint8:
@@ -82,23 +102,28 @@ class Checkpoint8:
         return x
 
 
+def _save8(x, ld):
+    """(codes, exponents) of x as rows (see _as_rows)."""
+    n = x.shape[-1]
+    rows = x.numel() // n
+    codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+    exps = torch.empty((rows, _blocks(n)), dtype=torch.uint8, device=x.device)
+    _check(_b.lib().tv_ckpt8_save(x.data_ptr(), codes.data_ptr(), exps.data_ptr(), rows, n, ld, _DTYPES[x.dtype], _b._stream(None)))
+    return codes, exps
+
+
 def tv_checkpoint8(x: torch.Tensor) -> Checkpoint8:
     """An 8-bit checkpoint of x, in blocks of 32 values of its last axis."""
     _check_tensor(x, "tv_checkpoint8")
     if x.dim() < 1 or x.shape[-1] < 1:
         raise ValueError("tv_checkpoint8: a last axis of at least one value expected")
-    x, ld = _as_rows(x.detach())
-    n = x.shape[-1]
-    rows = x.numel() // n
-    codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
-    exps = torch.empty((rows, _blocks(n)), dtype=torch.uint8, device=x.device)
-    _b.tv_ckpt8_save(x, codes, exps, rows, n, ld, _DTYPES[x.dtype])
+    codes, exps = _save8(*_as_rows(x.detach()))
     return Checkpoint8(codes, exps, x.dtype)
 
 
 def _forward(x, ldx, weight, ldw, bias, residual, act, hold):
-    """(y, what is held of z): x and weight as rows, hold one of None, "full", "8bit"."""
-    k, n, code = x.shape[-1], weight.shape[0], _ACTS[act]
+    """(y, what is held of z, its exponents): x and weight as rows, hold one of None, "full", "8bit"."""
+    k, n, code, dtype = x.shape[-1], weight.shape[0], _ACTS[act], _DTYPES[x.dtype]
     m = x.numel() // k
     y = torch.empty(x.shape[:-1] + (n,), dtype=x.dtype, device=x.device)
     ldr = n
@@ -114,10 +139,12 @@ def _forward(x, ldx, weight, ldw, bias, residual, act, hold):
             exps = torch.empty((m, _blocks(n)), dtype=torch.uint8, device=x.device)
         else:
             data, kind = torch.empty((m, n), dtype=x.dtype, device=x.device), _b.TV_HELD_PLAIN
-        held = _b.tv_held(data.data_ptr(), exps.data_ptr() if exps is not None else None, kind)
-    desc = _b.tv_linear_desc(m, k, n, ldx, ldw, ldr, n, _DTYPES[x.dtype], code)
-    nbytes = _b.tv_linear_fwd_workspace_bytes(desc)
-    _b.tv_linear_fwd(x, weight, bias, residual, y, held, desc, _scratch(nbytes, x.device), nbytes)
+        held = _b.tv_held(data.data_ptr(), _address(exps), kind)
+    nbytes = _fwd_bytes(m, k, n, dtype)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device) if nbytes else None
+    _check(_b.lib().tv_linear_fwd(x.data_ptr(), weight.data_ptr(), _address(bias), _address(residual), y.data_ptr(), held,
+                                  _b.tv_linear_desc(m, k, n, ldx, ldw, ldr, n, dtype, code), _address(ws), nbytes,
+                                  _b._stream(None)))
     return y, data, exps
 
 
@@ -125,18 +152,20 @@ def _backward(g, x, x_exps, ldx, data, exps, weight, ldw, act, want):
     """(dx, dw, db), None where not wanted.  x: rows, or the codes of its checkpoint (x_exps given)."""
     n, k = weight.shape
     m = g.numel() // n
+    code, dtype = _ACTS[act], _DTYPES[g.dtype]
     g, ldg = _as_rows(g)
     kind = _b.TV_HELD_NONE
     if data is not None:
-        kind = {torch.int32: _b.TV_HELD_BITS, torch.int8: _b.TV_HELD_8BIT}.get(data.dtype, _b.TV_HELD_PLAIN)
-    held = _b.tv_held(data.data_ptr() if data is not None else None, exps.data_ptr() if exps is not None else None, kind)
-    like = dict(dtype=g.dtype, device=g.device)
-    dx = torch.empty(g.shape[:-1] + (k,), **like) if want[0] else None
-    dw = torch.empty((n, k), **like) if want[1] else None
-    db = torch.empty(n, **like) if want[2] else None
-    desc = _b.tv_linear_desc(m, k, n, ldx, ldw, n, ldg, _DTYPES[g.dtype], _ACTS[act])
-    nbytes = _b.tv_linear_bwd_workspace_bytes(desc, x_exps is not None)
-    _b.tv_linear_bwd(g, x, x_exps, held, weight, dx, dw, db, desc, _scratch(nbytes, g.device), nbytes)
+        kind = _HELD_BY_DTYPE.get(data.dtype, _b.TV_HELD_PLAIN)
+    dx = torch.empty(g.shape[:-1] + (k,), dtype=g.dtype, device=g.device) if want[0] else None
+    dw = torch.empty((n, k), dtype=g.dtype, device=g.device) if want[1] else None
+    db = torch.empty(n, dtype=g.dtype, device=g.device) if want[2] else None
+    nbytes = _bwd_bytes(m, k, n, dtype, code, x_exps is not None)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=g.device) if nbytes else None
+    _check(_b.lib().tv_linear_bwd(g.data_ptr(), _address(x), _address(x_exps), _b.tv_held(_address(data), _address(exps), kind),
+                                  weight.data_ptr(), _address(dx), _address(dw), _address(db),
+                                  _b.tv_linear_desc(m, k, n, ldx, ldw, n, ldg, dtype, code), _address(ws), nbytes,
+                                  _b._stream(None)))
     return dx, dw, db
 
 
@@ -152,8 +181,8 @@ class _Linear(torch.autograd.Function):
         if not ctx.needs_input_grad[1]:
             rows = None                            # only dW reads x
         elif checkpoint == "8bit":
-            held = tv_checkpoint8(rows)
-            rows, x_exps, ldx = held.codes, held.exps, rows.shape[-1]
+            rows, x_exps = _save8(rows, ldx)
+            ldx = rows.shape[-1]
         ctx.save_for_backward(rows, x_exps, data, exps, wrows)
         ctx.strides, ctx.act, ctx.has_bias = (ldx, ldw), act, bias is not None
         return y
@@ -173,7 +202,7 @@ class _Linear(torch.autograd.Function):
 def _check_linear(x, weight, act, what):
     if act not in _ACTS:
         raise ValueError("%s: act must be one of %s, got %r" % (what, ", ".join(sorted(_ACTS)), act))
-    if weight.dim() != 2 or x.dim() < 1 or x.shape[-1] != weight.shape[1] or min(weight.shape) < 1:
+    if weight.dim() != 2 or x.dim() < 1 or x.shape[-1] != weight.shape[1] or 0 in weight.shape:
         raise ValueError("%s: x [..., k] and weight [n, k] expected, got %r and %r"
                          % (what, tuple(x.shape), tuple(weight.shape)))
 
@@ -186,22 +215,24 @@ def tv_linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None =
     "relu", "gelu" (with erf) or "silu".  checkpoint: what is kept for the backward pass, "full" (x and the
     pre-activation as they are) or "8bit" (both in 8-bit codes; ReLU keeps a bit a value either way).
     """
-    _check_tensor(x, "tv_linear")
-    _check_tensor(weight, "tv_linear (weight)", x)
+    if not (x.is_cuda and weight.is_cuda and x.dtype in _DTYPES and weight.dtype is x.dtype and weight.get_device() == x.get_device()):
+        _check_tensor(x, "tv_linear")
+        _check_tensor(weight, "tv_linear (weight)", x)
     _check_linear(x, weight, act, "tv_linear")
     if checkpoint not in _CHECKPOINTS:
         raise ValueError("tv_linear: checkpoint must be one of %s, got %r" % (", ".join(_CHECKPOINTS), checkpoint))
+    n = weight.shape[0]
     if bias is not None:
         _check_tensor(bias, "tv_linear (bias)", x)
-        if tuple(bias.shape) != (weight.shape[0],):
-            raise ValueError("tv_linear: bias of shape (%d,) expected, got %r" % (weight.shape[0], tuple(bias.shape)))
+        if bias.dim() != 1 or bias.shape[0] != n:
+            raise ValueError("tv_linear: bias of shape (%d,) expected, got %r" % (n, tuple(bias.shape)))
         bias = bias.contiguous()
     if residual is not None:
         _check_tensor(residual, "tv_linear (residual)", x)
-        if residual.shape != x.shape[:-1] + (weight.shape[0],):
-            raise ValueError("tv_linear: residual of shape %r expected, got %r"
-                             % (tuple(x.shape[:-1]) + (weight.shape[0],), tuple(residual.shape)))
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias, residual)):
+        if residual.shape[-1:] != weight.shape[:1] or residual.shape[:-1] != x.shape[:-1]:
+            raise ValueError("tv_linear: residual of shape %r expected, got %r" % (tuple(x.shape[:-1]) + (n,), tuple(residual.shape)))
+    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or (bias is not None and bias.requires_grad)
+                                    or (residual is not None and residual.requires_grad)):
         return _Linear.apply(x, weight, bias, residual, act, checkpoint)
     x, ldx = _as_rows(x)
     weight, ldw = _as_rows(weight)
