@@ -182,10 +182,17 @@ __global__ __launch_bounds__(256) void join_kernel(Product g, Epilogue e)
     const int64_t pitch = (g.N + 7) & ~7;
     f32x4 a = {0.0f, 0.0f, 0.0f, 0.0f}, b = a;
     if (m < g.M && n < g.N)
-        for (int s = 0; s < g.splits; ++s) {
-            const float *from = g.partial + ((int64_t)s * g.M + m) * pitch + n;
-            a += *(const f32x4 *)from;
-            b += *(const f32x4 *)(from + 4);
+        for (int s = 0; s < g.splits; s += 4) {       // four splits' sums on their way together
+            f32x4 va[4], vb[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float *from = g.partial + ((int64_t)min(s + i, g.splits - 1) * g.M + m) * pitch + n;
+                va[i] = *(const f32x4 *)from;
+                vb[i] = *(const f32x4 *)(from + 4);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (s + i < g.splits) { a += va[i]; b += vb[i]; }
         }
     float p[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
     finish8<T>(p, m, n, g.N, m < g.M, e);

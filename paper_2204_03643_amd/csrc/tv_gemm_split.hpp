@@ -124,7 +124,7 @@ __device__ __attribute__((noinline)) f32x16 tile_in_f32(const TA *a, const TB *b
 
 // T: A's type and the outputs'; TB: B's.
 template <class T, class TB, int BM, int BN, int WM, int WN, int KQ, int AHEAD, bool AT, bool BT>
-__global__ __launch_bounds__(WM * WN * 64) void gemm_split_kernel(Product g, Epilogue e)
+__global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void gemm_split_kernel(Product g, Epilogue e)
 {
     constexpr int W = WM * WN, THREADS = W * 64, TM = BM / WM / 32, TN = BN / WN / 32, P = Parts<T>::kCount, PB = Parts<TB>::kCount;
     constexpr int kOrders = P > PB ? P : PB;

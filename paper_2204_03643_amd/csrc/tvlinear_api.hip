@@ -70,9 +70,9 @@ Choice choose(int dtype, bool direct, bool transposed, int64_t M, int64_t N, int
     struct Cost { Kind kind; int64_t slots; double round, step; };
     constexpr Cost direct16[] = {{kTile64, 256, 1.0, 0.30}, {kTile128Deep, 256, 2.0, 0.47}, {kTile128, 512, 3.0, 0.88}, {kTile256, 256, 6.5, 1.50}};
     constexpr Cost any16[] = {{kSplit64, 256, 1.5, 0.62}, {kSplit64, 512, 2.0, 0.85}, {kSplit128, 256, 3.0, 0.95}};
-    constexpr Cost any32[] = {{kSplit64, 256, 2.0, 1.6}, {kSplit64, 512, 2.5, 3.2}, {kSplit128, 256, 3.0, 2.9}, {kSplit128, 512, 4.0, 5.4}, {kSplit256, 256, 8.0, 9.4}};
+    constexpr Cost any32[] = {{kSplit64, 256, 2.0, 1.6}, {kSplit64, 512, 2.5, 3.2}, {kSplit128, 256, 3.5, 2.65}, {kSplit256, 256, 8.0, 9.0}};
     const Cost *costs = dtype != TV_BF16 ? any32 : direct ? direct16 : any16;
-    const int kinds = dtype != TV_BF16 ? 5 : direct ? 4 : 3;
+    const int kinds = dtype == TV_BF16 && !direct ? 3 : 4;
     Choice best = cut(costs[0].kind, 1, K, 64);
     double least = 1e30;
     for (int i = 0; i < kinds; ++i) {
@@ -83,7 +83,7 @@ Choice choose(int dtype, bool direct, bool transposed, int64_t M, int64_t N, int
             if (s > 1 && (K < 128 * s || t * s > 1024)) break;
             const Choice x = cut(c.kind, s, K, 64);
             double us = 3.0 + (double)tiles(t * x.splits, c.slots) * (c.round + c.step * (double)tiles(x.k_per < K ? x.k_per : K, 64));
-            if (x.splits > 1) us += 5.0 + (double)M * (double)N * x.splits * 8 / 4e6;
+            if (x.splits > 1) us += 4.0 + (double)M * (double)N * x.splits * 8 / 6e6;
             if (us < least) { least = us; best = x; }
         }
     }
@@ -125,7 +125,7 @@ int run_product(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_
         if (c.kind == kSplit64) launch_tiles<64, 128, 256>(gemm_split_kernel<T, TB, 64, 128, 2, 2, 4, 2, AT, BT>, g, e, stream);
     } else {
         if (c.kind == kSplit256) launch_tiles<256, 256, 512>(gemm_split_kernel<T, TB, 256, 256, 2, 4, 1, 1, AT, BT>, g, e, stream);
-        if (c.kind == kSplit128) launch_tiles<128, 128, 256>(gemm_split_kernel<T, TB, 128, 128, 2, 2, 1, 2, AT, BT>, g, e, stream);
+        if (c.kind == kSplit128) launch_tiles<128, 128, 512>(gemm_split_kernel<T, TB, 128, 128, 4, 2, 2, 2, AT, BT>, g, e, stream);
         if (c.kind == kSplit64) launch_tiles<64, 128, 256>(gemm_split_kernel<T, TB, 64, 128, 2, 2, 2, 2, AT, BT>, g, e, stream);
     }
     if constexpr (!AT && !BT)
