@@ -41,17 +41,11 @@ template <class T> __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 
     }
 }
 
-typedef uint32_t u32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint32_t u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));
-
 // 16 bytes from any address that suits T, or the first `have` elements and zeros.
 template <class T> __device__ __forceinline__ u32x4 load16(const T *p, int have)
 {
     constexpr int E = Elems<T>::kPer16;
-    if (have >= E) {
-        if constexpr (sizeof(T) == 4) return *(const u32x4_at4 *)p;
-        else return *(const u32x4_at2 *)p;
-    }
+    if (have >= E) return get16(p);
     u32x4 v = {0, 0, 0, 0};
     if (have <= 0) return v;
     // (every load from an element that exists, so that none of them waits for a branch)
@@ -90,7 +84,7 @@ __device__ __forceinline__ void store_wave(float *piece, const Product &g, const
 {
     const int row = lane >> 3, col = (lane & 7) * 8;
     const float *from = piece + row * kOutPitch + col;
-    const bool whole = e.vec && at(PIECES - 1).x + R <= g.M && at(PIECES - 1).y + 64 <= g.N;      // (the last piece lies furthest)
+    const bool whole = at(PIECES - 1).x + R <= g.M && at(PIECES - 1).y + 64 <= g.N;      // (the last piece lies furthest)
     if (g.splits > 1) {
         const int64_t pitch = (g.N + 7) & ~7;
 #pragma unroll 1
@@ -133,7 +127,7 @@ __device__ __forceinline__ void store_wave(float *piece, const Product &g, const
 #pragma unroll
         for (int i = 0; i < R / 8; ++i)
 #pragma unroll
-            for (int j = 0; j < kRaw; ++j) next[i][j] = *((const u32x4 *)(p + i * 8 * e.ldr) + j);
+            for (int j = 0; j < kRaw; ++j) next[i][j] = get16(p + i * 8 * e.ldr + j * (16 / (int)sizeof(T)));
     };
     if (!PLAIN && e.res) ask(0);
     int column = -1;
@@ -143,7 +137,7 @@ __device__ __forceinline__ void store_wave(float *piece, const Product &g, const
         if (!PLAIN && e.bias && o.y != column) {
             column = o.y;
 #pragma unroll
-            for (int j = 0; j < kRaw; ++j) bias[j] = *((const u32x4 *)((const T *)e.bias + o.y + col) + j);
+            for (int j = 0; j < kRaw; ++j) bias[j] = get16((const T *)e.bias + o.y + col + j * (16 / (int)sizeof(T)));
         }
         if (!PLAIN && e.res) {
 #pragma unroll
@@ -161,11 +155,11 @@ __device__ __forceinline__ void store_wave(float *piece, const Product &g, const
             float p[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
             if (!PLAIN) {
                 if (e.bias) add8<T>(p, bias);
-                hold8<T>(p, o.x + i * 8 + row, o.y + col, g.N, 8, true, e);
+                hold8<T>(p, o.x + i * 8 + row, o.y + col, g.N, 8, e);
                 act8<sizeof(T) == 2>(p, e.act);
                 if (e.res) add8<T>(p, res[i]);
             }
-            store8(to + i * 8 * e.ldy, p, 8, true);
+            store8(to + i * 8 * e.ldy, p, 8);
         }
         wave_sync();
     }

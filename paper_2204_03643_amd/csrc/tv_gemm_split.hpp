@@ -136,7 +136,10 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     uint32_t tm, tn;
     tile_of(blockIdx.x, g.tiles_m, g.tiles_n, tm, tn);
-    const int m0 = (int)tm * BM, n0 = (int)tn * BN;
+    // (a transposed operand's last tile starts early enough to be whole: its first outputs are the tile before's too, to
+    // the bit, and a tile that reads past the last row would load element by element)
+    const int m0 = AT ? min((int)tm * BM, max(0, g.M - BM)) : (int)tm * BM;
+    const int n0 = BT ? min((int)tn * BN, max(0, g.N - BN)) : (int)tn * BN;
     const int k0 = (int)blockIdx.y * g.k_per, k_end = min(g.K, k0 + g.k_per);
     const int steps = (k_end - k0 + 16 * KQ - 1) / (16 * KQ);
     const int wm = wave % WM * (BM / WM), wn = wave / WM * (BN / WN);
@@ -159,7 +162,7 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
         TileA::put(r.a, to, t);
         TileB::put(r.b, to + kA, t);
     };
-    auto step = [&](auto all, Both &r, const char *from, char *to, int s) {
+    auto step = [&](auto which, Both &r, const char *from, char *to, int s) {
 #pragma unroll
         for (int q = 0; q < KQ; ++q) {
             bf16x8 fa[P][TM], fb[PB][TN];
@@ -184,7 +187,7 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
             });
         }
         put(r, to);
-        load(all, r, s + 1 + AHEAD);
+        load(which, r, s + 1 + AHEAD);
         if constexpr (AHEAD > 1) {
             constexpr int kReads = KQ * (P * TM * (AT ? 2 : 1) + PB * TN * (BT ? 2 : 1));
             constexpr int kMfma = (P * PB > 3 ? 6 : P * PB) * KQ * TM * TN;
@@ -201,17 +204,22 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
     };
     char *even = lds, *odd = lds + kA + kB;
     const std::false_type some;
-    load(some, raw[0], 0);
-    put(raw[0], even);
-#pragma unroll
-    for (int s = 0; s < AHEAD; ++s) load(some, raw[(s + 1) % AHEAD], s + 1);
-    __syncthreads();
+    const std::true_type all;
     const bool inside = (!AT || m0 + BM <= g.M) && (!BT || n0 + BN <= g.N);
     const int whole = inside ? (k_end - k0) / (16 * KQ) : 0;
+    auto first = [&](auto all_or_some) {
+        load(all_or_some, raw[0], 0);
+        put(raw[0], even);
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s) load(all_or_some, raw[(s + 1) % AHEAD], s + 1);
+    };
+    if (AHEAD < whole) first(all);
+    else first(some);
+    __syncthreads();
     int s = 0;
     for (; s + 2 + AHEAD < whole; s += 2) {
-        step(std::true_type{}, raw[1 % AHEAD], even, odd, s);
-        step(std::true_type{}, raw[0], odd, even, s + 1);
+        step(all, raw[1 % AHEAD], even, odd, s);
+        step(all, raw[0], odd, even, s + 1);
     }
     for (; s < steps; s += 2) {
         step(some, raw[1 % AHEAD], even, odd, s);

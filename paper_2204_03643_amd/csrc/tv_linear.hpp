@@ -107,78 +107,21 @@ struct Epilogue {
     uint8_t    *exps;        // [m, ceil(n / 32)] step bytes (kHeld8)
     int64_t     ldr, ldy;
     int32_t     act, kind;
-    uint32_t    vec;         // rows of y, res, z and the bias start on 16-byte boundaries, of codes on 8-byte ones
 };
 
-template <class T> __device__ __forceinline__ f32x4 load4(const T *p, int have, bool vec)
+// 16 bytes at any address that suits T (the hardware takes them in one access wherever they lie), and eight codes.
+typedef uint32_t u32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_at1 __attribute__((ext_vector_type(2), aligned(1)));
+template <class T> __device__ __forceinline__ u32x4 get16(const T *p)
 {
-    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (have == 4 && vec) {
-        if constexpr (sizeof(T) == 4) v = *(const f32x4 *)p;
-        else {
-            const bf16x4 h = *(const bf16x4 *)p;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = widen(h[i]);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < have) v[i] = widen(p[i]);
-    }
-    return v;
+    if constexpr (sizeof(T) == 4) return *(const u32x4_at4 *)p;
+    else return *(const u32x4_at2 *)p;
 }
-template <class T> __device__ __forceinline__ void store4(T *p, f32x4 v, int have, bool vec)
+template <class T> __device__ __forceinline__ void put16(T *p, u32x4 v)
 {
-    if (have == 4 && vec) {
-        if constexpr (sizeof(T) == 4) *(f32x4 *)p = v;
-        else {
-            bf16x4 h;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) h[i] = narrow<bf16>(v[i]);
-            *(bf16x4 *)p = h;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < have) p[i] = narrow<T>(v[i]);
-    }
-}
-
-// Eight consecutive values from p on, the first `have` of them; vec: p lies on a 16-byte boundary.
-template <class T> __device__ __forceinline__ void load8(float (&v)[8], const T *p, int have, bool vec)
-{
-    if (have == 8 && vec) {
-        if constexpr (sizeof(T) == 2) {
-            const bf16x8 h = *(const bf16x8 *)p;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = widen(h[i]);
-        } else {
-            const f32x4 a = *(const f32x4 *)p, b = *(const f32x4 *)(p + 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < have ? widen(p[i]) : 0.0f;
-    }
-}
-template <class T> __device__ __forceinline__ void store8(T *p, const float (&v)[8], int have, bool vec)
-{
-    if (have == 8 && vec) {
-        if constexpr (sizeof(T) == 2) {
-            bf16x8 h;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) h[i] = narrow<bf16>(v[i]);
-            *(bf16x8 *)p = h;
-        } else {
-            *(f32x4 *)p = f32x4{v[0], v[1], v[2], v[3]};
-            *(f32x4 *)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < have) p[i] = narrow<T>(v[i]);
-    }
+    if constexpr (sizeof(T) == 4) *(u32x4_at4 *)p = v;
+    else *(u32x4_at2 *)p = v;
 }
 
 // Adds the eight values of T that lie in v.
@@ -191,6 +134,49 @@ template <class T> __device__ __forceinline__ void add8(float (&p)[8], const u32
         else
             p[i] += __uint_as_float(v[i >> 2][i & 3]);
     }
+}
+
+// Eight consecutive values from p on, the first `have` of them (zeros for the others); and the way back.
+template <class T> __device__ __forceinline__ void load8(float (&v)[8], const T *p, int have)
+{
+    if (have == 8) {
+        u32x4 raw[sizeof(T) / 2];
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = get16(p + i * (16 / (int)sizeof(T)));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+        add8<T>(v, raw);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < have ? widen(p[i]) : 0.0f;
+    }
+}
+template <class T> __device__ __forceinline__ void store8(T *p, const float (&v)[8], int have)
+{
+    if (have == 8) {
+        if constexpr (sizeof(T) == 2) {
+            bf16x8 h;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] = narrow<bf16>(v[i]);
+            put16(p, __builtin_bit_cast(u32x4, h));
+        } else {
+            put16(p, __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]}));
+            put16(p + 4, __builtin_bit_cast(u32x4, f32x4{v[4], v[5], v[6], v[7]}));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < have) p[i] = narrow<T>(v[i]);
+    }
+}
+// Eight codes, four to a word, the first `have` of them.
+__device__ __forceinline__ void store_codes(int8_t *p, u32x2 c, int have)
+{
+    if (have == 8) *(u32x2_at1 *)p = c;
+    else
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < have) p[i] = (int8_t)(c[i >> 2] >> (8 * (i & 3)));
 }
 
 template <bool FAST> __device__ __forceinline__ void act8(float (&p)[8], int act)
@@ -209,10 +195,10 @@ template <bool FAST> __device__ __forceinline__ void act8(float (&p)[8], int act
 // Writes down z of (m, n .. n + 7), of which `have` exist, as e.kind says; four neighbouring lanes hold a block of 32
 // columns of one row, and all lanes take part in the exchanges.
 template <class T>
-__device__ __forceinline__ void hold8(const float (&p)[8], int64_t m, int n, int N, int have, bool vec, const Epilogue &e)
+__device__ __forceinline__ void hold8(const float (&p)[8], int64_t m, int n, int N, int have, const Epilogue &e)
 {
     if (e.kind == kHeldPlain) {
-        if (have) store8((T *)e.held + m * N + n, p, have, vec);
+        if (have) store8((T *)e.held + m * N + n, p, have);
     } else if (e.kind == kHeldBits) {
         uint32_t w = 0;
 #pragma unroll
@@ -229,16 +215,11 @@ __device__ __forceinline__ void hold8(const float (&p)[8], int64_t m, int n, int
         top = max(top, (uint32_t)__shfl_xor(top, 1));
         top = max(top, (uint32_t)__shfl_xor(top, 2));
         const uint32_t byte = step_byte(top);
-        uint32_t c[2] = {0, 0};
+        u32x2 c = {0, 0};
 #pragma unroll
         for (int i = 0; i < 8; ++i) c[i >> 2] |= ((uint32_t)code_of(p[i], byte) & 255u) << (8 * (i & 3));
         if (have && (n & 31) == 0) e.exps[m * ((N + 31) / 32) + n / 32] = (uint8_t)byte;
-        int8_t *to = (int8_t *)e.held + m * N + n;
-        if (have == 8 && vec) *(u32x2 *)to = u32x2{c[0], c[1]};
-        else
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < have) to[i] = (int8_t)(c[i >> 2] >> (8 * (i & 3)));
+        store_codes((int8_t *)e.held + m * N + n, c, have);
     }
 }
 
@@ -247,23 +228,22 @@ __device__ __forceinline__ void hold8(const float (&p)[8], int64_t m, int n, int
 template <class T>
 __device__ __forceinline__ void finish8(float (&p)[8], int64_t m, int n, int N, bool row, const Epilogue &e)
 {
-    const bool vec = e.vec != 0;
     const int have = row ? max(0, min(8, N - n)) : 0;
     float v[8];
     if (e.bias) {
-        load8(v, (const T *)e.bias + n, have, vec);
+        load8(v, (const T *)e.bias + n, have);
 #pragma unroll
         for (int i = 0; i < 8; ++i) p[i] += v[i];
     }
-    hold8<T>(p, m, n, N, have, vec, e);
+    hold8<T>(p, m, n, N, have, e);
     if (!have) return;
     act8<sizeof(T) == 2>(p, e.act);
     if (e.res) {
-        load8(v, (const T *)e.res + m * e.ldr + n, have, vec);
+        load8(v, (const T *)e.res + m * e.ldr + n, have);
 #pragma unroll
         for (int i = 0; i < 8; ++i) p[i] += v[i];
     }
-    store8((T *)e.y + m * e.ldy + n, p, have, vec);
+    store8((T *)e.y + m * e.ldy + n, p, have);
 }
 
 }  // namespace tvl

@@ -13,7 +13,6 @@ struct SlopeArgs {
     int64_t        ldg, ldz;
     int32_t        M, N, rows_per;
     int32_t        act, kind;
-    uint32_t       vec;
 };
 
 // Eight columns a thread, 32 threads a row, eight rows at a time; `rows_per` rows a workgroup, two of a thread's rows on
@@ -29,7 +28,6 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
     const int n = ((int)blockIdx.x * 32 + lane) * 8, have = max(0, min(8, a.N - n));
     const int blocks = (a.N + 31) / 32;
     const int64_t first = (int64_t)blockIdx.y * a.rows_per, last = min((int64_t)a.M, first + a.rows_per);
-    const bool vec = a.vec != 0 && have == 8;
     float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
 
     auto slopes = [&](float (&d)[8], const float (&z)[8]) {
@@ -54,11 +52,11 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
             for (int i = 0; i < 8; ++i) v[i] = value_of((int)(int8_t)(code[i >> 2] >> (8 * (i & 3))), byte);
             slopes(d, v);
         }
-        if (a.dz) store8((T *)a.dz + m * a.ldz + n, d, have, vec);
+        if (a.dz) store8((T *)a.dz + m * a.ldz + n, d, have);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[i] += d[i];
     };
-    if (vec) {
+    if (have == 8) {
         for (int64_t m = first + share; m < last; m += kRows * kAhead) {
             u32x4 g[kAhead][kRaw], z[kAhead][kRaw];
             u32x2 code[kAhead];
@@ -67,13 +65,13 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
             for (int u = 0; u < kAhead; ++u) {
                 const int64_t r = min(m + u * kRows, last - 1);
 #pragma unroll
-                for (int j = 0; j < kRaw; ++j) g[u][j] = *((const u32x4 *)((const T *)a.g + r * a.ldg + n) + j);
+                for (int j = 0; j < kRaw; ++j) g[u][j] = get16((const T *)a.g + r * a.ldg + n + j * (16 / (int)sizeof(T)));
                 if (a.kind == kHeldPlain)
 #pragma unroll
-                    for (int j = 0; j < kRaw; ++j) z[u][j] = *((const u32x4 *)((const T *)a.held + r * a.N + n) + j);
+                    for (int j = 0; j < kRaw; ++j) z[u][j] = get16((const T *)a.held + r * a.N + n + j * (16 / (int)sizeof(T)));
                 if (a.kind == kHeldBits) word[u] = ((const uint32_t *)a.held)[r * blocks + n / 32] >> (n & 31);
                 if (a.kind == kHeld8) {
-                    code[u] = *(const u32x2 *)((const int8_t *)a.held + r * a.N + n);
+                    code[u] = *(const u32x2_at1 *)((const int8_t *)a.held + r * a.N + n);
                     byte[u] = a.exps[r * blocks + n / 32];
                 }
             }
@@ -88,16 +86,16 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
     } else if (have) {
         for (int64_t m = first + share; m < last; m += kRows) {
             float d[8];
-            load8(d, (const T *)a.g + m * a.ldg + n, have, false);
+            load8(d, (const T *)a.g + m * a.ldg + n, have);
             uint32_t word = 0, byte = 1;
             u32x2 code = {0, 0};
             u32x4 z[kRaw] = {};
             if (a.kind == kHeldBits) word = ((const uint32_t *)a.held)[m * blocks + n / 32] >> (n & 31);
             if (a.kind == kHeldPlain) {
                 float v[8];
-                load8(v, (const T *)a.held + m * a.N + n, have, false);
+                load8(v, (const T *)a.held + m * a.N + n, have);
                 slopes(d, v);
-                if (a.dz) store8((T *)a.dz + m * a.ldz + n, d, have, false);
+                if (a.dz) store8((T *)a.dz + m * a.ldz + n, d, have);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum[i] += d[i];
                 continue;

@@ -142,21 +142,10 @@ int run_product(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_
     return launched();
 }
 
-// Eight columns at once where every row of every array that the epilogue touches starts on such a boundary.
-uint32_t epilogue_vec(const Epilogue &e, size_t size, int64_t N)
-{
-    const int64_t per = 16 / (int64_t)size;
-    if (N % 8 || e.ldy % per || !aligned(e.y, 16)) return 0;
-    if (e.res && (e.ldr % per || !aligned(e.res, 16))) return 0;
-    if (!aligned(e.bias, 16)) return 0;
-    return aligned(e.held, e.kind == kHeldPlain ? 16 : 8) || e.kind == kHeldBits;
-}
-
-Epilogue plain_output(void *y, int64_t ldy, size_t size, int64_t N)
+Epilogue plain_output(void *y, int64_t ldy)
 {
     Epilogue e{};
     e.y = y; e.ldy = ldy;
-    e.vec = epilogue_vec(e, size, N);
     return e;
 }
 
@@ -216,7 +205,6 @@ int linear_fwd(const void *x, const void *w, const void *bias, const void *res, 
     e.bias = bias; e.res = res; e.y = y;
     e.held = h.kind == TV_HELD_NONE ? nullptr : h.data; e.exps = h.exps;
     e.ldr = d.ldr; e.ldy = d.ldy; e.act = d.act; e.kind = h.kind;
-    e.vec = epilogue_vec(e, sizeof(T), d.n);
     return run_product<T, T, false, false>({x, d.ldx, d.k, false}, {w, d.ldw, d.k, false}, d.m, d.n, d.k, c, e, ws, stream);
 }
 
@@ -270,8 +258,6 @@ int linear_bwd(const void *g, const void *x, const uint8_t *x_exps, const tv_hel
         a.ldg = d.ldy; a.ldz = p.ldz;
         a.M = (int32_t)d.m; a.N = (int32_t)d.n; a.rows_per = p.rows_per;
         a.act = d.act; a.kind = d.act == TV_ACT_NONE ? TV_HELD_NONE : h.kind;
-        // (dz's rows start on 16-byte boundaries by themselves)
-        a.vec = d.n % 8 == 0 && d.ldy % (16 / (int64_t)sizeof(T)) == 0 && aligned(g, 16) && aligned(h.data, a.kind == kHeldPlain ? 16 : 8);
         hipLaunchKernelGGL((slope_kernel<T>), dim3((uint32_t)tiles(d.n, 256), p.groups), dim3(256), 0, stream, a);
         if (launched() != TV_OK) return TV_ERR_HIP;
         if (a.dz) dz = {a.dz, p.ldz, d.n, false};
@@ -284,7 +270,7 @@ int linear_bwd(const void *g, const void *x, const uint8_t *x_exps, const tv_hel
     if (dx && d.m > 0) {
         const Operand ow{w, d.ldw, d.k, false};
         const int st = run_product<T, T, false, true>(dz, ow, d.m, d.k, d.n, choose(d.dtype, direct(dz) && direct(ow), true, d.m, d.k, d.n),
-                                                   plain_output(dx, d.k, sizeof(T), d.k), ws + p.split, stream);
+                                                   plain_output(dx, d.k), ws + p.split, stream);
         if (st != TV_OK) return st;
     }
     if (dw) {
@@ -295,7 +281,7 @@ int linear_bwd(const void *g, const void *x, const uint8_t *x_exps, const tv_hel
             xs = {ws + p.x, p.ldx, d.k, false};
         }
         const Choice c = choose(d.dtype, direct(dz) && direct(xs), true, d.n, d.k, d.m);
-        const Epilogue e = plain_output(dw, d.k, sizeof(T), d.k);
+        const Epilogue e = plain_output(dw, d.k);
         return x_exps ? run_product<T, bf16, true, true>(dz, xs, d.n, d.k, d.m, c, e, ws + p.split, stream)
                       : run_product<T, T, true, true>(dz, xs, d.n, d.k, d.m, c, e, ws + p.split, stream);
     }
@@ -371,11 +357,10 @@ int tv_ckpt8_save(const void *x, int8_t *codes, uint8_t *exps, int64_t rows, int
     const size_t size = elem_bytes(dtype);
     if (!aligned(x, size)) return TV_ERR_STRIDE;
     const int blocks = (int)tiles(n, kBlock);
-    const uint32_t vec = n % 8 == 0 && ldx % 4 == 0 && aligned(x, 4 * size) && aligned(codes, 8);
     if (dtype == TV_BF16)
-        hipLaunchKernelGGL((ckpt8_save_kernel<bf16>), ckpt8_grid(rows, n), dim3(256), 0, stream, (const bf16 *)x, ldx, codes, exps, rows, (int)n, blocks, vec);
+        hipLaunchKernelGGL((ckpt8_save_kernel<bf16>), ckpt8_grid(rows, n), dim3(256), 0, stream, (const bf16 *)x, ldx, codes, exps, rows, (int)n, blocks);
     else
-        hipLaunchKernelGGL((ckpt8_save_kernel<float>), ckpt8_grid(rows, n), dim3(256), 0, stream, (const float *)x, ldx, codes, exps, rows, (int)n, blocks, vec);
+        hipLaunchKernelGGL((ckpt8_save_kernel<float>), ckpt8_grid(rows, n), dim3(256), 0, stream, (const float *)x, ldx, codes, exps, rows, (int)n, blocks);
     return launched();
 }
 
@@ -387,11 +372,10 @@ int tv_ckpt8_load(const int8_t *codes, const uint8_t *exps, void *x, int64_t row
     const size_t size = elem_bytes(dtype);
     if (!aligned(x, size)) return TV_ERR_STRIDE;
     const int blocks = (int)tiles(n, kBlock);
-    const uint32_t vec = n % 8 == 0 && ldx % 4 == 0 && aligned(x, 4 * size) && aligned(codes, 8);
     if (dtype == TV_BF16)
-        hipLaunchKernelGGL((ckpt8_load_kernel<bf16>), ckpt8_grid(rows, n), dim3(256), 0, stream, codes, exps, (bf16 *)x, ldx, rows, (int)n, blocks, vec);
+        hipLaunchKernelGGL((ckpt8_load_kernel<bf16>), ckpt8_grid(rows, n), dim3(256), 0, stream, codes, exps, (bf16 *)x, ldx, rows, (int)n, blocks);
     else
-        hipLaunchKernelGGL((ckpt8_load_kernel<float>), ckpt8_grid(rows, n), dim3(256), 0, stream, codes, exps, (float *)x, ldx, rows, (int)n, blocks, vec);
+        hipLaunchKernelGGL((ckpt8_load_kernel<float>), ckpt8_grid(rows, n), dim3(256), 0, stream, codes, exps, (float *)x, ldx, rows, (int)n, blocks);
     return launched();
 }
 
