@@ -123,15 +123,19 @@ __device__ __attribute__((noinline)) f32x16 tile_in_f32(const TA *a, const TB *b
 }
 
 // T: A's type and the outputs'; TB: B's.
-template <class T, class TB, int BM, int BN, int WM, int WN, int KQ, int AHEAD, bool AT, bool BT>
-__global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void gemm_split_kernel(Product g, Epilogue e)
+// G: groups of waves that share out a step's contraction, each with sums of its own for all outputs; they are joined in LDS at
+// the end.  (A small tile has few waves; two groups keep the matrix units busy where one waits.)
+template <class T, class TB, int BM, int BN, int WM, int WN, int KQ, int AHEAD, int G, bool AT, bool BT>
+__global__ __launch_bounds__(WM * WN * G * 64) __attribute__((amdgpu_waves_per_eu(2))) void gemm_split_kernel(Product g, Epilogue e)
 {
-    constexpr int W = WM * WN, THREADS = W * 64, TM = BM / WM / 32, TN = BN / WN / 32, P = Parts<T>::kCount, PB = Parts<TB>::kCount;
+    constexpr int W = WM * WN, THREADS = W * G * 64, TM = BM / WM / 32, TN = BN / WN / 32, P = Parts<T>::kCount, PB = Parts<TB>::kCount;
     constexpr int kOrders = P > PB ? P : PB;
     using TileA = Staged<T, BM, THREADS, KQ, AT>;
     using TileB = Staged<TB, BN, THREADS, KQ, BT>;
     constexpr int kA = P * TileA::kBytes, kB = PB * TileB::kBytes, kOut = W * 32 * kOutPitch * 4;
+    constexpr int kJoin = G > 1 ? (G - 1) * BM * BN * 4 : 0;
     static_assert(TN % 2 == 0, "a wave's outputs leave 64 columns at a time");
+    static_assert(KQ % G == 0 && kJoin <= 2 * (kA + kB), "");
     __shared__ __attribute__((aligned(1024))) char lds[2 * (kA + kB) > kOut ? 2 * (kA + kB) : kOut];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     uint32_t tm, tn;
@@ -142,7 +146,7 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
     const int n0 = BT ? min((int)tn * BN, max(0, g.N - BN)) : (int)tn * BN;
     const int k0 = (int)blockIdx.y * g.k_per, k_end = min(g.K, k0 + g.k_per);
     const int steps = (k_end - k0 + 16 * KQ - 1) / (16 * KQ);
-    const int wm = wave % WM * (BM / WM), wn = wave / WM * (BN / WN);
+    const int group = wave / W, wm = wave % WM * (BM / WM), wn = wave % W / WM * (BN / WN);
 
     f32x16 acc[TN][TM];
     each<TN * TM>([&](auto x) __attribute__((always_inline)) { acc[x % TN][x / TN] = f32x16{}; });
@@ -164,7 +168,8 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
     };
     auto step = [&](auto which, Both &r, const char *from, char *to, int s) {
 #pragma unroll
-        for (int q = 0; q < KQ; ++q) {
+        for (int i = 0; i < KQ / G; ++i) {
+            const int q = group * (KQ / G) + i;
             bf16x8 fa[P][TM], fb[PB][TN];
 #pragma unroll
             for (int o = 0; o < PB; ++o)
@@ -189,15 +194,15 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
         put(r, to);
         load(which, r, s + 1 + AHEAD);
         if constexpr (AHEAD > 1) {
-            constexpr int kReads = KQ * (P * TM * (AT ? 2 : 1) + PB * TN * (BT ? 2 : 1));
-            constexpr int kMfma = (P * PB > 3 ? 6 : P * PB) * KQ * TM * TN;
+            constexpr int kReads = KQ / G * (P * TM * (AT ? 2 : 1) + PB * TN * (BT ? 2 : 1));
+            constexpr int kMfma = (P * PB > 3 ? 6 : P * PB) * (KQ / G) * TM * TN;
             constexpr int kSplit = TileA::kUnits * (P > 1 ? 60 : 8) + TileB::kUnits * (PB > 1 ? 60 : 8), kEach = (kSplit + kMfma - 1) / kMfma;
-            __builtin_amdgcn_sched_group_barrier(0x100, kReads / KQ, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, kReads / (KQ / G), 0);
 #pragma unroll
             for (int x = 0; x < kMfma; ++x) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
                 __builtin_amdgcn_sched_group_barrier(0x002, kEach, 0);
-                if (x * 2 < kReads - kReads / KQ) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                if (x * 2 < kReads - kReads / (KQ / G)) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
             }
         }
         __syncthreads();
@@ -224,6 +229,28 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
     for (; s < steps; s += 2) {
         step(some, raw[1 % AHEAD], even, odd, s);
         step(some, raw[0], odd, even, s + 1);
+    }
+    if constexpr (G > 1) {
+        // sum by sum, so that a wave's lanes write side by side
+        float *mine = (float *)lds + (wave % W) * (TM * TN * 16 * 64) + lane;
+        each<G - 1>([&](auto y) __attribute__((always_inline)) {
+            constexpr int from = y + 1;
+            float *there = mine + y * (BM * BN);
+            if (group == from)
+                each<TM * TN>([&](auto x) __attribute__((always_inline)) {
+                    each<16>([&](auto q) __attribute__((always_inline)) { there[(x * 16 + q) * 64] = acc[x % TN][x / TN][decltype(q)::value]; });
+                });
+        });
+        __syncthreads();
+        if (group == 0)
+            each<G - 1>([&](auto y) __attribute__((always_inline)) {
+                const float *there = mine + y * (BM * BN);
+                each<TM * TN>([&](auto x) __attribute__((always_inline)) {
+                    each<16>([&](auto q) __attribute__((always_inline)) { acc[x % TN][x / TN][decltype(q)::value] += there[(x * 16 + q) * 64]; });
+                });
+            });
+        __syncthreads();
+        if (group) return;                            // (no barrier comes after this)
     }
     if constexpr (P * PB > 1) {
         uint32_t most = 0;                            // of all sums, a NaN's bits being above infinity's

@@ -10,6 +10,7 @@ struct SlopeArgs {
     const uint8_t *exps;
     void          *dz;         // [M, N] rows of ldz elements, or null (the column sums alone)
     float         *sums;       // [groups of rows, N] column sums, or null
+    void          *db;         // [N] column sums of all rows (where one group holds them), or null
     int64_t        ldg, ldz;
     int32_t        M, N, rows_per;
     int32_t        act, kind;
@@ -109,19 +110,18 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
             row(m, d, word, byte, z, code);
         }
     }
-    if (!a.sums) return;
+    if (!a.sums && !a.db) return;
     if (share)
 #pragma unroll
         for (int i = 0; i < 8; ++i) part[share - 1][lane][i] = sum[i];
     __syncthreads();
     if (share == 0 && have) {
-        float *to = a.sums + (int64_t)blockIdx.y * a.N + n;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int r = 0; r < kRows - 1; ++r) sum[i] += part[r][lane][i];
-            if (i < have) to[i] = sum[i];
-        }
+        if (a.db) store8((T *)a.db + n, sum, have);
+        else store8(a.sums + (int64_t)blockIdx.y * a.N + n, sum, have);
     }
 }
 

@@ -70,9 +70,9 @@ Choice choose(int dtype, bool direct, bool transposed, int64_t M, int64_t N, int
     struct Cost { Kind kind; int64_t slots; double round, step; };
     constexpr Cost direct16[] = {{kTile64, 256, 1.0, 0.30}, {kTile128Deep, 256, 2.0, 0.47}, {kTile128, 512, 3.0, 0.88}, {kTile256, 256, 6.5, 1.50}};
     constexpr Cost any16[] = {{kSplit64, 256, 1.5, 0.62}, {kSplit64, 512, 2.0, 0.85}, {kSplit128, 256, 3.0, 0.95}};
-    constexpr Cost any32[] = {{kSplit64, 256, 2.0, 1.6}, {kSplit64, 512, 2.5, 3.2}, {kSplit128, 256, 3.5, 2.65}, {kSplit256, 256, 8.0, 9.0}};
+    constexpr Cost any32[] = {{kSplit64, 256, 2.5, 1.35}, {kSplit128, 256, 3.5, 2.65}, {kSplit256, 256, 8.0, 9.0}};
     const Cost *costs = dtype != TV_BF16 ? any32 : direct ? direct16 : any16;
-    const int kinds = dtype == TV_BF16 && !direct ? 3 : 4;
+    const int kinds = dtype == TV_BF16 && direct ? 4 : 3;
     Choice best = cut(costs[0].kind, 1, K, 64);
     double least = 1e30;
     for (int i = 0; i < kinds; ++i) {
@@ -121,12 +121,12 @@ int run_product(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_
         if (c.kind == kTile128) launch_tiles<128, 128, 256>(gemm16_kernel<128, 128, 2, 2, 2, AT, BT>, g, e, stream);
         if (c.kind == kTile128Deep) launch_tiles<128, 128, 256>(gemm16_kernel<128, 128, 2, 2, 4, AT, BT>, g, e, stream);
         if (c.kind == kTile64) launch_tiles<64, 128, 256>(gemm16_kernel<64, 128, 2, 2, 4, AT, BT>, g, e, stream);
-        if (c.kind == kSplit128) launch_tiles<128, 128, 256>(gemm_split_kernel<T, TB, 128, 128, 2, 2, 4, 2, AT, BT>, g, e, stream);
-        if (c.kind == kSplit64) launch_tiles<64, 128, 256>(gemm_split_kernel<T, TB, 64, 128, 2, 2, 4, 2, AT, BT>, g, e, stream);
+        if (c.kind == kSplit128) launch_tiles<128, 128, 256>(gemm_split_kernel<T, TB, 128, 128, 2, 2, 4, 2, 1, AT, BT>, g, e, stream);
+        if (c.kind == kSplit64) launch_tiles<64, 128, 256>(gemm_split_kernel<T, TB, 64, 128, 2, 2, 4, 2, 1, AT, BT>, g, e, stream);
     } else {
-        if (c.kind == kSplit256) launch_tiles<256, 256, 512>(gemm_split_kernel<T, TB, 256, 256, 2, 4, 1, 1, AT, BT>, g, e, stream);
-        if (c.kind == kSplit128) launch_tiles<128, 128, 512>(gemm_split_kernel<T, TB, 128, 128, 4, 2, 2, 2, AT, BT>, g, e, stream);
-        if (c.kind == kSplit64) launch_tiles<64, 128, 256>(gemm_split_kernel<T, TB, 64, 128, 2, 2, 2, 2, AT, BT>, g, e, stream);
+        if (c.kind == kSplit256) launch_tiles<256, 256, 512>(gemm_split_kernel<T, TB, 256, 256, 2, 4, 1, 1, 1, AT, BT>, g, e, stream);
+        if (c.kind == kSplit128) launch_tiles<128, 128, 512>(gemm_split_kernel<T, TB, 128, 128, 4, 2, 2, 2, 1, AT, BT>, g, e, stream);
+        if (c.kind == kSplit64) launch_tiles<64, 128, 512>(gemm_split_kernel<T, TB, 64, 128, 2, 2, 4, 2, 2, AT, BT>, g, e, stream);
     }
     if constexpr (!AT && !BT)
         if (c.kind == kFew) {
@@ -228,7 +228,7 @@ BwdPlan bwd_plan(const tv_linear_desc &d, bool x8)
     if (x8) at += up(d.m * p.ldx * 2, 256);
     // about 1024 workgroups of 256 columns each, of sixteen rows at least
     const int64_t want = 1024 / tiles(d.n, 256) + 1;
-    p.rows_per = (int)(d.m > 0 ? up(tiles(d.m, want < 256 ? want : 256), 16) : 16);
+    p.rows_per = (int)(d.m > 64 ? up(tiles(d.m, want < 256 ? want : 256), 16) : 64);       // (up to 64 rows: one group, one launch)
     p.groups = (int)tiles(d.m, p.rows_per);
     p.sums = at;
     at += up((int64_t)p.groups * d.n * 4, 256);
@@ -254,7 +254,8 @@ int linear_bwd(const void *g, const void *x, const uint8_t *x_exps, const tv_hel
         SlopeArgs a{};
         a.g = g; a.held = h.data; a.exps = h.exps;
         a.dz = d.act != TV_ACT_NONE ? ws + p.dz : nullptr;
-        a.sums = db ? (float *)(ws + p.sums) : nullptr;
+        a.sums = db && p.groups > 1 ? (float *)(ws + p.sums) : nullptr;
+        a.db = p.groups == 1 ? db : nullptr;
         a.ldg = d.ldy; a.ldz = p.ldz;
         a.M = (int32_t)d.m; a.N = (int32_t)d.n; a.rows_per = p.rows_per;
         a.act = d.act; a.kind = d.act == TV_ACT_NONE ? TV_HELD_NONE : h.kind;
@@ -262,7 +263,7 @@ int linear_bwd(const void *g, const void *x, const uint8_t *x_exps, const tv_hel
         if (launched() != TV_OK) return TV_ERR_HIP;
         if (a.dz) dz = {a.dz, p.ldz, d.n, false};
     }
-    if (db) {
+    if (db && p.groups != 1) {
         hipLaunchKernelGGL((column_sum_kernel<T>), dim3((uint32_t)tiles(d.n, 32)), dim3(256), 0, stream,
                            (const float *)(ws + p.sums), (T *)db, d.m > 0 ? p.groups : 0, (int)d.n);
         if (launched() != TV_OK) return TV_ERR_HIP;
