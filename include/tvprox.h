@@ -323,10 +323,14 @@ int tv2d_prox_bwd_bf16(const uint16_t *g_up, uint16_t *grad_y, float *grad_lam, 
  * bf16, dz is rounded to bf16 before the products that give dx and dW (db sums it unrounded).
  * Activations: gelu is z Phi(z) (with erf), silu z / (1 + exp(-z)); ReLU is 0 where z <= 0, with slope 0 there.
  *
+ * Sizes are below 2^31 - 1024, and each of y, dx and dW has at most TV_LINEAR_MAX_TILES tiles of 128 x 128
+ * (TV_ERR_SHAPE beyond: 1.7e10 outputs).
+ *
  * m = 0: the forward call does nothing, the backward call sets dw and db to zero.  Results do not depend on the
  * stream, on timing or on what the workspace holds; how the contraction is split (and so the last bits of the
  * fp32 sums) depends on the sizes alone.
  */
+#define TV_LINEAR_MAX_TILES 1048576
 typedef enum { TV_F32 = 0, TV_BF16 = 1 } tv_dtype;
 typedef enum { TV_ACT_NONE = 0, TV_ACT_RELU = 1, TV_ACT_GELU = 2, TV_ACT_SILU = 3 } tv_act;
 

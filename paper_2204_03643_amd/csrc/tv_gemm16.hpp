@@ -75,6 +75,17 @@ template <int ROWS, int WAVES, bool TRANSPOSED> struct Tile16 {
     }
 };
 
+// Rows of `cols` values from anywhere to rows on 16-byte boundaries, zeros up to a multiple of eight: a unit of eight a thread.
+__global__ __launch_bounds__(256) void copy_rows_kernel(const bf16 *from, int64_t ld, bf16 *to, int cols, int64_t units)
+{
+    const int64_t at = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
+    if (at >= units) return;
+    const int per = (cols + 7) / 8;
+    const int64_t row = at / per;
+    const int col = (int)(at - row * per) * 8;
+    *(u32x4 *)(to + at * 8) = load16(from + row * ld + col, cols - col);
+}
+
 // Which tile a workgroup takes.  Workgroups go to the eight XCDs in turn; each XCD takes a run of consecutive tiles, and
 // consecutive tiles form columns of eight, so that what an XCD works on at a time shares rows of both operands in its L2.
 __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tm, uint32_t tn, uint32_t &m, uint32_t &n)

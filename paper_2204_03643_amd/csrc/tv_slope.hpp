@@ -8,7 +8,7 @@ struct SlopeArgs {
     const void    *g;          // [M, N] rows of ldg elements
     const void    *held;       // z as the forward call held it
     const uint8_t *exps;
-    void          *dz;         // [M, N] rows of ldz elements, or null (the column sums alone)
+    void          *dz;         // [M, ldz], rows on 16-byte boundaries, zeros past N; or null (the column sums alone)
     float         *sums;       // [groups of rows, N] column sums, or null
     void          *db;         // [N] column sums of all rows (where one group holds them), or null
     int64_t        ldg, ldz;
@@ -53,7 +53,7 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
             for (int i = 0; i < 8; ++i) v[i] = value_of((int)(int8_t)(code[i >> 2] >> (8 * (i & 3))), byte);
             slopes(d, v);
         }
-        if (a.dz) store8((T *)a.dz + m * a.ldz + n, d, have);
+        if (a.dz) store8((T *)a.dz + m * a.ldz + n, d, 8);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[i] += d[i];
     };
@@ -86,28 +86,32 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
         }
     } else if (have) {
         for (int64_t m = first + share; m < last; m += kRows) {
-            float d[8];
+            float d[8], v[8];
             load8(d, (const T *)a.g + m * a.ldg + n, have);
             uint32_t word = 0, byte = 1;
             u32x2 code = {0, 0};
             u32x4 z[kRaw] = {};
             if (a.kind == kHeldBits) word = ((const uint32_t *)a.held)[m * blocks + n / 32] >> (n & 31);
             if (a.kind == kHeldPlain) {
-                float v[8];
                 load8(v, (const T *)a.held + m * a.N + n, have);
-                slopes(d, v);
-                if (a.dz) store8((T *)a.dz + m * a.ldz + n, d, have);
+                if constexpr (sizeof(T) == 2) {
+                    bf16x8 h;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum[i] += d[i];
-                continue;
+                    for (int i = 0; i < 8; ++i) h[i] = narrow<bf16>(v[i]);       // (exact: they were bf16)
+                    z[0] = __builtin_bit_cast(u32x4, h);
+                } else {
+                    z[0] = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
+                    z[kRaw - 1] = __builtin_bit_cast(u32x4, f32x4{v[4], v[5], v[6], v[7]});
+                }
             }
             if (a.kind == kHeld8) {
+                // (past the end the code of zero)
                 const uint8_t *from = (const uint8_t *)a.held + m * a.N + n;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) code[i >> 2] |= (uint32_t)from[min(i, have - 1)] << (8 * (i & 3));
+                for (int i = 0; i < 8; ++i) code[i >> 2] |= (i < have ? (uint32_t)from[min(i, have - 1)] : 0u) << (8 * (i & 3));
                 byte = a.exps[m * blocks + n / 32];
             }
-            row(m, d, word, byte, z, code);
+            row(m, d, word, byte, z, code);          // g is zero past the end, and so is dz
         }
     }
     if (!a.sums && !a.db) return;

@@ -10,8 +10,9 @@ namespace {
 
 using namespace tvl;
 
-constexpr int64_t kMostIndex = (int64_t)1 << 31;      // sizes and strides stay below
-constexpr int64_t kMostTiles = (int64_t)1 << 22;      // workgroups of a launch
+constexpr int64_t kMostIndex = ((int64_t)1 << 31) - 1024;      // sizes stay below: a step past the end fits 32 bits too
+constexpr int64_t kMostStride = (int64_t)1 << 31;              // strides stay below
+constexpr int64_t kMostTiles = TV_LINEAR_MAX_TILES;            // so that every launch has fewer than 2^32 threads
 
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 int64_t tiles(int64_t v, int64_t of) { return (v + of - 1) / of; }
@@ -20,20 +21,26 @@ bool aligned(const void *p, size_t to) { return (uintptr_t)p % to == 0; }
 int launched() { return hipGetLastError() == hipSuccess ? TV_OK : TV_ERR_HIP; }
 
 // ---- products
-// One operand: rows of `cols` elements, ld apart; padded: readable, and zero, up to a multiple of eight columns.
+// One operand: `rows` rows of `cols` elements, ld apart.
 struct Operand {
     const void *p;
-    int64_t ld, cols;
-    bool padded;
+    int64_t ld, rows, cols;
 };
+
+// Rows on 16-byte boundaries, whole 16-byte pieces, and offsets within a tile of 256 rows that 32 bits hold.
+bool direct(const Operand &o)
+{
+    return aligned(o.p, 16) && o.ld % 8 == 0 && o.cols % 8 == 0 && o.ld <= ((int64_t)1 << 22);
+}
 
 constexpr int64_t kFewRows = 64;
 
-// Which kernel a product takes and how its contraction is split, from sizes and alignment alone.
+// Which kernel a product takes and how its contraction is split.
 enum Kind { kFew, kTile256, kTile128, kTile128Deep, kTile64, kSplit256, kSplit128, kSplit64 };
 struct Choice {
     Kind kind;
     int splits, k_per;
+    double us;           // what the model says
 };
 
 struct Tile { int m, n; };
@@ -44,51 +51,70 @@ Tile tile_of_kind(Kind k)
     return {128, 128};
 }
 
-int64_t few_columns(int64_t) { return 32; }
-
 // `s` splits of a contraction of K, each a multiple of `unit`
 Choice cut(Kind kind, int64_t s, int64_t K, int64_t unit)
 {
     if (s < 1) s = 1;
     const int64_t per = up(K > 0 ? tiles(K, s) : 1, unit);
-    return {kind, (int)(K > 0 ? tiles(K, per) : 1), (int)per};
+    return {kind, (int)(K > 0 ? tiles(K, per) : 1), (int)per, 0.0};
 }
 
+// Sizes, type and alignment alone decide.  A few rows stream the weight: up to 32 of them, or 64 where the operands
+// would not go straight to LDS (64 rows, 2048 -> 8192, bf16: 16 us against 13 through tiles, f32 34 against 42).
+//
+// Otherwise the cheapest by a model of the time in microseconds, fitted to sweeps of tiles and splits over outputs of
+// 128 x 128 to 8192 x 8192 and contractions of 64 to 8192: a launch, rounds of workgroups over 256 compute units (of
+// two workgroups each where there are more than 256 of a kernel that leaves room for two), in each a start and an end
+// and so much a step of 64, and for split contractions the second launch and the sums' trip through memory.
 Choice choose(int dtype, bool direct, bool transposed, int64_t M, int64_t N, int64_t K)
 {
     if (!transposed && M >= 1 && M <= (direct && dtype == TV_BF16 ? kFewRows / 2 : kFewRows)) {
         const int64_t turn = 8 * 64 / (int64_t)elem_bytes(dtype);            // a turn of all eight waves
-        const int64_t t = tiles(N, few_columns(M));
-        const int64_t s = t >= 256 ? 1 : 256 / t;
+        const int64_t t = tiles(N, 32), s = t >= 256 ? 1 : 256 / t;
         return cut(kFew, s < K / (8 * turn) ? s : K / (8 * turn), K, turn);
     }
     /*SWEEP*/
-    // The cheapest by a model of the time in microseconds, fitted to sweeps of tiles and splits over outputs of
-    // 128 x 128 to 8192 x 8192 and contractions of 64 to 8192: a launch, rounds of workgroups over 256 compute units (of
-    // two workgroups each where there are more than 256 of a kernel that leaves room for two), in each a start and an end
-    // and so much a step of 64, and for split contractions the second launch and the sums' trip through memory.
     struct Cost { Kind kind; int64_t slots; double round, step; };
     constexpr Cost direct16[] = {{kTile64, 256, 1.0, 0.30}, {kTile128Deep, 256, 2.0, 0.47}, {kTile128, 512, 3.0, 0.88}, {kTile256, 256, 6.5, 1.50}};
-    constexpr Cost any16[] = {{kSplit64, 256, 1.5, 0.62}, {kSplit64, 512, 2.0, 0.85}, {kSplit128, 256, 3.0, 0.95}};
+    constexpr Cost any16[] = {{kSplit64, 256, 1.5, 0.62}, {kSplit64, 512, 2.0, 0.85}};
     constexpr Cost any32[] = {{kSplit64, 256, 2.5, 1.35}, {kSplit128, 256, 3.5, 2.65}, {kSplit256, 256, 8.0, 9.0}};
     const Cost *costs = dtype != TV_BF16 ? any32 : direct ? direct16 : any16;
-    const int kinds = dtype == TV_BF16 && direct ? 4 : 3;
+    const int kinds = dtype != TV_BF16 ? 3 : direct ? 4 : 2;
     Choice best = cut(costs[0].kind, 1, K, 64);
-    double least = 1e30;
+    best.us = 1e30;
     for (int i = 0; i < kinds; ++i) {
         const Cost &c = costs[i];
         const Tile side = tile_of_kind(c.kind);
         const int64_t t = tiles(M, side.m) * tiles(N, side.n);
         for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
             if (s > 1 && (K < 128 * s || t * s > 1024)) break;
-            const Choice x = cut(c.kind, s, K, 64);
-            double us = 3.0 + (double)tiles(t * x.splits, c.slots) * (c.round + c.step * (double)tiles(x.k_per < K ? x.k_per : K, 64));
-            if (x.splits > 1) us += 4.0 + (double)M * (double)N * x.splits * 8 / 6e6;
-            if (us < least) { least = us; best = x; }
+            Choice x = cut(c.kind, s, K, 64);
+            x.us = 3.0 + (double)tiles(t * x.splits, c.slots) * (c.round + c.step * (double)tiles(x.k_per < K ? x.k_per : K, 64));
+            if (x.splits > 1) x.us += 4.0 + (double)M * (double)N * x.splits * 8 / 6e6;
+            if (x.us < best.us) best = x;
         }
     }
     return best;
 }
+
+// bf16 operands that cannot go straight to LDS are copied to rows that can, where the faster kernel pays for it
+// (8192 x 2047 -> 8191: 480 us without, 290 with): a launch and the bytes there and back each.
+struct Plan {
+    Choice c;
+    bool copy_a, copy_b;
+};
+double copy_us(int64_t rows, int64_t cols) { return 4.0 + (double)rows * (double)cols * 4 / 4e6; }
+
+Plan plan(int dtype, bool direct_a, bool direct_b, bool transposed, int64_t M, int64_t N, int64_t K)
+{
+    Plan p{choose(dtype, direct_a && direct_b, transposed, M, N, K), false, false};
+    if (dtype != TV_BF16 || (direct_a && direct_b) || p.c.kind == kFew || M < 1 || K < 1) return p;
+    Choice c = choose(dtype, true, true, M, N, K);
+    c.us += (direct_a ? 0.0 : copy_us(M, K)) + (direct_b ? 0.0 : copy_us(N, K));
+    return c.us < p.c.us ? Plan{c, !direct_a, !direct_b} : p;
+}
+
+int64_t copy_bytes(int64_t rows, int64_t cols) { return up(rows * up(cols, 8) * 2, 256); }
 
 size_t split_bytes(const Choice &c, int64_t M, int64_t N)
 {
@@ -97,10 +123,14 @@ size_t split_bytes(const Choice &c, int64_t M, int64_t N)
 
 bool product_fits(int64_t M, int64_t N) { return tiles(M, 128) * tiles(N, 128) <= kMostTiles; }
 
-// Rows on 16-byte boundaries, whole 16-byte pieces, and offsets within a tile of 256 rows that 32 bits hold.
-bool direct(const Operand &o)
+int copy_operand(Operand &o, void *to, hipStream_t stream)
 {
-    return aligned(o.p, 16) && o.ld % 8 == 0 && (o.cols % 8 == 0 || o.padded) && o.ld <= ((int64_t)1 << 22);
+    const int64_t ld = up(o.cols, 8), units = o.rows * (ld / 8);
+    const int64_t groups = tiles(units, 256), wide = (int64_t)1 << 22;
+    const dim3 grid = groups <= wide ? dim3((uint32_t)groups) : dim3((uint32_t)wide, (uint32_t)tiles(groups, wide));
+    hipLaunchKernelGGL(copy_rows_kernel, grid, dim3(256), 0, stream, (const bf16 *)o.p, o.ld, (bf16 *)to, (int)o.cols, units);
+    o = {to, ld, o.rows, ld};
+    return launched();
 }
 
 template <int BM, int BN, int THREADS>
@@ -121,7 +151,6 @@ int run_product(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_
         if (c.kind == kTile128) launch_tiles<128, 128, 256>(gemm16_kernel<128, 128, 2, 2, 2, AT, BT>, g, e, stream);
         if (c.kind == kTile128Deep) launch_tiles<128, 128, 256>(gemm16_kernel<128, 128, 2, 2, 4, AT, BT>, g, e, stream);
         if (c.kind == kTile64) launch_tiles<64, 128, 256>(gemm16_kernel<64, 128, 2, 2, 4, AT, BT>, g, e, stream);
-        if (c.kind == kSplit128) launch_tiles<128, 128, 256>(gemm_split_kernel<T, TB, 128, 128, 2, 2, 4, 2, 1, AT, BT>, g, e, stream);
         if (c.kind == kSplit64) launch_tiles<64, 128, 256>(gemm_split_kernel<T, TB, 64, 128, 2, 2, 4, 2, 1, AT, BT>, g, e, stream);
     } else {
         if (c.kind == kSplit256) launch_tiles<256, 256, 512>(gemm_split_kernel<T, TB, 256, 256, 2, 4, 1, 1, 1, AT, BT>, g, e, stream);
@@ -130,7 +159,7 @@ int run_product(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_
     }
     if constexpr (!AT && !BT)
         if (c.kind == kFew) {
-            const dim3 grid((uint32_t)tiles(N, few_columns(M)), c.splits), block(512);
+            const dim3 grid((uint32_t)tiles(N, 32), c.splits), block(512);
             if (M <= 16) hipLaunchKernelGGL((gemv_kernel<T, 1, 2, 8>), grid, block, 0, stream, g, e);
             else if (M <= 32) hipLaunchKernelGGL((gemv_kernel<T, 2, 2, 8>), grid, block, 0, stream, g, e);
             else hipLaunchKernelGGL((gemv_kernel<T, 4, 2, 4>), grid, block, 0, stream, g, e);
@@ -152,10 +181,10 @@ Epilogue plain_output(void *y, int64_t ldy)
 // ---- validation
 int check_sizes(const tv_linear_desc &d)
 {
-    if (d.m < 0 || d.k < 1 || d.n < 1 || d.m >= kMostIndex || d.k >= kMostIndex - 128 || d.n >= kMostIndex - 128) return TV_ERR_SHAPE;
+    if (d.m < 0 || d.k < 1 || d.n < 1 || d.m >= kMostIndex || d.k >= kMostIndex || d.n >= kMostIndex) return TV_ERR_SHAPE;
     if (!product_fits(d.m, d.n) || !product_fits(d.m, d.k) || !product_fits(d.n, d.k)) return TV_ERR_SHAPE;
     if ((d.dtype != TV_F32 && d.dtype != TV_BF16) || d.act < TV_ACT_NONE || d.act > TV_ACT_SILU) return TV_ERR_UNSUPPORTED;
-    if (d.ldx < d.k || d.ldw < d.k || d.ldy < d.n || d.ldx >= kMostIndex || d.ldw >= kMostIndex || d.ldy >= kMostIndex) return TV_ERR_STRIDE;
+    if (d.ldx < d.k || d.ldw < d.k || d.ldy < d.n || d.ldx >= kMostStride || d.ldw >= kMostStride || d.ldy >= kMostStride) return TV_ERR_STRIDE;
     return TV_OK;
 }
 
@@ -184,76 +213,85 @@ int check_workspace(const void *ws, size_t have, size_t need)
     return need && (!ws || !aligned(ws, 16) || have < need) ? TV_ERR_WORKSPACE : TV_OK;
 }
 
-Choice fwd_choice(const tv_linear_desc &d, const void *x, const void *w)
-{
-    return choose(d.dtype, direct({x, d.ldx, d.k, false}) && direct({w, d.ldw, d.k, false}), false, d.m, d.n, d.k);
-}
+// ---- the forward call's workspace: copies of x and W, split sums
+struct FwdPlan {
+    Plan product;
+    size_t w, split, bytes;
+};
 
-// (The workspace is asked for before there are pointers, and has to do for either choice.)
-size_t fwd_bytes(const tv_linear_desc &d)
+FwdPlan fwd_plan(const tv_linear_desc &d, bool direct_x, bool direct_w)
 {
-    const size_t a = split_bytes(choose(d.dtype, true, false, d.m, d.n, d.k), d.m, d.n);
-    const size_t b = split_bytes(choose(d.dtype, false, false, d.m, d.n, d.k), d.m, d.n);
-    return a > b ? a : b;
+    FwdPlan p{};
+    p.product = plan(d.dtype, direct_x, direct_w, false, d.m, d.n, d.k);
+    p.w = p.product.copy_a ? copy_bytes(d.m, d.k) : 0;
+    p.split = p.w + (p.product.copy_b ? copy_bytes(d.n, d.k) : 0);
+    p.bytes = p.split + split_bytes(p.product.c, d.m, d.n);
+    return p;
 }
 
 template <class T>
 int linear_fwd(const void *x, const void *w, const void *bias, const void *res, void *y, const tv_held &h,
-               const tv_linear_desc &d, const Choice &c, void *ws, hipStream_t stream)
+               const tv_linear_desc &d, const FwdPlan &p, char *ws, hipStream_t stream)
 {
     Epilogue e{};
     e.bias = bias; e.res = res; e.y = y;
     e.held = h.kind == TV_HELD_NONE ? nullptr : h.data; e.exps = h.exps;
     e.ldr = d.ldr; e.ldy = d.ldy; e.act = d.act; e.kind = h.kind;
-    return run_product<T, T, false, false>({x, d.ldx, d.k, false}, {w, d.ldw, d.k, false}, d.m, d.n, d.k, c, e, ws, stream);
+    Operand a{x, d.ldx, d.m, d.k}, b{w, d.ldw, d.n, d.k};
+    if (p.product.copy_a && copy_operand(a, ws, stream) != TV_OK) return TV_ERR_HIP;
+    if (p.product.copy_b && copy_operand(b, ws + p.w, stream) != TV_OK) return TV_ERR_HIP;
+    return run_product<T, T, false, false>(a, b, d.m, d.n, d.k, p.product.c, e, ws + p.split, stream);
 }
 
-// ---- the backward call's workspace: dz, x out of its checkpoint, the column sums of groups of rows, split sums
+// ---- the backward call's workspace: dz (or a copy of g), x out of its checkpoint or a copy of it, a copy of W, the column
+// sums of groups of rows, split sums
 struct BwdPlan {
-    size_t dz, x, sums, split, bytes;
+    Plan dx, dw;
+    size_t x, w, sums, split, bytes;
     int64_t ldz, ldx;
     int rows_per, groups;
+    bool own_dz, own_x;
 };
 
-BwdPlan bwd_plan(const tv_linear_desc &d, bool x8)
+BwdPlan bwd_plan(const tv_linear_desc &d, bool x8, bool direct_g, bool direct_x, bool direct_w)
 {
     BwdPlan p{};
-    const size_t size = elem_bytes(d.dtype);
-    size_t at = 0;
+    const int64_t size = (int64_t)elem_bytes(d.dtype);
+    const bool smooth = d.act != TV_ACT_NONE;
+    // dz is written, and codes are restored, into rows that go straight to LDS
+    p.dx = plan(d.dtype, smooth || direct_g, direct_w, true, d.m, d.k, d.n);
+    p.dw = plan(d.dtype, smooth || direct_g, x8 || direct_x, true, d.n, d.k, d.m);
+    p.own_dz = smooth || p.dx.copy_a || p.dw.copy_a;
+    p.own_x = x8 || p.dw.copy_b;
     p.ldz = up(d.n, 8);
-    p.dz = at;
-    if (d.act != TV_ACT_NONE) at += up(d.m * p.ldz * (int64_t)size, 256);
     p.ldx = up(d.k, 8);
+    size_t at = p.own_dz ? up(d.m * p.ldz * size, 256) : 0;
     p.x = at;
-    if (x8) at += up(d.m * p.ldx * 2, 256);
-    // about 1024 workgroups of 256 columns each, of sixteen rows at least
+    if (p.own_x) at += copy_bytes(d.m, d.k);
+    p.w = at;
+    if (p.dx.copy_b) at += copy_bytes(d.n, d.k);
+    // about 1024 workgroups of 256 columns each, of sixteen rows at least; up to 64 rows are one group, one launch
     const int64_t want = 1024 / tiles(d.n, 256) + 1;
-    p.rows_per = (int)(d.m > 64 ? up(tiles(d.m, want < 256 ? want : 256), 16) : 64);       // (up to 64 rows: one group, one launch)
+    p.rows_per = (int)(d.m > 64 ? up(tiles(d.m, want < 256 ? want : 256), 16) : 64);
     p.groups = (int)tiles(d.m, p.rows_per);
     p.sums = at;
     at += up((int64_t)p.groups * d.n * 4, 256);
     p.split = at;
-    size_t most = 0;
-    for (bool dir : {false, true}) {
-        const size_t s1 = split_bytes(choose(d.dtype, dir, true, d.m, d.k, d.n), d.m, d.k);
-        const size_t s2 = split_bytes(choose(d.dtype, dir, true, d.n, d.k, d.m), d.n, d.k);
-        most = most > s1 ? most : s1;
-        most = most > s2 ? most : s2;
-    }
-    p.bytes = at + most;
+    const size_t s1 = split_bytes(p.dx.c, d.m, d.k), s2 = split_bytes(p.dw.c, d.n, d.k);
+    p.bytes = at + (s1 > s2 ? s1 : s2);
     return p;
 }
 
 template <class T>
 int linear_bwd(const void *g, const void *x, const uint8_t *x_exps, const tv_held &h, const void *w, void *dx, void *dw,
-               void *db, const tv_linear_desc &d, char *ws, hipStream_t stream)
+               void *db, const tv_linear_desc &d, const BwdPlan &p, char *ws, hipStream_t stream)
 {
-    const BwdPlan p = bwd_plan(d, x_exps != nullptr);
-    Operand dz{g, d.ldy, d.n, false};
-    if (d.m > 0 && (d.act != TV_ACT_NONE || db)) {
+    Operand dz{g, d.ldy, d.m, d.n};
+    const bool own_dz = d.act != TV_ACT_NONE || (dx && p.dx.copy_a) || (dw && p.dw.copy_a);
+    if (d.m > 0 && (own_dz || db)) {
         SlopeArgs a{};
         a.g = g; a.held = h.data; a.exps = h.exps;
-        a.dz = d.act != TV_ACT_NONE ? ws + p.dz : nullptr;
+        a.dz = own_dz ? ws : nullptr;
         a.sums = db && p.groups > 1 ? (float *)(ws + p.sums) : nullptr;
         a.db = p.groups == 1 ? db : nullptr;
         a.ldg = d.ldy; a.ldz = p.ldz;
@@ -261,7 +299,7 @@ int linear_bwd(const void *g, const void *x, const uint8_t *x_exps, const tv_hel
         a.act = d.act; a.kind = d.act == TV_ACT_NONE ? TV_HELD_NONE : h.kind;
         hipLaunchKernelGGL((slope_kernel<T>), dim3((uint32_t)tiles(d.n, 256), p.groups), dim3(256), 0, stream, a);
         if (launched() != TV_OK) return TV_ERR_HIP;
-        if (a.dz) dz = {a.dz, p.ldz, d.n, false};
+        if (own_dz) dz = {ws, p.ldz, d.m, p.ldz};
     }
     if (db && p.groups != 1) {
         hipLaunchKernelGGL((column_sum_kernel<T>), dim3((uint32_t)tiles(d.n, 32)), dim3(256), 0, stream,
@@ -269,32 +307,31 @@ int linear_bwd(const void *g, const void *x, const uint8_t *x_exps, const tv_hel
         if (launched() != TV_OK) return TV_ERR_HIP;
     }
     if (dx && d.m > 0) {
-        const Operand ow{w, d.ldw, d.k, false};
-        const int st = run_product<T, T, false, true>(dz, ow, d.m, d.k, d.n, choose(d.dtype, direct(dz) && direct(ow), true, d.m, d.k, d.n),
-                                                   plain_output(dx, d.k), ws + p.split, stream);
+        Operand b{w, d.ldw, d.n, d.k};
+        if (p.dx.copy_b && copy_operand(b, ws + p.w, stream) != TV_OK) return TV_ERR_HIP;
+        const int st = run_product<T, T, false, true>(dz, b, d.m, d.k, d.n, p.dx.c, plain_output(dx, d.k), ws + p.split, stream);
         if (st != TV_OK) return st;
     }
     if (dw) {
-        Operand xs{x, d.ldx, d.k, false};
+        Operand b{x, d.ldx, d.m, d.k};
         if (x_exps && d.m > 0) {                      // what codes stand for is exact in bf16
             const int st = tv_ckpt8_load((const int8_t *)x, x_exps, ws + p.x, d.m, d.k, p.ldx, TV_BF16, stream);
             if (st != TV_OK) return st;
-            xs = {ws + p.x, p.ldx, d.k, false};
-        }
-        const Choice c = choose(d.dtype, direct(dz) && direct(xs), true, d.n, d.k, d.m);
+            b = {ws + p.x, p.ldx, d.m, p.ldx};
+        } else if (p.dw.copy_b && copy_operand(b, ws + p.x, stream) != TV_OK) return TV_ERR_HIP;
         const Epilogue e = plain_output(dw, d.k);
-        return x_exps ? run_product<T, bf16, true, true>(dz, xs, d.n, d.k, d.m, c, e, ws + p.split, stream)
-                      : run_product<T, T, true, true>(dz, xs, d.n, d.k, d.m, c, e, ws + p.split, stream);
+        return x_exps ? run_product<T, bf16, true, true>(dz, b, d.n, d.k, d.m, p.dw.c, e, ws + p.split, stream)
+                      : run_product<T, T, true, true>(dz, b, d.n, d.k, d.m, p.dw.c, e, ws + p.split, stream);
     }
     return TV_OK;
 }
 
 int check_ckpt8(int64_t rows, int64_t n, int64_t ld, int dtype)
 {
-    if (rows < 0 || n < 1 || rows >= kMostIndex || n >= kMostIndex - 128) return TV_ERR_SHAPE;
+    if (rows < 0 || n < 1 || rows >= kMostIndex || n >= kMostIndex) return TV_ERR_SHAPE;
     if (rows > ((int64_t)1 << 40) / n) return TV_ERR_SHAPE;
     if (dtype != TV_F32 && dtype != TV_BF16) return TV_ERR_UNSUPPORTED;
-    if (ld < n || ld >= kMostIndex) return TV_ERR_STRIDE;
+    if (ld < n || ld >= kMostStride) return TV_ERR_STRIDE;
     return TV_OK;
 }
 
@@ -308,9 +345,16 @@ dim3 ckpt8_grid(int64_t rows, int64_t n)
 
 extern "C" {
 
+// (The workspaces are asked for before there are pointers, and have to do wherever those lie.)
 size_t tv_linear_fwd_workspace_bytes(tv_linear_desc d)
 {
-    return check_sizes(d) == TV_OK ? fwd_bytes(d) : 0;
+    size_t most = 0;
+    if (check_sizes(d) == TV_OK && d.m > 0)
+        for (int i = 0; i < 4; ++i) {
+            const size_t b = fwd_plan(d, (i & 1) != 0, (i & 2) != 0).bytes;
+            most = most > b ? most : b;
+        }
+    return most;
 }
 
 int tv_linear_fwd(const void *x, const void *w, const void *bias, const void *res, void *y, tv_held held,
@@ -318,21 +362,27 @@ int tv_linear_fwd(const void *x, const void *w, const void *bias, const void *re
 {
     int st = check_sizes(d);
     if (st != TV_OK) return st;
-    if (res && (d.ldr < d.n || d.ldr >= kMostIndex)) return TV_ERR_STRIDE;
+    if (res && (d.ldr < d.n || d.ldr >= kMostStride)) return TV_ERR_STRIDE;
     if ((st = check_held(d, held, false)) != TV_OK) return st;
     if (d.m == 0) return TV_OK;
     if (!x || !w || !y) return TV_ERR_NULL;
     const size_t size = elem_bytes(d.dtype);
     if (!aligned(x, size) || !aligned(w, size) || !aligned(bias, size) || !aligned(res, size) || !aligned(y, size)) return TV_ERR_STRIDE;
-    const Choice c = fwd_choice(d, x, w);
-    if (c.splits > 1 && (st = check_workspace(ws, ws_bytes, fwd_bytes(d))) != TV_OK) return st;
-    return d.dtype == TV_BF16 ? linear_fwd<bf16>(x, w, bias, res, y, held, d, c, ws, stream)
-                              : linear_fwd<float>(x, w, bias, res, y, held, d, c, ws, stream);
+    const FwdPlan p = fwd_plan(d, direct({x, d.ldx, d.m, d.k}), direct({w, d.ldw, d.n, d.k}));
+    if ((st = check_workspace(ws, ws_bytes, p.bytes)) != TV_OK) return st;
+    return d.dtype == TV_BF16 ? linear_fwd<bf16>(x, w, bias, res, y, held, d, p, (char *)ws, stream)
+                              : linear_fwd<float>(x, w, bias, res, y, held, d, p, (char *)ws, stream);
 }
 
 size_t tv_linear_bwd_workspace_bytes(tv_linear_desc d, int x_is_8bit)
 {
-    return check_sizes(d) == TV_OK ? bwd_plan(d, x_is_8bit != 0).bytes : 0;
+    size_t most = 0;
+    if (check_sizes(d) == TV_OK)
+        for (int i = 0; i < 8; ++i) {
+            const size_t b = bwd_plan(d, x_is_8bit != 0, (i & 1) != 0, (i & 2) != 0, (i & 4) != 0).bytes;
+            most = most > b ? most : b;
+        }
+    return most;
 }
 
 int tv_linear_bwd(const void *g, const void *x, const uint8_t *x_exps, tv_held held, const void *w, void *dx, void *dw,
@@ -345,9 +395,10 @@ int tv_linear_bwd(const void *g, const void *x, const uint8_t *x_exps, tv_held h
     const size_t size = elem_bytes(d.dtype);
     if (!aligned(g, size) || (!x_exps && !aligned(x, size)) || !aligned(w, size) || !aligned(dx, size) || !aligned(dw, size) ||
         !aligned(db, size)) return TV_ERR_STRIDE;
-    if ((st = check_workspace(ws, ws_bytes, bwd_plan(d, x_exps != nullptr).bytes)) != TV_OK) return st;
-    return d.dtype == TV_BF16 ? linear_bwd<bf16>(g, x, x_exps, held, w, dx, dw, db, d, (char *)ws, stream)
-                              : linear_bwd<float>(g, x, x_exps, held, w, dx, dw, db, d, (char *)ws, stream);
+    const BwdPlan p = bwd_plan(d, x_exps != nullptr, direct({g, d.ldy, d.m, d.n}), direct({x, d.ldx, d.m, d.k}), direct({w, d.ldw, d.n, d.k}));
+    if ((st = check_workspace(ws, ws_bytes, p.bytes)) != TV_OK) return st;
+    return d.dtype == TV_BF16 ? linear_bwd<bf16>(g, x, x_exps, held, w, dx, dw, db, d, p, (char *)ws, stream)
+                              : linear_bwd<float>(g, x, x_exps, held, w, dx, dw, db, d, p, (char *)ws, stream);
 }
 
 int tv_ckpt8_save(const void *x, int8_t *codes, uint8_t *exps, int64_t rows, int64_t n, int64_t ldx, int dtype, hipStream_t stream)

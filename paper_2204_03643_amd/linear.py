@@ -60,6 +60,17 @@ def _bwd_bytes(m, k, n, dtype, act, x_is_8bit):
     return _b.tv_linear_bwd_workspace_bytes(_b.tv_linear_desc(m, k, n, k, k, n, n, dtype, act), x_is_8bit)
 
 
+def _on_device(call):
+    """`call` with its first argument's device as the current one: that device's stream is the one it uses."""
+    @functools.wraps(call)
+    def wrapped(t, *rest):
+        if t.get_device() == torch.cuda.current_device():
+            return call(t, *rest)
+        with torch.cuda.device(t.device):
+            return call(t, *rest)
+    return wrapped
+
+
 def _address(t):
     return None if t is None else t.data_ptr()
 
@@ -96,12 +107,18 @@ class Checkpoint8:
 
     def restore(self) -> torch.Tensor:
         """The values that the codes stand for."""
-        n = self.codes.shape[-1]
-        x = torch.empty(self.codes.shape, dtype=self.dtype, device=self.codes.device)
-        _b.tv_ckpt8_load(self.codes, self.exps, x, self.exps.shape[0], n, n, _DTYPES[self.dtype])
-        return x
+        return _restore8(self.codes, self.exps, self.dtype)
 
 
+@_on_device
+def _restore8(codes, exps, dtype):
+    n = codes.shape[-1]
+    x = torch.empty(codes.shape, dtype=dtype, device=codes.device)
+    _check(_b.lib().tv_ckpt8_load(codes.data_ptr(), exps.data_ptr(), x.data_ptr(), exps.shape[0], n, n, _DTYPES[dtype], _b._stream(None)))
+    return x
+
+
+@_on_device
 def _save8(x, ld):
     """(codes, exponents) of x as rows (see _as_rows)."""
     n = x.shape[-1]
@@ -121,6 +138,7 @@ def tv_checkpoint8(x: torch.Tensor) -> Checkpoint8:
     return Checkpoint8(codes, exps, x.dtype)
 
 
+@_on_device
 def _forward(x, ldx, weight, ldw, bias, residual, act, hold):
     """(y, what is held of z, its exponents): x and weight as rows, hold one of None, "full", "8bit"."""
     k, n, code, dtype = x.shape[-1], weight.shape[0], _ACTS[act], _DTYPES[x.dtype]
@@ -148,6 +166,7 @@ def _forward(x, ldx, weight, ldw, bias, residual, act, hold):
     return y, data, exps
 
 
+@_on_device
 def _backward(g, x, x_exps, ldx, data, exps, weight, ldw, act, want):
     """(dx, dw, db), None where not wanted.  x: rows, or the codes of its checkpoint (x_exps given)."""
     n, k = weight.shape
