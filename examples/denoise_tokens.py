@@ -1,5 +1,5 @@
-"""Trains a small residual block (TV pass along the tokens, two channel products, activations held in 8 bits) to denoise
-piecewise-constant tokens, then runs one more sequence through it without gradients.
+"""Trains a small residual block (TV pass along the tokens, two channel products, activations held in 8 bits) to find the
+noise in piecewise-constant tokens, then runs one more sequence through it without gradients.
 
     python examples/denoise_tokens.py [--steps 200] [--tokens 512] [--channels 64] [--checkpoint 8bit|full]
 """
@@ -32,11 +32,11 @@ def main():
     a = p.parse_args()
     torch.manual_seed(0)
     gen = torch.Generator(device="cuda").manual_seed(0)
-    block = TVMixer(a.channels, 4 * a.channels, checkpoint=a.checkpoint, init_lambda=0.3, device="cuda")
+    block = TVMixer(a.channels, 4 * a.channels, checkpoint=a.checkpoint, init_lambda=1.0, device="cuda")
     opt = torch.optim.Adam(block.parameters(), lr=2e-3)
     for step in range(a.steps):
         clean, noisy = batch(16, a.tokens, a.channels, gen)
-        loss = (block(noisy) - clean).square().mean()
+        loss = (noisy - block(noisy) - clean).square().mean()
         opt.zero_grad()
         loss.backward()
         opt.step()
@@ -44,7 +44,7 @@ def main():
             print("step %4d  loss %.4f  (noise alone %.4f)" % (step, loss.item(), (noisy - clean).square().mean().item()), flush=True)
     with torch.no_grad():
         clean, noisy = batch(1, a.tokens, a.channels, gen)
-        print("one more sequence: %.4f" % (block(noisy) - clean).square().mean().item())
+        print("one more sequence: %.4f" % (noisy - block(noisy) - clean).square().mean().item())
 
 
 if __name__ == "__main__":

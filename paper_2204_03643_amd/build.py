@@ -48,13 +48,29 @@ def build_library(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     tmp = LIB + ".tmp%d" % os.getpid()
     digest = source_digest()
-    cmd = [hipcc] + HIPCC_FLAGS + sources() + ["-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError("hipcc failed")
+    # a source a process, then the link
+    objects = [tmp + ".%d.o" % i for i in range(len(sources()))]
+    flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+    compiles = [[hipcc] + flags + ["-c", src, "-o", obj] for src, obj in zip(sources(), objects)]
+    link = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + objects + ["-o", tmp]
+    try:
+        running = []
+        for cmd in compiles:
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            running.append(subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True))
+        said = [p.communicate()[0] for p in running]
+        if any(p.returncode for p in running):
+            sys.stderr.write("".join(said))
+            raise RuntimeError("hipcc failed")
+        res = subprocess.run(link, capture_output=True, text=True)
+        if res.returncode != 0:
+            sys.stderr.write(res.stdout + res.stderr)
+            raise RuntimeError("hipcc failed")
+    finally:
+        for obj in objects:
+            if os.path.exists(obj):
+                os.remove(obj)
     os.replace(tmp, LIB)
     with open(STAMP, "w") as f:
         f.write(digest + "\n")
