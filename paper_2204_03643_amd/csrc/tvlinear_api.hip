@@ -59,8 +59,12 @@ Choice cut(Kind kind, int64_t s, int64_t K, int64_t unit)
     return {kind, (int)(K > 0 ? tiles(K, per) : 1), (int)per, 0.0};
 }
 
-// Sizes, type and alignment alone decide.  A few rows stream the weight: up to 32 of them, or 64 where the operands
-// would not go straight to LDS (64 rows, 2048 -> 8192, bf16: 16 us against 13 through tiles, f32 34 against 42).
+// Sizes, type and alignment alone decide.  Few rows stream the weight, where that is faster than tiles.  bf16 operands that
+// go straight to LDS: up to 32 rows (2048 -> 8192, streamed and through tiles: 32 rows 11.6 and 12.8 us, 48 rows 14.7 and
+// 13.8); f32 ones up to 16 (16 rows 22.7 and 23.2 us, 32 rows 28.4 and 23.8).  More rows, and rows on other boundaries, cost
+// so much a turn of the waves that only short streams pay: where `few_turns` is the turns one after the other times tiles
+// of 16 rows, up to 16 in f32 (1024 -> 1024, 32 rows, 16: 12.3 and 12.4 us; 64 rows, 32: 18.9 and 12.8) and 6 in bf16
+// (513 -> 2047, 32 rows, 6: 8.9 and 11.6 us; 1001 -> 777, 48 rows, 16: 14.2 and 11.0; 2047 -> 513, one row, 8: 15.1 and 10.7).
 //
 // Otherwise the cheapest by a model of the time in microseconds, fitted to sweeps of tiles and splits over outputs of
 // 128 x 128 to 8192 x 8192 and contractions of 64 to 8192: a launch, rounds of workgroups over 256 compute units (of
@@ -68,12 +72,13 @@ Choice cut(Kind kind, int64_t s, int64_t K, int64_t unit)
 // and so much a step of 64, and for split contractions the second launch and the sums' trip through memory.
 Choice choose(int dtype, bool direct, bool transposed, int64_t M, int64_t N, int64_t K)
 {
-    if (!transposed && M >= 1 && M <= (direct && dtype == TV_BF16 ? kFewRows / 2 : kFewRows)) {
+    if (!transposed && M >= 1 && M <= kFewRows) {
         const int64_t turn = 8 * 64 / (int64_t)elem_bytes(dtype);            // a turn of all eight waves
         const int64_t t = tiles(N, 32), s = t >= 256 ? 1 : 256 / t;
-        return cut(kFew, s < K / (8 * turn) ? s : K / (8 * turn), K, turn);
+        const Choice x = cut(kFew, s < K / (8 * turn) ? s : K / (8 * turn), K, turn);
+        const int64_t few_turns = tiles(t * x.splits, 256) * tiles(x.k_per < K ? x.k_per : K, turn) * (M <= 16 ? 1 : M <= 32 ? 2 : 4);
+        if ((direct && M <= (dtype == TV_BF16 ? 32 : 16)) || few_turns <= (dtype == TV_BF16 ? 6 : 16)) return x;
     }
-    /*SWEEP*/
     struct Cost { Kind kind; int64_t slots; double round, step; };
     constexpr Cost direct16[] = {{kTile64, 256, 1.0, 0.30}, {kTile128Deep, 256, 2.0, 0.47}, {kTile128, 512, 3.0, 0.88}, {kTile256, 256, 6.5, 1.50}};
     constexpr Cost any16[] = {{kSplit64, 256, 1.5, 0.62}, {kSplit64, 512, 2.0, 0.85}};
@@ -98,7 +103,7 @@ Choice choose(int dtype, bool direct, bool transposed, int64_t M, int64_t N, int
 }
 
 // bf16 operands that cannot go straight to LDS are copied to rows that can, where the faster kernel pays for it
-// (8192 x 2047 -> 8191: 480 us without, 290 with): a launch and the bytes there and back each.
+// (8192 x 2047 -> 8191: 504 us without, 247 with): a launch and the bytes there and back each.
 struct Plan {
     Choice c;
     bool copy_a, copy_b;
