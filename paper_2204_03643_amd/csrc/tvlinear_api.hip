@@ -62,9 +62,9 @@ Choice cut(Kind kind, int64_t s, int64_t K, int64_t unit)
 // Sizes, type and alignment alone decide.  Few rows stream the weight, where that is faster than tiles.  bf16 operands that
 // go straight to LDS: up to 32 rows (2048 -> 8192, streamed and through tiles: 32 rows 11.6 and 12.8 us, 48 rows 14.7 and
 // 13.8); f32 ones up to 16 (16 rows 22.7 and 23.2 us, 32 rows 28.4 and 23.8).  More rows, and rows on other boundaries, cost
-// so much a turn of the waves that only short streams pay: where `few_turns` is the turns one after the other times tiles
-// of 16 rows, up to 16 in f32 (1024 -> 1024, 32 rows, 16: 12.3 and 12.4 us; 64 rows, 32: 18.9 and 12.8) and 6 in bf16
-// (513 -> 2047, 32 rows, 6: 8.9 and 11.6 us; 1001 -> 777, 48 rows, 16: 14.2 and 11.0; 2047 -> 513, one row, 8: 15.1 and 10.7).
+// so much a turn of the waves that only short streams pay: turns one after the other, times the 2, 3 or 6 that one costs
+// with up to 16, 32 or 64 rows, up to 36 in f32 (1024 -> 1024: 32 rows, 24, 9.1 and 12.2 us; 64 rows, 48,
+// 14.1 and 12.8) and 12 in bf16 (1001 -> 777, 32 rows, 12: 9.0 and 10.8 us; 2047 -> 513, 16 rows, 16: 15.1 and 11.3).
 //
 // Otherwise the cheapest by a model of the time in microseconds, fitted to sweeps of tiles and splits over outputs of
 // 128 x 128 to 8192 x 8192 and contractions of 64 to 8192: a launch, rounds of workgroups over 256 compute units (of
@@ -76,8 +76,8 @@ Choice choose(int dtype, bool direct, bool transposed, int64_t M, int64_t N, int
         const int64_t turn = 8 * 64 / (int64_t)elem_bytes(dtype);            // a turn of all eight waves
         const int64_t t = tiles(N, 32), s = t >= 256 ? 1 : 256 / t;
         const Choice x = cut(kFew, s < K / (8 * turn) ? s : K / (8 * turn), K, turn);
-        const int64_t few_turns = tiles(t * x.splits, 256) * tiles(x.k_per < K ? x.k_per : K, turn) * (M <= 16 ? 1 : M <= 32 ? 2 : 4);
-        if ((direct && M <= (dtype == TV_BF16 ? 32 : 16)) || few_turns <= (dtype == TV_BF16 ? 6 : 16)) return x;
+        const int64_t turns = tiles(t * x.splits, 256) * tiles(x.k_per < K ? x.k_per : K, turn);
+        if ((direct && M <= (dtype == TV_BF16 ? 32 : 16)) || turns * (M <= 16 ? 2 : M <= 32 ? 3 : 6) <= (dtype == TV_BF16 ? 12 : 36)) return x;
     }
     struct Cost { Kind kind; int64_t slots; double round, step; };
     constexpr Cost direct16[] = {{kTile64, 256, 1.0, 0.30}, {kTile128Deep, 256, 2.0, 0.47}, {kTile128, 512, 3.0, 0.88}, {kTile256, 256, 6.5, 1.50}};
@@ -146,6 +146,17 @@ void launch_tiles(void (*kernel)(Product, Epilogue), Product g, const Epilogue &
     hipLaunchKernelGGL(kernel, dim3(g.tiles_m * g.tiles_n, g.splits), dim3(THREADS), 0, stream, g, e);
 }
 
+// NT * 16 columns a workgroup: 16 where 32 would leave half of the compute units without one (2047 -> 513, one row: f32 8.3 us
+// with 16, 13.5 with 32; 2048 -> 8192, 16 bf16 rows: 11.4 and 10.1).
+template <class T, int NT>
+void launch_few(const Product &g, const Epilogue &e, hipStream_t stream)
+{
+    const dim3 grid((uint32_t)tiles(g.N, NT * 16), g.splits), block(512);
+    if (g.M <= 16) hipLaunchKernelGGL((gemv_kernel<T, 1, NT, 8>), grid, block, 0, stream, g, e);
+    else if (g.M <= 32) hipLaunchKernelGGL((gemv_kernel<T, 2, NT, 8>), grid, block, 0, stream, g, e);
+    else hipLaunchKernelGGL((gemv_kernel<T, 4, NT, 4>), grid, block, 0, stream, g, e);
+}
+
 template <class T, class TB, bool AT, bool BT>
 int run_product(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const Choice &c, const Epilogue &e,
                 void *ws, hipStream_t stream)
@@ -164,10 +175,9 @@ int run_product(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_
     }
     if constexpr (!AT && !BT)
         if (c.kind == kFew) {
-            const dim3 grid((uint32_t)tiles(N, 32), c.splits), block(512);
-            if (M <= 16) hipLaunchKernelGGL((gemv_kernel<T, 1, 2, 8>), grid, block, 0, stream, g, e);
-            else if (M <= 32) hipLaunchKernelGGL((gemv_kernel<T, 2, 2, 8>), grid, block, 0, stream, g, e);
-            else hipLaunchKernelGGL((gemv_kernel<T, 4, 2, 4>), grid, block, 0, stream, g, e);
+            const bool whole_blocks = c.splits == 1 && (e.kind == kHeldBits || e.kind == kHeld8);    // (of 32 columns)
+            if (tiles(N, 32) * c.splits > 128 || whole_blocks) launch_few<T, 2>(g, e, stream);
+            else launch_few<T, 1>(g, e, stream);
         }
     if (c.splits > 1) {
         if (launched() != TV_OK) return TV_ERR_HIP;

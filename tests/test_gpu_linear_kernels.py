@@ -13,7 +13,8 @@ DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 # and long contractions (one or many splits), and rows that do not start on 16-byte boundaries
 SHAPES = [(4096, 192, 4096), (2048, 136, 2048), (4104, 72, 2056), (2049, 96, 2047), (1100, 328, 1160), (257, 4096, 257),
           (96, 8192, 136), (4095, 513, 1025), (40, 640, 1300), (32, 512, 96), (33, 512, 96), (64, 8200, 72), (65, 8200, 72), (8192, 64, 64),
-          (130, 63, 4097), (1024, 1000, 1024), (1000, 2500, 64), (4096, 4096, 200), (264, 4096, 4096)]
+          (130, 63, 4097), (1024, 1000, 1024), (1000, 2500, 64), (4096, 4096, 200), (264, 4096, 4096),
+          (32, 1001, 777), (64, 500, 4133), (7, 4096, 5000), (60, 256, 40)]
 
 
 def linear():
