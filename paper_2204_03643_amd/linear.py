@@ -49,15 +49,17 @@ def _blocks(n: int) -> int:
     return -(-n // _b.TV_CKPT8_BLOCK)
 
 
+# A call's descriptor and workspace size, which sizes, strides and dtype say in full.
 @functools.lru_cache(maxsize=4096)
-def _fwd_bytes(m, k, n, dtype):
-    """The forward call's workspace: the sizes and the dtype say it all."""
-    return _b.tv_linear_fwd_workspace_bytes(_b.tv_linear_desc(m, k, n, k, k, n, n, dtype, 0))
+def _fwd_desc(*fields):
+    desc = _b.tv_linear_desc(*fields)
+    return desc, _b.tv_linear_fwd_workspace_bytes(desc)
 
 
 @functools.lru_cache(maxsize=4096)
-def _bwd_bytes(m, k, n, dtype, act, x_is_8bit):
-    return _b.tv_linear_bwd_workspace_bytes(_b.tv_linear_desc(m, k, n, k, k, n, n, dtype, act), x_is_8bit)
+def _bwd_desc(x_is_8bit, *fields):
+    desc = _b.tv_linear_desc(*fields)
+    return desc, _b.tv_linear_bwd_workspace_bytes(desc, x_is_8bit)
 
 
 def _on_device(call):
@@ -97,6 +99,13 @@ class Checkpoint8:
             raise RuntimeError("Checkpoint8: runs on the GPU only, codes and exponents on one device")
         self.codes, self.exps, self.dtype = codes.contiguous(), exps.contiguous(), dtype
 
+    @classmethod
+    def _saved(cls, codes, exps, dtype):
+        """Of what the library has just written, which needs no looking over."""
+        made = cls.__new__(cls)
+        made.codes, made.exps, made.dtype = codes, exps, dtype
+        return made
+
     @property
     def shape(self):
         return self.codes.shape
@@ -113,7 +122,7 @@ class Checkpoint8:
 @_on_device
 def _restore8(codes, exps, dtype):
     n = codes.shape[-1]
-    x = torch.empty(codes.shape, dtype=dtype, device=codes.device)
+    x = codes.new_empty(codes.shape, dtype=dtype)
     _check(_b.lib().tv_ckpt8_load(codes.data_ptr(), exps.data_ptr(), x.data_ptr(), exps.shape[0], n, n, _DTYPES[dtype], _b._stream(None)))
     return x
 
@@ -123,8 +132,8 @@ def _save8(x, ld):
     """(codes, exponents) of x as rows (see _as_rows)."""
     n = x.shape[-1]
     rows = x.numel() // n
-    codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
-    exps = torch.empty((rows, _blocks(n)), dtype=torch.uint8, device=x.device)
+    codes = x.new_empty(x.shape, dtype=torch.int8)
+    exps = x.new_empty((rows, _blocks(n)), dtype=torch.uint8)
     _check(_b.lib().tv_ckpt8_save(x.data_ptr(), codes.data_ptr(), exps.data_ptr(), rows, n, ld, _DTYPES[x.dtype], _b._stream(None)))
     return codes, exps
 
@@ -135,7 +144,7 @@ def tv_checkpoint8(x: torch.Tensor) -> Checkpoint8:
     if x.dim() < 1 or x.shape[-1] < 1:
         raise ValueError("tv_checkpoint8: a last axis of at least one value expected")
     codes, exps = _save8(*_as_rows(x.detach()))
-    return Checkpoint8(codes, exps, x.dtype)
+    return Checkpoint8._saved(codes, exps, x.dtype)
 
 
 @_on_device
@@ -143,7 +152,7 @@ def _forward(x, ldx, weight, ldw, bias, residual, act, hold):
     """(y, what is held of z, its exponents): x and weight as rows, hold one of None, "full", "8bit"."""
     k, n, code, dtype = x.shape[-1], weight.shape[0], _ACTS[act], _DTYPES[x.dtype]
     m = x.numel() // k
-    y = torch.empty(x.shape[:-1] + (n,), dtype=x.dtype, device=x.device)
+    y = x.new_empty((*x.shape[:-1], n))
     ldr = n
     if residual is not None:
         residual, ldr = _as_rows(residual)
@@ -151,18 +160,17 @@ def _forward(x, ldx, weight, ldw, bias, residual, act, hold):
     held = _NOTHING_HELD
     if hold is not None and code != _b.TV_ACT_NONE:
         if code == _b.TV_ACT_RELU:
-            data, kind = torch.empty((m, _blocks(n)), dtype=torch.int32, device=x.device), _b.TV_HELD_BITS
+            data, kind = x.new_empty((m, _blocks(n)), dtype=torch.int32), _b.TV_HELD_BITS
         elif hold == "8bit":
-            data, kind = torch.empty((m, n), dtype=torch.int8, device=x.device), _b.TV_HELD_8BIT
-            exps = torch.empty((m, _blocks(n)), dtype=torch.uint8, device=x.device)
+            data, kind = x.new_empty((m, n), dtype=torch.int8), _b.TV_HELD_8BIT
+            exps = x.new_empty((m, _blocks(n)), dtype=torch.uint8)
         else:
-            data, kind = torch.empty((m, n), dtype=x.dtype, device=x.device), _b.TV_HELD_PLAIN
+            data, kind = x.new_empty((m, n)), _b.TV_HELD_PLAIN
         held = _b.tv_held(data.data_ptr(), _address(exps), kind)
-    nbytes = _fwd_bytes(m, k, n, dtype)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device) if nbytes else None
-    _check(_b.lib().tv_linear_fwd(x.data_ptr(), weight.data_ptr(), _address(bias), _address(residual), y.data_ptr(), held,
-                                  _b.tv_linear_desc(m, k, n, ldx, ldw, ldr, n, dtype, code), _address(ws), nbytes,
-                                  _b._stream(None)))
+    desc, nbytes = _fwd_desc(m, k, n, ldx, ldw, ldr, n, dtype, code)
+    ws = x.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+    _check(_b.lib().tv_linear_fwd(x.data_ptr(), weight.data_ptr(), _address(bias), _address(residual), y.data_ptr(), held, desc,
+                                  _address(ws), nbytes, _b._stream(None)))
     return y, data, exps
 
 
@@ -176,15 +184,14 @@ def _backward(g, x, x_exps, ldx, data, exps, weight, ldw, act, want):
     kind = _b.TV_HELD_NONE
     if data is not None:
         kind = _HELD_BY_DTYPE.get(data.dtype, _b.TV_HELD_PLAIN)
-    dx = torch.empty(g.shape[:-1] + (k,), dtype=g.dtype, device=g.device) if want[0] else None
-    dw = torch.empty((n, k), dtype=g.dtype, device=g.device) if want[1] else None
-    db = torch.empty(n, dtype=g.dtype, device=g.device) if want[2] else None
-    nbytes = _bwd_bytes(m, k, n, dtype, code, x_exps is not None)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=g.device) if nbytes else None
+    dx = g.new_empty((*g.shape[:-1], k)) if want[0] else None
+    dw = g.new_empty((n, k)) if want[1] else None
+    db = g.new_empty(n) if want[2] else None
+    desc, nbytes = _bwd_desc(x_exps is not None, m, k, n, ldx, ldw, n, ldg, dtype, code)
+    ws = g.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
     _check(_b.lib().tv_linear_bwd(g.data_ptr(), _address(x), _address(x_exps), _b.tv_held(_address(data), _address(exps), kind),
                                   weight.data_ptr(), _address(dx), _address(dw), _address(db),
-                                  _b.tv_linear_desc(m, k, n, ldx, ldw, n, ldg, dtype, code), _address(ws), nbytes,
-                                  _b._stream(None)))
+                                  desc, _address(ws), nbytes, _b._stream(None)))
     return dx, dw, db
 
 
@@ -248,8 +255,8 @@ def tv_linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None =
         bias = bias.contiguous()
     if residual is not None:
         _check_tensor(residual, "tv_linear (residual)", x)
-        if residual.shape[-1:] != weight.shape[:1] or residual.shape[:-1] != x.shape[:-1]:
-            raise ValueError("tv_linear: residual of shape %r expected, got %r" % (tuple(x.shape[:-1]) + (n,), tuple(residual.shape)))
+        if residual.shape != (*x.shape[:-1], n):
+            raise ValueError("tv_linear: residual of shape %r expected, got %r" % ((*x.shape[:-1], n), tuple(residual.shape)))
     if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or (bias is not None and bias.requires_grad)
                                     or (residual is not None and residual.requires_grad)):
         return _Linear.apply(x, weight, bias, residual, act, checkpoint)
