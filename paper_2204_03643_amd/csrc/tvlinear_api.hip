@@ -67,9 +67,26 @@ Choice cut(Kind kind, int64_t s, int64_t K, int64_t unit)
 // 14.1 and 12.8) and 12 in bf16 (1001 -> 777, 32 rows, 12: 9.0 and 10.8 us; 2047 -> 513, 16 rows, 16: 15.1 and 11.3).
 //
 // Otherwise the cheapest by a model of the time in microseconds, fitted to sweeps of tiles and splits over outputs of
-// 128 x 128 to 8192 x 8192 and contractions of 64 to 8192: a launch, rounds of workgroups over 256 compute units (of
-// two workgroups each where there are more than 256 of a kernel that leaves room for two), in each a start and an end
-// and so much a step of 64, and for split contractions the second launch and the sums' trip through memory.
+// 128 x 512 to 8192 x 8192 and contractions of 256 to 16384 (what it takes there is 0.3 to 1 % slower than the best of the sweep, 14 %
+// at most): a launch; rounds of workgroups over 256 compute units, in each a start and an end and so much a step of 64,
+// more where two workgroups share a unit or, at lower clocks, where more than half of the units are busy; for split
+// contractions the second launch and the sums' trip through memory.
+struct Cost {
+    Kind kind;
+    int64_t slots;               // workgroups at a time
+    double round, step, more;
+};
+
+double rounds_us(const Cost &c, int64_t workgroups, int64_t steps)
+{
+    const int64_t full = workgroups / c.slots, rest = workgroups % c.slots;
+    // (the second half of 256 workgroups does not spread evenly where units take two)
+    const double half = rest > 128 ? rest / 128.0 - 1.0 : 0.0, load = c.slots == 256 ? half : rest > 256 ? 1.0 : 0.5 * half;
+    double us = (double)full * (c.round + (c.step + c.more) * (double)steps);
+    if (rest) us += c.round + (c.step + c.more * load) * (double)steps;
+    return us;
+}
+
 Choice choose(int dtype, bool direct, bool transposed, int64_t M, int64_t N, int64_t K)
 {
     if (!transposed && M >= 1 && M <= kFewRows) {
@@ -79,12 +96,11 @@ Choice choose(int dtype, bool direct, bool transposed, int64_t M, int64_t N, int
         const int64_t turns = tiles(t * x.splits, 256) * tiles(x.k_per < K ? x.k_per : K, turn);
         if ((direct && M <= (dtype == TV_BF16 ? 32 : 16)) || turns * (M <= 16 ? 2 : M <= 32 ? 3 : 6) <= (dtype == TV_BF16 ? 12 : 36)) return x;
     }
-    struct Cost { Kind kind; int64_t slots; double round, step; };
-    constexpr Cost direct16[] = {{kTile64, 256, 1.0, 0.30}, {kTile128Deep, 256, 2.0, 0.47}, {kTile128, 512, 3.0, 0.88}, {kTile256, 256, 6.5, 1.50}};
-    constexpr Cost any16[] = {{kSplit64, 256, 1.5, 0.62}, {kSplit64, 512, 2.0, 0.85}};
-    constexpr Cost any32[] = {{kSplit64, 256, 2.5, 1.35}, {kSplit128, 256, 3.5, 2.65}, {kSplit256, 256, 8.0, 9.0}};
+    constexpr Cost direct16[] = {{kTile64, 256, 1.0, 0.25, 0.08}, {kTile128Deep, 256, 1.8, 0.38, 0.13}, {kTile128, 512, 1.5, 0.42, 0.52}, {kTile256, 256, 4.2, 1.14, 0.49}};
+    constexpr Cost any16[] = {{kSplit64, 512, 3.2, 0.45, 0.44}};
+    constexpr Cost any32[] = {{kSplit64, 256, 4.2, 1.26, 0.35}, {kSplit128, 256, 3.6, 1.97, 0.80}, {kSplit256, 256, 7.4, 6.6, 2.5}};
     const Cost *costs = dtype != TV_BF16 ? any32 : direct ? direct16 : any16;
-    const int kinds = dtype != TV_BF16 ? 3 : direct ? 4 : 2;
+    const int kinds = dtype != TV_BF16 ? 3 : direct ? 4 : 1;
     Choice best = cut(costs[0].kind, 1, K, 64);
     best.us = 1e30;
     for (int i = 0; i < kinds; ++i) {
@@ -94,8 +110,8 @@ Choice choose(int dtype, bool direct, bool transposed, int64_t M, int64_t N, int
         for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
             if (s > 1 && (K < 128 * s || t * s > 1024)) break;
             Choice x = cut(c.kind, s, K, 64);
-            x.us = 3.0 + (double)tiles(t * x.splits, c.slots) * (c.round + c.step * (double)tiles(x.k_per < K ? x.k_per : K, 64));
-            if (x.splits > 1) x.us += 4.0 + (double)M * (double)N * x.splits * 8 / 6e6;
+            x.us = 3.0 + rounds_us(c, t * x.splits, tiles(x.k_per < K ? x.k_per : K, 64));
+            if (x.splits > 1) x.us += 2.6 + 0.18 * x.splits + (double)M * (double)N * x.splits * 8 / 7e6;
             if (x.us < best.us) best = x;
         }
     }
@@ -103,7 +119,7 @@ Choice choose(int dtype, bool direct, bool transposed, int64_t M, int64_t N, int
 }
 
 // bf16 operands that cannot go straight to LDS are copied to rows that can, where the faster kernel pays for it
-// (8192 x 2047 -> 8191: 504 us without, 247 with): a launch and the bytes there and back each.
+// (8192 x 2047 -> 8191: 505 us without, 250 with): a launch and the bytes there and back each.
 struct Plan {
     Choice c;
     bool copy_a, copy_b;
