@@ -1,6 +1,8 @@
-"""MI355X-native batched TV proximal operators (paper 2204.03643, Eq. 1-6, Alg. 1).
+"""MI355X-native batched TV proximal operators (paper 2204.03643, Eq. 1-6, Alg. 1), and the channel products and
+8-bit activation checkpoints of networks that hold them.
 
 A thin ctypes binding over the C-ABI library ``libtvprox.so`` (see ``include/tvprox.h``).
+The modules are in ``layer`` (``TVLayer``) and ``linear`` (``TVLinear``, ``TVMixer``).
 PyTorch is used only for device memory and streams; every step of the path runs in the
 library's HIP kernels.  There is no CPU fallback: if the library is missing it is built
 with hipcc, and if that fails the import raises.

