@@ -18,6 +18,14 @@
 
 namespace tvl {
 
+// The two values next to one another, the first in the lower half.
+__device__ __forceinline__ uint32_t narrow2(float x, float y)
+{
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2));
+}
+
 template <class T> struct Parts { static constexpr int kCount = sizeof(T) == 4 ? 3 : 1; };
 
 // ROWS output indices by 16 KQ contraction indices of an operand, on its way through THREADS threads: eight consecutive
@@ -77,17 +85,20 @@ template <class T, int ROWS, int THREADS, int KQ, bool TRANSPOSED> struct Staged
             }
             if constexpr (sizeof(T) == 2) *(u32x4 *)to = raw.v[u][0];
             else {
-                bf16x8 part[3];
+                u32x4 part[3];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float x = __uint_as_float(raw.v[u][i >> 2][i & 3]);
-                    part[0][i] = (bf16)x;
-                    const float y = x - (float)part[0][i];
-                    part[1][i] = (bf16)y;
-                    part[2][i] = (bf16)(y - (float)part[1][i]);
+                for (int i = 0; i < 4; ++i) {          // (one instruction rounds two values)
+                    float x = __uint_as_float(raw.v[u][i >> 1][i * 2 & 2]), y = __uint_as_float(raw.v[u][i >> 1][(i * 2 & 2) + 1]);
+#pragma unroll
+                    for (int j = 0; j < 3; ++j) {
+                        const uint32_t two = narrow2(x, y);
+                        part[j][i] = two;
+                        x -= __uint_as_float(two << 16);
+                        y -= __uint_as_float(two & 0xffff0000u);
+                    }
                 }
 #pragma unroll
-                for (int j = 0; j < 3; ++j) *(bf16x8 *)(to + j * kBytes) = part[j];
+                for (int j = 0; j < 3; ++j) *(u32x4 *)(to + j * kBytes) = part[j];
             }
         }
     }
