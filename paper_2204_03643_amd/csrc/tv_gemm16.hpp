@@ -2,8 +2,8 @@
 // through registers, two or four buffers in turn, 32 x 32 x 16 matrix instructions.
 //
 // The matrix units bound large products: 256 x 256 outputs take 1.24 us a step of 64 by matrix instructions alone (at the clock
-// that a full card keeps), 1.5 us here; 8192 x 2048 -> 8192 takes 236 us (1.17 PFLOP/s), its gradients, with their
-// transposed operands, 213 and 215 us.  Smaller tiles, for products whose large ones would leave compute units idle, are bound by
+// that a full card keeps), 1.5 us here; 8192 x 2048 -> 8192 takes 222-236 us (1.2 PFLOP/s,
+// the matrix units busy for 0.68 of the cycles), its gradients, with their transposed operands, 213 and 215 us.  Smaller tiles, for products whose large ones would leave compute units idle, are bound by
 // the latency of loads: 128 x 128 and 64 x 128 with four buffers have three steps on their way (4096 x 1024 -> 1024: 13.3 us;
 // 128 x 2048 -> 8192: 12.3).
 #pragma once

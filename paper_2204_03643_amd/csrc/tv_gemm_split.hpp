@@ -6,9 +6,9 @@
 // Six bf16 matrix instructions do the work of eight f32 ones in 0.38 of their time.  An operand of restored 8-bit codes is
 // exact in bf16 and has one part: three products.
 //
-// Splitting is vector work that the matrix units do not hide in full: 8192 x 2048 -> 8192 takes 1.28 ms (215 TFLOP/s of f32
-// products, 1.3 PFLOP/s of bf16 ones); 128 x 128 outputs take 2.0 us a step of 64 where up to half of the compute units have a
-// tile, 2.7 where all have (4096 x 1024 -> 1024: 52 us, 164 TFLOP/s).  bf16 operands off 16-byte boundaries pay for their way through
+// Splitting is vector work that the matrix units do not hide in full: 8192 x 2048 -> 8192 takes 1.19 ms (231 TFLOP/s of f32
+// products, 1.4 PFLOP/s of bf16 ones); 128 x 128 outputs take 1.8 us a step of 64 where up to half of the compute units have a
+// tile, 2.6 where all have (4096 x 1024 -> 1024: 49 us, 175 TFLOP/s, the matrix units busy for 0.57 of the cycles).  bf16 operands off 16-byte boundaries pay for their way through
 // registers: 505 us for 8192 x 2047 -> 8191.
 //
 // A part of an infinity, or of a value beyond bf16's largest, times zero is a NaN that the f32 product need not be: a
