@@ -22,7 +22,8 @@ struct Operand {
     int64_t ld, rows, cols;
 };
 
-// Rows on 16-byte boundaries, whole 16-byte pieces, and offsets within a tile of 256 rows that 32 bits hold.
+// Rows on 16-byte boundaries, whole 16-byte pieces, and offsets within a tile of 256 rows that 32 bits hold.  (Rows that the
+// library lays out itself are on such boundaries whatever their length: offsets_fit() says which tiles reach them.)
 inline bool direct(const Operand &o)
 {
     return aligned(o.p, 16) && o.ld % 8 == 0 && o.cols % 8 == 0 && o.ld <= ((int64_t)1 << 22);
@@ -82,15 +83,24 @@ inline double rounds_us(const Cost &c, int64_t workgroups, int64_t steps)
     return us;
 }
 
-inline Choice choose(int dtype, bool direct, bool transposed, int64_t M, int64_t N, int64_t K)
+// The strides of a product's operands, and which of them have the output index contiguous.
+struct Layout {
+    int64_t lda, ldb;
+    bool at, bt;
+};
+
+// The kernels that load straight to LDS keep 32-bit offsets from a tile's origin: to the tile's last row and 64 contraction
+// indices of it, or to the last contraction index of a step and the tile's columns there.
+inline bool offsets_fit(Kind kind, const Layout &l, int64_t M, int64_t N)
 {
-    if (!transposed && M >= 1 && M <= kFewRows) {
-        const int64_t turn = 8 * 64 / (int64_t)elem_bytes(dtype);            // a turn of all eight waves
-        const int64_t t = tiles(N, 32), s = t >= 256 ? 1 : 256 / t;
-        const Choice x = cut(kFew, s < K / (8 * turn) ? s : K / (8 * turn), K, turn);
-        const int64_t turns = tiles(t * x.splits, 256) * tiles(x.k_per < K ? x.k_per : K, turn);
-        if ((direct && M <= (dtype == TV_BF16 ? 32 : 16)) || turns * (M <= 16 ? 2 : M <= 32 ? 3 : 6) <= (dtype == TV_BF16 ? 12 : 36)) return x;
-    }
+    const Tile side = tile_of_kind(kind);
+    const int64_t a = l.at ? 63 * l.lda + side.m : ((M < side.m ? M : side.m) - 1) * l.lda + 64;
+    const int64_t b = l.bt ? 63 * l.ldb + side.n : ((N < side.n ? N : side.n) - 1) * l.ldb + 64;
+    return a * 2 < (int64_t)1 << 32 && b * 2 < (int64_t)1 << 32;
+}
+
+inline Choice choose_tiles(int dtype, bool direct, const Layout &l, int64_t M, int64_t N, int64_t K)
+{
     constexpr Cost direct16[] = {{kTile64, 256, 1.0, 0.25, 0.08}, {kTile128Deep, 256, 1.8, 0.38, 0.13}, {kTile128, 512, 1.5, 0.42, 0.52}, {kTile256, 256, 4.2, 1.14, 0.49}};
     constexpr Cost any16[] = {{kSplit64, 512, 3.2, 0.45, 0.44}};
     constexpr Cost any32[] = {{kSplit64, 256, 4.2, 1.26, 0.35}, {kSplit128, 256, 3.6, 1.97, 0.80}, {kSplit256, 256, 7.4, 6.6, 2.5}};
@@ -100,6 +110,7 @@ inline Choice choose(int dtype, bool direct, bool transposed, int64_t M, int64_t
     best.us = 1e30;
     for (int i = 0; i < kinds; ++i) {
         const Cost &c = costs[i];
+        if (costs == direct16 && !offsets_fit(c.kind, l, M, N)) continue;
         const Tile side = tile_of_kind(c.kind);
         const int64_t t = tiles(M, side.m) * tiles(N, side.n);
         for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
@@ -110,7 +121,20 @@ inline Choice choose(int dtype, bool direct, bool transposed, int64_t M, int64_t
             if (x.us < best.us) best = x;
         }
     }
+    if (best.us == 1e30) return choose_tiles(dtype, false, l, M, N, K);      // (rows too long for all of them: 64-bit addresses)
     return best;
+}
+
+inline Choice choose(int dtype, bool direct, const Layout &l, int64_t M, int64_t N, int64_t K)
+{
+    if (!l.at && !l.bt && M >= 1 && M <= kFewRows) {
+        const int64_t turn = 8 * 64 / (int64_t)elem_bytes(dtype);            // a turn of all eight waves
+        const int64_t t = tiles(N, 32), s = t >= 256 ? 1 : 256 / t;
+        const Choice x = cut(kFew, s < K / (8 * turn) ? s : K / (8 * turn), K, turn);
+        const int64_t turns = tiles(t * x.splits, 256) * tiles(x.k_per < K ? x.k_per : K, turn);
+        if ((direct && M <= (dtype == TV_BF16 ? 32 : 16)) || turns * (M <= 16 ? 2 : M <= 32 ? 3 : 6) <= (dtype == TV_BF16 ? 12 : 36)) return x;
+    }
+    return choose_tiles(dtype, direct, l, M, N, K);
 }
 
 // bf16 operands that cannot go straight to LDS are copied to rows that can, where the faster kernel pays for it
@@ -121,11 +145,12 @@ struct Plan {
 };
 inline double copy_us(int64_t rows, int64_t cols) { return 4.0 + (double)rows * (double)cols * 4 / 4e6; }
 
-inline Plan plan(int dtype, bool direct_a, bool direct_b, bool transposed, int64_t M, int64_t N, int64_t K)
+inline Plan plan(int dtype, bool direct_a, bool direct_b, const Layout &l, int64_t M, int64_t N, int64_t K)
 {
-    Plan p{choose(dtype, direct_a && direct_b, transposed, M, N, K), false, false};
+    Plan p{choose(dtype, direct_a && direct_b, l, M, N, K), false, false};
     if (dtype != TV_BF16 || (direct_a && direct_b) || p.c.kind == kFew || M < 1 || K < 1) return p;
-    Choice c = choose(dtype, true, true, M, N, K);
+    const Layout copied{direct_a ? l.lda : up(l.at ? M : K, 8), direct_b ? l.ldb : up(l.bt ? N : K, 8), l.at, l.bt};
+    Choice c = choose_tiles(dtype, true, copied, M, N, K);
     c.us += (direct_a ? 0.0 : copy_us(M, K)) + (direct_b ? 0.0 : copy_us(N, K));
     return c.us < p.c.us ? Plan{c, !direct_a, !direct_b} : p;
 }
@@ -148,7 +173,7 @@ struct FwdPlan {
 inline FwdPlan fwd_plan(const tv_linear_desc &d, bool direct_x, bool direct_w)
 {
     FwdPlan p{};
-    p.product = plan(d.dtype, direct_x, direct_w, false, d.m, d.n, d.k);
+    p.product = plan(d.dtype, direct_x, direct_w, {d.ldx, d.ldw, false, false}, d.m, d.n, d.k);
     p.w = p.product.copy_a ? copy_bytes(d.m, d.k) : 0;
     p.split = p.w + (p.product.copy_b ? copy_bytes(d.n, d.k) : 0);
     p.bytes = p.split + split_bytes(p.product.c, d.m, d.n);
@@ -170,13 +195,14 @@ inline BwdPlan bwd_plan(const tv_linear_desc &d, bool x8, bool direct_g, bool di
     BwdPlan p{};
     const int64_t size = (int64_t)elem_bytes(d.dtype);
     const bool smooth = d.act != TV_ACT_NONE;
-    // dz is written, and codes are restored, into rows that go straight to LDS
-    p.dx = plan(d.dtype, smooth || direct_g, direct_w, true, d.m, d.k, d.n);
-    p.dw = plan(d.dtype, smooth || direct_g, x8 || direct_x, true, d.n, d.k, d.m);
-    p.own_dz = smooth || p.dx.copy_a || p.dw.copy_a;
-    p.own_x = x8 || p.dw.copy_b;
     p.ldz = up(d.n, 8);
     p.ldx = up(d.k, 8);
+    // dz is written, and codes are restored, into rows that go straight to LDS
+    const int64_t ldz = smooth ? p.ldz : d.ldy, ldx = x8 ? p.ldx : d.ldx;
+    p.dx = plan(d.dtype, smooth || direct_g, direct_w, {ldz, d.ldw, false, true}, d.m, d.k, d.n);
+    p.dw = plan(d.dtype, smooth || direct_g, x8 || direct_x, {ldz, ldx, true, true}, d.n, d.k, d.m);
+    p.own_dz = smooth || p.dx.copy_a || p.dw.copy_a;
+    p.own_x = x8 || p.dw.copy_b;
     size_t at = p.own_dz ? up(d.m * p.ldz * size, 256) : 0;
     p.x = at;
     if (p.own_x) at += copy_bytes(d.m, d.k);
