@@ -11,8 +11,9 @@
 // tile, 2.6 where all have (4096 x 1024 -> 1024: 49 us, 175 TFLOP/s, the matrix units busy for 0.57 of the cycles).  bf16 operands off 16-byte boundaries pay for their way through
 // registers: 505 us for 8192 x 2047 -> 8191.
 //
-// A part of an infinity, or of a value beyond bf16's largest, times zero is a NaN that the f32 product need not be: a
-// wave that finds a NaN among its sums takes those from f32 matrix instructions.
+// A part of an infinity, or of a value beyond bf16's largest, times zero is a NaN that the f32 product need not be, and
+// parts that were rounded up may multiply to an infinity where the f32 product is finite: a wave that finds a sum that is not
+// finite among its own takes it from f32 matrix instructions.
 #pragma once
 #include "tv_gemm16.hpp"
 
@@ -122,7 +123,7 @@ template <class T, int ROWS, int THREADS, int KQ, bool TRANSPOSED> struct Staged
 };
 
 // A 32 x 32 tile of outputs from (m0, n0) on with f32 matrix instructions, two contraction indices at a time, straight
-// from memory: what is left for tiles that hold NaNs.
+// from memory: what is left for tiles with sums that are not finite.
 template <class TA, class TB, bool AT, bool BT>
 __device__ __attribute__((noinline)) f32x16 tile_in_f32(const TA *a, const TB *b, int64_t lda, int64_t ldb, int M, int N, int k0, int k_end, int m0, int n0, int lane)
 {
@@ -271,18 +272,22 @@ __global__ __launch_bounds__(WM * WN * G * 64) __attribute__((amdgpu_waves_per_e
         if (group) return;                            // (no barrier comes after this)
     }
     if constexpr (P * PB > 1) {
-        uint32_t most = 0;                            // of all sums, a NaN's bits being above infinity's
+        uint32_t most = 0;                            // of all sums, the bits of what is not finite being above the others'
         each<TM * TN>([&](auto x) __attribute__((always_inline)) {
             each<16>([&](auto q) __attribute__((always_inline)) {
                 most = max(most, __float_as_uint(acc[x % TN][x / TN][decltype(q)::value]) & 0x7fffffffu);
             });
         });
-        if (__any(most > 0x7f800000u))
+        if (__any(most >= 0x7f800000u))
             each<TM * TN>([&](auto x) __attribute__((always_inline)) {
                 constexpr int i = x % TN, j = x / TN;
                 const f32x16 again = tile_in_f32<T, TB, AT, BT>((const T *)g.a, (const TB *)g.b, g.lda, g.ldb, g.M, g.N, k0, k_end,
                                                                 m0 + wm + 32 * j, n0 + wn + 32 * i, lane);
-                each<16>([&](auto y) __attribute__((always_inline)) { constexpr int q = y; acc[i][j][q] = acc[i][j][q] != acc[i][j][q] ? again[q] : acc[i][j][q]; });
+                each<16>([&](auto y) __attribute__((always_inline)) {
+                    constexpr int q = y;
+                    const bool finite = (__float_as_uint(acc[i][j][q]) & 0x7fffffffu) < 0x7f800000u;
+                    acc[i][j][q] = finite ? acc[i][j][q] : again[q];
+                });
             });
     }
     float *piece = (float *)lds + wave * 32 * kOutPitch;
