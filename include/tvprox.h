@@ -320,7 +320,8 @@ int tv2d_prox_bwd_bf16(const uint16_t *g_up, uint16_t *grad_y, float *grad_lam, 
  * Arrays are dense rows with the last index contiguous; ld* are row strides in ELEMENTS (at least the row's
  * length, below 2^31), any alignment that suits the type.  W's rows are ldw apart, b is packed.  One dtype for
  * all of x, W, b, r, y, g and the gradients; sums and activations are fp32, each output is rounded once.  In
- * bf16, dz is rounded to bf16 before the products that give dx and dW (db sums it unrounded).
+ * bf16, dz is rounded to bf16 before the products that give dx and dW (db sums it unrounded).  In
+ * fp32, products of more than a few rows take an operand's values below 2^-110 in magnitude to within 2^-134 only.
  * Activations: gelu is z Phi(z) (with erf), silu z / (1 + exp(-z)); ReLU is 0 where z <= 0, with slope 0 there.
  *
  * Sizes are below 2^31 - 1024, and each of y, dx and dW has at most TV_LINEAR_MAX_TILES tiles of 128 x 128

@@ -6,6 +6,11 @@
 // Six bf16 matrix instructions do the work of eight f32 ones in 0.38 of their time.  An operand of restored 8-bit codes is
 // exact in bf16 and has one part: three products.
 //
+// That holds for magnitudes of 2^-110 and more (and zero).  Below, the last bits of m and l are below bf16's least number,
+// 2^-133, and a value is taken to half of that, 2^-134: a product is then off by up to 2^-134 times the other value.  (Telling
+// such values while they are split takes one and a half instructions a value beside 5.5, and would send every tile that holds
+// one among larger values, where it does not count, to the slow f32 instructions.)
+//
 // Splitting is vector work that the matrix units do not hide in full: 8192 x 2048 -> 8192 takes 1.19 ms (231 TFLOP/s of f32
 // products, 1.4 PFLOP/s of bf16 ones); 128 x 128 outputs take 1.8 us a step of 64 where up to half of the compute units have a
 // tile, 2.6 where all have (4096 x 1024 -> 1024: 49 us, 175 TFLOP/s, the matrix units busy for 0.57 of the cycles).  bf16 operands off 16-byte boundaries pay for their way through

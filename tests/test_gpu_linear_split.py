@@ -60,3 +60,18 @@ def test_many_terms_in_the_2_norm(M, K, N):
     near(dx, g.double() @ w.double(), N)
     near(dw, gt @ x.double(), M)
     near(lin.tv_linear_backward(g, held, None, w)[1], gt @ held.restore().double(), M)
+
+
+@pytest.mark.parametrize("M,K,N", [(300, 64, 260), (2048, 2048, 2048), (4096, 192, 4096), (264, 2048, 200)])
+def test_values_whose_parts_leave_bf16_range(M, K, N):
+    """Below 2^-110 the last bits of an f32 value lie below bf16's least number, 2^-133: a value is then taken to half of
+    that, 2^-134, and the products are off by that much of the other operand on top of the usual bound."""
+    lin = linear()
+    gen = torch.Generator(device="cuda").manual_seed(K)
+    for e in (-105, -115, -125):
+        x = torch.randn(M, K, generator=gen, device="cuda") * 2.0 ** e
+        w = torch.randn(N, K, generator=gen, device="cuda") * 2.0 ** 20
+        x64, w64 = x.double(), w.double()
+        size, other = x64.abs() @ w64.t().abs().contiguous(), w64.abs().sum(1)
+        off = (K + 8) * 2.0 ** -24 * size + 2.0 ** -134 * other + 2.0 ** -149
+        assert ((lin.tv_linear(x, w).double() - x64 @ w64.t().contiguous()).abs() <= off).all(), e
