@@ -13,6 +13,7 @@ import functools
 import math
 
 import torch
+from torch.autograd import forward_ad as _forward_ad
 
 from . import binding as _b
 from .layer import tv_prox_1d
@@ -43,6 +44,13 @@ def _as_rows(t: torch.Tensor):
     if t.dim() == 2 and (t.stride(1) == 1 or n == 1) and (t.stride(0) >= n or t.shape[0] == 1):
         return t, (t.stride(0) if t.shape[0] > 1 else n)
     return t.contiguous(), n
+
+
+def _tangent_among(*tensors) -> bool:
+    """Whether forward-mode differentiation has given one of them a tangent, which the kernels would not see.  (A level
+    that is not open is told by one look at its number.)"""
+    return (getattr(_forward_ad, "_current_level", 0) >= 0
+            and any(t is not None and _forward_ad.unpack_dual(t).tangent is not None for t in tensors))
 
 
 def _blocks(n: int) -> int:
@@ -216,6 +224,8 @@ class _Linear(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, g):
+        if _tangent_among(g):
+            raise NotImplementedError("tv_linear: the gradients have no forward-mode derivative")
         x, x_exps, data, exps, weight = ctx.saved_tensors
         need = ctx.needs_input_grad
         want = (need[0], need[1], ctx.has_bias and need[2])
@@ -258,7 +268,8 @@ def tv_linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None =
         if residual.shape != (*x.shape[:-1], n):
             raise ValueError("tv_linear: residual of shape %r expected, got %r" % ((*x.shape[:-1], n), tuple(residual.shape)))
     if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or (bias is not None and bias.requires_grad)
-                                    or (residual is not None and residual.requires_grad)):
+                                    or (residual is not None and residual.requires_grad)) \
+            or _tangent_among(x, weight, bias, residual):              # (which apply refuses)
         return _Linear.apply(x, weight, bias, residual, act, checkpoint)
     x, ldx = _as_rows(x)
     weight, ldw = _as_rows(weight)
@@ -277,6 +288,8 @@ def tv_linear_backward(g: torch.Tensor, x, z, weight: torch.Tensor, act: str = "
         raise ValueError("tv_linear_backward: g of shape %r expected, got %r" % (tuple(x.shape[:-1]) + (n,), tuple(g.shape)))
     m = g.numel() // n
     x_exps = None
+    if _tangent_among(g, weight, *(t for t in (x, z) if isinstance(t, torch.Tensor))):
+        raise NotImplementedError("tv_linear_backward: the gradients have no forward-mode derivative")
     if isinstance(x, Checkpoint8):
         x, x_exps, ldx = x.codes, x.exps, x.shape[-1]
         if x.device != g.device:
