@@ -359,18 +359,23 @@ typedef struct {
 /*
  * y may be r exactly (same pointer and stride); no other output may overlap an input.  ws: device scratch of at
  * least tv_linear_fwd_workspace_bytes() bytes, 16-byte aligned (may be NULL where that is 0), contents undefined
- * afterwards.
+ * afterwards.  That is enough wherever x and W lie; tv_linear_fwd_workspace_bytes_at() is what the call with these
+ * pointers needs (it looks at their alignment alone): nothing like as much where rows start on 16-byte boundaries.
  */
 size_t tv_linear_fwd_workspace_bytes(tv_linear_desc desc);
+size_t tv_linear_fwd_workspace_bytes_at(const void *x, const void *w, tv_linear_desc desc);
 int tv_linear_fwd(const void *x, const void *w, const void *bias, const void *res, void *y, tv_held held,
                   tv_linear_desc desc, void *ws, size_t ws_bytes, hipStream_t stream);
 
 /*
  * x: the forward call's input, or (x_exps given) the codes of its 8-bit checkpoint, packed [m, k]; held: as the
  * forward call wrote it; g: rows of desc.ldy elements.  dx [m, k], dw [n, k] and db [n] are packed; each may be
- * NULL where it is not wanted (w is not read without dx, x not without dw).
+ * NULL where it is not wanted (w is not read without dx, x not without dw).  Workspaces as in the forward call;
+ * ..._bytes_at() also leaves out what an output that is NULL would have needed.
  */
 size_t tv_linear_bwd_workspace_bytes(tv_linear_desc desc, int x_is_8bit);
+size_t tv_linear_bwd_workspace_bytes_at(const void *g, const void *x, const uint8_t *x_exps, const void *w, const void *dx,
+                                        const void *dw, const void *db, tv_linear_desc desc);
 int tv_linear_bwd(const void *g, const void *x, const uint8_t *x_exps, tv_held held, const void *w, void *dx,
                   void *dw, void *db, tv_linear_desc desc, void *ws, size_t ws_bytes, hipStream_t stream);
 

@@ -13,7 +13,8 @@ from .binding import (TVError, lib, status_str, tv_dispatch_thresholds, tv_dispa
                       tv1d_prox_bwd_seg, tv1d_prox_fwd, tv1d_prox_fwd_info, tv1d_prox_fwd_seg, tv1d_prox_fwd_seg_bf16,
                       tv1d_prox_bwd_seg_bf16, tv2d_prox_bwd, tv2d_prox_fwd, tv2d_prox_fwd_bf16, tv2d_prox_bwd_bf16,
                       tv2d_workspace_bytes, tv_lambda, tv_rows, rows_along, tv_linear_desc, tv_held, tv_linear_fwd,
-                      tv_linear_fwd_workspace_bytes, tv_linear_bwd, tv_linear_bwd_workspace_bytes, tv_ckpt8_save,
+                      tv_linear_fwd_workspace_bytes, tv_linear_fwd_workspace_bytes_at, tv_linear_bwd,
+                      tv_linear_bwd_workspace_bytes, tv_linear_bwd_workspace_bytes_at, tv_ckpt8_save,
                       tv_ckpt8_load, TV_F32, TV_BF16, TV_ACT_NONE, TV_ACT_RELU, TV_ACT_GELU, TV_ACT_SILU, TV_HELD_NONE,
                       TV_HELD_PLAIN, TV_HELD_BITS, TV_HELD_8BIT, TV_CKPT8_BLOCK)
 
@@ -23,7 +24,7 @@ __all__ = ["TVError", "lib", "status_str", "tv_dispatch_thresholds", "tv_dispatc
            "tv1d_fwd_workspace_bytes", "tv_fwd_extra", "TV_FWD_ORDER_READY", "TV_FWD_PARALLEL_SEARCH", "tv1d_prox_fwd_steps",
            "tv1d_fwd_steps_floats_per_row", "tv1d_bwd_workspace_bytes", "tv2d_prox_fwd",
            "tv2d_prox_bwd", "tv2d_workspace_bytes", "tv2d_prox_fwd_bf16", "tv2d_prox_bwd_bf16",
-           "tv_linear_desc", "tv_held", "tv_linear_fwd", "tv_linear_fwd_workspace_bytes", "tv_linear_bwd",
-           "tv_linear_bwd_workspace_bytes", "tv_ckpt8_save", "tv_ckpt8_load", "TV_F32", "TV_BF16", "TV_ACT_NONE",
+           "tv_linear_desc", "tv_held", "tv_linear_fwd", "tv_linear_fwd_workspace_bytes", "tv_linear_fwd_workspace_bytes_at", "tv_linear_bwd",
+           "tv_linear_bwd_workspace_bytes", "tv_linear_bwd_workspace_bytes_at", "tv_ckpt8_save", "tv_ckpt8_load", "TV_F32", "TV_BF16", "TV_ACT_NONE",
            "TV_ACT_RELU", "TV_ACT_GELU", "TV_ACT_SILU", "TV_HELD_NONE", "TV_HELD_PLAIN", "TV_HELD_BITS", "TV_HELD_8BIT",
            "TV_CKPT8_BLOCK"]

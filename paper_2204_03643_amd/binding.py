@@ -126,10 +126,14 @@ def lib() -> ctypes.CDLL:
         L.tv2d_prox_bwd_bf16.restype = ctypes.c_int
         L.tv_linear_fwd_workspace_bytes.argtypes = [tv_linear_desc]
         L.tv_linear_fwd_workspace_bytes.restype = ctypes.c_size_t
+        L.tv_linear_fwd_workspace_bytes_at.argtypes = [_vp, _vp, tv_linear_desc]
+        L.tv_linear_fwd_workspace_bytes_at.restype = ctypes.c_size_t
         L.tv_linear_fwd.argtypes = [_vp, _vp, _vp, _vp, _vp, tv_held, tv_linear_desc, _vp, ctypes.c_size_t, _vp]
         L.tv_linear_fwd.restype = ctypes.c_int
         L.tv_linear_bwd_workspace_bytes.argtypes = [tv_linear_desc, ctypes.c_int]
         L.tv_linear_bwd_workspace_bytes.restype = ctypes.c_size_t
+        L.tv_linear_bwd_workspace_bytes_at.argtypes = [_vp] * 7 + [tv_linear_desc]
+        L.tv_linear_bwd_workspace_bytes_at.restype = ctypes.c_size_t
         L.tv_linear_bwd.argtypes = [_vp, _vp, _vp, tv_held, _vp, _vp, _vp, _vp, tv_linear_desc, _vp, ctypes.c_size_t, _vp]
         L.tv_linear_bwd.restype = ctypes.c_int
         L.tv_ckpt8_save.argtypes = [_vp, _vp, _vp, _i64, _i64, _i64, ctypes.c_int, _vp]
@@ -294,6 +298,10 @@ def tv_linear_fwd_workspace_bytes(desc: tv_linear_desc) -> int:
     return int(lib().tv_linear_fwd_workspace_bytes(desc))
 
 
+def tv_linear_fwd_workspace_bytes_at(x, w, desc: tv_linear_desc) -> int:
+    return int(lib().tv_linear_fwd_workspace_bytes_at(_ptr(x), _ptr(w), desc))
+
+
 def tv_linear_fwd(x, w, bias, res, y, held: tv_held, desc: tv_linear_desc, ws=None, ws_bytes: int = 0, stream=None):
     _check(lib().tv_linear_fwd(_ptr(x), _ptr(w), _ptr(bias), _ptr(res), _ptr(y), held, desc, _ptr(ws), int(ws_bytes),
                                _stream(stream)))
@@ -301,6 +309,10 @@ def tv_linear_fwd(x, w, bias, res, y, held: tv_held, desc: tv_linear_desc, ws=No
 
 def tv_linear_bwd_workspace_bytes(desc: tv_linear_desc, x_is_8bit: bool) -> int:
     return int(lib().tv_linear_bwd_workspace_bytes(desc, int(bool(x_is_8bit))))
+
+
+def tv_linear_bwd_workspace_bytes_at(g, x, x_exps, w, dx, dw, db, desc: tv_linear_desc) -> int:
+    return int(lib().tv_linear_bwd_workspace_bytes_at(_ptr(g), _ptr(x), _ptr(x_exps), _ptr(w), _ptr(dx), _ptr(dw), _ptr(db), desc))
 
 
 def tv_linear_bwd(g, x, x_exps, held: tv_held, w, dx, dw, db, desc: tv_linear_desc, ws=None, ws_bytes: int = 0,

@@ -190,7 +190,9 @@ struct BwdPlan {
     bool own_dz, own_x;
 };
 
-inline BwdPlan bwd_plan(const tv_linear_desc &d, bool x8, bool direct_g, bool direct_x, bool direct_w)
+struct Wanted { bool dx, dw, db; };
+
+inline BwdPlan bwd_plan(const tv_linear_desc &d, bool x8, bool direct_g, bool direct_x, bool direct_w, Wanted want)
 {
     BwdPlan p{};
     const int64_t size = (int64_t)elem_bytes(d.dtype);
@@ -201,21 +203,21 @@ inline BwdPlan bwd_plan(const tv_linear_desc &d, bool x8, bool direct_g, bool di
     const int64_t ldz = smooth ? p.ldz : d.ldy, ldx = x8 ? p.ldx : d.ldx;
     p.dx = plan(d.dtype, smooth || direct_g, direct_w, {ldz, d.ldw, false, true}, d.m, d.k, d.n);
     p.dw = plan(d.dtype, smooth || direct_g, x8 || direct_x, {ldz, ldx, true, true}, d.n, d.k, d.m);
-    p.own_dz = smooth || p.dx.copy_a || p.dw.copy_a;
-    p.own_x = x8 || p.dw.copy_b;
+    p.own_dz = (want.dx && (smooth || p.dx.copy_a)) || (want.dw && (smooth || p.dw.copy_a));
+    p.own_x = want.dw && (x8 || p.dw.copy_b);
     size_t at = p.own_dz ? up(d.m * p.ldz * size, 256) : 0;
     p.x = at;
     if (p.own_x) at += copy_bytes(d.m, d.k);
     p.w = at;
-    if (p.dx.copy_b) at += copy_bytes(d.n, d.k);
+    if (want.dx && p.dx.copy_b) at += copy_bytes(d.n, d.k);
     // about 1024 workgroups of 256 columns each, of sixteen rows at least; up to 64 rows are one group, one launch
-    const int64_t want = 1024 / tiles(d.n, 256) + 1;
-    p.rows_per = (int)(d.m > 64 ? up(tiles(d.m, want < 256 ? want : 256), 16) : 64);
+    const int64_t share = 1024 / tiles(d.n, 256) + 1;
+    p.rows_per = (int)(d.m > 64 ? up(tiles(d.m, share < 256 ? share : 256), 16) : 64);
     p.groups = (int)tiles(d.m, p.rows_per);
     p.sums = at;
-    at += up((int64_t)p.groups * d.n * 4, 256);
+    if (want.db) at += up((int64_t)p.groups * d.n * 4, 256);
     p.split = at;
-    const size_t s1 = split_bytes(p.dx.c, d.m, d.k), s2 = split_bytes(p.dw.c, d.n, d.k);
+    const size_t s1 = want.dx ? split_bytes(p.dx.c, d.m, d.k) : 0, s2 = want.dw ? split_bytes(p.dw.c, d.n, d.k) : 0;
     p.bytes = at + (s1 > s2 ? s1 : s2);
     return p;
 }

@@ -132,11 +132,10 @@ int linear_bwd(const void *g, const void *x, const uint8_t *x_exps, const tv_hel
                void *db, const tv_linear_desc &d, const BwdPlan &p, char *ws, hipStream_t stream)
 {
     Operand dz{g, d.ldy, d.m, d.n};
-    const bool own_dz = d.act != TV_ACT_NONE || (dx && p.dx.copy_a) || (dw && p.dw.copy_a);
-    if (d.m > 0 && (own_dz || db)) {
+    if (d.m > 0 && (p.own_dz || db)) {
         SlopeArgs a{};
         a.g = g; a.held = h.data; a.exps = h.exps;
-        a.dz = own_dz ? ws : nullptr;
+        a.dz = p.own_dz ? ws : nullptr;
         a.sums = db && p.groups > 1 ? (float *)(ws + p.sums) : nullptr;
         a.db = p.groups == 1 ? db : nullptr;
         a.ldg = d.ldy; a.ldz = p.ldz;
@@ -144,7 +143,7 @@ int linear_bwd(const void *g, const void *x, const uint8_t *x_exps, const tv_hel
         a.act = d.act; a.kind = d.act == TV_ACT_NONE ? TV_HELD_NONE : h.kind;
         hipLaunchKernelGGL((slope_kernel<T>), dim3((uint32_t)tiles(d.n, 256), p.groups), dim3(256), 0, stream, a);
         if (launched() != TV_OK) return TV_ERR_HIP;
-        if (own_dz) dz = {ws, p.ldz, d.m, p.ldz};
+        if (p.own_dz) dz = {ws, p.ldz, d.m, p.ldz};
     }
     if (db && p.groups != 1) {
         hipLaunchKernelGGL((column_sum_kernel<T>), dim3((uint32_t)tiles(d.n, 32)), dim3(256), 0, stream,
@@ -171,6 +170,17 @@ int linear_bwd(const void *g, const void *x, const uint8_t *x_exps, const tv_hel
     return TV_OK;
 }
 
+// The plans of calls with these pointers, of which alignments count, and whether outputs are there at all.
+FwdPlan fwd_plan_of(const void *x, const void *w, const tv_linear_desc &d)
+{
+    return fwd_plan(d, direct({x, d.ldx, d.m, d.k}), direct({w, d.ldw, d.n, d.k}));
+}
+BwdPlan bwd_plan_of(const void *g, const void *x, const uint8_t *x_exps, const void *w, const void *dx, const void *dw, const void *db, const tv_linear_desc &d)
+{
+    return bwd_plan(d, x_exps != nullptr, direct({g, d.ldy, d.m, d.n}), direct({x, d.ldx, d.m, d.k}), direct({w, d.ldw, d.n, d.k}),
+                    {dx != nullptr, dw != nullptr, db != nullptr});
+}
+
 int check_ckpt8(int64_t rows, int64_t n, int64_t ld, int dtype)
 {
     if (rows < 0 || n < 1 || rows >= kMostIndex || n >= kMostIndex) return TV_ERR_SHAPE;
@@ -190,7 +200,7 @@ dim3 ckpt8_grid(int64_t rows, int64_t n)
 
 extern "C" {
 
-// (The workspaces are asked for before there are pointers, and have to do wherever those lie.)
+// (The workspaces that are asked for without pointers have to do wherever those lie.)
 size_t tv_linear_fwd_workspace_bytes(tv_linear_desc d)
 {
     size_t most = 0;
@@ -200,6 +210,11 @@ size_t tv_linear_fwd_workspace_bytes(tv_linear_desc d)
             most = most > b ? most : b;
         }
     return most;
+}
+
+size_t tv_linear_fwd_workspace_bytes_at(const void *x, const void *w, tv_linear_desc d)
+{
+    return check_sizes(d) == TV_OK && d.m > 0 ? fwd_plan_of(x, w, d).bytes : 0;
 }
 
 int tv_linear_fwd(const void *x, const void *w, const void *bias, const void *res, void *y, tv_held held,
@@ -213,7 +228,7 @@ int tv_linear_fwd(const void *x, const void *w, const void *bias, const void *re
     if (!x || !w || !y) return TV_ERR_NULL;
     const size_t size = elem_bytes(d.dtype);
     if (!aligned(x, size) || !aligned(w, size) || !aligned(bias, size) || !aligned(res, size) || !aligned(y, size)) return TV_ERR_STRIDE;
-    const FwdPlan p = fwd_plan(d, direct({x, d.ldx, d.m, d.k}), direct({w, d.ldw, d.n, d.k}));
+    const FwdPlan p = fwd_plan_of(x, w, d);
     if ((st = check_workspace(ws, ws_bytes, p.bytes)) != TV_OK) return st;
     return d.dtype == TV_BF16 ? linear_fwd<bf16>(x, w, bias, res, y, held, d, p, (char *)ws, stream)
                               : linear_fwd<float>(x, w, bias, res, y, held, d, p, (char *)ws, stream);
@@ -224,10 +239,16 @@ size_t tv_linear_bwd_workspace_bytes(tv_linear_desc d, int x_is_8bit)
     size_t most = 0;
     if (check_sizes(d) == TV_OK)
         for (int i = 0; i < 8; ++i) {
-            const size_t b = bwd_plan(d, x_is_8bit != 0, (i & 1) != 0, (i & 2) != 0, (i & 4) != 0).bytes;
+            const size_t b = bwd_plan(d, x_is_8bit != 0, (i & 1) != 0, (i & 2) != 0, (i & 4) != 0, {true, true, true}).bytes;
             most = most > b ? most : b;
         }
     return most;
+}
+
+size_t tv_linear_bwd_workspace_bytes_at(const void *g, const void *x, const uint8_t *x_exps, const void *w, const void *dx,
+                                        const void *dw, const void *db, tv_linear_desc d)
+{
+    return check_sizes(d) == TV_OK ? bwd_plan_of(g, x, x_exps, w, dx, dw, db, d).bytes : 0;
 }
 
 int tv_linear_bwd(const void *g, const void *x, const uint8_t *x_exps, tv_held held, const void *w, void *dx, void *dw,
@@ -240,7 +261,7 @@ int tv_linear_bwd(const void *g, const void *x, const uint8_t *x_exps, tv_held h
     const size_t size = elem_bytes(d.dtype);
     if (!aligned(g, size) || (!x_exps && !aligned(x, size)) || !aligned(w, size) || !aligned(dx, size) || !aligned(dw, size) ||
         !aligned(db, size)) return TV_ERR_STRIDE;
-    const BwdPlan p = bwd_plan(d, x_exps != nullptr, direct({g, d.ldy, d.m, d.n}), direct({x, d.ldx, d.m, d.k}), direct({w, d.ldw, d.n, d.k}));
+    const BwdPlan p = bwd_plan_of(g, x, x_exps, w, dx, dw, db, d);
     if ((st = check_workspace(ws, ws_bytes, p.bytes)) != TV_OK) return st;
     return d.dtype == TV_BF16 ? linear_bwd<bf16>(g, x, x_exps, held, w, dx, dw, db, d, p, (char *)ws, stream)
                               : linear_bwd<float>(g, x, x_exps, held, w, dx, dw, db, d, p, (char *)ws, stream);

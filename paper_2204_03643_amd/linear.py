@@ -57,17 +57,24 @@ def _blocks(n: int) -> int:
     return -(-n // _b.TV_CKPT8_BLOCK)
 
 
-# A call's descriptor and workspace size, which sizes, strides and dtype say in full.
+# A call's descriptor and workspace size, which sizes, strides, dtype, and where the operands lie between 16-byte boundaries
+# say in full.
 @functools.lru_cache(maxsize=4096)
-def _fwd_desc(*fields):
+def _fwd_desc(x_at, w_at, *fields):
     desc = _b.tv_linear_desc(*fields)
-    return desc, _b.tv_linear_fwd_workspace_bytes(desc)
+    return desc, _b.tv_linear_fwd_workspace_bytes_at(x_at, w_at, desc)
 
 
 @functools.lru_cache(maxsize=4096)
-def _bwd_desc(x_is_8bit, *fields):
+def _bwd_desc(g_at, x_at, x_is_8bit, w_at, dx, dw, db, *fields):
     desc = _b.tv_linear_desc(*fields)
-    return desc, _b.tv_linear_bwd_workspace_bytes(desc, x_is_8bit)
+    there = [16 if t else None for t in (x_is_8bit, dx, dw, db)]
+    return desc, _b.tv_linear_bwd_workspace_bytes_at(g_at, x_at, there[0], w_at, *there[1:], desc)
+
+
+def _place(address):
+    """A small address that lies between 16-byte boundaries as this one does."""
+    return 16 + address % 16
 
 
 def _on_device(call):
@@ -175,9 +182,10 @@ def _forward(x, ldx, weight, ldw, bias, residual, act, hold):
         else:
             data, kind = x.new_empty((m, n)), _b.TV_HELD_PLAIN
         held = _b.tv_held(data.data_ptr(), _address(exps), kind)
-    desc, nbytes = _fwd_desc(m, k, n, ldx, ldw, ldr, n, dtype, code)
+    at_x, at_w = x.data_ptr(), weight.data_ptr()
+    desc, nbytes = _fwd_desc(_place(at_x), _place(at_w), m, k, n, ldx, ldw, ldr, n, dtype, code)
     ws = x.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
-    _check(_b.lib().tv_linear_fwd(x.data_ptr(), weight.data_ptr(), _address(bias), _address(residual), y.data_ptr(), held, desc,
+    _check(_b.lib().tv_linear_fwd(at_x, at_w, _address(bias), _address(residual), y.data_ptr(), held, desc,
                                   _address(ws), nbytes, _b._stream(None)))
     return y, data, exps
 
@@ -195,10 +203,11 @@ def _backward(g, x, x_exps, ldx, data, exps, weight, ldw, act, want):
     dx = g.new_empty((*g.shape[:-1], k)) if want[0] else None
     dw = g.new_empty((n, k)) if want[1] else None
     db = g.new_empty(n) if want[2] else None
-    desc, nbytes = _bwd_desc(x_exps is not None, m, k, n, ldx, ldw, n, ldg, dtype, code)
+    at_g, at_x, at_w = g.data_ptr(), _address(x), weight.data_ptr()
+    desc, nbytes = _bwd_desc(_place(at_g), _place(at_x or 0), x_exps is not None, _place(at_w), *want, m, k, n, ldx, ldw, n, ldg, dtype, code)
     ws = g.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
-    _check(_b.lib().tv_linear_bwd(g.data_ptr(), _address(x), _address(x_exps), _b.tv_held(_address(data), _address(exps), kind),
-                                  weight.data_ptr(), _address(dx), _address(dw), _address(db),
+    _check(_b.lib().tv_linear_bwd(at_g, at_x, _address(x_exps), _b.tv_held(_address(data), _address(exps), kind),
+                                  at_w, _address(dx), _address(dw), _address(db),
                                   desc, _address(ws), nbytes, _b._stream(None)))
     return dx, dw, db
 

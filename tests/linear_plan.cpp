@@ -21,7 +21,7 @@ int main()
         const size_t off = elem_bytes(dtype);
         const bool dg = direct({base + (ag ? 0 : off), ldg, m, n}), dx = direct({base + (ax ? 0 : off), ldx, m, k}), dw = direct({base + (aw ? 0 : off), ldw, n, k});
         const FwdPlan f = fwd_plan(d, dx, dw);
-        const BwdPlan b = bwd_plan(d, x8 != 0, dg, dx, dw);
+        const BwdPlan b = bwd_plan(d, x8 != 0, dg, dx, dw, {true, true, true});
         const int64_t ldz = b.own_dz ? b.ldz : ldg;
         print(f.product, f.product.copy_a ? up(k, 8) : ldx, f.product.copy_b ? up(k, 8) : ldw);
         print(b.dx, ldz, b.dx.copy_b ? up(k, 8) : ldw);

@@ -1,0 +1,44 @@
+"""What the channel products allocate."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+def peak(call):
+    """Bytes that a call holds at its most, beyond what there was (in blocks of 512 bytes, and large ones of 2 MiB)."""
+    call()
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    torch.cuda.reset_peak_memory_stats()
+    kept = call()                                      # noqa: F841 (alive until the peak is read)
+    return torch.cuda.max_memory_allocated() - before
+
+
+def test_no_more_than_the_operands_need():
+    from paper_2204_03643_amd.linear import tv_linear, tv_linear_backward
+    M, K, N, t = 4096, 2048, 4096, torch.bfloat16
+    x, w, g = (torch.randn(*s, device="cuda").to(t) for s in ((M, K), (N, K), (M, N)))
+    slack = 4 << 20
+    assert peak(lambda: tv_linear(x, w)) <= 2 * M * N + slack
+    z = torch.randn(M, N, device="cuda").to(t)
+    assert peak(lambda: tv_linear_backward(g, x, z, w, "gelu", True)) <= 2 * (M * N + M * K + N * K) + slack
+    # off 16-byte boundaries copies are made, and asked for
+    off = torch.randn(M * K + 1, device="cuda").to(t)[1:].view(M, K)
+    assert torch.equal(tv_linear(off, w), tv_linear(off.clone(), w))
+
+
+@pytest.mark.parametrize("wanted", ([0], [1], [2], [0, 2], [1, 2]))
+@pytest.mark.parametrize("act", ("none", "gelu", "relu"))
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+def test_some_of_the_gradients(wanted, act, dtype):
+    """Any of dx, dW and db alone has the bits that it has beside the others."""
+    from paper_2204_03643_amd.linear import tv_linear
+    for M, K, N in ((40, 72, 88), (300, 1001, 130), (1000, 264, 512)):
+        x, w, b, g = (torch.randn(*s, device="cuda").to(dtype) for s in ((M, K), (N, K), (N,), (M, N)))
+        leaves = [v.clone().requires_grad_() for v in (x, w, b)]
+        everything = torch.autograd.grad(tv_linear(*leaves, act=act), leaves, g)
+        some = [v.clone().requires_grad_(i in wanted) for i, v in enumerate((x, w, b))]
+        got = torch.autograd.grad(tv_linear(*some, act=act), [some[i] for i in wanted], g)
+        for i, v in zip(wanted, got):
+            assert torch.equal(v, everything[i]), (M, K, N, i)

@@ -71,3 +71,59 @@ def test_offsets_within_a_tile_fit_32_bits(plans, what, act, x8, on16):
                 assert farthest(M, q["lda"], tile[0], at) < 1 << 32, (c, name, q)
                 assert farthest(N, q["ldb"], tile[1], bt) < 1 << 32, (c, name, q)
     assert {TILE256, SPLIT64} <= taken
+
+
+FAKE = 1 << 20
+
+
+@pytest.mark.parametrize("dtype", (tv.TV_F32, tv.TV_BF16))
+@pytest.mark.parametrize("act", (tv.TV_ACT_NONE, tv.TV_ACT_GELU))
+def test_workspaces_of_pointers(dtype, act):
+    """What is enough everywhere is what the neediest pointers need (or more, where rows cannot all start on 16-byte
+    boundaries), and nobody is asked for more than that."""
+    size = 2 if dtype == tv.TV_BF16 else 4
+    for m, k, n in ((1, 64, 64), (64, 8192, 256), (300, 1001, 777), (8192, 2048, 8192), (4096, 8192, 2048), (0, 8, 8)):
+        d = tv.tv_linear_desc(m, k, n, k, k, n, n, dtype, act)
+        places = list(itertools.product((FAKE, FAKE + size), repeat=3))
+        have = [tv.tv_linear_fwd_workspace_bytes_at(x, w, d) for x, w, _ in places]
+        even = k % 8 == 0 and n % 8 == 0
+        query = tv.tv_linear_fwd_workspace_bytes(d)
+        assert max(have) == query if even else max(have) <= query
+        for x8 in (False, True):
+            def at(p, dx=FAKE, dw=FAKE, db=FAKE):
+                return tv.tv_linear_bwd_workspace_bytes_at(p[0], p[1], FAKE if x8 else None, p[2], dx, dw, db, d)
+            have = [at(p) for p in places]
+            query = tv.tv_linear_bwd_workspace_bytes(d, x8)
+            assert max(have) == query if even else max(have) <= query
+            for p in places:
+                for wanted in itertools.product((FAKE, None), repeat=3):
+                    assert at(p, *wanted) <= at(p)
+                assert at(p, None, None, None) == 0
+
+
+def test_no_workspace_for_copies_that_are_not_made():
+    """8192 x 2048 -> 8192 in bf16 on 16-byte boundaries: nothing forward, dz and the column sums' groups backward."""
+    m, k, n = 8192, 2048, 8192
+    d = tv.tv_linear_desc(m, k, n, k, k, n, n, tv.TV_BF16, tv.TV_ACT_GELU)
+    assert tv.tv_linear_fwd_workspace_bytes_at(FAKE, FAKE, d) == 0
+    full = tv.tv_linear_bwd_workspace_bytes_at(FAKE, FAKE, None, FAKE, FAKE, FAKE, FAKE, d)
+    assert 2 * m * n < full < 2.1 * m * n
+    assert tv.tv_linear_bwd_workspace_bytes_at(FAKE, FAKE, None, FAKE, None, None, FAKE, d) < 1 << 22     # db alone
+    bad = tv.tv_linear_desc(m, k, n, k - 1, k, n, n, tv.TV_BF16, tv.TV_ACT_GELU)
+    assert tv.tv_linear_fwd_workspace_bytes_at(FAKE, FAKE, bad) == 0
+    assert tv.tv_linear_bwd_workspace_bytes_at(FAKE, FAKE, None, FAKE, FAKE, FAKE, FAKE, bad) == 0
+
+
+def test_a_call_takes_the_workspace_of_its_pointers():
+    """A byte less is refused, before any launch."""
+    nothing = tv.tv_held(None, None, tv.TV_HELD_NONE)
+    d = tv.tv_linear_desc(64, 8192, 256, 8192, 8192, 256, 256, tv.TV_BF16, tv.TV_ACT_NONE)
+    need = tv.tv_linear_fwd_workspace_bytes_at(FAKE, FAKE, d)
+    assert need > 0
+    assert tv.lib().tv_linear_fwd(FAKE, FAKE, None, None, FAKE, nothing, d, FAKE, need - 1, None) == 5
+    d.act = tv.TV_ACT_GELU                                                  # dz has a place of its own
+    held = tv.tv_held(FAKE, None, tv.TV_HELD_PLAIN)
+    for dx, dw, db in ((FAKE, None, None), (None, FAKE, None), (None, None, FAKE)):
+        need = tv.tv_linear_bwd_workspace_bytes_at(FAKE, FAKE + 2, None, FAKE, dx, dw, db, d)
+        assert need > 0
+        assert tv.lib().tv_linear_bwd(FAKE, FAKE + 2, None, held, FAKE, dx, dw, db, d, FAKE, need - 1, None) == 5
