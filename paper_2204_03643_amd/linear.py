@@ -219,7 +219,9 @@ class _Linear(torch.autograd.Function):
     def forward(ctx, x, weight, bias, residual, act, checkpoint):
         rows, ldx = _as_rows(x)
         wrows, ldw = _as_rows(weight)
-        y, data, exps = _forward(rows, ldx, wrows, ldw, bias, residual, act, checkpoint)
+        # (z is for the slopes, which the residual's gradient does without)
+        hold = checkpoint if any(ctx.needs_input_grad[:3]) else None
+        y, data, exps = _forward(rows, ldx, wrows, ldw, bias, residual, act, hold)
         x_exps = None
         if not ctx.needs_input_grad[1]:
             rows = None                            # only dW reads x

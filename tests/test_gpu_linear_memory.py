@@ -42,3 +42,17 @@ def test_some_of_the_gradients(wanted, act, dtype):
         got = torch.autograd.grad(tv_linear(*some, act=act), [some[i] for i in wanted], g)
         for i, v in zip(wanted, got):
             assert torch.equal(v, everything[i]), (M, K, N, i)
+
+
+@pytest.mark.parametrize("checkpoint", ("full", "8bit"))
+@pytest.mark.parametrize("act", ("none", "relu", "gelu", "silu"))
+def test_nothing_of_z_is_held_for_a_residual_alone(act, checkpoint):
+    from paper_2204_03643_amd.linear import tv_linear
+    x, w, b, r, g = (torch.randn(*s, device="cuda") for s in ((70, 64), (48, 64), (48,), (70, 48), (70, 48)))
+    y = tv_linear(x, w, b, r.requires_grad_(), act=act, checkpoint=checkpoint)
+    held = [t for t in y.grad_fn.saved_tensors if t is not None and t.data_ptr() != w.data_ptr()]
+    assert held == []
+    assert torch.equal(torch.autograd.grad(y, r, g)[0], g)
+    # a bias alone needs z
+    y = tv_linear(x, w, b.requires_grad_(), act=act, checkpoint=checkpoint)
+    assert sum(t is not None for t in y.grad_fn.saved_tensors[1:4]) == {"none": 0, "relu": 1}.get(act, 2 if checkpoint == "8bit" else 1)
