@@ -287,10 +287,12 @@ def tv_linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None =
     return _forward(x, ldx, weight, ldw, bias, residual, act, None)[0]
 
 
-def tv_linear_backward(g: torch.Tensor, x, z, weight: torch.Tensor, act: str = "none", bias_grad: bool = False):
+def tv_linear_backward(g: torch.Tensor, x, z, weight: torch.Tensor, act: str = "none", bias_grad: bool = False,
+                       input_grad: bool = True, weight_grad: bool = True):
     """(dx, dw, db) of ``tv_linear`` from what a program holds itself: x the input or its Checkpoint8; z the
     pre-activation or its Checkpoint8 (gelu, silu), the int32 words of its signs (relu: bit j % 32 of word j / 32 of a
-    row set where not z <= 0) or None (none).  db is None unless bias_grad."""
+    row set where not z <= 0) or None (none).  db is None unless bias_grad; input_grad and weight_grad say whether dx and dW
+    are wanted (None otherwise)."""
     _check_tensor(g, "tv_linear_backward")
     _check_tensor(weight, "tv_linear_backward (weight)", g)
     n = weight.shape[0] if weight.dim() == 2 else -1
@@ -325,7 +327,10 @@ def tv_linear_backward(g: torch.Tensor, x, z, weight: torch.Tensor, act: str = "
             raise ValueError("tv_linear_backward: z of g's shape, or its Checkpoint8, expected")
         data = _check_tensor(z, "tv_linear_backward (z)", g).contiguous()
     wrows, ldw = _as_rows(weight)
-    return _backward(g, x, x_exps, ldx, data, exps, wrows, ldw, act, (True, True, bias_grad))
+    want = (bool(input_grad), bool(weight_grad), bool(bias_grad))
+    if not any(want):
+        return None, None, None
+    return _backward(g, x, x_exps, ldx, data, exps, wrows, ldw, act, want)
 
 
 class TVLinear(torch.nn.Module):
