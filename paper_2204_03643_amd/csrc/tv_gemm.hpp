@@ -96,8 +96,9 @@ __device__ __forceinline__ void store_wave(float *piece, const Product &g, const
 #pragma unroll
             for (int i = 0; i < R / 8; ++i)
                 if (o.x + i * 8 + row < g.M && o.y + col < g.N) {
-                    *(f32x4 *)(to + i * 8 * pitch) = *(const f32x4 *)(from + i * 8 * kOutPitch);
-                    *(f32x4 *)(to + i * 8 * pitch + 4) = *(const f32x4 *)(from + i * 8 * kOutPitch + 4);
+                    // (a tile that was moved to end with the last column may start at any)
+                    put16(to + i * 8 * pitch, *(const u32x4 *)(from + i * 8 * kOutPitch));
+                    put16(to + i * 8 * pitch + 4, *(const u32x4 *)(from + i * 8 * kOutPitch + 4));
                 }
             wave_sync();
         }

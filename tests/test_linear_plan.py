@@ -127,3 +127,15 @@ def test_a_call_takes_the_workspace_of_its_pointers():
         need = tv.tv_linear_bwd_workspace_bytes_at(FAKE, FAKE + 2, None, FAKE, dx, dw, db, d)
         assert need > 0
         assert tv.lib().tv_linear_bwd(FAKE, FAKE + 2, None, held, FAKE, dx, dw, db, d, FAKE, need - 1, None) == 5
+
+
+def test_split_sums_of_a_moved_tile_promise_no_alignment(plans):
+    """f32 dx of 1001 columns: the last tile starts at column 873 (1001 - 128), and its sums go to the workspace from there on;
+    the store must not promise 16 bytes (the hardware takes it, the compiler need not)."""
+    (p,) = plans([call(1024, 1001, 1024, dtype=tv.TV_F32)])
+    q = p["dx"]
+    assert q["splits"] > 1 and (1001 - TILES[q["kind"]][1]) % 4 != 0
+    source = open(os.path.join(HERE, "..", "paper_2204_03643_amd", "csrc", "tv_gemm.hpp")).read()
+    body = source[source.index("if (g.splits > 1) {"):source.index("if (!whole) {")]
+    stores = [line.strip() for line in body.splitlines() if line.strip().startswith(("*(", "put16("))]
+    assert stores and all(s.startswith("put16(") for s in stores), stores
