@@ -37,11 +37,12 @@ def _check_tensor(t: torch.Tensor, what: str, like: torch.Tensor | None = None) 
 
 def _as_rows(t: torch.Tensor):
     """(tensor, row stride) of t as rows of its last axis: a matrix whose rows are dense stays where it is, anything
-    else is made contiguous (and with it a view that stands for its memory's negative, as the imaginary part of a conjugate)."""
+    else is made contiguous (and with it a view that stands for its memory's negative, as the imaginary part of a conjugate,
+    and rows further apart than the library takes)."""
     n = t.shape[-1]
     if t.is_contiguous():
         return t, n
-    if t.dim() == 2 and (t.stride(1) == 1 or n == 1) and (t.stride(0) >= n or t.shape[0] == 1) and not t.is_neg():
+    if t.dim() == 2 and (t.stride(1) == 1 or n == 1) and (n <= t.stride(0) < 1 << 31 or t.shape[0] == 1) and not t.is_neg():
         return t, (t.stride(0) if t.shape[0] > 1 else n)
     return t.contiguous(), n
 
