@@ -328,8 +328,10 @@ int tv2d_prox_bwd_bf16(const uint16_t *g_up, uint16_t *grad_y, float *grad_lam, 
  * (TV_ERR_SHAPE beyond: 1.7e10 outputs).
  *
  * m = 0: the forward call does nothing, the backward call sets dw and db to zero.  Results do not depend on the
- * stream, on timing or on what the workspace holds; how the contraction is split (and so the last bits of the
- * fp32 sums) depends on the sizes alone.
+ * stream, on timing or on what the workspace holds.  Which kernel runs and how the contraction is split, and so the
+ * last bits of the fp32 sums, depends on the sizes, the dtype, the row strides and whether the operands start on
+ * 16-byte boundaries, in the backward call also on whether there is an activation and whether x is codes: the same
+ * rows as a view and as a copy may differ in them.
  */
 #define TV_LINEAR_MAX_TILES 1048576
 typedef enum { TV_F32 = 0, TV_BF16 = 1 } tv_dtype;

@@ -63,7 +63,7 @@ inline Choice cut(Kind kind, int64_t s, int64_t K, int64_t unit)
 // 14.1 and 12.8) and 12 in bf16 (1001 -> 777, 32 rows, 12: 9.0 and 10.8 us; 2047 -> 513, 16 rows, 16: 15.1 and 11.3).
 //
 // Otherwise the cheapest by a model of the time in microseconds, fitted to sweeps of tiles and splits over outputs of
-// 128 x 512 to 8192 x 8192 and contractions of 256 to 16384 (what it takes there is 0.1 to 0.7 % slower than the best of the sweep, 11 %
+// 128 x 512 to 8192 x 8192 and contractions of 256 to 16384 (what it takes there is 0.1 to 0.8 % slower than the best of the sweep, 11 %
 // at most): a launch; rounds of workgroups over 256 compute units, in each a start and an end and so much a step of 64,
 // more where two workgroups share a unit or, at lower clocks, where more than half of the units are busy; for split
 // contractions the second launch and the sums' trip through memory.
