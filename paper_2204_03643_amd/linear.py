@@ -228,9 +228,10 @@ class _Linear(torch.autograd.Function):
             rows = None                            # only dW reads x
         elif checkpoint == "8bit":
             rows, x_exps = _save8(rows, ldx)
-            ldx = rows.shape[-1]
-        ctx.save_for_backward(rows, x_exps, data, exps, wrows)
-        ctx.strides, ctx.act, ctx.has_bias = (ldx, ldw), act, bias is not None
+        saved = (rows, x_exps, data, exps, wrows)
+        ctx.save_for_backward(*saved)
+        ctx.saved_as = [None if t is None else (t.shape, t.dtype) for t in saved]
+        ctx.act, ctx.has_bias = act, bias is not None
         return y
 
     @staticmethod
@@ -238,12 +239,22 @@ class _Linear(torch.autograd.Function):
     def backward(ctx, g):
         if _tangent_among(g):
             raise NotImplementedError("tv_linear: the gradients have no forward-mode derivative")
-        x, x_exps, data, exps, weight = ctx.saved_tensors
+        # (hooks on saved tensors may bring back others, with the same values in strides of their own)
+        saved = ctx.saved_tensors
+        for t, was in zip(saved, ctx.saved_as):
+            if (None if t is None else (t.shape, t.dtype)) != was or (t is not None and t.device != g.device):
+                raise RuntimeError("tv_linear: a hook on saved tensors has brought back one of another shape, type or device")
+        x, x_exps, data, exps, weight = saved
         need = ctx.needs_input_grad
         want = (need[0], need[1], ctx.has_bias and need[2])
         dx = dw = db = None
         if any(want):
-            dx, dw, db = _backward(g, x, x_exps, ctx.strides[0], data, exps, weight, ctx.strides[1], ctx.act, want)
+            if x_exps is not None:
+                x, x_exps = x.contiguous(), x_exps.contiguous()
+            x, ldx = (None, weight.shape[1]) if x is None else _as_rows(x)
+            weight, ldw = _as_rows(weight)
+            data, exps = (t if t is None else t.contiguous() for t in (data, exps))
+            dx, dw, db = _backward(g, x, x_exps, ldx, data, exps, weight, ldw, ctx.act, want)
         return dx, dw, db, (g if need[3] else None), None, None
 
 
