@@ -58,3 +58,19 @@ def test_long_inputs(held):
         assert torch.equal(dx[:, k:k + CHUNK].float(), g.float() @ b), k
         assert torch.equal(dw[:, k:k + CHUNK].float(), g.float().t().contiguous() @ a), k
     assert torch.equal(y, want.to(BF))
+
+
+def test_long_outputs():
+    """64 rows of 36 million outputs: y with bias, ReLU and residual, and the signs that are held."""
+    lin, M, K, N = linear(), 64, 64, LONG
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x, w, r = signs(M, K, gen), signs(N, K, gen), signs(M, N, gen)
+    b = signs(1, N, gen)[0]
+    y, words, _ = lin._forward(x, K, w, K, b, r, "relu", "full")
+    shifts = torch.arange(32, device="cuda", dtype=torch.int32)
+    for n in range(0, N, CHUNK):
+        e = min(N, n + CHUNK)
+        z = x.float() @ w[n:e].float().t().contiguous() + b[n:e].float()
+        assert torch.equal(y[:, n:e].float(), z.clamp(min=0) + r[:, n:e].float()), n
+        on = ((words[:, n // 32:-(-e // 32)].unsqueeze(-1) >> shifts) & 1).view(M, -1)[:, :e - n]
+        assert torch.equal(on.bool(), z > 0), n
