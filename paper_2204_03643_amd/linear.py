@@ -240,9 +240,9 @@ class _Linear(torch.autograd.Function):
         if _tangent_among(g):
             raise NotImplementedError("tv_linear: the gradients have no forward-mode derivative")
         # (hooks on saved tensors may bring back others, with the same values in strides of their own)
-        saved = ctx.saved_tensors
+        saved, where = ctx.saved_tensors, g.get_device()
         for t, was in zip(saved, ctx.saved_as):
-            if (None if t is None else (t.shape, t.dtype)) != was or (t is not None and t.device != g.device):
+            if t is not None and (t.dtype is not was[1] or t.shape != was[0] or t.get_device() != where or t.is_meta):
                 raise RuntimeError("tv_linear: a hook on saved tensors has brought back one of another shape, type or device")
         x, x_exps, data, exps, weight = saved
         need = ctx.needs_input_grad
@@ -251,9 +251,12 @@ class _Linear(torch.autograd.Function):
         if any(want):
             if x_exps is not None:
                 x, x_exps = x.contiguous(), x_exps.contiguous()
-            x, ldx = (None, weight.shape[1]) if x is None else _as_rows(x)
+            if data is not None:
+                data = data.contiguous()
+            if exps is not None:
+                exps = exps.contiguous()
             weight, ldw = _as_rows(weight)
-            data, exps = (t if t is None else t.contiguous() for t in (data, exps))
+            x, ldx = (None, ldw) if x is None else _as_rows(x)
             dx, dw, db = _backward(g, x, x_exps, ldx, data, exps, weight, ldw, ctx.act, want)
         return dx, dw, db, (g if need[3] else None), None, None
 

@@ -49,7 +49,7 @@ def test_strides_are_those_of_the_tensors_that_come_back(seen, hook):
     assert torch.equal(seen["z"], y.detach())
 
 
-@pytest.mark.parametrize("change", (lambda t: t.double(), lambda t: t[:-1], lambda t: t.to("meta")))
+@pytest.mark.parametrize("change", (lambda t: t.double(), lambda t: t[:-1], lambda t: t.flatten(), lambda t: t.to("meta")))
 def test_other_tensors_are_refused(seen, change):
     x, w = torch.randn(6, 8, requires_grad=True), torch.randn(5, 8, requires_grad=True)
     with torch.autograd.graph.saved_tensors_hooks(lambda t: t, change):
