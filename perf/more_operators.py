@@ -15,7 +15,8 @@ is below q.
 4 bits: blocks of 32 along a row (the last one may be shorter) share a scale 2^(floor(log2 max) - 2), max the block's largest
 magnitude (2^-120 at least); a value over its scale is rounded to the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 and their
 negatives, halfway cases to the even code, and to 6 beyond.  Two codes lie in a byte, the first in its lower half: sign bit,
-two exponent bits, one of the fraction.  A row's codes and scale bytes (exponent + 127) are padded to whole 128 values.
+two exponent bits, one of the fraction.  A row's codes are padded to whole groups of 128 values; the four scale bytes
+(exponent + 127) of a group lie side by side, those of one group of all rows (padded to a multiple of four) one after another.
 
   kind  "norm"     forward only                       "norm_train"   forward and gradients
         "block"    y (and h where there is a next norm)  "block_train"  forward and gradients
@@ -206,7 +207,7 @@ def _quantized(v):
 
 
 def _packed(v):
-    """Codes [rows, 64 a 128 values] and scale bytes [rows, 4 a 128 values] of f32 v, both uint8."""
+    """Codes [rows, 64 a group] and scale bytes [groups, rows padded to a multiple of four, 4] of f32 v, both uint8."""
     rows, n = v.shape
     q, e = _quantized(v)
     a = q.abs()
@@ -214,9 +215,9 @@ def _packed(v):
     groups = -(-n // 128)
     codes = torch.zeros(rows, groups * 128, dtype=torch.uint8, device=v.device)
     codes[:, :code.shape[1] * 32] = code.view(rows, -1)
-    exps = torch.full((rows, groups * 4), 127, dtype=torch.uint8, device=v.device)
-    exps[:, :e.shape[1]] = (e + 127).to(torch.uint8)
-    return codes[:, ::2] + 16 * codes[:, 1::2], exps
+    exps = torch.full((-(-rows // 4) * 4, groups * 4), 127, dtype=torch.uint8, device=v.device)
+    exps[:rows, :e.shape[1]] = (e + 127).to(torch.uint8)
+    return codes[:, ::2] + 16 * codes[:, 1::2], exps.view(-1, groups, 4).transpose(0, 1).contiguous()
 
 
 def _unpacked(codes, exps, n):
@@ -224,7 +225,8 @@ def _unpacked(codes, exps, n):
     c = torch.stack((codes & 15, codes >> 4), -1).view(codes.shape[0], -1).to(torch.int32)
     m, top = (c & 1).float(), (c >> 1) & 3
     a = torch.where(top == 0, 0.5 * m, (1.0 + 0.5 * m) * _power_of_two(top - 1))
-    v = torch.where(c >= 8, -a, a) * _power_of_two(exps.to(torch.int32) - 127).repeat_interleave(32, 1)
+    e = exps.transpose(0, 1).reshape(exps.shape[1], -1)[:codes.shape[0]].to(torch.int32)
+    v = torch.where(c >= 8, -a, a) * _power_of_two(e - 127).repeat_interleave(32, 1)
     return v[:, :n]
 
 
@@ -482,8 +484,12 @@ def exact(case, seed):
         stands = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6, -0.0, -0.5, -1, -1.5, -2, -3, -4, -6], dtype=torch.float64, device="cuda")
         w[:, 0::2] = stands[torch.remainder(s["w4"].long(), 16)]
         w[:, 1::2] = stands[torch.div(s["w4"].long(), 16, rounding_mode="floor")]
-        w = w.view(case["N"], -1, 32) * ((s["we"].long() - 127 + 1023) << 52).view(torch.float64).unsqueeze(-1)
-        w = w.view(case["N"], -1)[:, :case["K"]]
+        scales = ((s["we"].long() - 127 + 1023) << 52).view(torch.float64)
+        for group in range(scales.shape[0]):
+            for i in range(4):
+                first = group * 128 + i * 32
+                w[:, first:first + 32] *= scales[group, :case["N"], i].unsqueeze(1)
+        w = w[:, :case["K"]]
         y = torch.matmul(in_four_bits(wide("x")), w.transpose(0, 1).contiguous())
         if s["b"] is not None:
             y += wide("b")
