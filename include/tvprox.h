@@ -394,6 +394,103 @@ int tv_ckpt8_save(const void *x, int8_t *codes, uint8_t *exps, int64_t rows, int
 int tv_ckpt8_load(const int8_t *codes, const uint8_t *exps, void *x, int64_t rows, int64_t n, int64_t ldx, int dtype,
                   hipStream_t stream);
 
+/*
+ * Dropout by numbers that are computed where they are used: nothing of the mask is stored, the backward call makes the
+ * same numbers again.  Philox 4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011)
+ * with the 64-bit key `seed` (plus *seed_at, device memory of 8 bytes, where that is given: a captured graph gets other
+ * numbers in every replay that way) and the counter (j / 8, i, low half of offset, high half of offset) gives the eight
+ * 16-bit numbers of columns 8 (j / 8) .. of row i, the lower half of each word first.  Column j is dropped (0, whatever it
+ * held) where its number is below `drop`, multiplied by 65536 / (65536 - drop) otherwise: drop = 65536 p, 0 .. 65536
+ * (TV_ERR_UNSUPPORTED beyond).  The same (seed, offset) always means the same mask.
+ */
+typedef struct {
+    uint64_t seed, offset;
+    const int64_t *seed_at;        /* device memory, or NULL */
+    uint32_t drop;
+} tv_drop;
+
+/* y = dropout of x (rows of ldx elements), y packed [rows, n]; y may be x exactly.  Applied to a gradient it is its own
+ * backward call.  rows, n < 2^31 - 1024. */
+int tv_drop_apply(const void *x, void *y, int64_t rows, int64_t n, int64_t ldx, int dtype, tv_drop drop, hipStream_t stream);
+
+/*
+ * The border between two residual blocks, over rows of n channels:
+ *
+ *   norm(v) = (v - mu) r w + b,  r = (mean((v - mu)^2) + eps)^(-1/2),  mu = mean(v) (TV_NORM_LAYER) or 0 (TV_NORM_RMS)
+ *   y = x + d scale act(gate) norm(f),   h = next_norm(y)             d: dropout's 0 or 65536 / (65536 - drop)
+ *
+ * f NULL: no residual (y = x is not written), h = next_norm(x).  y NULL: y is not wanted, only where f is NULL or h is
+ * given.  h NULL: no next norm (next_norm is TV_NORM_NONE).  weight, bias, gate, scale, next_weight, next_bias may be
+ * NULL: ones, zeros.  x, f, gate are dense rows ldx, ldf, ldg elements apart (below 2^31), y, h and the vectors of n are
+ * packed.  Row i reads the gate's row i / gate_div (m a multiple of gate_div: 1 a gate for each row, m one for
+ * all).  One dtype for all; everything between is fp32, y and h are rounded once each (h is of y before its rounding).
+ * Values whose squares, summed over a row, overflow fp32 are outside what a norm takes.  n is at most TV_MAX_LENGTH
+ * (TV_ERR_UNSUPPORTED).  A row that holds a value that is not finite makes no other row's outputs other than they were.
+ *
+ * stats [m, 4] floats (16-byte aligned), NULL without a backward call: (mu, r) of f and of y.
+ */
+typedef enum { TV_NORM_NONE = 0, TV_NORM_RMS = 1, TV_NORM_LAYER = 2 } tv_norm_kind;
+typedef enum { TV_GATE_PLAIN = 0, TV_GATE_SIGMOID = 1, TV_GATE_SILU = 2 } tv_gate_act;
+
+typedef struct {
+    int64_t m, n;
+    int64_t ldx, ldf, ldg, gate_div;        /* ldf, ldg, gate_div: read where f, gate are given */
+    int32_t dtype, norm, next_norm, gate_act;
+    float eps;
+    tv_drop drop;
+} tv_block_desc;
+
+typedef struct {
+    const void *x, *f, *weight, *bias, *gate, *scale, *next_weight, *next_bias;
+} tv_block_in;
+
+int tv_block_fwd(tv_block_in in, void *y, void *h, float *stats, tv_block_desc desc, hipStream_t stream);
+
+/*
+ * The gradients, from dy and dh (packed; either may be NULL: zero), the forward call's `stats` and, as in.x, its y (rows
+ * of ldx elements; x where f is NULL; may be NULL without next_norm), all else as in the forward call:
+ *
+ *   g = dy + next_norm'(dh),  dx = g,  t = d g,  dP = t scale act(gate),  df = norm'(dP)
+ *   dscale = sum_i t act(gate) norm(f),  dgate = t scale act'(gate) norm(f), summed over the rows that share it
+ *   dweight, dbias = sum_i dP (f - mu) r, sum_i dP;  dnext_weight, dnext_bias = sum_i dh (y - mu) r, sum_i dh
+ *
+ * Each output is packed and may be NULL where it is not wanted.  Sums over rows are fp32, in an order that depends on
+ * the sizes alone: results do not change from run to run.  m = 0 sets the vectors to zero.  ws: as in tv_linear_bwd.
+ */
+typedef struct {
+    void *dx, *df, *dgate, *dweight, *dbias, *dscale, *dnext_weight, *dnext_bias;
+} tv_block_grads;
+
+size_t tv_block_bwd_workspace_bytes(tv_block_in in, tv_block_grads grads, tv_block_desc desc);
+int tv_block_bwd(const void *dy, const void *dh, tv_block_in in, const float *stats, tv_block_grads grads,
+                 tv_block_desc desc, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Values in 4 bits: blocks of 32 consecutive values of a row (the last may be shorter) share a scale
+ * s = 2^(floor(log2 M) - 2), M the largest magnitude (2^-120 at least), kept as the byte log2(s) + 127; a value over s is
+ * rounded to the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives, halfway cases to the even code, and to 6
+ * beyond: off by at most s (where it is clamped, 2 s).  A block that holds a value that is not finite has the byte 255
+ * and stands for NaNs.  (The element and scale formats e2m1 and e8m0 of the OCP microscaling formats.)
+ *
+ * A group is 128 values; G = ceil(n / 128).  codes [rows, 64 G] bytes: value 2 i of a row in the lower half of byte i,
+ * zeros from n on.  exps [G, up(rows, 4), 4]: the four scale bytes of a group (127 beyond n), rows side by side; what stands for rows beyond
+ * the last is not looked at.  codes 16-byte, exps 16-byte aligned (TV_ERR_STRIDE).
+ */
+#define TV_MX4_GROUP 128
+int tv_mx4_save(const void *x, uint8_t *codes, uint8_t *exps, int64_t rows, int64_t n, int64_t ldx, int dtype,
+                hipStream_t stream);
+int tv_mx4_load(const uint8_t *codes, const uint8_t *exps, void *x, int64_t rows, int64_t n, int64_t ldx, int dtype,
+                hipStream_t stream);
+
+/*
+ * y = act(x4 W4^T + b) + r on values in 4 bits, for serving: x4 is what the codes of x stand for, or (x_exps NULL) of x's
+ * rows as tv_mx4_save would make them, W4 [n, k] in its codes.  bias, residual and y of desc.dtype as in tv_linear_fwd;
+ * ldw is not read, ldx only where x is rows.  Products are exact, sums fp32.  Sizes as in tv_linear_fwd; m = 0 does nothing.
+ */
+size_t tv_linear4_workspace_bytes(tv_linear_desc desc, int x_is_codes);
+int tv_linear4_fwd(const void *x, const uint8_t *x_exps, const uint8_t *w, const uint8_t *w_exps, const void *bias,
+                   const void *res, void *y, tv_linear_desc desc, void *ws, size_t ws_bytes, hipStream_t stream);
+
 const char *tv_status_str(int status);
 
 /*

@@ -32,10 +32,32 @@ class tv_held(ctypes.Structure):
     _fields_ = [("data", _vp), ("exps", _vp), ("kind", ctypes.c_int32)]
 
 
+class tv_drop(ctypes.Structure):
+    _fields_ = [("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("seed_at", _vp), ("drop", ctypes.c_uint32)]
+
+
+class tv_block_desc(ctypes.Structure):
+    _fields_ = [("m", _i64), ("n", _i64), ("ldx", _i64), ("ldf", _i64), ("ldg", _i64), ("gate_div", _i64),
+                ("dtype", ctypes.c_int32), ("norm", ctypes.c_int32), ("next_norm", ctypes.c_int32),
+                ("gate_act", ctypes.c_int32), ("eps", ctypes.c_float), ("drop", tv_drop)]
+
+
+class tv_block_in(ctypes.Structure):
+    _fields_ = [(k, _vp) for k in ("x", "f", "weight", "bias", "gate", "scale", "next_weight", "next_bias")]
+
+
+class tv_block_grads(ctypes.Structure):
+    _fields_ = [(k, _vp) for k in ("dx", "df", "dgate", "dweight", "dbias", "dscale", "dnext_weight", "dnext_bias")]
+
+
 TV_F32, TV_BF16 = 0, 1
 TV_ACT_NONE, TV_ACT_RELU, TV_ACT_GELU, TV_ACT_SILU = 0, 1, 2, 3
 TV_HELD_NONE, TV_HELD_PLAIN, TV_HELD_BITS, TV_HELD_8BIT = 0, 1, 2, 3
 TV_CKPT8_BLOCK = 32
+TV_NORM_NONE, TV_NORM_RMS, TV_NORM_LAYER = 0, 1, 2
+TV_GATE_PLAIN, TV_GATE_SIGMOID, TV_GATE_SILU = 0, 1, 2
+TV_MAX_LENGTH = 16384
+TV_MX4_GROUP = 128
 
 TV_FWD_ORDER_READY = 1
 TV_FWD_PARALLEL_SEARCH = 2
@@ -140,6 +162,22 @@ def lib() -> ctypes.CDLL:
         L.tv_ckpt8_save.restype = ctypes.c_int
         L.tv_ckpt8_load.argtypes = [_vp, _vp, _vp, _i64, _i64, _i64, ctypes.c_int, _vp]
         L.tv_ckpt8_load.restype = ctypes.c_int
+        L.tv_drop_apply.argtypes = [_vp, _vp, _i64, _i64, _i64, ctypes.c_int, tv_drop, _vp]
+        L.tv_drop_apply.restype = ctypes.c_int
+        L.tv_block_fwd.argtypes = [tv_block_in, _vp, _vp, _vp, tv_block_desc, _vp]
+        L.tv_block_fwd.restype = ctypes.c_int
+        L.tv_block_bwd_workspace_bytes.argtypes = [tv_block_in, tv_block_grads, tv_block_desc]
+        L.tv_block_bwd_workspace_bytes.restype = ctypes.c_size_t
+        L.tv_block_bwd.argtypes = [_vp, _vp, tv_block_in, _vp, tv_block_grads, tv_block_desc, _vp, ctypes.c_size_t, _vp]
+        L.tv_block_bwd.restype = ctypes.c_int
+        L.tv_mx4_save.argtypes = [_vp, _vp, _vp, _i64, _i64, _i64, ctypes.c_int, _vp]
+        L.tv_mx4_save.restype = ctypes.c_int
+        L.tv_mx4_load.argtypes = [_vp, _vp, _vp, _i64, _i64, _i64, ctypes.c_int, _vp]
+        L.tv_mx4_load.restype = ctypes.c_int
+        L.tv_linear4_workspace_bytes.argtypes = [tv_linear_desc, ctypes.c_int]
+        L.tv_linear4_workspace_bytes.restype = ctypes.c_size_t
+        L.tv_linear4_fwd.argtypes = [_vp] * 7 + [tv_linear_desc, _vp, ctypes.c_size_t, _vp]
+        L.tv_linear4_fwd.restype = ctypes.c_int
         _current_stream = _stream_lookup(torch)
         _lib = L
     return _lib
@@ -327,3 +365,36 @@ def tv_ckpt8_save(x, codes, exps, rows: int, n: int, ldx: int, dtype: int, strea
 
 def tv_ckpt8_load(codes, exps, x, rows: int, n: int, ldx: int, dtype: int, stream=None):
     _check(lib().tv_ckpt8_load(_ptr(codes), _ptr(exps), _ptr(x), int(rows), int(n), int(ldx), int(dtype), _stream(stream)))
+
+
+def tv_drop_apply(x, y, rows: int, n: int, ldx: int, dtype: int, drop: tv_drop, stream=None):
+    _check(lib().tv_drop_apply(_ptr(x), _ptr(y), int(rows), int(n), int(ldx), int(dtype), drop, _stream(stream)))
+
+
+def tv_block_fwd(ins: tv_block_in, y, h, stats, desc: tv_block_desc, stream=None):
+    _check(lib().tv_block_fwd(ins, _ptr(y), _ptr(h), _ptr(stats), desc, _stream(stream)))
+
+
+def tv_block_bwd_workspace_bytes(ins: tv_block_in, grads: tv_block_grads, desc: tv_block_desc) -> int:
+    return int(lib().tv_block_bwd_workspace_bytes(ins, grads, desc))
+
+
+def tv_block_bwd(dy, dh, ins: tv_block_in, stats, grads: tv_block_grads, desc: tv_block_desc, ws=None, ws_bytes: int = 0, stream=None):
+    _check(lib().tv_block_bwd(_ptr(dy), _ptr(dh), ins, _ptr(stats), grads, desc, _ptr(ws), int(ws_bytes), _stream(stream)))
+
+
+def tv_mx4_save(x, codes, exps, rows: int, n: int, ldx: int, dtype: int, stream=None):
+    _check(lib().tv_mx4_save(_ptr(x), _ptr(codes), _ptr(exps), int(rows), int(n), int(ldx), int(dtype), _stream(stream)))
+
+
+def tv_mx4_load(codes, exps, x, rows: int, n: int, ldx: int, dtype: int, stream=None):
+    _check(lib().tv_mx4_load(_ptr(codes), _ptr(exps), _ptr(x), int(rows), int(n), int(ldx), int(dtype), _stream(stream)))
+
+
+def tv_linear4_workspace_bytes(desc: tv_linear_desc, x_is_codes: bool) -> int:
+    return int(lib().tv_linear4_workspace_bytes(desc, int(bool(x_is_codes))))
+
+
+def tv_linear4_fwd(x, x_exps, w, w_exps, bias, res, y, desc: tv_linear_desc, ws=None, ws_bytes: int = 0, stream=None):
+    _check(lib().tv_linear4_fwd(_ptr(x), _ptr(x_exps), _ptr(w), _ptr(w_exps), _ptr(bias), _ptr(res), _ptr(y), desc, _ptr(ws),
+                                int(ws_bytes), _stream(stream)))

@@ -1,0 +1,481 @@
+// The border between two residual blocks: y = x + d scale act(gate) norm(f), h = next_norm(y), and its gradients.
+//
+// Reads and writes are all there is to it: a row is read once, its statistics are taken of what the lanes hold, and what
+// follows from them is written.  Lanes side by side in a row hold eight neighbouring channels each.
+#pragma once
+#include "tv_block_plan.hpp"
+#include "tv_drop.hpp"
+
+namespace tvl {
+
+enum Norm : int { kNormNone = 0, kNormRms = 1, kNormLayer = 2 };
+enum Gate : int { kGatePlain = 0, kGateSigmoid = 1, kGateSilu = 2 };
+
+struct Block {
+    const void *x, *f, *w, *b, *gate, *scale, *nw, *nb;
+    int64_t m, ldx, ldf, ldg;
+    int32_t n, gate_div, norm, next, act;
+    float   eps, inv_n;
+    Drop    drop;
+};
+
+// Sums over the LANES lanes of a row.  More than a wave: through LDS, in two places in turn, so that one barrier a sum is
+// enough (between the read of a place and its next write lies the barrier of the sum in between).
+template <int LANES> struct RowSum {
+    static constexpr int kWaves = LANES > 64 ? LANES / 64 : 1;
+    float2 (*place)[kWaves];
+    int turn = 0;
+    __device__ __forceinline__ explicit RowSum(float2 (*lds)[kWaves]) : place(lds) {}
+    __device__ __forceinline__ float2 operator()(float a, float b)
+    {
+#pragma unroll
+        for (int i = 1; i < (LANES < 64 ? LANES : 64); i <<= 1) {
+            a += __shfl_xor(a, i);
+            b += __shfl_xor(b, i);
+        }
+        if constexpr (LANES > 64) {
+            if ((threadIdx.x & 63) == 0) place[turn][threadIdx.x >> 6] = float2{a, b};
+            __syncthreads();
+            a = b = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) {
+                a += place[turn][i].x;
+                b += place[turn][i].y;
+            }
+            turn ^= 1;
+        }
+        return {a, b};
+    }
+    __device__ __forceinline__ float operator()(float a) { return (*this)(a, 0.0f).x; }
+};
+
+// act(z) and, where it is asked for, its slope.
+template <bool FAST> __device__ __forceinline__ float gate_of(float z, int act)
+{
+    if (act == kGateSigmoid) return logistic<FAST>(z);
+    if (act == kGateSilu) return z * logistic<FAST>(z);
+    return z;
+}
+template <bool FAST> __device__ __forceinline__ float gate_slope(float z, int act)
+{
+    if (act == kGatePlain) return 1.0f;
+    const float s = logistic<FAST>(z);
+    return act == kGateSigmoid ? s * (1.0f - s) : s * (1.0f + z * (1.0f - s));
+}
+
+template <class T> __device__ __forceinline__ void load_or(float (&v)[8], const void *p, int col, int have, float otherwise)
+{
+    if (p) get8(v, (const T *)p + col, have);
+    else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = otherwise;
+}
+
+// (mean, r) of a row that the lanes hold; v becomes (v - mean) r.  The variance is taken of the differences from the mean.
+template <int LANES, int V>
+__device__ __forceinline__ float2 normalise(float (&v)[V][8], const int (&have)[V], bool layer, float eps, float inv_n,
+                                            RowSum<LANES> &sum)
+{
+    float mean = 0.0f;
+    if (layer) {
+        float s = 0.0f;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += v[j][i];        // (zeros beyond the row's end)
+        mean = sum(s) * inv_n;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[j][i] = i < have[j] ? v[j][i] - mean : 0.0f;
+    }
+    float s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s = fmaf(v[j][i], v[j][i], s);
+    const float r = 1.0f / sqrtf(fmaf(sum(s), inv_n, eps));
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[j][i] *= r;
+    return {mean, r};
+}
+
+// LANES lanes a row, V vectors of eight channels a lane.  F: there is an f; N: there is a next norm.
+template <class T, int LANES, int V, bool F, bool N>
+__global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_fwd_kernel(Block a, T *y, T *h, float4 *stats)
+{
+    constexpr bool FAST = sizeof(T) == 2;
+    constexpr int kThreads = LANES > 64 ? LANES : 256, kRows = kThreads / LANES;
+    __shared__ float2 lds[2][RowSum<LANES>::kWaves];
+    RowSum<LANES> sum(lds);
+    const int lane = threadIdx.x % LANES;
+    int col[V], have[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        col[j] = (j * LANES + lane) * 8;
+        have[j] = max(0, min(8, a.n - col[j]));
+    }
+    const bool drops = F && a.drop.below != 0;
+    const DropKey key = drops ? drop_key(a.drop) : DropKey{};
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; row < a.m; row += step) {
+        float v[V][8];
+        float4 st = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < V; ++j) get8(v[j], (const T *)a.x + row * a.ldx + col[j], have[j]);
+        if constexpr (F) {
+            float f[V][8], p[8];
+#pragma unroll
+            for (int j = 0; j < V; ++j) get8(f[j], (const T *)a.f + row * a.ldf + col[j], have[j]);
+            if (a.norm != kNormNone) {
+                const float2 s = normalise<LANES, V>(f, have, a.norm == kNormLayer, a.eps, a.inv_n, sum);
+                st.x = s.x;
+                st.y = s.y;
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    if (a.w) {
+                        get8(p, (const T *)a.w + col[j], have[j]);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) f[j][i] *= p[i];
+                    }
+                    if (a.b) {
+                        get8(p, (const T *)a.b + col[j], have[j]);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) f[j][i] += p[i];
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                if (a.gate) {
+                    get8(p, (const T *)a.gate + (row / a.gate_div) * a.ldg + col[j], have[j]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) f[j][i] *= gate_of<FAST>(p[i], a.act);
+                }
+                if (a.scale) {
+                    get8(p, (const T *)a.scale + col[j], have[j]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) f[j][i] *= p[i];
+                }
+                if (drops) drop8(f[j], drop_numbers(key, (uint32_t)row, (uint32_t)col[j] / 8), a.drop);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[j][i] += f[j][i];
+                if (y) store8(y + row * a.n + col[j], v[j], have[j]);
+            }
+        }
+        if constexpr (N) {
+            const float2 s = normalise<LANES, V>(v, have, a.next == kNormLayer, a.eps, a.inv_n, sum);
+            st.z = s.x;
+            st.w = s.y;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                float p[8];
+                if (a.nw) {
+                    get8(p, (const T *)a.nw + col[j], have[j]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[j][i] *= p[i];
+                }
+                if (a.nb) {
+                    get8(p, (const T *)a.nb + col[j], have[j]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[j][i] += p[i];
+                }
+                store8(h + row * a.n + col[j], v[j], have[j]);
+            }
+        }
+        if (stats && lane == 0) stats[row] = st;
+    }
+}
+
+// ---- gradients
+__device__ __forceinline__ void range_of(const Units &u, int unit, int64_t m, int64_t &begin, int64_t &end)
+{
+    const int64_t first = unit / u.per * u.span;
+    begin = first + (int64_t)(unit % u.per) * u.rows;
+    end = min(min(begin + u.rows, first + u.span), m);
+}
+
+struct BlockGrads {
+    const void *dy, *dh;
+    const float4 *stats;
+    void *dx, *df, *dgate;
+    float2 *row_sums;        // [m] of the next norm, for the kernel that sums over rows by itself
+    float *sums;             // [wanted ones][units][n]: the vectors', then the gate's where its rows are cut
+    uint32_t want;           // a bit each
+    Units units;
+    __device__ __forceinline__ float *place(int k, int unit, int n) const
+    {
+        return sums + ((int64_t)__popc(want & ((1u << k) - 1)) * units.count + unit) * n;
+    }
+};
+
+// One row's gradients.  D: gradient of y on entry of the second half.
+template <class T, bool N>
+__device__ __forceinline__ void next_norm_terms(float (&t)[8], float (&yh)[8], float (&g)[8], const Block &a, const BlockGrads &o,
+                                                float4 st, int64_t row, int col, int have)
+{
+    float p[8];
+    get8(g, (const T *)o.dh + row * a.n + col, have);
+    get8(yh, (const T *)a.x + row * a.ldx + col, have);
+    load_or<T>(p, a.nw, col, have, 1.0f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        yh[i] = (yh[i] - st.z) * st.w;
+        t[i] = g[i] * p[i];
+    }
+}
+
+// From the gradient d of y: dP, the normalised f, and what goes to dscale and dgate, each for eight channels.
+template <class T>
+__device__ __forceinline__ void branch_terms(float (&d)[8], float (&fh)[8], float (&dscale)[8], float (&dgate)[8], const Block &a,
+                                             float4 st, bool drops, DropKey key, int64_t row, int col, int have)
+{
+    constexpr bool FAST = sizeof(T) == 2;
+    float p[8], P[8];
+    if (drops) drop8(d, drop_numbers(key, (uint32_t)row, (uint32_t)col / 8), a.drop);
+    get8(fh, (const T *)a.f + row * a.ldf + col, have);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) P[i] = fh[i];
+    if (a.norm != kNormNone) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) P[i] = fh[i] = i < have ? (fh[i] - st.x) * st.y : 0.0f;
+        if (a.w) {
+            get8(p, (const T *)a.w + col, have);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) P[i] *= p[i];
+        }
+        if (a.b) {
+            get8(p, (const T *)a.b + col, have);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) P[i] += p[i];
+        }
+    }
+    load_or<T>(p, a.scale, col, have, 1.0f);
+    if (a.gate) {
+        float z[8];
+        get8(z, (const T *)a.gate + (row / a.gate_div) * a.ldg + col, have);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float G = gate_of<FAST>(z[i], a.act), q = d[i] * p[i];
+            dscale[i] = d[i] * G * P[i];
+            dgate[i] = q * P[i] * gate_slope<FAST>(z[i], a.act);
+            d[i] = q * G;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            dscale[i] = d[i] * P[i];
+            dgate[i] = 0.0f;
+            d[i] *= p[i];
+        }
+    }
+}
+
+template <class T, int LANES, int V, bool F, bool N, bool SUMS>
+__global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Block a, BlockGrads o)
+{
+    static_assert(V == 1 || !SUMS, "sums over rows of eight channels a lane");
+    __shared__ float2 lds[2][RowSum<LANES>::kWaves];
+    RowSum<LANES> sum(lds);
+    const int lane = threadIdx.x % LANES;
+    int col[V], have[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        col[j] = (j * LANES + lane) * 8;
+        have[j] = max(0, min(8, a.n - col[j]));
+    }
+    const bool drops = F && a.drop.below != 0;
+    const DropKey key = drops ? drop_key(a.drop) : DropKey{};
+    const bool next = N && o.dh;
+    constexpr int kUnits = LANES > 64 ? 1 : 64 / LANES;
+    const int unit = (int)blockIdx.x * kUnits + (LANES > 64 ? 0 : threadIdx.x / LANES);
+    if (unit >= o.units.count) return;               // (whole rows of lanes; whole workgroups where there are barriers)
+    int64_t row, end;
+    range_of(o.units, unit, a.m, row, end);
+    float acc[SUMS ? kVectors + 1 : 1][8];
+    if constexpr (SUMS)
+#pragma unroll
+        for (int k = 0; k <= kVectors; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[k][i] = 0.0f;
+    for (; row < end; ++row) {
+        const float4 st = (N || F) && o.stats ? o.stats[row] : float4{0.0f, 1.0f, 0.0f, 1.0f};
+        float d[V][8];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if (o.dy) get8(d[j], (const T *)o.dy + row * a.n + col[j], have[j]);
+            else
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[j][i] = 0.0f;
+        }
+        if constexpr (N) {
+            if (next) {
+                float t[V][8], yh[V][8], g[8], s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    next_norm_terms<T, N>(t[j], yh[j], g, a, o, st, row, col[j], have[j]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        s1 += t[j][i];
+                        s2 = fmaf(t[j][i], yh[j][i], s2);
+                        if constexpr (SUMS) {
+                            acc[kDnw][i] = fmaf(g[i], yh[j][i], acc[kDnw][i]);
+                            acc[kDnb][i] += g[i];
+                        }
+                    }
+                }
+                float2 c = sum(s1, s2);
+                c.x = a.next == kNormLayer ? c.x * a.inv_n : 0.0f;
+                c.y *= a.inv_n;
+                if (!SUMS && o.row_sums && lane == 0) o.row_sums[row] = c;
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        d[j][i] = i < have[j] ? fmaf(st.w, t[j][i] - c.x - yh[j][i] * c.y, d[j][i]) : 0.0f;
+            }
+        }
+        if (o.dx)
+#pragma unroll
+            for (int j = 0; j < V; ++j) store8((T *)o.dx + row * a.n + col[j], d[j], have[j]);
+        if constexpr (F) {
+            float fh[V][8], dscale[8], dgate[8], s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                branch_terms<T>(d[j], fh[j], dscale, dgate, a, st, drops, key, row, col[j], have[j]);
+                if (o.dgate && a.gate_div == 1) store8((T *)o.dgate + row * a.n + col[j], dgate, have[j]);
+                if constexpr (SUMS)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        acc[kDscale][i] += dscale[i];
+                        acc[kVectors][i] += dgate[i];
+                        acc[kDw][i] = fmaf(d[j][i], fh[j][i], acc[kDw][i]);
+                        acc[kDb][i] += d[j][i];
+                    }
+                if (a.norm != kNormNone) {
+                    float p[8];
+                    load_or<T>(p, a.w, col[j], have[j], 1.0f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        d[j][i] *= p[i];
+                        s1 += d[j][i];
+                        s2 = fmaf(d[j][i], fh[j][i], s2);
+                    }
+                }
+            }
+            if (a.norm != kNormNone) {
+                float2 c = sum(s1, s2);
+                c.x = a.norm == kNormLayer ? c.x * a.inv_n : 0.0f;
+                c.y *= a.inv_n;
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) d[j][i] = st.y * (d[j][i] - c.x - fh[j][i] * c.y);
+            }
+            if (o.df)
+#pragma unroll
+                for (int j = 0; j < V; ++j) store8((T *)o.df + row * a.n + col[j], d[j], have[j]);
+            if constexpr (SUMS)
+                if (o.dgate && a.gate_div > 1 && o.units.cuts == 1 && (row + 1) % a.gate_div == 0) {
+                    store8((T *)o.dgate + row / a.gate_div * a.n + col[0], acc[kVectors], have[0]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[kVectors][i] = 0.0f;
+                }
+        }
+    }
+    if constexpr (SUMS) {
+#pragma unroll
+        for (int k = 0; k <= kVectors; ++k)
+            if (o.want >> k & 1) store8(o.place(k, unit, a.n) + col[0], acc[k], have[0]);
+    }
+}
+
+// The sums over rows where a row has more channels than its lanes could keep sums of: a lane has eight channels of a run of
+// rows, and takes each row's own sums (its gradient's mean and the like) from the kernel above.
+template <class T, bool F, bool N>
+__global__ __launch_bounds__(256) void block_sums_kernel(Block a, BlockGrads o)
+{
+    const int col = ((int)blockIdx.x * 256 + threadIdx.x) * 8, have = max(0, min(8, a.n - col)), unit = blockIdx.y;
+    if (have == 0) return;
+    const bool drops = F && a.drop.below != 0;
+    const DropKey key = drops ? drop_key(a.drop) : DropKey{};
+    int64_t row, end;
+    range_of(o.units, unit, a.m, row, end);
+    float acc[kVectors + 1][8];
+#pragma unroll
+    for (int k = 0; k <= kVectors; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[k][i] = 0.0f;
+    for (; row < end; ++row) {
+        const float4 st = o.stats ? o.stats[row] : float4{0.0f, 1.0f, 0.0f, 1.0f};
+        float d[8];
+        if (o.dy) get8(d, (const T *)o.dy + row * a.n + col, have);
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] = 0.0f;
+        if constexpr (N)
+            if (o.dh) {
+                float t[8], yh[8], g[8];
+                next_norm_terms<T, N>(t, yh, g, a, o, st, row, col, have);
+                const float2 c = o.row_sums[row];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    acc[kDnw][i] = fmaf(g[i], yh[i], acc[kDnw][i]);
+                    acc[kDnb][i] += g[i];
+                    d[i] = i < have ? fmaf(st.w, t[i] - c.x - yh[i] * c.y, d[i]) : 0.0f;
+                }
+            }
+        if constexpr (F) {
+            float fh[8], dscale[8], dgate[8];
+            branch_terms<T>(d, fh, dscale, dgate, a, st, drops, key, row, col, have);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                acc[kDscale][i] += dscale[i];
+                acc[kVectors][i] += dgate[i];
+                acc[kDw][i] = fmaf(d[i], fh[i], acc[kDw][i]);
+                acc[kDb][i] += d[i];
+            }
+            if (o.dgate && a.gate_div > 1 && o.units.cuts == 1 && (row + 1) % a.gate_div == 0) {
+                store8((T *)o.dgate + row / a.gate_div * a.n + col, acc[kVectors], have);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[kVectors][i] = 0.0f;
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k <= kVectors; ++k)
+        if (o.want >> k & 1) store8(o.place(k, unit, a.n) + col, acc[k], have);
+}
+
+// The units' sums, joined in their order: workgroup (columns, y) has the y-th wanted sum.
+struct Joins {
+    const float *from[kVectors];
+    void *to[kVectors];
+    const float *gate_from;
+    void *gate_to;
+    int32_t vectors, units, cuts, n;
+};
+template <class T> __global__ __launch_bounds__(256) void block_join_kernel(Joins j)
+{
+    __shared__ float part[8][32];
+    const int c = threadIdx.x & 31, g = threadIdx.x >> 5, col = (int)blockIdx.x * 32 + c, y = blockIdx.y;
+    const float *from = y < j.vectors ? j.from[y] : j.gate_from + (int64_t)(y - j.vectors) * j.cuts * j.n;
+    T *to = y < j.vectors ? (T *)j.to[y] : (T *)j.gate_to + (int64_t)(y - j.vectors) * j.n;
+    const int count = y < j.vectors ? j.units : j.cuts;
+    float s = 0.0f;
+    if (col < j.n)
+#pragma unroll 8
+        for (int u = g; u < count; u += 8) s += from[(int64_t)u * j.n + col];
+    part[g][c] = s;
+    __syncthreads();
+    if (g == 0 && col < j.n) {
+        s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += part[i][c];
+        to[col] = narrow<T>(s);
+    }
+}
+
+}  // namespace tvl

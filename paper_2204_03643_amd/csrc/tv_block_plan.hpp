@@ -1,0 +1,72 @@
+// How the rows of a residual border are shared out and how the backward call's workspace is laid out.  Host code alone: it
+// needs no GPU compiler.
+#pragma once
+#include "tv_linear_plan.hpp"
+
+namespace tvl {
+
+constexpr int kVectors = 5;                  // sums over rows, in this order; the gate's are the sixth
+enum Vector : int { kDw = 0, kDb = 1, kDscale = 2, kDnw = 3, kDnb = 4 };
+
+// Lanes side by side in a row of n channels, eight channels each (twice eight from 8193 channels on).
+inline int block_lanes(int64_t n)
+{
+    const int64_t per = tiles(n, 8);
+    for (int lanes : {8, 32, 64, 128, 256, 512})
+        if (per <= lanes) return lanes;
+    return 1024;
+}
+constexpr int kMostSumLanes = 512;           // with more, lanes keep no sums over rows
+
+// Units are runs of rows whose sums one group of lanes makes.  A gate's rows that are shared by several rows of x are either
+// cut into `cuts` units each, whose sums are joined afterwards, or lie whole within a unit (cuts 1).
+struct Units {
+    int64_t span;            // rows that a gate's row stands for (cuts > 1), or all rows
+    int32_t rows, cuts, per; // rows of a unit; units a gate's row; units a span
+    int32_t count;
+};
+
+inline Units block_units(int64_t m, int64_t n, bool shared_gate, int64_t gate_div)
+{
+    const int lanes = block_lanes(n);
+    const int64_t most = lanes > kMostSumLanes ? 256 : lanes >= 64 ? 1024 : 1024 * 64 / lanes;
+    int64_t rows = m > most ? tiles(m, most) : 1;
+    Units u{m, 0, 1, 0, 0};
+    if (shared_gate && gate_div > rows) {
+        u.cuts = (int32_t)tiles(gate_div, rows);
+        rows = tiles(gate_div, u.cuts);
+        u.cuts = (int32_t)tiles(gate_div, rows);
+        u.span = gate_div;
+        u.per = u.cuts;
+        u.count = m > 0 ? (int32_t)(m / gate_div * u.cuts) : 0;
+    } else {
+        if (shared_gate) rows = rows / gate_div * gate_div;
+        u.per = u.count = (int32_t)tiles(m, rows);
+    }
+    u.rows = (int32_t)rows;
+    return u;
+}
+
+struct BlockBwdPlan {
+    Units units;
+    uint32_t want;           // a bit a vector, and the gate's where its rows are cut
+    size_t row_sums, bytes;  // where the rows' own sums lie
+};
+
+inline BlockBwdPlan block_bwd_plan(const tv_block_in &in, const tv_block_grads &g, const tv_block_desc &d)
+{
+    BlockBwdPlan p{};
+    const bool shared = in.f && in.gate && g.dgate && d.gate_div > 1;
+    p.units = block_units(d.m, d.n, shared, d.gate_div);
+    const void *vectors[kVectors] = {in.f ? g.dweight : nullptr, in.f ? g.dbias : nullptr, in.f ? g.dscale : nullptr, g.dnext_weight, g.dnext_bias};
+    int64_t wanted = 0;
+    for (int k = 0; k < kVectors; ++k)
+        if (vectors[k]) p.want |= 1u << k, ++wanted;
+    if (shared && p.units.cuts > 1) p.want |= 1u << kVectors, ++wanted;
+    p.row_sums = (size_t)up(wanted * p.units.count * d.n * 4, 256);
+    p.bytes = p.row_sums;
+    if (block_lanes(d.n) > kMostSumLanes && (p.want || shared)) p.bytes += (size_t)up(d.m * 8, 256);
+    return p;
+}
+
+}  // namespace tvl

@@ -151,6 +151,23 @@ template <class T> __device__ __forceinline__ void load8(float (&v)[8], const T 
         for (int i = 0; i < 8; ++i) v[i] = i < have ? widen(p[i]) : 0.0f;
     }
 }
+// The same to the bit: load8 adds to zeros, which makes a -0 a 0.
+template <class T> __device__ __forceinline__ void get8(float (&v)[8], const T *p, int have)
+{
+    if (have == 8) {
+        u32x4 raw[sizeof(T) / 2];
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = get16(p + i * (16 / (int)sizeof(T)));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (sizeof(T) == 2) v[i] = __uint_as_float(i & 1 ? raw[0][i >> 1] & 0xffff0000u : raw[0][i >> 1] << 16);
+            else v[i] = __uint_as_float(raw[i >> 2][i & 3]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < have ? widen(p[i]) : 0.0f;
+    }
+}
 template <class T> __device__ __forceinline__ void store8(T *p, const float (&v)[8], int have)
 {
     if (have == 8) {

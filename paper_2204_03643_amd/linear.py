@@ -9,6 +9,7 @@ a TV pass along the tokens and two channel products.  float32 and bfloat16, CUDA
 """
 from __future__ import annotations
 
+import copy
 import functools
 import math
 
@@ -381,10 +382,16 @@ class TVMixer(torch.nn.Module):
 
     The TV pass runs in fp32 (its rows lie along the second axis, for which the library has no bf16 storage); the
     products run in the block's dtype and keep their activations as `checkpoint` says.
+
+    For deep stacks: `norm` ("rms", "layer") is a norm before the TV pass, `post_norm` one of the block's output before it is
+    added, `init_scale` a trainable scale a channel of it, `dropout` acts on it in training, and forward's gate, of x's shape
+    or [B, 1, C], multiplies it through `gate_act` (see ``block.tv_residual``; its dropout takes forward's seed).
+    ``quantized4()`` is the block for serving.
     """
 
     def __init__(self, channels: int, hidden: int, act: str = "gelu", checkpoint: str = "8bit",
-                 init_lambda: float = 0.05, device=None, dtype=None):
+                 init_lambda: float = 0.05, device=None, dtype=None, norm: str = "none", post_norm: str = "none",
+                 init_scale: float | None = None, dropout: float = 0.0, gate_act: str = "none"):
         super().__init__()
         if init_lambda <= 0.0:
             raise ValueError("TVMixer: init_lambda must be positive")
@@ -393,10 +400,28 @@ class TVMixer(torch.nn.Module):
         like = dict(checkpoint=checkpoint, device=device, dtype=dtype)
         self.expand = TVLinear(channels, hidden, act=act, **like)
         self.reduce = TVLinear(hidden, channels, **like)
+        like = dict(device=device, dtype=dtype)
+        self.norm = _block.TVNorm(channels, norm, **like) if norm != "none" else None
+        # (none of it: the residual is added by the second product)
+        self.residual = _block.TVResidual(channels, post_norm, "none", gate_act, init_scale, dropout, **like)
 
-    def forward(self, x: torch.Tensor) -> torch.Tensor:
+    def forward(self, x: torch.Tensor, gate: torch.Tensor | None = None, seed=None) -> torch.Tensor:
         if x.dim() != 3 or x.shape[-1] != self.raw_lambda.numel():
             raise ValueError("TVMixer: [B, T, %d] expected, got %r" % (self.raw_lambda.numel(), tuple(x.shape)))
         lam = torch.nn.functional.softplus(self.raw_lambda)
-        smooth = tv_prox_1d(x.float(), lam, axis=1).to(x.dtype)
-        return self.reduce(self.expand(smooth), residual=x)
+        before = x if self.norm is None else self.norm(x)
+        smooth = tv_prox_1d(before.float(), lam, axis=1).to(x.dtype)
+        border = self.residual
+        if gate is None and border.norm is None and border.scale is None and not (border.dropout and self.training):
+            return self.reduce(self.expand(smooth), residual=x)
+        return border(x, self.reduce(self.expand(smooth)), gate, seed)
+
+    def quantized4(self) -> "TVMixer":
+        """A copy whose products run in 4 bits, for serving: it has no gradients."""
+        made = copy.deepcopy(self)
+        made.expand, made.reduce = (_quant4.TVLinear4.from_linear(m) for m in (self.expand, self.reduce))
+        return made.eval().requires_grad_(False)
+
+
+# (at the end: both are built on what is above)
+from . import block as _block, quant4 as _quant4  # noqa: E402

@@ -1,0 +1,149 @@
+"""Refusals of residual borders, dropout and values in 4 bits, before any device is touched (no GPU needed)."""
+import pytest
+import torch
+
+import paper_2204_03643_amd as tv
+from paper_2204_03643_amd import block, quant4
+
+FAKE = 0x1000
+OK, NULL, SHAPE, STRIDE, WORKSPACE, UNSUPPORTED = 0, 1, 2, 3, 5, 6
+NO_DROP = tv.tv_drop(0, 0, None, 0)
+
+
+def desc(m=4, n=32, ldx=None, ldf=None, ldg=None, div=1, dtype=tv.TV_F32, norm=1, after=1, act=0, eps=1e-6, drop=NO_DROP):
+    return tv.tv_block_desc(m, n, n if ldx is None else ldx, n if ldf is None else ldf, n if ldg is None else ldg, div, dtype, norm,
+                            after, act, eps, drop)
+
+
+def ins(x=FAKE, f=FAKE, weight=None, bias=None, gate=None, scale=None, next_weight=None, next_bias=None):
+    return tv.tv_block_in(x, f, weight, bias, gate, scale, next_weight, next_bias)
+
+
+def fwd(d, i=None, y=FAKE, h=FAKE, stats=None):
+    return tv.lib().tv_block_fwd(ins() if i is None else i, y, h, stats, d, None)
+
+
+def bwd(d, i=None, dy=FAKE, dh=FAKE, stats=FAKE, ws=FAKE, nbytes=1 << 40, **g):
+    grads = tv.tv_block_grads(*(g.get(k) for k in ("dx", "df", "dgate", "dweight", "dbias", "dscale", "dnext_weight", "dnext_bias")))
+    return tv.lib().tv_block_bwd(dy, dh, ins() if i is None else i, stats, grads, d, ws, nbytes, None)
+
+
+BAD = [(desc(m=-1), SHAPE), (desc(n=0), SHAPE), (desc(m=1 << 31), SHAPE), (desc(n=16385), UNSUPPORTED), (desc(dtype=2), UNSUPPORTED),
+       (desc(norm=3), UNSUPPORTED), (desc(norm=-1), UNSUPPORTED), (desc(after=3), UNSUPPORTED), (desc(act=3), UNSUPPORTED),
+       (desc(eps=-1.0), UNSUPPORTED), (desc(eps=float("nan")), UNSUPPORTED), (desc(ldx=31), STRIDE), (desc(ldf=31), STRIDE),
+       (desc(ldx=1 << 31), STRIDE), (desc(drop=tv.tv_drop(0, 0, None, 65537)), UNSUPPORTED), (desc(drop=tv.tv_drop(0, 0, 4, 1)), STRIDE)]
+
+
+@pytest.mark.parametrize("d,status", BAD)
+def test_bad_descriptors(d, status):
+    assert fwd(d) == status and bwd(d, dx=FAKE) == status
+    assert tv.tv_block_bwd_workspace_bytes(ins(), tv.tv_block_grads(FAKE, FAKE, None, FAKE, None, None, None, None), d) == 0
+
+
+def test_gates():
+    gate = ins(gate=FAKE)
+    assert fwd(desc(div=0), gate) == SHAPE and fwd(desc(m=5, div=2), gate) == SHAPE and fwd(desc(ldg=31), gate) == STRIDE
+    assert fwd(desc(m=0, div=3), gate) == OK
+
+
+def test_forward_refusals():
+    assert fwd(desc(), ins(x=None)) == NULL and fwd(desc(), h=None) == NULL and fwd(desc(after=0), y=None, h=None) == NULL
+    assert fwd(desc(after=0)) == UNSUPPORTED                     # h without a next norm
+    assert fwd(desc(), ins(f=None)) == UNSUPPORTED               # y without f
+    assert fwd(desc(), y=FAKE + 2) == STRIDE and fwd(desc(), stats=FAKE + 8) == STRIDE and fwd(desc(), ins(weight=FAKE + 1)) == STRIDE
+    assert fwd(desc(m=0), ins(x=None, f=None), y=None, h=None) == OK
+
+
+def test_backward_refusals():
+    assert bwd(desc(), dy=None, dh=None) == NULL and bwd(desc(), stats=None) == NULL and bwd(desc(), ins(x=None)) == NULL
+    assert bwd(desc(after=0), dx=FAKE) == UNSUPPORTED                                # dh without a next norm
+    assert bwd(desc(), ins(f=None), df=FAKE) == UNSUPPORTED and bwd(desc(), dgate=FAKE) == UNSUPPORTED
+    assert bwd(desc(norm=0), dweight=FAKE) == UNSUPPORTED and bwd(desc(after=0), dh=None, dnext_bias=FAKE) == UNSUPPORTED
+    need = tv.tv_block_bwd_workspace_bytes(ins(), tv.tv_block_grads(FAKE, FAKE, None, FAKE, None, FAKE, None, None), desc())
+    assert need >= 2 * 4 * 32 * 4                                                    # two sums of four units
+    for ws, have in ((None, need), (FAKE + 8, need), (FAKE, need - 1)):
+        assert bwd(desc(), dweight=FAKE, dscale=FAKE, ws=ws, nbytes=have) == WORKSPACE
+    assert tv.tv_block_bwd_workspace_bytes(ins(), tv.tv_block_grads(FAKE, FAKE, None, None, None, None, None, None), desc()) == 0
+    assert bwd(desc(), dx=FAKE + 1) == STRIDE
+
+
+def test_dropout_refusals():
+    call = lambda rows=4, n=8, ldx=8, dtype=0, drop=tv.tv_drop(0, 0, None, 5), x=FAKE, y=FAKE: tv.lib().tv_drop_apply(  # noqa: E731
+        x, y, rows, n, ldx, dtype, drop, None)
+    assert call(rows=-1) == SHAPE and call(n=0) == SHAPE and call(rows=1 << 31) == SHAPE and call(dtype=2) == UNSUPPORTED
+    assert call(ldx=7) == STRIDE and call(drop=tv.tv_drop(0, 0, None, 65537)) == UNSUPPORTED and call(x=None) == NULL
+    assert call(y=FAKE + 2) == STRIDE and call(rows=0, x=None, y=None) == OK
+
+
+def test_values_refusals():
+    for name in ("tv_mx4_save", "tv_mx4_load"):
+        def call(x=FAKE, codes=FAKE, exps=FAKE, rows=4, n=8, ldx=8, dtype=0):
+            a = (x, codes, exps) if name == "tv_mx4_save" else (codes, exps, x)
+            return getattr(tv.lib(), name)(*a, rows, n, ldx, dtype, None)
+        assert call(rows=-1) == SHAPE and call(n=0) == SHAPE and call(n=1 << 31, ldx=1 << 31) == SHAPE and call(dtype=3) == UNSUPPORTED
+        assert call(ldx=7) == STRIDE and call(codes=FAKE + 8) == STRIDE and call(exps=FAKE + 4) == STRIDE and call(x=FAKE + 2) == STRIDE
+        assert call(x=None) == NULL and call(codes=None) == NULL and call(exps=None) == NULL and call(rows=0, x=None) == OK
+
+
+def test_product_refusals():
+    def d(m=4, k=32, n=16, ldx=None, ldr=None, ldy=None, dtype=0, act=0):
+        return tv.tv_linear_desc(m, k, n, k if ldx is None else ldx, 0, n if ldr is None else ldr, n if ldy is None else ldy, dtype, act)
+
+    def call(dd, x=FAKE, xe=None, w=FAKE, we=FAKE, b=None, r=None, y=FAKE, ws=FAKE, nbytes=1 << 40):
+        return tv.lib().tv_linear4_fwd(x, xe, w, we, b, r, y, dd, ws, nbytes, None)
+    for bad, status in ((d(m=-1), SHAPE), (d(k=0), SHAPE), (d(n=0), SHAPE), (d(m=1 << 31), SHAPE), (d(dtype=2), UNSUPPORTED), (d(act=4), UNSUPPORTED),
+                        (d(ldx=31), STRIDE), (d(ldy=15), STRIDE), (d(m=(1 << 31) - 2000, n=(1 << 31) - 2000), SHAPE)):
+        assert call(bad) == status and tv.tv_linear4_workspace_bytes(bad, False) == 0
+    assert call(d(ldr=15), r=FAKE) == STRIDE
+    for name in ("x", "w", "we", "y"):
+        assert call(d(), **{name: None}) == NULL
+        assert call(d(), **{name: FAKE + 2}) == STRIDE
+    assert call(d(), x=FAKE + 4, xe=FAKE) == STRIDE and call(d(), xe=FAKE + 4) == STRIDE and call(d(), b=FAKE + 1) == STRIDE
+    need = tv.tv_linear4_workspace_bytes(d(), False)
+    assert need >= 4 * 64 + 16
+    for ws, have in ((None, need), (FAKE + 8, need), (FAKE, need - 1)):
+        assert call(d(), ws=ws, nbytes=have) == WORKSPACE
+    assert call(d(m=0), x=None, w=None, we=None, y=None) == OK
+
+
+def test_python_refusals():
+    x, f = torch.zeros(2, 3, 8), torch.zeros(2, 3, 8)
+    for call in (lambda: block.tv_norm(x), lambda: block.tv_residual(x, f), lambda: block.tv_dropout(x, 0.5, 1), lambda: quant4.tv_quantize4(x),
+                 lambda: quant4.Quantized4(torch.zeros(1, 64, dtype=torch.uint8), torch.zeros(1, 4, 4, dtype=torch.uint8), (1, 8), torch.float32)):
+        with pytest.raises(RuntimeError):
+            call()
+    with pytest.raises(TypeError):
+        quant4.tv_linear4(x, torch.zeros(4, 8))
+    with pytest.raises(TypeError):
+        quant4.Quantized4(torch.zeros(1, 64), torch.zeros(1, 4, 4, dtype=torch.uint8), (1, 8), torch.float32)
+    with pytest.raises(ValueError):
+        quant4.Quantized4(torch.zeros(1, 63, dtype=torch.uint8), torch.zeros(1, 4, 4, dtype=torch.uint8), (1, 8), torch.float32)
+    for kwargs in (dict(norm="l2"), dict(next_norm="x"), dict(gate_act="relu"), dict(dropout=1.5), dict(init_scale=None, channels=0)):
+        with pytest.raises(ValueError):
+            block.TVResidual(**{"channels": 8, **kwargs})
+    with pytest.raises(ValueError):
+        block.TVNorm(8, "none")
+    with pytest.raises(ValueError):
+        quant4.TVLinear4(8, 0)
+
+
+@pytest.mark.parametrize("x,gate,div", [((2, 3, 8), (2, 3, 8), 1), ((2, 3, 8), (2, 1, 8), 3), ((2, 3, 8), (1, 1, 8), 6), ((2, 3, 8), (8,), 6), ((2, 1, 8), (2, 1, 8), 1),
+                                        ((8,), (8,), 1), ((5, 8), (1, 8), 5), ((1, 1, 8), (1, 1, 8), 1), ((2, 0, 8), (2, 1, 8), 1)])
+def test_which_rows_share_a_gate(x, gate, div):
+    assert block._gate_div(torch.zeros(x), torch.zeros(gate), "gate") == div
+
+
+@pytest.mark.parametrize("x,gate", [((2, 3, 8), (1, 3, 8)), ((2, 3, 8), (2, 3, 1)), ((2, 3, 8), (3, 8)), ((2, 3, 8), (2, 2, 8)), ((2, 3, 8), ())])
+def test_gates_that_do_not_fit(x, gate):
+    with pytest.raises(ValueError):
+        block._gate_div(torch.zeros(x), torch.zeros(gate), "gate")
+
+
+def test_probabilities_and_seeds():
+    x = torch.zeros(1)
+    assert block._check_drop(0.1, -1, 3, x, "") == (6554, (1 << 64) - 1, None, 3) and block._check_drop(1.0, 0, 0, x, "")[0] == 65536
+    assert block._check_drop(0.0, None, 0, x, "")[0] == 0
+    for p, seed, offset, error in ((1.5, 0, 0, ValueError), (float("nan"), 0, 0, ValueError), (0.5, None, 0, ValueError), (0.5, 1 << 64, 0, ValueError),
+                                   (0.5, 1.0, 0, TypeError), (0.5, 0, "1", TypeError), (0.5, True, 0, TypeError)):
+        with pytest.raises(error):
+            block._check_drop(p, seed, offset, x, "")

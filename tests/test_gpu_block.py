@@ -1,0 +1,293 @@
+"""Residual borders (tv_norm, tv_residual) against 64 bits."""
+import blockref
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+NAMES = ("weight", "bias", "gate", "scale", "next_weight", "next_bias")
+
+
+def made(m, n, dtype, seed, norm, next_norm, bias, gate, scale):
+    gen = torch.Generator().manual_seed(seed)
+    normal = lambda *s: torch.randn(*s, generator=gen)              # noqa: E731
+    loud = torch.where(torch.rand(n, generator=gen) < 0.05, 8.0, 1.0)
+    rows = lambda: normal(m, n) * loud * torch.exp2(normal(m, 1) * 0.5) + 0.3      # noqa: E731
+    t = dict(x=rows(), f=rows(), weight=1 + 0.2 * normal(n) if norm != "none" else None,
+             bias=0.2 * normal(n) if norm != "none" and bias else None, gate=normal(gate, n) if gate else None,
+             scale=0.5 + 0.1 * normal(n) if scale else None, next_weight=1 + 0.2 * normal(n) if next_norm != "none" else None,
+             next_bias=0.2 * normal(n) if next_norm != "none" and bias else None, dy=normal(m, n), dh=normal(m, n) if next_norm != "none" else None)
+    return {k: None if v is None else v.to(dtype) for k, v in t.items()}
+
+
+def wide(t):
+    return {k: None if v is None else v.double() for k, v in t.items()}
+
+
+def run(t, shape=None, gate_shape=None, upstream=("dy", "dh"), **how):
+    """{name: tensor} of tv_residual's outputs and gradients."""
+    from paper_2204_03643_amd.block import tv_residual
+    shape = shape or t["x"].shape
+    c = {k: None if v is None else v.cuda() for k, v in t.items()}
+    for k in ("x", "f", "dy", "dh"):
+        c[k] = None if c[k] is None else c[k].reshape(shape)
+    if c["gate"] is not None and gate_shape is not None:
+        c["gate"] = c["gate"].reshape(gate_shape)
+    leaves = [k for k in ("x", "f") + NAMES if c[k] is not None]
+    for k in leaves:
+        c[k].requires_grad_()
+    out = tv_residual(c["x"], c["f"], **{k: c[k] for k in NAMES}, **how)
+    out = dict(zip(("y", "h"), out if isinstance(out, tuple) else (out,)))
+    with_grad = [(out[k], c["d" + k]) for k in out if "d" + k in upstream]
+    grads = torch.autograd.grad([a for a, _ in with_grad], [c[k] for k in leaves], [b for _, b in with_grad], allow_unused=True)
+    out.update(("d" + k, g) for k, g in zip(leaves, grads))
+    return {k: None if v is None else v.detach() for k, v in out.items()}
+
+
+def check(t, dtype, got, p=0.0, seed=0, offset=0, upstream=("dy", "dh"), **how):
+    ref = wide(t)
+    for k in ("dy", "dh"):
+        if k not in upstream:
+            ref[k] = None
+    want = blockref.border(dtype, p=p, seed=seed, offset=offset, **{k: ref[k] for k in ("x", "f", "dy", "dh") + NAMES}, **how)
+    for k, v in got.items():
+        if v is not None:
+            blockref.within(v, want[k], k)
+
+
+SIZES = [(1, 1), (3, 5), (2, 8), (7, 63), (33, 64), (5, 65), (17, 256), (4, 257), (3, 512), (5, 513), (9, 1001), (2, 1024), (3, 1025),
+         (70, 2048), (2, 2049), (1, 4096), (3, 4097), (2, 8192), (3, 8193), (5, 16383), (2, 16384)]
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("m,n", SIZES)
+def test_sizes(m, n, dtype):
+    how = dict(norm="layer", next_norm="rms", gate_act="silu")
+    t = made(m, n, dtype, m * 31 + n, "layer", "rms", True, m, True)
+    got = run(t, dropout=0.2, seed=99, offset=3, **how)
+    check(t, dtype, got, p=0.2, seed=99, offset=3, **how)
+
+
+FORMS = [(norm, after, gate, act, scale, p) for i, (norm, after) in enumerate((a, b) for a in ("none", "rms", "layer") for b in ("none", "rms", "layer"))
+         for gate, act, scale, p in (((0, "none", False, 0.0), (4, "sigmoid", True, 0.3), (12, "none", False, 0.5)),
+                                     ((0, "none", True, 0.1), (1, "silu", False, 0.0), (12, "sigmoid", True, 0.0)))[i % 2]]
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("norm,next_norm,gate,act,scale,p", FORMS)
+def test_forms(norm, next_norm, gate, act, scale, p, dtype):
+    """Each pair of norms with gates for each row, for three rows and for all, with and without the rest."""
+    m, n = 12, 200
+    how = dict(norm=norm, next_norm=next_norm, gate_act=act)
+    t = made(m, n, dtype, 5, norm, next_norm, True, gate, scale)
+    shape = (4, 3, n)
+    got = run(t, shape, {4: (4, 1, n), 1: (n,), 12: shape}.get(gate), dropout=p, seed=7, offset=1 << 40, **how)
+    assert ("h" in got) == (next_norm != "none")
+    check(t, dtype, got, p=p, seed=7, offset=1 << 40, **how)
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("m,n,gate", [(2600, 40, 1), (2600, 40, 2), (2600, 40, 1300), (9000, 24, 3), (2500, 520, 5), (700, 8200, 7), (700, 8200, 100), (1300, 4104, 1)])
+def test_many_rows(m, n, gate, dtype):
+    """More rows than there are groups of lanes, with gates that several groups share and gates that a group has several of."""
+    how = dict(norm="rms", next_norm="layer", gate_act="sigmoid")
+    t = made(m, n, dtype, m + gate, "rms", "layer", False, gate, True)
+    got = run(t, (gate, m // gate, n), (gate, 1, n), dropout=0.0, **how)
+    check(t, dtype, got, **how)
+    again = run(t, (gate, m // gate, n), (gate, 1, n), dropout=0.0, **how)
+    assert all(torch.equal(got[k], again[k]) for k in got)
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("upstream", (("dy",), ("dh",)))
+def test_a_gradient_of_one_output_alone(upstream, dtype):
+    how = dict(norm="rms", next_norm="layer")
+    t = made(9, 72, dtype, 3, "rms", "layer", True, 0, True)
+    got = run(t, dropout=0.25, seed=1, upstream=upstream, **how)
+    check(t, dtype, got, p=0.25, seed=1, upstream=upstream, **how)
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("kind", ("rms", "layer"))
+@pytest.mark.parametrize("m,n", [(1, 1), (1, 2048), (3, 7), (40, 64), (1500, 96), (5, 1001), (2, 16384), (300, 8200)])
+def test_norm_alone(m, n, kind, dtype):
+    from paper_2204_03643_amd.block import tv_norm
+    t = made(m, n, dtype, m + n, "none", kind, kind == "layer", 0, False)
+    c = {k: t[k].cuda().requires_grad_() for k in ("x", "next_weight", "next_bias") if t[k] is not None}
+    h = tv_norm(c["x"], c["next_weight"], c.get("next_bias"), kind=kind)
+    grads = torch.autograd.grad(h, list(c.values()), t["dh"].cuda())
+    ref = wide(t)
+    want = blockref.border(dtype, ref["x"], next_norm=kind, next_weight=ref["next_weight"], next_bias=ref["next_bias"], dh=ref["dh"])
+    blockref.within(h, want["h"], "h")
+    for k, g in zip(c, grads):
+        blockref.within(g, want["d" + k], "d" + k)
+    with torch.no_grad():
+        assert torch.equal(tv_norm(c["x"], c["next_weight"], c.get("next_bias"), kind=kind), h)
+        bare = tv_norm(c["x"], kind=kind, eps=1e-3)
+    blockref.within(bare, blockref.border(dtype, ref["x"], next_norm=kind, eps=1e-3)["h"], "h without weights")
+
+
+def test_gradients_against_differences():
+    """Each gradient in one random direction against the difference of 64-bit losses on either side."""
+    how = dict(norm="layer", next_norm="rms", gate_act="silu")
+    m, n = 6, 40
+    t = made(m, n, torch.float32, 21, "layer", "rms", True, 3, True)
+    got = run(t, (3, 2, n), (3, 1, n), dropout=0.3, seed=5, **how)
+    ref = wide(t)
+    gen = torch.Generator().manual_seed(4)
+
+    def loss(at):
+        o = blockref.border(torch.float32, p=0.3, seed=5, **{k: at[k] for k in ("x", "f") + NAMES}, **how)
+        return float((o["y"][0] * ref["dy"]).sum() + (o["h"][0] * ref["dh"]).sum())
+    for k in ("x", "f") + NAMES:
+        way = torch.randn(ref[k].shape, generator=gen, dtype=torch.float64)
+        step = 1e-5
+        diff = (loss({**ref, k: ref[k] + step * way}) - loss({**ref, k: ref[k] - step * way})) / (2 * step)
+        g = got["d" + k].double().cpu().reshape(way.shape)
+        # the differences are good to about 1e-9 of the loss's terms over the step, the gradients to 1e-5 of theirs
+        assert abs(diff - float((g * way).sum())) <= 1e-5 * float((g * way).abs().sum()) + 1e-6, k
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+def test_rows_that_are_not_finite_stay_by_themselves(dtype):
+    from paper_2204_03643_amd.block import tv_residual
+    t = made(9, 300, dtype, 8, "rms", "layer", False, 0, False)
+    x, f, w, nw = (t[k].cuda() for k in ("x", "f", "weight", "next_weight"))
+    clean = tv_residual(x, f, norm="rms", weight=w, next_norm="layer", next_weight=nw)
+    x[2, 299], f[4, 0], f[6, 150] = float("nan"), float("inf"), float("-inf")
+    spoiled = tv_residual(x, f, norm="rms", weight=w, next_norm="layer", next_weight=nw)
+    others = [0, 1, 3, 5, 7, 8]
+    for a, b in zip(clean, spoiled):
+        assert torch.equal(a[others], b[others]) and b[[2, 4, 6]].isnan().any(-1).all()
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+def test_views(dtype):
+    """Rows that are further apart than they are long, that start off 16-byte boundaries, that are transposed or repeated."""
+    from paper_2204_03643_amd.block import tv_norm, tv_residual
+    t = made(10, 203, dtype, 9, "rms", "rms", False, 0, True)
+    dense = {k: v.cuda() for k, v in t.items() if v is not None}
+    want = tv_residual(dense["x"], dense["f"], norm="rms", weight=dense["weight"], scale=dense["scale"], next_norm="rms")
+    pad = torch.zeros(10, 411, dtype=dtype, device="cuda")
+    pad[:, 1:204] = dense["x"]
+    pad[:, 206:409] = dense["f"]
+    x, f = pad[:, 1:204], pad[:, 206:409]
+    vectors = torch.zeros(3 * 203, dtype=dtype, device="cuda")
+    vectors[1:610:3][:203] = dense["weight"]
+    got = tv_residual(x, f, norm="rms", weight=vectors[1:610:3], scale=dense["scale"], next_norm="rms")
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    turned = dense["x"].t().contiguous().t()
+    assert torch.equal(tv_norm(turned), tv_norm(dense["x"]))
+    row = dense["x"][:1].expand(10, 203)
+    assert torch.equal(tv_norm(row), tv_norm(row.contiguous()))
+    # gradients that come as views: of a sum, the same number everywhere
+    leaf = dense["x"].clone().requires_grad_()
+    g1 = torch.autograd.grad(tv_norm(leaf).sum(), leaf)[0]
+    g2 = torch.autograd.grad(tv_norm(leaf), leaf, torch.ones(10, 203, dtype=dtype, device="cuda"))[0]
+    assert torch.equal(g1, g2)
+
+
+def test_no_rows():
+    from paper_2204_03643_amd.block import tv_dropout, tv_norm, tv_residual
+    x = torch.zeros(2, 0, 16, device="cuda", requires_grad=True)
+    gate = torch.ones(2, 1, 16, device="cuda", requires_grad=True)
+    w = torch.ones(16, device="cuda", requires_grad=True)
+    y, h = tv_residual(x, x, norm="rms", weight=w, gate=gate, next_norm="rms", dropout=0.5, seed=1)
+    assert y.shape == h.shape == x.shape and tv_dropout(x, 0.5, 1).shape == x.shape and tv_norm(x, w).shape == x.shape
+    grads = torch.autograd.grad([y, h], [x, gate, w], [torch.zeros_like(y), torch.zeros_like(h)])
+    assert [g.shape for g in grads] == [x.shape, gate.shape, w.shape] and all(g.abs().sum() == 0 for g in grads)
+
+
+def test_an_output_that_is_changed_in_place_is_noticed():
+    from paper_2204_03643_amd.block import tv_residual
+    x = torch.randn(4, 32, device="cuda", requires_grad=True)
+    y, h = tv_residual(x, x * 2, next_norm="rms")
+    y.mul_(2)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        h.sum().backward()
+
+
+def test_another_stream():
+    from paper_2204_03643_amd.block import tv_residual
+    t = made(2000, 500, torch.float32, 1, "rms", "rms", False, 0, False)
+    want = run(t, norm="rms", next_norm="rms")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        got = run(t, norm="rms", next_norm="rms")
+    side.synchronize()
+    assert all(torch.equal(want[k], got[k]) for k in want if want[k] is not None)
+
+
+def test_forward_mode_and_second_derivatives_are_refused():
+    from paper_2204_03643_amd.block import tv_dropout, tv_norm
+    x = torch.randn(3, 8, device="cuda")
+    with torch.autograd.forward_ad.dual_level():
+        dual = torch.autograd.forward_ad.make_dual(x, torch.ones_like(x))
+        for call in (lambda: tv_norm(dual), lambda: tv_dropout(dual, 0.5, 1)):
+            with pytest.raises((NotImplementedError, RuntimeError)):
+                call()
+    x.requires_grad_()
+    g = torch.autograd.grad(tv_norm(x).square().sum(), x, create_graph=True)[0]
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+def test_captured_training_step(dtype):
+    """A step in a graph, replayed with other inputs and other numbers for dropout, against the eager step."""
+    from paper_2204_03643_amd.block import tv_residual
+    m, n = 40, 264
+    t = made(m, n, dtype, 13, "rms", "layer", False, 8, True)
+    c = {k: v.cuda() for k, v in t.items() if v is not None}
+    c["gate"] = c["gate"].view(8, 1, n)
+    for k in ("x", "f", "dy", "dh"):
+        c[k] = c[k].view(8, 5, n)
+    leaves = [k for k in ("x", "f", "weight", "gate", "scale", "next_weight", "next_bias") if k in c]
+    seed = torch.zeros(1, dtype=torch.int64, device="cuda")
+
+    def step(at):
+        for k in leaves:
+            at[k] = at[k].detach().requires_grad_()
+        y, h = tv_residual(at["x"], at["f"], norm="rms", weight=at["weight"], gate=at["gate"], gate_act="silu", scale=at["scale"],
+                           dropout=0.3, seed=seed, offset=2, next_norm="layer", next_weight=at["next_weight"])
+        return [y.detach(), h.detach(), *torch.autograd.grad([y, h], [at[k] for k in leaves if k != "next_bias"], [at["dy"], at["dh"]])]
+    static = dict(c)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(dict(static))
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step(dict(static))
+    masks = []
+    for i in range(4):
+        for k in ("x", "f", "dy", "dh"):
+            c[k].copy_(torch.randn(8, 5, n, device="cuda").to(dtype))
+        seed.fill_(1000 + i // 2 * 17)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [o.clone() for o in outs]
+        want = step({k: v.clone() for k, v in c.items()})
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+        masks.append((got[0] == c["x"]).float())
+    assert not torch.equal(masks[0], masks[3])
+
+
+def test_modules():
+    from paper_2204_03643_amd.block import TVNorm, TVResidual, tv_norm, tv_residual
+    torch.manual_seed(0)
+    border = TVResidual(48, norm="layer", next_norm="rms", gate_act="sigmoid", init_scale=0.1, dropout=0.5, device="cuda")
+    x, f, gate = (torch.randn(2, 7, 48, device="cuda") for _ in range(3))
+    y, h = border(x, f, gate, seed=11)
+    want = tv_residual(x, f, "layer", border.norm.weight, border.norm.bias, gate, "sigmoid", border.scale, 0.5, 11, 0, "rms", border.next.weight)
+    assert torch.equal(y, want[0]) and torch.equal(h, want[1])
+    torch.manual_seed(3)
+    a = border(x, f, gate)[0]
+    torch.manual_seed(3)
+    assert torch.equal(a, border(x, f, gate)[0]) and not torch.equal(a, border(x, f, gate)[0])
+    border.eval()
+    assert torch.equal(border(x, f, gate)[0], tv_residual(x, f, "layer", border.norm.weight, border.norm.bias, gate, "sigmoid", border.scale))
+    norm = TVNorm(48, "layer", device="cuda")
+    assert norm.bias is not None and TVNorm(48).bias is None and torch.equal(norm(x), tv_norm(x, norm.weight, norm.bias, "layer"))
