@@ -485,8 +485,11 @@ int tv_mx4_load(const uint8_t *codes, const uint8_t *exps, void *x, int64_t rows
 /*
  * y = act(x4 W4^T + b) + r on values in 4 bits, for serving: x4 is what the codes of x stand for, or (x_exps NULL) of x's
  * rows as tv_mx4_save would make them, W4 [n, k] in its codes.  bias, residual and y of desc.dtype as in tv_linear_fwd;
- * ldw is not read, ldx only where x is rows.  Products are exact, sums fp32.  Sizes as in tv_linear_fwd; m = 0 does nothing.
+ * ldw is not read, ldx only where x is rows.  Products are exact, sums fp32.  Sizes as in tv_linear_fwd, k at most
+ * TV_LINEAR4_MAX_K (TV_ERR_UNSUPPORTED); m = 0 does nothing.  Results do not depend on whether x comes as rows or as codes
+ * but in the order of their fp32 sums, which goes by the sizes and that.
  */
+#define TV_LINEAR4_MAX_K 16777216
 size_t tv_linear4_workspace_bytes(tv_linear_desc desc, int x_is_codes);
 int tv_linear4_fwd(const void *x, const uint8_t *x_exps, const uint8_t *w, const uint8_t *w_exps, const void *bias,
                    const void *res, void *y, tv_linear_desc desc, void *ws, size_t ws_bytes, hipStream_t stream);

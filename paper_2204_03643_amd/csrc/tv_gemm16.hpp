@@ -83,7 +83,7 @@ template <int ROWS, int WAVES, bool TRANSPOSED> struct Tile16 {
 
 // Rows of `cols` values from anywhere to rows on 16-byte boundaries, zeros up to a multiple of eight: a unit of eight a thread.
 // Bound by bytes: 8192 x 2047 in 12 us, 5.6 TB/s.
-__global__ __launch_bounds__(256) void copy_rows_kernel(const bf16 *from, int64_t ld, bf16 *to, int cols, int64_t units)
+static __global__ __launch_bounds__(256) void copy_rows_kernel(const bf16 *from, int64_t ld, bf16 *to, int cols, int64_t units)
 {
     const int64_t at = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
     if (at >= units) return;

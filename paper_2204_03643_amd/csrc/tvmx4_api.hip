@@ -1,7 +1,7 @@
 // C-ABI entry points of values in 4 bits and their products: argument validation and launches.
 #include "../../include/tvprox.h"
-#include "tv_gemm4.hpp"
-#include "tv_linear_plan.hpp"
+#include "tv_gemv4.hpp"
+#include "tv_linear4_plan.hpp"
 
 namespace {
 
@@ -36,36 +36,55 @@ int check_sizes(const tv_linear_desc &d, bool codes)
 {
     if (d.m < 0 || d.k < 1 || d.n < 1 || d.m >= kMostIndex || d.k >= kMostIndex || d.n >= kMostIndex) return TV_ERR_SHAPE;
     if (!product_fits(d.m, d.n)) return TV_ERR_SHAPE;
+    if (d.k > TV_LINEAR4_MAX_K) return TV_ERR_UNSUPPORTED;
     if ((d.dtype != TV_F32 && d.dtype != TV_BF16) || d.act < TV_ACT_NONE || d.act > TV_ACT_SILU) return TV_ERR_UNSUPPORTED;
     if (d.ldy < d.n || d.ldy >= kMostStride || (!codes && (d.ldx < d.k || d.ldx >= kMostStride))) return TV_ERR_STRIDE;
     return TV_OK;
 }
 
-// The workspace: x's codes and scale words.
-struct Plan4 {
-    size_t exps, bytes;
-};
-Plan4 plan4(const tv_linear_desc &d, bool codes)
+template <class T, int BM, int BN, int WM, int WN, int BUF>
+void launch_tiles(Product g, const Scales &scales, const Epilogue &e, hipStream_t stream)
 {
-    Plan4 p{};
-    if (!codes) {
-        p.exps = (size_t)up(d.m * groups4(d.k) * 64, 256);
-        p.bytes = p.exps + (size_t)up(rows4(d.m) * groups4(d.k) * 4, 256);
+    g.tiles_m = (uint32_t)tiles(g.M, BM);
+    g.tiles_n = (uint32_t)tiles(g.N, BN);
+    hipLaunchKernelGGL((gemm4_kernel<T, BM, BN, WM, WN, BUF>), dim3(g.tiles_m * g.tiles_n, g.splits), dim3(WM * WN * 64), 0, stream, g, scales, e);
+}
+
+template <class T, int NT, bool OWN>
+void launch_few(const Product &g, const Rows4 &x, const Scales &s, const Epilogue &e, hipStream_t stream)
+{
+    const dim3 grid((uint32_t)tiles(g.N, NT * 16), g.splits), block(512);
+    if (g.M <= 16) hipLaunchKernelGGL((gemv4_kernel<T, 1, NT, OWN ? 2 : 4, OWN>), grid, block, 0, stream, g, x, s.w, s.w_rows, e);
+    else if constexpr (!OWN) {
+        if (g.M <= 32) hipLaunchKernelGGL((gemv4_kernel<T, 2, NT, 4, OWN>), grid, block, 0, stream, g, x, s.w, s.w_rows, e);
+        else hipLaunchKernelGGL((gemv4_kernel<T, 4, NT, 4, OWN>), grid, block, 0, stream, g, x, s.w, s.w_rows, e);
     }
-    return p;
 }
 
 template <class T>
 int linear4(const void *x, const uint8_t *x_exps, const uint8_t *w, const uint8_t *w_exps, const Epilogue &e,
             const tv_linear_desc &d, const Plan4 &p, char *ws, hipStream_t stream)
 {
-    Product4 g{(const uint8_t *)x, w, (const uint32_t *)x_exps, (const uint32_t *)w_exps, (int32_t)d.m, (int32_t)d.n, (int32_t)groups4(d.k)};
-    if (!x_exps) {
+    const int64_t ld = groups_of(d.k) * 32;
+    Product g{x, w, ld, ld, (int32_t)d.m, (int32_t)d.n, (int32_t)ld, p.c.k_per, p.c.splits, (float *)(ws + p.split), 0, 0};
+    const Scales s{p.c.own ? nullptr : x_exps ? (const uint32_t *)x_exps : (const uint32_t *)(ws + p.exps), (const uint32_t *)w_exps,
+                   (uint32_t)scale_rows(d.m), (uint32_t)scale_rows(d.n)};
+    if (!x_exps && !p.c.own) {
         if (save<T>(x, ws, ws + p.exps, d.m, d.k, d.ldx, stream) != TV_OK) return TV_ERR_HIP;
-        g.x = (const uint8_t *)ws;
-        g.xs = (const uint32_t *)(ws + p.exps);
+        g.a = ws;
     }
-    hipLaunchKernelGGL((linear4_kernel<T>), dim3((uint32_t)(tiles(d.n, 64) * tiles(d.m, 32))), dim3(256), 0, stream, g, e);
+    if (p.c.kind == kTile256x4) launch_tiles<T, 256, 256, 2, 4, 2>(g, s, e, stream);
+    if (p.c.kind == kTile128x4) launch_tiles<T, 128, 128, 2, 2, 4>(g, s, e, stream);
+    if (p.c.kind == kTile64x4) launch_tiles<T, 64, 128, 2, 2, 4>(g, s, e, stream);
+    if (p.c.kind == kFew4) {
+        const Rows4 rows{g.a, s.x, d.ldx, s.x_rows, (int32_t)d.k};
+        if (p.c.own) launch_few<T, 1, true>(g, rows, s, e, stream);
+        else launch_few<T, 1, false>(g, rows, s, e, stream);
+    }
+    if (p.c.splits > 1) {
+        if (launched() != TV_OK) return TV_ERR_HIP;
+        hipLaunchKernelGGL((join_kernel<T>), dim3((uint32_t)tiles(d.m * tiles(d.n, 32) * 4, 256)), dim3(256), 0, stream, g, e);
+    }
     return launched();
 }
 
