@@ -19,6 +19,29 @@ struct Block {
     Drop    drop;
 };
 
+// Sums over LANES lanes of a wave, in all of them: neighbours, pairs, quads and eights by moves within sixteen lanes, then the
+// sixteens and halves of the wave by exchanging them.
+template <int CTRL> __device__ __forceinline__ float lanes_moved(float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+template <int LANES> __device__ __forceinline__ float wave_sum(float v)
+{
+    v += lanes_moved<0xB1>(v);                       // [1, 0, 3, 2]
+    v += lanes_moved<0x4E>(v);                       // [2, 3, 0, 1]
+    v += lanes_moved<0x141>(v);                      // mirrored within 8
+    if constexpr (LANES > 8) v += lanes_moved<0x140>(v);      // within 16
+    if constexpr (LANES > 16) {
+        const auto o = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(o[0]) + __uint_as_float(o[1]);
+    }
+    if constexpr (LANES > 32) {
+        const auto o = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(o[0]) + __uint_as_float(o[1]);
+    }
+    return v;
+}
+
 // Sums over the LANES lanes of a row.  More than a wave: through LDS, in two places in turn, so that one barrier a sum is
 // enough (between the read of a place and its next write lies the barrier of the sum in between).
 template <int LANES> struct RowSum {
@@ -28,11 +51,9 @@ template <int LANES> struct RowSum {
     __device__ __forceinline__ explicit RowSum(float2 (*lds)[kWaves]) : place(lds) {}
     __device__ __forceinline__ float2 operator()(float a, float b)
     {
-#pragma unroll
-        for (int i = 1; i < (LANES < 64 ? LANES : 64); i <<= 1) {
-            a += __shfl_xor(a, i);
-            b += __shfl_xor(b, i);
-        }
+        constexpr int kLanes = LANES < 64 ? LANES : 64;
+        a = wave_sum<kLanes>(a);
+        b = wave_sum<kLanes>(b);
         if constexpr (LANES > 64) {
             if ((threadIdx.x & 63) == 0) place[turn][threadIdx.x >> 6] = float2{a, b};
             __syncthreads();
@@ -46,7 +67,19 @@ template <int LANES> struct RowSum {
         }
         return {a, b};
     }
-    __device__ __forceinline__ float operator()(float a) { return (*this)(a, 0.0f).x; }
+    __device__ __forceinline__ float operator()(float a)
+    {
+        a = wave_sum<LANES < 64 ? LANES : 64>(a);
+        if constexpr (LANES > 64) {
+            if ((threadIdx.x & 63) == 0) place[turn][threadIdx.x >> 6].x = a;
+            __syncthreads();
+            a = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) a += place[turn][i].x;
+            turn ^= 1;
+        }
+        return a;
+    }
 };
 
 // act(z) and, where it is asked for, its slope.
@@ -150,7 +183,7 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_fwd_kernel(Blo
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 if (a.gate) {
-                    get8(p, (const T *)a.gate + (row / a.gate_div) * a.ldg + col[j], have[j]);
+                    get8(p, (const T *)a.gate + (int64_t)((uint32_t)row / (uint32_t)a.gate_div) * a.ldg + col[j], have[j]);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) f[j][i] *= gate_of<FAST>(p[i], a.act);
                 }
@@ -255,7 +288,7 @@ __device__ __forceinline__ void branch_terms(float (&d)[8], float (&fh)[8], floa
     load_or<T>(p, a.scale, col, have, 1.0f);
     if (a.gate) {
         float z[8];
-        get8(z, (const T *)a.gate + (row / a.gate_div) * a.ldg + col, have);
+        get8(z, (const T *)a.gate + (int64_t)((uint32_t)row / (uint32_t)a.gate_div) * a.ldg + col, have);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float G = gate_of<FAST>(z[i], a.act), q = d[i] * p[i];
@@ -273,10 +306,202 @@ __device__ __forceinline__ void branch_terms(float (&d)[8], float (&fh)[8], floa
     }
 }
 
-template <class T, int LANES, int V, bool F, bool N, bool SUMS>
+// Eight neighbouring values as they lie in memory.
+template <class T> struct Raw8 {
+    u32x4 v[sizeof(T) / 2];
+    __device__ __forceinline__ float operator[](int i) const
+    {
+        if constexpr (sizeof(T) == 2) return __uint_as_float(i & 1 ? v[0][i >> 1] & 0xffff0000u : v[0][i >> 1] << 16);
+        else return __uint_as_float(v[i >> 2][i & 3]);
+    }
+};
+// The first `have` values from p on and zeros; without a TAIL `have` is eight.
+template <bool TAIL, class T> __device__ __forceinline__ Raw8<T> raw8(const T *p, int have)
+{
+    Raw8<T> r;
+    if (!TAIL || have == 8) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.v[i] = get16(p + i * (16 / (int)sizeof(T)));
+    } else {
+        constexpr int E = 16 / (int)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            r.v[i] = u32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (i * E + j < have) {
+                    if constexpr (sizeof(T) == 2) r.v[i][j >> 1] |= (uint32_t)((const uint16_t *)p)[j] << (16 * (j & 1));
+                    else r.v[i][j] = ((const uint32_t *)p)[i * E + j];
+                }
+        }
+    }
+    return r;
+}
+// eight of a vector's values in 32 bits, or `otherwise` where there is none
+template <bool TAIL, class T> __device__ __forceinline__ void vector8(float (&v)[8], const void *p, int col, int have, float otherwise)
+{
+    if (p) {
+        const Raw8<T> r = raw8<TAIL>((const T *)p + col, have);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = r[i];
+    } else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = otherwise;
+}
+
+// A lane has the same eight channels of every row of its unit, the vectors' values for them and their sums over the rows in
+// registers, and the next row's values on their way while it works on one.  Without a TAIL the channels are a multiple
+// of eight: a lane has eight or none, and one that has none goes along with the first lane's (in bounds, left out of
+// the row's sums and not stored).
+//
+// With s = t act(gate), A = sum s (f - mu) r and B = sum s two sums over rows give three gradients:
+// dscale = w A + b B, dweight = scale A, dbias = scale B.
+template <class T, int LANES, bool F, bool N, bool TAIL>
 __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Block a, BlockGrads o)
 {
-    static_assert(V == 1 || !SUMS, "sums over rows of eight channels a lane");
+    constexpr bool FAST = sizeof(T) == 2;
+    __shared__ float2 lds[2][RowSum<LANES>::kWaves];
+    RowSum<LANES> sum(lds);
+    const int lane = threadIdx.x % LANES;
+    const bool live = lane * 8 < a.n;
+    const int col = TAIL || live ? lane * 8 : 0, have = TAIL ? max(0, min(8, a.n - col)) : 8;
+    constexpr int kUnits = LANES > 64 ? 1 : 64 / LANES;
+    int unit = (int)blockIdx.x * kUnits + (LANES > 64 ? 0 : threadIdx.x / LANES);
+    if constexpr (LANES == 64) unit = __builtin_amdgcn_readfirstlane(unit);
+    if (unit >= o.units.count) return;               // (whole rows of lanes; whole workgroups where there are barriers)
+    int64_t row, end;
+    range_of(o.units, unit, a.m, row, end);
+    const bool drops = F && a.drop.below != 0, next = N && o.dh, normed = F && a.norm != kNormNone;
+    const bool own_gates = F && o.dgate && a.gate_div == 1, whole_gates = F && o.dgate && a.gate_div > 1 && o.units.cuts == 1;
+    const DropKey key = drops ? drop_key(a.drop) : DropKey{};
+
+    float nw[8], w[8], b[8], scale[8];
+    if constexpr (N) vector8<TAIL, T>(nw, a.nw, col, have, 1.0f);
+    if constexpr (F) {
+        vector8<TAIL, T>(w, a.w, col, have, 1.0f);
+        vector8<TAIL, T>(b, a.b, col, have, 0.0f);
+        vector8<TAIL, T>(scale, a.scale, col, have, 1.0f);
+    }
+    float A[8], B[8], dgate[8], dnw[8], dnb[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) A[i] = B[i] = dgate[i] = dnw[i] = dnb[i] = 0.0f;
+
+    struct Row {
+        Raw8<T> dy, dh, y, f, z;
+        float4 st;
+    };
+    auto fetch = [&](int64_t r) __attribute__((always_inline)) {
+        Row v;
+        if (o.stats) v.st = o.stats[r];
+        else v.st = float4{0.0f, 1.0f, 0.0f, 1.0f};
+        if (o.dy) v.dy = raw8<TAIL>((const T *)o.dy + r * a.n + col, have);
+        if (next) {
+            v.dh = raw8<TAIL>((const T *)o.dh + r * a.n + col, have);
+            v.y = raw8<TAIL>((const T *)a.x + r * a.ldx + col, have);
+        }
+        if constexpr (F) {
+            v.f = raw8<TAIL>((const T *)a.f + r * a.ldf + col, have);
+            if (a.gate) v.z = raw8<TAIL>((const T *)a.gate + (int64_t)((uint32_t)r / (uint32_t)a.gate_div) * a.ldg + col, have);
+        }
+        return v;
+    };
+    Row ahead = fetch(row);                          // (a unit has at least one row)
+    for (; row < end; ++row) {
+        const Row v = ahead;
+        if (row + 1 < end) ahead = fetch(row + 1);
+        float d[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] = o.dy ? v.dy[i] : 0.0f;
+        if (next) {
+            float t[8], yh[8], s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float g = v.dh[i];
+                yh[i] = a.next == kNormLayer ? (v.y[i] - v.st.z) * v.st.w : v.y[i] * v.st.w;
+                t[i] = g * nw[i];
+                s1 += t[i];
+                s2 = fmaf(t[i], yh[i], s2);
+                dnw[i] = fmaf(g, yh[i], dnw[i]);
+                dnb[i] += g;
+            }
+            if (!TAIL && !live) s1 = s2 = 0.0f;
+            const float2 c = sum(s1, s2);
+            const float k1 = a.next == kNormLayer ? -v.st.w * c.x * a.inv_n : 0.0f, k2 = -v.st.w * c.y * a.inv_n;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                d[i] += fmaf(v.st.w, t[i], fmaf(yh[i], k2, k1));
+                if (TAIL && i >= have) d[i] = 0.0f;
+            }
+        }
+        if (o.dx && live) store8((T *)o.dx + row * a.n + col, d, have);
+        if constexpr (F) {
+            float fh[8], s1 = 0.0f, s2 = 0.0f;
+            if (drops) drop8(d, drop_numbers(key, (uint32_t)row, (uint32_t)col / 8), a.drop);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) fh[i] = !normed ? v.f[i] : a.norm == kNormLayer ? (v.f[i] - v.st.x) * v.st.y : v.f[i] * v.st.y;
+            if (a.gate) {
+                float dg[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float z = v.z[i], p = d[i] * fmaf(fh[i], w[i], b[i]) * scale[i];
+                    dg[i] = p * gate_slope<FAST>(z, a.act);
+                    dgate[i] += dg[i];
+                    d[i] *= gate_of<FAST>(z, a.act);
+                }
+                if (own_gates && live) store8((T *)o.dgate + row * a.n + col, dg, have);
+                if (whole_gates && ((uint32_t)row + 1) % (uint32_t)a.gate_div == 0) {
+                    if (live) store8((T *)o.dgate + (int64_t)((uint32_t)row / (uint32_t)a.gate_div) * a.n + col, dgate, have);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) dgate[i] = 0.0f;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                A[i] = fmaf(d[i], fh[i], A[i]);
+                B[i] += d[i];
+                d[i] *= scale[i];
+            }
+            if (normed) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    d[i] *= w[i];
+                    s1 += d[i];
+                    s2 = fmaf(d[i], fh[i], s2);
+                }
+                if (!TAIL && !live) s1 = s2 = 0.0f;
+                const float2 c = sum(s1, s2);
+                const float k1 = a.norm == kNormLayer ? -v.st.y * c.x * a.inv_n : 0.0f, k2 = -v.st.y * c.y * a.inv_n;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] = fmaf(v.st.y, d[i], fmaf(fh[i], k2, k1));
+            }
+            if (o.df && live) store8((T *)o.df + row * a.n + col, d, have);
+        }
+    }
+    if (!live) return;
+    auto leave = [&](int k, const float (&v)[8]) __attribute__((always_inline)) {
+        if (o.want >> k & 1) store8(o.place(k, unit, a.n) + col, v, have);
+    };
+    if constexpr (F) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = scale[i] * A[i];
+        leave(kDw, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = scale[i] * B[i];
+        leave(kDb, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = fmaf(w[i], A[i], b[i] * B[i]);
+        leave(kDscale, v);
+        leave(kVectors, dgate);
+    }
+    leave(kDnw, dnw);
+    leave(kDnb, dnb);
+}
+
+// Rows of more channels: one row after the other, without sums over them.
+template <class T, int LANES, int V, bool F, bool N>
+__global__ __launch_bounds__(LANES) void block_rows_kernel(Block a, BlockGrads o)
+{
     __shared__ float2 lds[2][RowSum<LANES>::kWaves];
     RowSum<LANES> sum(lds);
     const int lane = threadIdx.x % LANES;
@@ -289,18 +514,7 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
     const bool drops = F && a.drop.below != 0;
     const DropKey key = drops ? drop_key(a.drop) : DropKey{};
     const bool next = N && o.dh;
-    constexpr int kUnits = LANES > 64 ? 1 : 64 / LANES;
-    const int unit = (int)blockIdx.x * kUnits + (LANES > 64 ? 0 : threadIdx.x / LANES);
-    if (unit >= o.units.count) return;               // (whole rows of lanes; whole workgroups where there are barriers)
-    int64_t row, end;
-    range_of(o.units, unit, a.m, row, end);
-    float acc[SUMS ? kVectors + 1 : 1][8];
-    if constexpr (SUMS)
-#pragma unroll
-        for (int k = 0; k <= kVectors; ++k)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) acc[k][i] = 0.0f;
-    for (; row < end; ++row) {
+    for (int64_t row = blockIdx.x; row < a.m; row += gridDim.x) {
         const float4 st = (N || F) && o.stats ? o.stats[row] : float4{0.0f, 1.0f, 0.0f, 1.0f};
         float d[V][8];
 #pragma unroll
@@ -320,16 +534,12 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
                     for (int i = 0; i < 8; ++i) {
                         s1 += t[j][i];
                         s2 = fmaf(t[j][i], yh[j][i], s2);
-                        if constexpr (SUMS) {
-                            acc[kDnw][i] = fmaf(g[i], yh[j][i], acc[kDnw][i]);
-                            acc[kDnb][i] += g[i];
-                        }
                     }
                 }
                 float2 c = sum(s1, s2);
                 c.x = a.next == kNormLayer ? c.x * a.inv_n : 0.0f;
                 c.y *= a.inv_n;
-                if (!SUMS && o.row_sums && lane == 0) o.row_sums[row] = c;
+                if (o.row_sums && lane == 0) o.row_sums[row] = c;
 #pragma unroll
                 for (int j = 0; j < V; ++j)
 #pragma unroll
@@ -346,14 +556,6 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
             for (int j = 0; j < V; ++j) {
                 branch_terms<T>(d[j], fh[j], dscale, dgate, a, st, drops, key, row, col[j], have[j]);
                 if (o.dgate && a.gate_div == 1) store8((T *)o.dgate + row * a.n + col[j], dgate, have[j]);
-                if constexpr (SUMS)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        acc[kDscale][i] += dscale[i];
-                        acc[kVectors][i] += dgate[i];
-                        acc[kDw][i] = fmaf(d[j][i], fh[j][i], acc[kDw][i]);
-                        acc[kDb][i] += d[j][i];
-                    }
                 if (a.norm != kNormNone) {
                     float p[8];
                     load_or<T>(p, a.w, col[j], have[j], 1.0f);
@@ -377,18 +579,7 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
             if (o.df)
 #pragma unroll
                 for (int j = 0; j < V; ++j) store8((T *)o.df + row * a.n + col[j], d[j], have[j]);
-            if constexpr (SUMS)
-                if (o.dgate && a.gate_div > 1 && o.units.cuts == 1 && (row + 1) % a.gate_div == 0) {
-                    store8((T *)o.dgate + row / a.gate_div * a.n + col[0], acc[kVectors], have[0]);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) acc[kVectors][i] = 0.0f;
-                }
         }
-    }
-    if constexpr (SUMS) {
-#pragma unroll
-        for (int k = 0; k <= kVectors; ++k)
-            if (o.want >> k & 1) store8(o.place(k, unit, a.n) + col[0], acc[k], have[0]);
     }
 }
 
@@ -437,8 +628,8 @@ __global__ __launch_bounds__(256) void block_sums_kernel(Block a, BlockGrads o)
                 acc[kDw][i] = fmaf(d[i], fh[i], acc[kDw][i]);
                 acc[kDb][i] += d[i];
             }
-            if (o.dgate && a.gate_div > 1 && o.units.cuts == 1 && (row + 1) % a.gate_div == 0) {
-                store8((T *)o.dgate + row / a.gate_div * a.n + col, acc[kVectors], have);
+            if (o.dgate && a.gate_div > 1 && o.units.cuts == 1 && ((uint32_t)row + 1) % (uint32_t)a.gate_div == 0) {
+                store8((T *)o.dgate + (int64_t)((uint32_t)row / (uint32_t)a.gate_div) * a.n + col, acc[kVectors], have);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) acc[kVectors][i] = 0.0f;
             }
@@ -457,9 +648,10 @@ struct Joins {
     void *gate_to;
     int32_t vectors, units, cuts, n;
 };
-template <class T> __global__ __launch_bounds__(256) void block_join_kernel(Joins j)
+template <class T> __global__ __launch_bounds__(1024) void block_join_kernel(Joins j)
 {
-    __shared__ float part[8][32];
+    constexpr int kGroups = 32;
+    __shared__ float part[kGroups][32];
     const int c = threadIdx.x & 31, g = threadIdx.x >> 5, col = (int)blockIdx.x * 32 + c, y = blockIdx.y;
     const float *from = y < j.vectors ? j.from[y] : j.gate_from + (int64_t)(y - j.vectors) * j.cuts * j.n;
     T *to = y < j.vectors ? (T *)j.to[y] : (T *)j.gate_to + (int64_t)(y - j.vectors) * j.n;
@@ -467,13 +659,13 @@ template <class T> __global__ __launch_bounds__(256) void block_join_kernel(Join
     float s = 0.0f;
     if (col < j.n)
 #pragma unroll 8
-        for (int u = g; u < count; u += 8) s += from[(int64_t)u * j.n + col];
+        for (int u = g; u < count; u += kGroups) s += from[(int64_t)u * j.n + col];
     part[g][c] = s;
     __syncthreads();
     if (g == 0 && col < j.n) {
         s = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s += part[i][c];
+        for (int i = 0; i < kGroups; ++i) s += part[i][c];
         to[col] = narrow<T>(s);
     }
 }

@@ -29,8 +29,9 @@ struct Units {
 inline Units block_units(int64_t m, int64_t n, bool shared_gate, int64_t gate_div)
 {
     const int lanes = block_lanes(n);
-    const int64_t most = lanes > kMostSumLanes ? 256 : lanes >= 64 ? 1024 : 1024 * 64 / lanes;
-    int64_t rows = m > most ? tiles(m, most) : 1;
+    const int64_t most = lanes > kMostSumLanes ? 256 : 256 * 768 / lanes;
+    int64_t rows = tiles(m, most);
+    if (rows < 2) rows = m > 512 ? 2 : 1;
     Units u{m, 0, 1, 0, 0};
     if (shared_gate && gate_div > rows) {
         u.cuts = (int32_t)tiles(gate_div, rows);

@@ -11,7 +11,7 @@ inline int64_t groups_of(int64_t n) { return tiles(n, TV_MX4_GROUP); }
 inline int64_t scale_rows(int64_t rows) { return up(rows, 4); }
 
 // How a call goes.  kFew4: the weight streamed through registers, x taken to 4 bits by each workgroup (own) or before.
-enum Kind4 { kFew4, kTile64x4, kTile128x4, kTile256x4 };
+enum Kind4 { kFew4, kTile64x4, kTile128x4, kTile256x4, kTile128x4Two };
 struct Choice4 {
     Kind4 kind;
     bool own;

@@ -96,14 +96,25 @@ int block_fwd(const Block &a, void *y, void *h, float *stats, hipStream_t stream
     }
 }
 
-template <class T, int LANES, int V, bool SUMS>
+template <class T, int LANES>
 int launch_bwd(const Block &a, const BlockGrads &o, hipStream_t stream)
 {
     const int units = LANES > 64 ? 1 : 64 / LANES;
     const dim3 grid((uint32_t)tiles(o.units.count, units)), block(LANES > 64 ? LANES : 64);
-    if (a.f && a.next) hipLaunchKernelGGL((block_bwd_kernel<T, LANES, V, true, true, SUMS>), grid, block, 0, stream, a, o);
-    else if (a.f) hipLaunchKernelGGL((block_bwd_kernel<T, LANES, V, true, false, SUMS>), grid, block, 0, stream, a, o);
-    else hipLaunchKernelGGL((block_bwd_kernel<T, LANES, V, false, true, SUMS>), grid, block, 0, stream, a, o);
+    const bool tail = a.n % 8 != 0;
+    if (a.f && a.next) hipLaunchKernelGGL((tail ? block_bwd_kernel<T, LANES, true, true, true> : block_bwd_kernel<T, LANES, true, true, false>), grid, block, 0, stream, a, o);
+    else if (a.f) hipLaunchKernelGGL((tail ? block_bwd_kernel<T, LANES, true, false, true> : block_bwd_kernel<T, LANES, true, false, false>), grid, block, 0, stream, a, o);
+    else hipLaunchKernelGGL((tail ? block_bwd_kernel<T, LANES, false, true, true> : block_bwd_kernel<T, LANES, false, true, false>), grid, block, 0, stream, a, o);
+    return launched();
+}
+
+template <class T, int V>
+int launch_rows(const Block &a, const BlockGrads &o, hipStream_t stream)
+{
+    const dim3 grid((uint32_t)(a.m < kMostGroups ? a.m : kMostGroups)), block(1024);
+    if (a.f && a.next) hipLaunchKernelGGL((block_rows_kernel<T, 1024, V, true, true>), grid, block, 0, stream, a, o);
+    else if (a.f) hipLaunchKernelGGL((block_rows_kernel<T, 1024, V, true, false>), grid, block, 0, stream, a, o);
+    else hipLaunchKernelGGL((block_rows_kernel<T, 1024, V, false, true>), grid, block, 0, stream, a, o);
     return launched();
 }
 
@@ -113,17 +124,15 @@ int block_bwd(const Block &a, BlockGrads o, const tv_block_grads &g, const Block
     int st = TV_OK;
     switch (a.m > 0 ? block_lanes(a.n) : 0) {
     case 0: break;
-    case 8: st = launch_bwd<T, 8, 1, true>(a, o, stream); break;
-    case 32: st = launch_bwd<T, 32, 1, true>(a, o, stream); break;
-    case 64: st = launch_bwd<T, 64, 1, true>(a, o, stream); break;
-    case 128: st = launch_bwd<T, 128, 1, true>(a, o, stream); break;
-    case 256: st = launch_bwd<T, 256, 1, true>(a, o, stream); break;
-    case 512: st = launch_bwd<T, 512, 1, true>(a, o, stream); break;
+    case 8: st = launch_bwd<T, 8>(a, o, stream); break;
+    case 32: st = launch_bwd<T, 32>(a, o, stream); break;
+    case 64: st = launch_bwd<T, 64>(a, o, stream); break;
+    case 128: st = launch_bwd<T, 128>(a, o, stream); break;
+    case 256: st = launch_bwd<T, 256>(a, o, stream); break;
+    case 512: st = launch_bwd<T, 512>(a, o, stream); break;
     default: {
-        // rows one by one first, each a unit; then the sums over them
-        BlockGrads rows = o;
-        rows.units = {a.m, 1, 1, (int32_t)a.m, (int32_t)a.m};
-        st = a.n <= 8192 ? launch_bwd<T, 1024, 1, false>(a, rows, stream) : launch_bwd<T, 1024, 2, false>(a, rows, stream);
+        // rows first; then the sums over them
+        st = a.n <= 8192 ? launch_rows<T, 1>(a, o, stream) : launch_rows<T, 2>(a, o, stream);
         if (st != TV_OK || !(p.want || (o.dgate && a.gate_div > 1))) break;
         const dim3 grid((uint32_t)tiles(a.n, 2048), (uint32_t)o.units.count), block(256);
         if (a.f && a.next) hipLaunchKernelGGL((block_sums_kernel<T, true, true>), grid, block, 0, stream, a, o);
@@ -150,7 +159,7 @@ int block_bwd(const Block &a, BlockGrads o, const tv_block_grads &g, const Block
     }
     j.units = p.units.count; j.cuts = p.units.cuts; j.n = a.n;
     if (sums == 0) return TV_OK;
-    hipLaunchKernelGGL((block_join_kernel<T>), dim3((uint32_t)tiles(a.n, 32), (uint32_t)sums), dim3(256), 0, stream, j);
+    hipLaunchKernelGGL((block_join_kernel<T>), dim3((uint32_t)tiles(a.n, 32), (uint32_t)sums), dim3(1024), 0, stream, j);
     return launched();
 }
 

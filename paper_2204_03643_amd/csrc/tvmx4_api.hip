@@ -42,12 +42,12 @@ int check_sizes(const tv_linear_desc &d, bool codes)
     return TV_OK;
 }
 
-template <class T, int BM, int BN, int WM, int WN, int BUF>
+template <class T, int BM, int BN, int WM, int WN, int BUF, int G>
 void launch_tiles(Product g, const Scales &scales, const Epilogue &e, hipStream_t stream)
 {
     g.tiles_m = (uint32_t)tiles(g.M, BM);
     g.tiles_n = (uint32_t)tiles(g.N, BN);
-    hipLaunchKernelGGL((gemm4_kernel<T, BM, BN, WM, WN, BUF>), dim3(g.tiles_m * g.tiles_n, g.splits), dim3(WM * WN * 64), 0, stream, g, scales, e);
+    hipLaunchKernelGGL((gemm4_kernel<T, BM, BN, WM, WN, BUF, G>), dim3(g.tiles_m * g.tiles_n, g.splits), dim3(WM * WN * 64), 0, stream, g, scales, e);
 }
 
 template <class T, int NT, bool OWN>
@@ -73,9 +73,10 @@ int linear4(const void *x, const uint8_t *x_exps, const uint8_t *w, const uint8_
         if (save<T>(x, ws, ws + p.exps, d.m, d.k, d.ldx, stream) != TV_OK) return TV_ERR_HIP;
         g.a = ws;
     }
-    if (p.c.kind == kTile256x4) launch_tiles<T, 256, 256, 2, 4, 2>(g, s, e, stream);
-    if (p.c.kind == kTile128x4) launch_tiles<T, 128, 128, 2, 2, 4>(g, s, e, stream);
-    if (p.c.kind == kTile64x4) launch_tiles<T, 64, 128, 2, 2, 4>(g, s, e, stream);
+    if (p.c.kind == kTile256x4) launch_tiles<T, 256, 256, 2, 4, 2, 2>(g, s, e, stream);
+    if (p.c.kind == kTile128x4) launch_tiles<T, 128, 128, 2, 2, 4, 2>(g, s, e, stream);
+    if (p.c.kind == kTile128x4Two) launch_tiles<T, 128, 256, 2, 2, 3, 1>(g, s, e, stream);
+    if (p.c.kind == kTile64x4) launch_tiles<T, 64, 128, 2, 2, 4, 2>(g, s, e, stream);
     if (p.c.kind == kFew4) {
         const Rows4 rows{g.a, s.x, d.ldx, s.x_rows, (int32_t)d.k};
         if (p.c.own) launch_few<T, 1, true>(g, rows, s, e, stream);
