@@ -104,6 +104,49 @@ template <class T> __device__ __forceinline__ void load_or(float (&v)[8], const 
         for (int i = 0; i < 8; ++i) v[i] = otherwise;
 }
 
+// Eight neighbouring values as they lie in memory.
+template <class T> struct Raw8 {
+    u32x4 v[sizeof(T) / 2];
+    __device__ __forceinline__ float operator[](int i) const
+    {
+        if constexpr (sizeof(T) == 2) return __uint_as_float(i & 1 ? v[0][i >> 1] & 0xffff0000u : v[0][i >> 1] << 16);
+        else return __uint_as_float(v[i >> 2][i & 3]);
+    }
+};
+// The first `have` values from p on and zeros; without a TAIL `have` is eight.
+template <bool TAIL, class T> __device__ __forceinline__ Raw8<T> raw8(const T *p, int have)
+{
+    Raw8<T> r;
+    if (!TAIL || have == 8) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.v[i] = get16(p + i * (16 / (int)sizeof(T)));
+    } else {
+        constexpr int E = 16 / (int)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            r.v[i] = u32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (i * E + j < have) {
+                    if constexpr (sizeof(T) == 2) r.v[i][j >> 1] |= (uint32_t)((const uint16_t *)p)[j] << (16 * (j & 1));
+                    else r.v[i][j] = ((const uint32_t *)p)[i * E + j];
+                }
+        }
+    }
+    return r;
+}
+// eight of a vector's values in 32 bits, or `otherwise` where there is none
+template <bool TAIL, class T> __device__ __forceinline__ void vector8(float (&v)[8], const void *p, int col, int have, float otherwise)
+{
+    if (p) {
+        const Raw8<T> r = raw8<TAIL>((const T *)p + col, have);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = r[i];
+    } else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = otherwise;
+}
+
 // (mean, r) of a row that the lanes hold; v becomes (v - mean) r.  The variance is taken of the differences from the mean.
 template <int LANES, int V>
 __device__ __forceinline__ float2 normalise(float (&v)[V][8], const int (&have)[V], bool layer, float eps, float inv_n,
@@ -135,9 +178,106 @@ __device__ __forceinline__ float2 normalise(float (&v)[V][8], const int (&have)[
     return {mean, r};
 }
 
-// LANES lanes a row, V vectors of eight channels a lane.  F: there is an f; N: there is a next norm.
-template <class T, int LANES, int V, bool F, bool N>
+// Eight channels of each row a lane, LANES lanes a row.  F: there is an f; N: there is a next norm.  TAIL as in the backward
+// kernel below: without one, lanes beyond the row's end go along with the first lane's channels.
+template <class T, int LANES, bool F, bool N, bool TAIL>
 __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_fwd_kernel(Block a, T *y, T *h, float4 *stats)
+{
+    constexpr bool FAST = sizeof(T) == 2;
+    constexpr int kThreads = LANES > 64 ? LANES : 256, kRows = kThreads / LANES;
+    __shared__ float2 lds[2][RowSum<LANES>::kWaves];
+    RowSum<LANES> sum(lds);
+    const int lane = threadIdx.x % LANES;
+    const bool live = lane * 8 < a.n;
+    const int col = TAIL || live ? lane * 8 : 0, have = TAIL ? max(0, min(8, a.n - col)) : 8;
+    const bool drops = F && a.drop.below != 0;
+    const DropKey key = drops ? drop_key(a.drop) : DropKey{};
+    // (mean, r) of the values that the lanes hold, which become (v - mean) r; the variance is that of the differences
+    auto normalise = [&](float (&v)[8], int kind) __attribute__((always_inline)) {
+        float mean = 0.0f, s = 0.0f;
+        if (kind == kNormLayer) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += v[i];            // (zeros beyond the row's end)
+            mean = sum(TAIL || live ? s : 0.0f) * a.inv_n;
+            s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = !TAIL || i < have ? v[i] - mean : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s = fmaf(v[i], v[i], s);
+        const float r = 1.0f / sqrtf(fmaf(sum(TAIL || live ? s : 0.0f), a.inv_n, a.eps));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= r;
+        return float2{mean, r};
+    };
+    int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES;
+    if constexpr (LANES == 64) row = (int64_t)blockIdx.x * kRows + __builtin_amdgcn_readfirstlane(threadIdx.x / LANES);
+    for (; row < a.m; row += (int64_t)gridDim.x * kRows) {
+        float v[8];
+        float4 st = {0.0f, 0.0f, 0.0f, 0.0f};
+        const Raw8<T> x = raw8<TAIL>((const T *)a.x + row * a.ldx + col, have);
+        if constexpr (F) {
+            const Raw8<T> raw = raw8<TAIL>((const T *)a.f + row * a.ldf + col, have);
+            Raw8<T> z;
+            if (a.gate) z = raw8<TAIL>((const T *)a.gate + (int64_t)((uint32_t)row / (uint32_t)a.gate_div) * a.ldg + col, have);
+            float f[8], p[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = raw[i];
+            if (a.norm != kNormNone) {
+                const float2 s = normalise(f, a.norm);
+                st.x = s.x;
+                st.y = s.y;
+                if (a.w) {
+                    vector8<TAIL, T>(p, a.w, col, have, 1.0f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) f[i] *= p[i];
+                }
+                if (a.b) {
+                    vector8<TAIL, T>(p, a.b, col, have, 0.0f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) f[i] += p[i];
+                }
+            }
+            if (a.gate)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] *= gate_of<FAST>(z[i], a.act);
+            if (a.scale) {
+                vector8<TAIL, T>(p, a.scale, col, have, 1.0f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] *= p[i];
+            }
+            if (drops) drop8(f, drop_numbers(key, (uint32_t)row, (uint32_t)col / 8), a.drop);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = x[i] + f[i];
+            if (y && live) store8(y + row * a.n + col, v, have);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = x[i];
+        }
+        if constexpr (N) {
+            const float2 s = normalise(v, a.next);
+            st.z = s.x;
+            st.w = s.y;
+            float p[8];
+            if (a.nw) {
+                vector8<TAIL, T>(p, a.nw, col, have, 1.0f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= p[i];
+            }
+            if (a.nb) {
+                vector8<TAIL, T>(p, a.nb, col, have, 0.0f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] += p[i];
+            }
+            if (live) store8(h + row * a.n + col, v, have);
+        }
+        if (stats && lane == 0) stats[row] = st;
+    }
+}
+
+// Rows of more than 8192 channels: V vectors of eight a lane.
+template <class T, int LANES, int V, bool F, bool N>
+__global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_fwd_long_kernel(Block a, T *y, T *h, float4 *stats)
 {
     constexpr bool FAST = sizeof(T) == 2;
     constexpr int kThreads = LANES > 64 ? LANES : 256, kRows = kThreads / LANES;
@@ -304,49 +444,6 @@ __device__ __forceinline__ void branch_terms(float (&d)[8], float (&fh)[8], floa
             d[i] *= p[i];
         }
     }
-}
-
-// Eight neighbouring values as they lie in memory.
-template <class T> struct Raw8 {
-    u32x4 v[sizeof(T) / 2];
-    __device__ __forceinline__ float operator[](int i) const
-    {
-        if constexpr (sizeof(T) == 2) return __uint_as_float(i & 1 ? v[0][i >> 1] & 0xffff0000u : v[0][i >> 1] << 16);
-        else return __uint_as_float(v[i >> 2][i & 3]);
-    }
-};
-// The first `have` values from p on and zeros; without a TAIL `have` is eight.
-template <bool TAIL, class T> __device__ __forceinline__ Raw8<T> raw8(const T *p, int have)
-{
-    Raw8<T> r;
-    if (!TAIL || have == 8) {
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.v[i] = get16(p + i * (16 / (int)sizeof(T)));
-    } else {
-        constexpr int E = 16 / (int)sizeof(T);
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-            r.v[i] = u32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int j = 0; j < E; ++j)
-                if (i * E + j < have) {
-                    if constexpr (sizeof(T) == 2) r.v[i][j >> 1] |= (uint32_t)((const uint16_t *)p)[j] << (16 * (j & 1));
-                    else r.v[i][j] = ((const uint32_t *)p)[i * E + j];
-                }
-        }
-    }
-    return r;
-}
-// eight of a vector's values in 32 bits, or `otherwise` where there is none
-template <bool TAIL, class T> __device__ __forceinline__ void vector8(float (&v)[8], const void *p, int col, int have, float otherwise)
-{
-    if (p) {
-        const Raw8<T> r = raw8<TAIL>((const T *)p + col, have);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = r[i];
-    } else
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = otherwise;
 }
 
 // A lane has the same eight channels of every row of its unit, the vectors' values for them and their sums over the rows in

@@ -70,15 +70,26 @@ Block block_of(const tv_block_in &in, const tv_block_desc &d)
     return a;
 }
 
-template <class T, int LANES, int V>
+template <class T, int LANES>
 int launch_fwd(const Block &a, void *y, void *h, float *stats, hipStream_t stream)
 {
     constexpr int kThreads = LANES > 64 ? LANES : 256;
     const int64_t groups = tiles(a.m, kThreads / LANES);
     const dim3 grid((uint32_t)(groups < kMostGroups ? groups : kMostGroups)), block(kThreads);
-    if (a.f && a.next) hipLaunchKernelGGL((block_fwd_kernel<T, LANES, V, true, true>), grid, block, 0, stream, a, (T *)y, (T *)h, (float4 *)stats);
-    else if (a.f) hipLaunchKernelGGL((block_fwd_kernel<T, LANES, V, true, false>), grid, block, 0, stream, a, (T *)y, (T *)h, (float4 *)stats);
-    else hipLaunchKernelGGL((block_fwd_kernel<T, LANES, V, false, true>), grid, block, 0, stream, a, (T *)y, (T *)h, (float4 *)stats);
+    const bool tail = a.n % 8 != 0;
+    if (a.f && a.next) hipLaunchKernelGGL((tail ? block_fwd_kernel<T, LANES, true, true, true> : block_fwd_kernel<T, LANES, true, true, false>), grid, block, 0, stream, a, (T *)y, (T *)h, (float4 *)stats);
+    else if (a.f) hipLaunchKernelGGL((tail ? block_fwd_kernel<T, LANES, true, false, true> : block_fwd_kernel<T, LANES, true, false, false>), grid, block, 0, stream, a, (T *)y, (T *)h, (float4 *)stats);
+    else hipLaunchKernelGGL((tail ? block_fwd_kernel<T, LANES, false, true, true> : block_fwd_kernel<T, LANES, false, true, false>), grid, block, 0, stream, a, (T *)y, (T *)h, (float4 *)stats);
+    return launched();
+}
+
+template <class T>
+int launch_fwd_long(const Block &a, void *y, void *h, float *stats, hipStream_t stream)
+{
+    const dim3 grid((uint32_t)(a.m < kMostGroups ? a.m : kMostGroups)), block(1024);
+    if (a.f && a.next) hipLaunchKernelGGL((block_fwd_long_kernel<T, 1024, 2, true, true>), grid, block, 0, stream, a, (T *)y, (T *)h, (float4 *)stats);
+    else if (a.f) hipLaunchKernelGGL((block_fwd_long_kernel<T, 1024, 2, true, false>), grid, block, 0, stream, a, (T *)y, (T *)h, (float4 *)stats);
+    else hipLaunchKernelGGL((block_fwd_long_kernel<T, 1024, 2, false, true>), grid, block, 0, stream, a, (T *)y, (T *)h, (float4 *)stats);
     return launched();
 }
 
@@ -86,13 +97,13 @@ template <class T>
 int block_fwd(const Block &a, void *y, void *h, float *stats, hipStream_t stream)
 {
     switch (block_lanes(a.n)) {
-    case 8: return launch_fwd<T, 8, 1>(a, y, h, stats, stream);
-    case 32: return launch_fwd<T, 32, 1>(a, y, h, stats, stream);
-    case 64: return launch_fwd<T, 64, 1>(a, y, h, stats, stream);
-    case 128: return launch_fwd<T, 128, 1>(a, y, h, stats, stream);
-    case 256: return launch_fwd<T, 256, 1>(a, y, h, stats, stream);
-    case 512: return launch_fwd<T, 512, 1>(a, y, h, stats, stream);
-    default: return a.n <= 8192 ? launch_fwd<T, 1024, 1>(a, y, h, stats, stream) : launch_fwd<T, 1024, 2>(a, y, h, stats, stream);
+    case 8: return launch_fwd<T, 8>(a, y, h, stats, stream);
+    case 32: return launch_fwd<T, 32>(a, y, h, stats, stream);
+    case 64: return launch_fwd<T, 64>(a, y, h, stats, stream);
+    case 128: return launch_fwd<T, 128>(a, y, h, stats, stream);
+    case 256: return launch_fwd<T, 256>(a, y, h, stats, stream);
+    case 512: return launch_fwd<T, 512>(a, y, h, stats, stream);
+    default: return a.n <= 8192 ? launch_fwd<T, 1024>(a, y, h, stats, stream) : launch_fwd_long<T>(a, y, h, stats, stream);
     }
 }
 
