@@ -30,8 +30,10 @@ class _Border(typing.NamedTuple):
     eps: float
     gate_div: int
     drop: int                # of 65536
-    seed: int
     offset: int
+
+
+_border = functools.lru_cache(maxsize=4096)(_Border)
 
 
 def _check_number(v, what):
@@ -63,10 +65,11 @@ def _check_drop(p, seed, offset, like, what):
 def _check_channels(t, n, what, like):
     if t is None:
         return None
-    _check_tensor(t, what, like)
-    if t.dim() != 1 or t.shape[0] != n:
+    if t.dtype is not like.dtype or t.device != like.device:
+        _check_tensor(t, what, like)
+    if t.shape != (n,):
         raise ValueError("%s: shape (%d,) expected, got %r" % (what, n, tuple(t.shape)))
-    return t.contiguous()
+    return t if t.is_contiguous() else t.contiguous()
 
 
 def _gate_div(x, gate, what):
@@ -82,77 +85,97 @@ def _gate_div(x, gate, what):
     return max(1, math.prod(lead[k:]))
 
 
+# How much workspace a backward call needs, which its sizes and what is given and wanted say in full.
+@functools.lru_cache(maxsize=4096)
+def _workspace_bytes(m, n, dtype, has_f, has_gate, border, want):
+    ins = _b.tv_block_in(16, 16 if has_f else None, None, None, 16 if has_gate else None, None, None, None)
+    dx, df, dweight, dbias, dgate, dscale, dnext_weight, dnext_bias = (16 if w else None for w in want)
+    return _b.tv_block_bwd_workspace_bytes(ins, _b.tv_block_grads(dx, df, dgate, dweight, dbias, dscale, dnext_weight, dnext_bias),
+                                           _desc(m, n, n, n, n, dtype, border))
+
+
 @functools.lru_cache(maxsize=4096)
 def _desc(m, n, ldx, ldf, ldg, dtype, border):
     return _b.tv_block_desc(m, n, ldx, ldf, ldg, border.gate_div, dtype, border.norm, border.next_norm, border.act, border.eps,
                             _NO_DROP)
 
 
-def _desc_of(m, n, ldx, ldf, ldg, dtype, border, seed_at):
+def _desc_of(m, n, ldx, ldf, ldg, dtype, border, seed, seed_at):
     if not border.drop:
         return _desc(m, n, ldx, ldf, ldg, dtype, border)
     return _b.tv_block_desc(m, n, ldx, ldf, ldg, border.gate_div, dtype, border.norm, border.next_norm, border.act, border.eps,
-                            _b.tv_drop(border.seed, border.offset, _address(seed_at), border.drop))
-
-
-def _rows_of(t, n):
-    return (None, n) if t is None else _as_rows(t)
+                            _b.tv_drop(seed, border.offset, _address(seed_at), border.drop))
 
 
 @_on_device
-def _forward(x, f, weight, bias, gate, scale, next_weight, next_bias, border, seed_at, hold):
+def _forward(x, f, weight, bias, gate, scale, next_weight, next_bias, border, seed, seed_at, hold):
     """(y, h, stats): None where there is none."""
     n = x.shape[-1]
     m = x.numel() // n
     rows, ldx = _as_rows(x)
-    frows, ldf = _rows_of(f, n)
-    grows, ldg = _rows_of(gate, n)
-    y = x.new_empty(x.shape) if f is not None else None
-    h = x.new_empty(x.shape) if border.next_norm else None
-    stats = x.new_empty((m, 4), dtype=torch.float32) if hold else None
-    ins = _b.tv_block_in(rows.data_ptr(), _address(frows), _address(weight), _address(bias), _address(grows), _address(scale),
-                         _address(next_weight), _address(next_bias))
-    _check(_b.lib().tv_block_fwd(ins, _address(y), _address(h), _address(stats),
-                                 _desc_of(m, n, ldx, ldf, ldg, _DTYPES[x.dtype], border, seed_at), _b._stream(None)))
+    y = h = stats = at_f = at_gate = at_y = at_h = at_stats = None
+    ldf = ldg = n
+    if f is not None:
+        frows, ldf = _as_rows(f)
+        y = x.new_empty(x.shape)
+        at_f, at_y = frows.data_ptr(), y.data_ptr()
+        if gate is not None:
+            grows, ldg = _as_rows(gate)
+            at_gate = grows.data_ptr()
+    if border.next_norm:
+        h = x.new_empty(x.shape)
+        at_h = h.data_ptr()
+    if hold:
+        stats = x.new_empty((m, 4), dtype=torch.float32)
+        at_stats = stats.data_ptr()
+    ins = _b.tv_block_in(rows.data_ptr(), at_f, _address(weight), _address(bias), at_gate, _address(scale), _address(next_weight),
+                         _address(next_bias))
+    _check(_b.lib().tv_block_fwd(ins, at_y, at_h, at_stats, _desc_of(m, n, ldx, ldf, ldg, _DTYPES[x.dtype], border, seed, seed_at),
+                                 _b._stream(None)))
     return y, h, stats
 
 
 @_on_device
-def _backward(like, dy, dh, x, f, weight, bias, gate, scale, next_weight, stats, border, seed_at, want):
+def _backward(like, dy, dh, x, f, weight, bias, gate, scale, next_weight, stats, border, seed, seed_at, want):
     """Gradients of x, f, weight, bias, gate, scale, next_weight, next_bias, None where not wanted."""
-    n = like.shape[-1]
-    m = like.numel() // n
-    rows, ldx = _rows_of(x, n)
-    frows, ldf = _rows_of(f, n)
-    grows, ldg = _rows_of(gate, n)
-    made = [like.new_empty(like.shape) if want[0] else None, like.new_empty(like.shape) if want[1] else None,
-            like.new_empty(n) if want[2] else None, like.new_empty(n) if want[3] else None,
-            like.new_empty(gate.shape) if want[4] else None, like.new_empty(n) if want[5] else None,
-            like.new_empty(n) if want[6] else None, like.new_empty(n) if want[7] else None]
-    dx, df, dweight, dbias, dgate, dscale, dnext_weight, dnext_bias = map(_address, made)
-    ins = _b.tv_block_in(_address(rows), _address(frows), _address(weight), _address(bias), _address(grows), _address(scale),
-                         _address(next_weight), None)
-    grads = _b.tv_block_grads(dx, df, dgate, dweight, dbias, dscale, dnext_weight, dnext_bias)
-    desc = _desc_of(m, n, ldx, ldf, ldg, _DTYPES[like.dtype], border, seed_at)
-    nbytes = _b.lib().tv_block_bwd_workspace_bytes(ins, grads, desc)
+    shape, n = like.shape, like.shape[-1]
+    m, dtype = like.numel() // n, _DTYPES[like.dtype]
+    at_x = at_f = at_gate = None
+    ldx = ldf = ldg = n
+    if x is not None:
+        x, ldx = _as_rows(x)
+        at_x = x.data_ptr()
+    if f is not None:
+        f, ldf = _as_rows(f)
+        at_f = f.data_ptr()
+        if gate is not None:
+            grows, ldg = _as_rows(gate)
+            at_gate = grows.data_ptr()
+    shapes = (shape, shape, n, n, None if gate is None else gate.shape, n, n, n)
+    made = [like.new_empty(s) if w else None for s, w in zip(shapes, want)]
+    dx, df, dweight, dbias, dgate, dscale, dnext_weight, dnext_bias = [None if t is None else t.data_ptr() for t in made]
+    ins = _b.tv_block_in(at_x, at_f, _address(weight), _address(bias), at_gate, _address(scale), _address(next_weight), None)
+    nbytes = _workspace_bytes(m, n, dtype, f is not None, gate is not None, border, want)
     ws = like.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
-    _check(_b.lib().tv_block_bwd(_address(dy), _address(dh), ins, _address(stats), grads, desc, _address(ws), nbytes, _b._stream(None)))
+    _check(_b.lib().tv_block_bwd(_address(dy), _address(dh), ins, _address(stats),
+                                 _b.tv_block_grads(dx, df, dgate, dweight, dbias, dscale, dnext_weight, dnext_bias),
+                                 _desc_of(m, n, ldx, ldf, ldg, dtype, border, seed, seed_at), _address(ws), nbytes, _b._stream(None)))
     return made
 
 
 class _BorderFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, f, weight, bias, gate, scale, next_weight, next_bias, border, seed_at):
+    def forward(ctx, x, f, weight, bias, gate, scale, next_weight, next_bias, border, seed, seed_at):
         if _tangent_among(x, f, weight, bias, gate, scale, next_weight, next_bias):
             raise NotImplementedError("tv_norm, tv_residual: no forward-mode derivative")
         normed = border.next_norm or (f is not None and border.norm)
-        y, h, stats = _forward(x, f, weight, bias, gate, scale, next_weight, next_bias, border, seed_at, normed)
+        y, h, stats = _forward(x, f, weight, bias, gate, scale, next_weight, next_bias, border, seed, seed_at, normed)
         # the next norm's gradient is taken at y as it was returned
         at = (x if f is None else y) if border.next_norm else None
         saved = (at, f, weight, bias, gate, scale, next_weight, stats, seed_at)
         ctx.save_for_backward(*saved)
         ctx.saved_as = [None if t is None else (t.shape, t.dtype) for t in saved]
-        ctx.border = border
+        ctx.border, ctx.seed = border, seed
         ctx.set_materialize_grads(False)
         return h if y is None else y if h is None else (y, h)
 
@@ -163,7 +186,7 @@ class _BorderFunction(torch.autograd.Function):
         saved = ctx.saved_tensors
         like = next((g for g in grads if g is not None), None)
         if like is None:
-            return (None,) * 10
+            return (None,) * 11
         if _tangent_among(*grads):
             raise NotImplementedError("tv_norm, tv_residual: the gradients have no forward-mode derivative")
         # (hooks on saved tensors may bring back others, with the same values in strides of their own)
@@ -175,31 +198,37 @@ class _BorderFunction(torch.autograd.Function):
             dy, dh = None, grads[0]
         else:
             dy, dh = grads if border.next_norm else (grads[0], None)
-        dy, dh = (None if g is None else g.contiguous() for g in (dy, dh))
+        if dy is not None:
+            dy = dy.contiguous()
+        if dh is not None:
+            dh = dh.contiguous()
         # without a gradient through the next norm, x's is y's
-        want = [need[0] and dh is not None] + list(need[1:8])
+        want = (need[0] and dh is not None, *need[1:8])
         if like.numel() == 0:
             shapes = [like.shape, like.shape] + [like.shape[-1:]] * 6
             if gate is not None:
                 shapes[4] = gate.shape
             made = [like.new_zeros(s) if w else None for s, w in zip(shapes, need)]
         elif any(want):
-            weight, bias, scale, next_weight, stats = (None if t is None else t.contiguous() for t in (weight, bias, scale, next_weight, stats))
-            made = _backward(like, dy, dh, at, f, weight, bias, gate, scale, next_weight, stats, border, seed_at, want)
+            weight, bias, scale, next_weight, stats = [t if t is None or t.is_contiguous() else t.contiguous()
+                                                       for t in (weight, bias, scale, next_weight, stats)]
+            made = _backward(like, dy, dh, at, f, weight, bias, gate, scale, next_weight, stats, border, ctx.seed, seed_at, want)
         else:
             made = [None] * 8
         if need[0] and dh is None:
             made[0] = dy
-        return (*made, None, None)
+        return (*made, None, None, None)
 
 
 def _check_rows(x, what):
-    _check_tensor(x, what)
-    if x.dim() < 1 or x.shape[-1] < 1:
+    if not x.is_cuda or x.dtype not in _DTYPES:
+        _check_tensor(x, what)
+    n = x.shape[-1] if x.dim() else 0
+    if n < 1:
         raise ValueError("%s: a last axis of at least one channel expected" % what)
-    if x.shape[-1] > _b.TV_MAX_LENGTH:
-        raise ValueError("%s: at most %d channels, got %d" % (what, _b.TV_MAX_LENGTH, x.shape[-1]))
-    return x.shape[-1]
+    if n > _b.TV_MAX_LENGTH:
+        raise ValueError("%s: at most %d channels, got %d" % (what, _b.TV_MAX_LENGTH, n))
+    return n
 
 
 def _check_eps(eps, what):
@@ -208,11 +237,15 @@ def _check_eps(eps, what):
     return float(eps)
 
 
-def _apply(what, x, f, weight, bias, gate, scale, next_weight, next_bias, border, seed_at):
-    tensors = (x, f, weight, bias, gate, scale, next_weight, next_bias)
-    if (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)) or _tangent_among(*tensors):
-        return _BorderFunction.apply(*tensors, border, seed_at)
-    y, h, _ = _forward(*tensors, border, seed_at, False)
+def _apply(x, f, weight, bias, gate, scale, next_weight, next_bias, border, seed, seed_at):
+    grad = torch.is_grad_enabled() and (
+        x.requires_grad or (f is not None and (f.requires_grad or (weight is not None and weight.requires_grad)
+                                               or (bias is not None and bias.requires_grad) or (gate is not None and gate.requires_grad)
+                                               or (scale is not None and scale.requires_grad)))
+        or (next_weight is not None and next_weight.requires_grad) or (next_bias is not None and next_bias.requires_grad))
+    if grad or _tangent_among(x, f, weight, bias, gate, scale, next_weight, next_bias):
+        return _BorderFunction.apply(x, f, weight, bias, gate, scale, next_weight, next_bias, border, seed, seed_at)
+    y, h, _ = _forward(x, f, weight, bias, gate, scale, next_weight, next_bias, border, seed, seed_at, False)
     return h if y is None else y if h is None else (y, h)
 
 
@@ -225,8 +258,8 @@ def tv_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Ten
         raise ValueError("tv_norm: kind must be rms or layer, got %r" % (kind,))
     weight = _check_channels(weight, n, "tv_norm (weight)", x)
     bias = _check_channels(bias, n, "tv_norm (bias)", x)
-    border = _Border(0, _NORMS[kind], 0, _check_eps(eps, "tv_norm"), 1, 0, 0, 0)
-    return _apply("tv_norm", x, None, None, None, None, None, weight, bias, border, None)
+    border = _border(0, _NORMS[kind], 0, _check_eps(eps, "tv_norm"), 1, 0, 0)
+    return _apply(x, None, None, None, None, None, weight, bias, border, 0, None)
 
 
 def tv_residual(x: torch.Tensor, f: torch.Tensor, norm: str = "none", weight: torch.Tensor | None = None,
@@ -261,8 +294,8 @@ def tv_residual(x: torch.Tensor, f: torch.Tensor, norm: str = "none", weight: to
         _check_tensor(gate, "tv_residual (gate)", x)
         div = _gate_div(x, gate, what)
     drop, seed, seed_at, offset = _check_drop(dropout, seed, offset, x, what)
-    border = _Border(_NORMS[norm], _NORMS[next_norm], _GATE_ACTS[gate_act], _check_eps(eps, what), div, drop, seed, offset)
-    return _apply(what, x, f, weight, bias, gate, scale, next_weight, next_bias, border, seed_at)
+    border = _border(_NORMS[norm], _NORMS[next_norm], _GATE_ACTS[gate_act], _check_eps(eps, what), div, drop, offset)
+    return _apply(x, f, weight, bias, gate, scale, next_weight, next_bias, border, seed, seed_at)
 
 
 @_on_device

@@ -1,7 +1,7 @@
-// Products of a few rows with a weight in 4 bits: D[m, n] = sum_k X(m, k) W(n, k), M at most 64.
+// Products of a few rows with a weight in 4 bits: D[m, n] = sum_k X(m, k) W(n, k), M at most 32.
 //
 // W is read once, straight into the matrix instructions' registers (16 x 16 x 128: a lane has a block of 32 of one row):
-// what bounds the kernel is W's bytes, or for a small W the latency of one pass.  A workgroup of eight waves has 16 NT
+// what bounds the kernel is W's bytes, or for a small W the latency of one pass.  A workgroup of eight waves has 16
 // columns; the waves share out the groups of 128 in turn, so that they read 512 neighbouring bytes of a row together, and
 // their sums are joined in LDS, in order.
 #pragma once
@@ -65,43 +65,32 @@ template <class T, bool OWN> struct RawPiece4 {
     }
 };
 
-// MT: tiles of 16 rows.  NT: tiles of 16 columns.  UNROLL: groups whose loads are in flight together.
-template <class T, int MT, int NT, int UNROLL, bool OWN>
+// MT: tiles of 16 rows.  UNROLL: groups whose loads are in flight together.
+template <class T, int MT, int UNROLL, bool OWN>
 __global__ __launch_bounds__(512) void gemv4_kernel(Product g, Rows4 x, const uint32_t *w_scales, uint32_t w_rows, Epilogue e)
 {
-    constexpr int kWaves = 8, kPitch = NT * 16 + 4;
+    constexpr int kWaves = 8, kPitch = 20;
     __shared__ __attribute__((aligned(16))) float sums[kWaves][MT * 16 * kPitch];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n0 = (int)blockIdx.x * (NT * 16), row = lane & 15, block = lane >> 4;
+    const int n0 = (int)blockIdx.x * 16, row = lane & 15, block = lane >> 4, n = min(n0 + row, g.N - 1);
     const int64_t pitch = g.ldb / 32;                // groups of a row
-    const char *pw[NT];
-    const uint32_t *ps[NT];
+    const char *pw = (const char *)g.b + (int64_t)n * pitch * 64 + block * 16;
+    const uint32_t *ps = w_scales + n;
+    f32x4 acc[MT];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-        const int n = min(n0 + 16 * i + row, g.N - 1);
-        pw[i] = (const char *)g.b + (int64_t)n * pitch * 64 + block * 16;
-        ps[i] = w_scales + n;
-    }
-    f32x4 acc[NT][MT];
-#pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int j = 0; j < MT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j = 0; j < MT; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    const int first = (int)blockIdx.y * g.k_per / 32, end = min(g.K / 32, first + g.k_per / 32);
-    for (int k = first + wave; k < end; k += UNROLL * kWaves) {
-        u32x4 fw[UNROLL][NT];
-        uint32_t sw[UNROLL][NT];
+    const int end = g.K / 32;
+    for (int k = wave; k < end; k += UNROLL * kWaves) {
+        u32x4 fw[UNROLL];
+        uint32_t sw[UNROLL];
         RawPiece4<T, OWN> fx[UNROLL][MT];
         // (beyond the end the last group once more: what is loaded is not multiplied)
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             const int at = min(k + u * kWaves, end - 1);
-#pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                fw[u][i] = *(const u32x4 *)(pw[i] + (int64_t)at * 64);
-                sw[u][i] = ps[i][(int64_t)at * w_rows];
-            }
+            fw[u] = *(const u32x4 *)(pw + (int64_t)at * 64);
+            sw[u] = ps[(int64_t)at * w_rows];
 #pragma unroll
             for (int j = 0; j < MT; ++j) fx[u][j].load(x, min(16 * j + row, g.M - 1), at, block, pitch);
         }
@@ -111,38 +100,25 @@ __global__ __launch_bounds__(512) void gemv4_kernel(Product g, Rows4 x, const ui
 #pragma unroll
             for (int j = 0; j < MT; ++j) {
                 const Piece4 p = fx[u][j].get();
-#pragma unroll
-                for (int i = 0; i < NT; ++i)
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand4(fw[u][i]), operand4(p.codes), acc[i][j], 4, 4, 0,
-                                                                                 (int)(sw[u][i] >> (8 * block)), 0, p.scale);
+                acc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand4(fw[u]), operand4(p.codes), acc[j], 4, 4, 0,
+                                                                          (int)(sw[u] >> (8 * block)), 0, p.scale);
             }
         }
     }
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int j = 0; j < MT; ++j)
-            *(f32x4 *)&sums[wave][(16 * j + row) * kPitch + 16 * i + block * 4] = acc[i][j];
+    for (int j = 0; j < MT; ++j) *(f32x4 *)&sums[wave][(16 * j + row) * kPitch + block * 4] = acc[j];
     __syncthreads();
-    // whole waves: NT * 2 threads a row, eight columns each
-    for (int at = (int)threadIdx.x; at < MT * 16 * NT * 2; at += 512) {
-        const int m = at / (NT * 2), c = at % (NT * 2) * 8, n = n0 + c;
+    // two threads a row, eight columns each
+    const int m = threadIdx.x / 2, c = threadIdx.x % 2 * 8;
+    if (m < MT * 16) {
         f32x4 a = {0.0f, 0.0f, 0.0f, 0.0f}, b = a;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
             a += *(const f32x4 *)&sums[w][m * kPitch + c];
             b += *(const f32x4 *)&sums[w][m * kPitch + c + 4];
         }
-        if (g.splits > 1) {
-            if (m < g.M && n < g.N) {
-                float *to = g.partial + ((int64_t)blockIdx.y * g.M + m) * ((g.N + 7) & ~7) + n;
-                *(f32x4 *)to = a;
-                *(f32x4 *)(to + 4) = b;
-            }
-        } else {
-            float p[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-            finish8<T>(p, m, n, g.N, m < g.M, e);
-        }
+        float p[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        finish8<T>(p, m, n0 + c, g.N, m < g.M, e);
     }
 }
 

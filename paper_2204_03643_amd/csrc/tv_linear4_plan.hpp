@@ -11,7 +11,7 @@ inline int64_t groups_of(int64_t n) { return tiles(n, TV_MX4_GROUP); }
 inline int64_t scale_rows(int64_t rows) { return up(rows, 4); }
 
 // How a call goes.  kFew4: the weight streamed through registers, x taken to 4 bits by each workgroup (own) or before.
-enum Kind4 { kFew4, kTile64x4, kTile128x4, kTile256x4, kTile128x4Two };
+enum Kind4 { kFew4, kTile64x4, kTile128x4, kTile256x4 };
 struct Choice4 {
     Kind4 kind;
     bool own;
@@ -25,14 +25,19 @@ inline Choice4 cut4(Kind4 kind, bool own, int64_t s, int64_t groups, int64_t uni
     return {kind, own, (int)tiles(groups, per), (int)per * 32, 0.0};
 }
 
-inline Choice4 choose4(int dtype, bool codes, int64_t M, int64_t N, int64_t groups)
+constexpr int64_t kFewRows4 = 32, kOwnValues4 = 16384;
+
+// Sizes alone decide.  Up to 32 rows stream the weight (2048 -> 8192, x taken to 4 bits included: 32 rows 7.6 us streamed, 8.1
+// through tiles; 64 rows 9.8 and 8.4), few values of x in the same launch (one row 5.6 us in one, 5.9 in two and a launch's time on the
+// host; 16 rows, 32768 values, 7.5 and 6.6).  Otherwise the cheapest by a model of the time in microseconds, fitted to
+// sweeps of tiles and splits over outputs of 64 x 1024 to 8192 x 8192 and contractions of 1024 to 8192: a launch; rounds of
+// workgroups over 256 compute units, in each a start and an end and so much a step of 256; for split contractions the second launch
+// and the sums' trip through memory.
+inline Choice4 choose4(bool codes, int64_t M, int64_t N, int64_t K, int64_t groups)
 {
-    if (M <= 64) {
-        const int64_t t = tiles(N, 32), s = t >= 256 ? 1 : 256 / t;
-        return cut4(kFew4, !codes && M <= 16, s < groups / 32 ? s : groups / 32, groups, 8);
-    }
-    struct Cost { Kind4 kind; int m, n; int64_t slots; double round, step; };
-    constexpr Cost costs[] = {{kTile64x4, 64, 128, 256, 1.5, 0.30}, {kTile128x4, 128, 128, 256, 2.0, 0.45}, {kTile256x4, 256, 256, 256, 4.2, 1.3}};
+    if (M <= kFewRows4) return cut4(kFew4, !codes && M <= 16 && M * K <= kOwnValues4, 1, groups, 8);
+    struct Cost { Kind4 kind; int m, n; double round, step; };
+    constexpr Cost costs[] = {{kTile64x4, 64, 128, 1.5, 0.30}, {kTile128x4, 128, 128, 2.4, 0.60}, {kTile256x4, 256, 256, 6.0, 1.75}};
     Choice4 best{};
     best.us = 1e30;
     for (const Cost &c : costs) {
@@ -40,7 +45,7 @@ inline Choice4 choose4(int dtype, bool codes, int64_t M, int64_t N, int64_t grou
         for (int s : {1, 2, 3, 4, 6, 8}) {
             if (s > 1 && (groups < 4 * s || t * s > 1024)) break;
             Choice4 x = cut4(c.kind, false, s, groups, 2);
-            x.us = 3.0 + (double)tiles(t * x.splits, c.slots) * (c.round + c.step * (double)tiles(x.k_per, 64));
+            x.us = 3.0 + (double)tiles(t * x.splits, 256) * (c.round + c.step * (double)tiles(x.k_per, 64));
             if (x.splits > 1) x.us += 2.6 + 0.18 * x.splits + (double)M * (double)N * x.splits * 8 / 7e6;
             if (x.us < best.us) best = x;
         }
@@ -57,7 +62,7 @@ struct Plan4 {
 inline Plan4 plan4(const tv_linear_desc &d, bool codes)
 {
     Plan4 p{};
-    p.c = choose4(d.dtype, codes, d.m, d.n, groups_of(d.k));
+    p.c = choose4(codes, d.m, d.n, d.k, groups_of(d.k));
     if (!codes && !p.c.own) {
         p.exps = (size_t)up(d.m * groups_of(d.k) * 64, 256);
         p.split = p.exps + (size_t)up(scale_rows(d.m) * groups_of(d.k) * 4, 256);

@@ -50,15 +50,13 @@ void launch_tiles(Product g, const Scales &scales, const Epilogue &e, hipStream_
     hipLaunchKernelGGL((gemm4_kernel<T, BM, BN, WM, WN, BUF, G>), dim3(g.tiles_m * g.tiles_n, g.splits), dim3(WM * WN * 64), 0, stream, g, scales, e);
 }
 
-template <class T, int NT, bool OWN>
-void launch_few(const Product &g, const Rows4 &x, const Scales &s, const Epilogue &e, hipStream_t stream)
+template <class T>
+void launch_few(const Product &g, const Rows4 &x, bool own, const Scales &s, const Epilogue &e, hipStream_t stream)
 {
-    const dim3 grid((uint32_t)tiles(g.N, NT * 16), g.splits), block(512);
-    if (g.M <= 16) hipLaunchKernelGGL((gemv4_kernel<T, 1, NT, OWN ? 2 : 4, OWN>), grid, block, 0, stream, g, x, s.w, s.w_rows, e);
-    else if constexpr (!OWN) {
-        if (g.M <= 32) hipLaunchKernelGGL((gemv4_kernel<T, 2, NT, 4, OWN>), grid, block, 0, stream, g, x, s.w, s.w_rows, e);
-        else hipLaunchKernelGGL((gemv4_kernel<T, 4, NT, 4, OWN>), grid, block, 0, stream, g, x, s.w, s.w_rows, e);
-    }
+    const dim3 grid((uint32_t)tiles(g.N, 16)), block(512);
+    if (own) hipLaunchKernelGGL((gemv4_kernel<T, 1, 2, true>), grid, block, 0, stream, g, x, s.w, s.w_rows, e);
+    else if (g.M <= 16) hipLaunchKernelGGL((gemv4_kernel<T, 1, 4, false>), grid, block, 0, stream, g, x, s.w, s.w_rows, e);
+    else hipLaunchKernelGGL((gemv4_kernel<T, 2, 4, false>), grid, block, 0, stream, g, x, s.w, s.w_rows, e);
 }
 
 template <class T>
@@ -75,12 +73,10 @@ int linear4(const void *x, const uint8_t *x_exps, const uint8_t *w, const uint8_
     }
     if (p.c.kind == kTile256x4) launch_tiles<T, 256, 256, 2, 4, 2, 2>(g, s, e, stream);
     if (p.c.kind == kTile128x4) launch_tiles<T, 128, 128, 2, 2, 4, 2>(g, s, e, stream);
-    if (p.c.kind == kTile128x4Two) launch_tiles<T, 128, 256, 2, 2, 3, 1>(g, s, e, stream);
     if (p.c.kind == kTile64x4) launch_tiles<T, 64, 128, 2, 2, 4, 2>(g, s, e, stream);
     if (p.c.kind == kFew4) {
         const Rows4 rows{g.a, s.x, d.ldx, s.x_rows, (int32_t)d.k};
-        if (p.c.own) launch_few<T, 1, true>(g, rows, s, e, stream);
-        else launch_few<T, 1, false>(g, rows, s, e, stream);
+        launch_few<T>(g, rows, p.c.own, s, e, stream);
     }
     if (p.c.splits > 1) {
         if (launched() != TV_OK) return TV_ERR_HIP;

@@ -32,11 +32,12 @@ class Quantized4:
     def __init__(self, codes: torch.Tensor, exps: torch.Tensor, shape, dtype: torch.dtype):
         if codes.dtype != torch.uint8 or exps.dtype != torch.uint8 or dtype not in _DTYPES:
             raise TypeError("Quantized4: uint8 codes and scale bytes and a float32 or bfloat16 dtype expected")
-        shape = torch.Size(shape)
+        if type(shape) is not torch.Size:
+            shape = torch.Size(shape)
         if len(shape) < 1 or shape[-1] < 1:
             raise ValueError("Quantized4: a last axis of at least one value expected")
         want = _layout(shape.numel() // shape[-1], shape[-1])
-        if (tuple(codes.shape), tuple(exps.shape)) != want:
+        if (codes.shape, exps.shape) != want:
             raise ValueError("Quantized4: codes and scale bytes of shapes %r and %r expected, got %r and %r"
                              % (*want, tuple(codes.shape), tuple(exps.shape)))
         if not codes.is_cuda or exps.device != codes.device:
@@ -65,7 +66,8 @@ class Quantized4:
 
 def _on_16(t):
     """t dense and on a 16-byte boundary, as the kernels read it."""
-    t = t.contiguous()
+    if not t.is_contiguous():
+        t = t.contiguous()
     return t if t.data_ptr() % 16 == 0 else t.clone()
 
 
@@ -129,25 +131,26 @@ def tv_linear4(x, weight: Quantized4, bias: torch.Tensor | None = None, residual
     if act not in _ACTS:
         raise ValueError("tv_linear4: act must be one of %s, got %r" % (", ".join(sorted(_ACTS)), act))
     codes = isinstance(x, Quantized4)
-    if not codes:
+    if not codes and (not x.is_cuda or x.dtype not in _DTYPES):
         _check_tensor(x, what)
     if len(weight.shape) != 2 or 0 in weight.shape or len(x.shape) < 1 or x.shape[-1] != weight.shape[1]:
         raise ValueError("tv_linear4: x [..., k] and weight [n, k] expected, got %r and %r" % (tuple(x.shape), tuple(weight.shape)))
     if weight.device != x.device:
         raise TypeError("tv_linear4 (weight): one on %s expected, got one on %s" % (x.device, weight.device))
     n, lead = weight.shape[0], x.shape[:-1]
+    grad = not codes and x.requires_grad
     for t, shape, name in ((bias, (n,), "bias"), (residual, (*lead, n), "residual")):
         if t is None:
             continue
-        _check_tensor(t, "tv_linear4 (%s)" % name)
-        if t.dtype != x.dtype or t.device != x.device:
+        if t.dtype is not x.dtype or t.device != x.device:
+            _check_tensor(t, "tv_linear4 (%s)" % name)
             raise TypeError("tv_linear4 (%s): %s on %s expected, got %s on %s" % (name, x.dtype, x.device, t.dtype, t.device))
-        if tuple(t.shape) != shape:
+        if t.shape != shape:
             raise ValueError("tv_linear4: %s of shape %r expected, got %r" % (name, shape, tuple(t.shape)))
-    tensors = (None if codes else x, bias, residual)
-    if (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)) or _tangent_among(*tensors):
+        grad = grad or t.requires_grad
+    if (grad and torch.is_grad_enabled()) or _tangent_among(None if codes else x, bias, residual):
         raise RuntimeError("tv_linear4: products in 4 bits have no gradients; call it under torch.no_grad() or detach its inputs")
-    if bias is not None:
+    if bias is not None and not bias.is_contiguous():
         bias = bias.contiguous()
     if codes:
         return _linear4(x.codes, x.exps, x.shape[-1], lead, weight, bias, residual, act, x.dtype)
