@@ -473,8 +473,8 @@ int tv_block_bwd(const void *dy, const void *dh, tv_block_in in, const float *st
  * and stands for NaNs.  (The element and scale formats e2m1 and e8m0 of the OCP microscaling formats.)
  *
  * A group is 128 values; G = ceil(n / 128).  codes [rows, 64 G] bytes: value 2 i of a row in the lower half of byte i,
- * zeros from n on.  exps [G, up(rows, 4), 4]: the four scale bytes of a group (127 beyond n), rows side by side; what stands for rows beyond
- * the last is not looked at.  codes 16-byte, exps 16-byte aligned (TV_ERR_STRIDE).
+ * zeros from n on.  exps [G, up(rows, 4), 4]: the four scale bytes of a group, rows side by side, 127 beyond n and for the
+ * rows that only fill up (which no call looks at).  codes and exps 16-byte aligned (TV_ERR_STRIDE).
  */
 #define TV_MX4_GROUP 128
 int tv_mx4_save(const void *x, uint8_t *codes, uint8_t *exps, int64_t rows, int64_t n, int64_t ldx, int dtype,

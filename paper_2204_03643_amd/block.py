@@ -69,7 +69,16 @@ def _check_channels(t, n, what, like):
         _check_tensor(t, what, like)
     if t.shape != (n,):
         raise ValueError("%s: shape (%d,) expected, got %r" % (what, n, tuple(t.shape)))
-    return t if t.is_contiguous() else t.contiguous()
+    return _dense(t)
+
+
+def _dense(t):
+    """t without gaps, and not as a view that stands for its memory's negative."""
+    return t if t.is_contiguous() and not t.is_neg() else t.resolve_neg().contiguous()
+
+
+def _rows(t):
+    return _as_rows(t.resolve_neg() if t.is_neg() else t)
 
 
 def _gate_div(x, gate, what):
@@ -112,15 +121,15 @@ def _forward(x, f, weight, bias, gate, scale, next_weight, next_bias, border, se
     """(y, h, stats): None where there is none."""
     n = x.shape[-1]
     m = x.numel() // n
-    rows, ldx = _as_rows(x)
+    rows, ldx = _rows(x)
     y = h = stats = at_f = at_gate = at_y = at_h = at_stats = None
     ldf = ldg = n
     if f is not None:
-        frows, ldf = _as_rows(f)
+        frows, ldf = _rows(f)
         y = x.new_empty(x.shape)
         at_f, at_y = frows.data_ptr(), y.data_ptr()
         if gate is not None:
-            grows, ldg = _as_rows(gate)
+            grows, ldg = _rows(gate)
             at_gate = grows.data_ptr()
     if border.next_norm:
         h = x.new_empty(x.shape)
@@ -143,13 +152,13 @@ def _backward(like, dy, dh, x, f, weight, bias, gate, scale, next_weight, stats,
     at_x = at_f = at_gate = None
     ldx = ldf = ldg = n
     if x is not None:
-        x, ldx = _as_rows(x)
+        x, ldx = _rows(x)
         at_x = x.data_ptr()
     if f is not None:
-        f, ldf = _as_rows(f)
+        f, ldf = _rows(f)
         at_f = f.data_ptr()
         if gate is not None:
-            grows, ldg = _as_rows(gate)
+            grows, ldg = _rows(gate)
             at_gate = grows.data_ptr()
     shapes = (shape, shape, n, n, None if gate is None else gate.shape, n, n, n)
     made = [like.new_empty(s) if w else None for s, w in zip(shapes, want)]
@@ -199,9 +208,9 @@ class _BorderFunction(torch.autograd.Function):
         else:
             dy, dh = grads if border.next_norm else (grads[0], None)
         if dy is not None:
-            dy = dy.contiguous()
+            dy = _dense(dy)
         if dh is not None:
-            dh = dh.contiguous()
+            dh = _dense(dh)
         # without a gradient through the next norm, x's is y's
         want = (need[0] and dh is not None, *need[1:8])
         if like.numel() == 0:
@@ -210,8 +219,7 @@ class _BorderFunction(torch.autograd.Function):
                 shapes[4] = gate.shape
             made = [like.new_zeros(s) if w else None for s, w in zip(shapes, need)]
         elif any(want):
-            weight, bias, scale, next_weight, stats = [t if t is None or t.is_contiguous() else t.contiguous()
-                                                       for t in (weight, bias, scale, next_weight, stats)]
+            weight, bias, scale, next_weight, stats = [None if t is None else _dense(t) for t in (weight, bias, scale, next_weight, stats)]
             made = _backward(like, dy, dh, at, f, weight, bias, gate, scale, next_weight, stats, border, ctx.seed, seed_at, want)
         else:
             made = [None] * 8
@@ -301,7 +309,7 @@ def tv_residual(x: torch.Tensor, f: torch.Tensor, norm: str = "none", weight: to
 @_on_device
 def _drop(x, drop, seed, seed_at, offset):
     n = x.shape[-1] if x.dim() else 1
-    rows, ldx = _as_rows(x) if x.dim() else (x, 1)
+    rows, ldx = _rows(x) if x.dim() else (x, 1)
     y = x.new_empty(x.shape)
     _check(_b.lib().tv_drop_apply(rows.data_ptr(), y.data_ptr(), x.numel() // n, n, ldx, _DTYPES[x.dtype],
                                   _b.tv_drop(seed, offset, _address(seed_at), drop), _b._stream(None)))
@@ -332,7 +340,7 @@ def tv_dropout(x: torch.Tensor, p: float, seed, offset: int = 0) -> torch.Tensor
     Which values are dropped is a function of seed and offset (whole numbers of 64 bits), the row (of the last axis) and the
     column alone.  seed may be an int64 tensor of one element on x's device, which is read when the kernel runs: a captured graph
     drops others in every replay if the program changes it in between.  It must not change between a call and its backward pass;
-    calls of one step are told apart by their offsets.
+    calls of one step are told apart by their offsets.  With p below 2^-17 the result is x itself.
     """
     _check_tensor(x, "tv_dropout")
     drop, seed, seed_at, offset = _check_drop(p, seed, offset, x, "tv_dropout")

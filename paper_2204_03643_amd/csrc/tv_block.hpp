@@ -363,13 +363,6 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_fwd_long_kerne
 }
 
 // ---- gradients
-__device__ __forceinline__ void range_of(const Units &u, int unit, int64_t m, int64_t &begin, int64_t &end)
-{
-    const int64_t first = unit / u.per * u.span;
-    begin = first + (int64_t)(unit % u.per) * u.rows;
-    end = min(min(begin + u.rows, first + u.span), m);
-}
-
 struct BlockGrads {
     const void *dy, *dh;
     const float4 *stats;

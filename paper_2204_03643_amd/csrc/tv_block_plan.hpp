@@ -26,6 +26,19 @@ struct Units {
     int32_t count;
 };
 
+// The rows of a unit.
+#ifdef __HIPCC__
+__host__ __device__
+#endif
+inline void range_of(const Units &u, int unit, int64_t m, int64_t &begin, int64_t &end)
+{
+    const int64_t first = unit / u.per * u.span, last = first + u.span < m ? first + u.span : m;
+    begin = first + (int64_t)(unit % u.per) * u.rows;
+    end = begin + u.rows < last ? begin + u.rows : last;
+}
+
+// As many units as fill the card three waves to a SIMD deep, two rows at least from 513 rows on (every unit writes its sums
+// once: a row each would cost more bytes than the row has).
 inline Units block_units(int64_t m, int64_t n, bool shared_gate, int64_t gate_div)
 {
     const int lanes = block_lanes(n);

@@ -35,7 +35,8 @@ constexpr int64_t kFewRows4 = 32, kOwnValues4 = 16384;
 // and the sums' trip through memory.
 inline Choice4 choose4(bool codes, int64_t M, int64_t N, int64_t K, int64_t groups)
 {
-    if (M <= kFewRows4) return cut4(kFew4, !codes && M <= 16 && M * K <= kOwnValues4, 1, groups, 8);
+    // (as long as a launch of 512 threads for every 16 columns has fewer than 2^32)
+    if (M <= kFewRows4 && N <= ((int64_t)1 << 26)) return cut4(kFew4, !codes && M <= 16 && M * K <= kOwnValues4, 1, groups, 8);
     struct Cost { Kind4 kind; int m, n; double round, step; };
     constexpr Cost costs[] = {{kTile64x4, 64, 128, 1.5, 0.30}, {kTile128x4, 128, 128, 2.4, 0.60}, {kTile256x4, 256, 256, 6.0, 1.75}};
     Choice4 best{};

@@ -37,31 +37,43 @@ __device__ __forceinline__ uint32_t codes4_of(const float (&v)[8], float scale)
     return c;
 }
 
-// 16 lanes a group of a row, eight values a lane; a workgroup has 16 rows at a time.
+// 16 lanes a group of a row, eight values a lane; a workgroup has 16 rows at a time, so that their scale words leave side by
+// side, and four groups, whose loads are on their way together.
+constexpr int kGroupsAtOnce4 = 4;
+
 template <class T>
 __global__ __launch_bounds__(256) void mx4_save_kernel(const T *x, int64_t ldx, uint8_t *codes, uint32_t *exps, int64_t rows,
                                                        int n, int groups)
 {
+    constexpr int U = kGroupsAtOnce4;
     const int lane = threadIdx.x & 15;
     const int64_t pitch = rows4(rows);
-    for (int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); row < rows; row += (int64_t)gridDim.x * 16)
-        for (int g = blockIdx.y; g < groups; g += gridDim.y) {
-            const int k = g * kGroup4 + lane * 8, have = max(0, min(8, n - k));
-            float v[8];
-            get8(v, x + row * ldx + k, have);
-            uint32_t top = 0;
+    for (int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); row < pitch; row += (int64_t)gridDim.x * 16)
+        for (int first = blockIdx.y * U; first < groups; first += gridDim.y * U) {
+            float v[U][8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
-            top = max(top, (uint32_t)__shfl_xor(top, 1));
-            top = max(top, (uint32_t)__shfl_xor(top, 2));
-            uint32_t byte = scale4_byte(top);
-            uint32_t c = byte == 255u ? 0u : codes4_of(v, __uint_as_float(byte << 23));
-            if ((k & ~31) >= n) byte = 127u;              // a block that only fills the group
-            byte <<= 8 * (lane >> 2);
-            byte |= (uint32_t)__shfl_xor(byte, 4);
-            byte |= (uint32_t)__shfl_xor(byte, 8);
-            *(uint32_t *)(codes + row * groups * 64 + g * 64 + lane * 4) = c;
-            if (lane == 0) exps[g * pitch + row] = byte;
+            for (int u = 0; u < U; ++u) {
+                const int k = (first + u) * kGroup4 + lane * 8;
+                get8(v[u], x + row * ldx + k, row < rows && first + u < groups ? max(0, min(8, n - k)) : 0);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int g = first + u, k = g * kGroup4 + lane * 8;
+                if (g >= groups) break;
+                uint32_t top = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[u][i]) & 0x7fffffffu);
+                top = max(top, (uint32_t)__shfl_xor(top, 1));
+                top = max(top, (uint32_t)__shfl_xor(top, 2));
+                uint32_t byte = scale4_byte(top);
+                const uint32_t c = byte == 255u ? 0u : codes4_of(v[u], __uint_as_float(byte << 23));
+                if ((k & ~31) >= n || row >= rows) byte = 127u;          // a block that only fills up
+                byte <<= 8 * (lane >> 2);
+                byte |= (uint32_t)__shfl_xor(byte, 4);
+                byte |= (uint32_t)__shfl_xor(byte, 8);
+                if (row < rows) *(uint32_t *)(codes + row * groups * 64 + g * 64 + lane * 4) = c;
+                if (lane == 0) exps[g * pitch + row] = byte;
+            }
         }
 }
 

@@ -18,17 +18,17 @@ int check_values(int64_t rows, int64_t n, int64_t ld, int dtype)
     return TV_OK;
 }
 
-// 16 rows by a group a workgroup; beyond 65536 by 64 they take further ones in turn
-dim3 values_grid(int64_t rows, int64_t n)
+// 16 rows by `each` groups a workgroup; beyond 65536 by 64 they take further ones in turn
+dim3 values_grid(int64_t rows, int64_t n, int each)
 {
-    const int64_t x = tiles(rows, 16), y = groups4(n);
+    const int64_t x = tiles(rows, 16), y = tiles(groups4(n), each);
     return dim3((uint32_t)(x < 65536 ? x : 65536), (uint32_t)(y < 64 ? y : 64));
 }
 
 template <class T>
 int save(const void *x, void *codes, void *exps, int64_t rows, int64_t n, int64_t ldx, hipStream_t stream)
 {
-    hipLaunchKernelGGL((mx4_save_kernel<T>), values_grid(rows, n), dim3(256), 0, stream, (const T *)x, ldx, (uint8_t *)codes, (uint32_t *)exps, rows, (int)n, (int)groups4(n));
+    hipLaunchKernelGGL((mx4_save_kernel<T>), values_grid(rows, n, kGroupsAtOnce4), dim3(256), 0, stream, (const T *)x, ldx, (uint8_t *)codes, (uint32_t *)exps, rows, (int)n, (int)groups4(n));
     return launched();
 }
 
@@ -105,9 +105,9 @@ int tv_mx4_load(const uint8_t *codes, const uint8_t *exps, void *x, int64_t rows
     if (!x || !codes || !exps) return TV_ERR_NULL;
     if (!aligned(x, elem_bytes(dtype)) || !aligned(codes, 16) || !aligned(exps, 16)) return TV_ERR_STRIDE;
     if (dtype == TV_BF16)
-        hipLaunchKernelGGL((mx4_load_kernel<bf16>), values_grid(rows, n), dim3(256), 0, stream, codes, exps, (bf16 *)x, ldx, rows, (int)n, (int)groups4(n));
+        hipLaunchKernelGGL((mx4_load_kernel<bf16>), values_grid(rows, n, 1), dim3(256), 0, stream, codes, exps, (bf16 *)x, ldx, rows, (int)n, (int)groups4(n));
     else
-        hipLaunchKernelGGL((mx4_load_kernel<float>), values_grid(rows, n), dim3(256), 0, stream, codes, exps, (float *)x, ldx, rows, (int)n, (int)groups4(n));
+        hipLaunchKernelGGL((mx4_load_kernel<float>), values_grid(rows, n, 1), dim3(256), 0, stream, codes, exps, (float *)x, ldx, rows, (int)n, (int)groups4(n));
     return launched();
 }
 

@@ -71,6 +71,11 @@ def _on_16(t):
     return t if t.data_ptr() % 16 == 0 else t.clone()
 
 
+def _rows(t):
+    """(t, row stride) as the kernels read it: not as a view that stands for its memory's negative."""
+    return _as_rows(t.resolve_neg() if t.is_neg() else t)
+
+
 @_on_device
 def _restore4(codes, exps, shape, dtype):
     n = shape[-1]
@@ -94,7 +99,7 @@ def tv_quantize4(x: torch.Tensor) -> Quantized4:
     _check_tensor(x, "tv_quantize4")
     if x.dim() < 1 or x.shape[-1] < 1:
         raise ValueError("tv_quantize4: a last axis of at least one value expected")
-    codes, exps = _save4(*_as_rows(x.detach()))
+    codes, exps = _save4(*_rows(x.detach()))
     return Quantized4._saved(codes, exps, x.shape, x.dtype)
 
 
@@ -110,7 +115,7 @@ def _linear4(x, x_exps, ldx, lead, weight, bias, residual, act, dtype):
     y = x.new_empty((*lead, n), dtype=dtype)
     ldr = n
     if residual is not None:
-        residual, ldr = _as_rows(residual)
+        residual, ldr = _rows(residual)
     desc, nbytes = _linear_desc(x_exps is not None, lead.numel(), k, n, ldx, k, ldr, n, _DTYPES[dtype], _ACTS[act])
     ws = x.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
     _check(_b.lib().tv_linear4_fwd(x.data_ptr(), _address(x_exps), weight.codes.data_ptr(), weight.exps.data_ptr(), _address(bias),
@@ -150,11 +155,11 @@ def tv_linear4(x, weight: Quantized4, bias: torch.Tensor | None = None, residual
         grad = grad or t.requires_grad
     if (grad and torch.is_grad_enabled()) or _tangent_among(None if codes else x, bias, residual):
         raise RuntimeError("tv_linear4: products in 4 bits have no gradients; call it under torch.no_grad() or detach its inputs")
-    if bias is not None and not bias.is_contiguous():
-        bias = bias.contiguous()
+    if bias is not None and not (bias.is_contiguous() and not bias.is_neg()):
+        bias = bias.resolve_neg().contiguous()
     if codes:
         return _linear4(x.codes, x.exps, x.shape[-1], lead, weight, bias, residual, act, x.dtype)
-    rows, ldx = _as_rows(x)
+    rows, ldx = _rows(x)
     return _linear4(rows, None, ldx, lead, weight, bias, residual, act, x.dtype)
 
 

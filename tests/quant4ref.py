@@ -9,7 +9,7 @@ BORDERS = ((0.25, False), (0.75, True), (1.25, False), (1.75, True), (2.5, False
 
 
 def save(v):
-    """(codes [rows, 64 G], scale bytes [G, rows up to 4, 4]) of a [rows, n] array; the rows that only fill up are zero."""
+    """(codes [rows, 64 G], scale bytes [G, rows up to 4, 4]) of a [rows, n] array."""
     v = np.asarray(v, np.float64)
     rows, n = v.shape
     groups = -(-n // 128)
@@ -25,7 +25,7 @@ def save(v):
     code = code.reshape(rows, groups * 128)
     byte = np.where(fine, e + 127, 255)
     byte[:, -(-n // 32):] = 127
-    exps = np.zeros((groups, -(-rows // 4) * 4, 4), np.uint8)
+    exps = np.full((groups, -(-rows // 4) * 4, 4), 127, np.uint8)
     exps[:, :rows] = byte.reshape(rows, groups, 4).transpose(1, 0, 2)
     return (code[:, ::2] | code[:, 1::2] << 4).astype(np.uint8), exps
 

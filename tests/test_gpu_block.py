@@ -187,6 +187,21 @@ def test_views(dtype):
     assert torch.equal(g1, g2)
 
 
+def test_views_that_stand_for_the_negative_of_their_memory():
+    from paper_2204_03643_amd.block import tv_dropout, tv_residual
+    for n in (1, 24):
+        z = torch.randn(4, n, dtype=torch.complex64, device="cuda")
+        v = z.conj().imag
+        d = v.resolve_neg().clone()
+        assert v.is_neg()
+        for m in (1, 4):
+            def call(t):
+                leaf = torch.ones(m, n, device="cuda", requires_grad=True)
+                y, h = tv_residual(t[:m], leaf, norm="rms", weight=t[0], gate=t[:m], gate_act="silu", scale=t[1], next_norm="layer", next_weight=t[2])
+                return y, h, torch.autograd.grad([y, h], leaf, [t[:m], t[:m]])[0], tv_dropout(t[:m], 0.5, 3)
+            assert all(torch.equal(a, b) for a, b in zip(call(v), call(d)))
+
+
 def test_no_rows():
     from paper_2204_03643_amd.block import tv_dropout, tv_norm, tv_residual
     x = torch.zeros(2, 0, 16, device="cuda", requires_grad=True)

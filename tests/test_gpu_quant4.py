@@ -15,7 +15,7 @@ def held(x):
     rows = x.reshape(-1, x.shape[-1])
     codes, exps = quant4ref.save(rows.double().cpu().numpy())
     assert q.codes.cpu().numpy().tolist() == codes.tolist()
-    assert (q.exps.cpu().numpy()[:, :rows.shape[0]] == exps[:, :rows.shape[0]]).all()
+    assert np.array_equal(q.exps.cpu().numpy(), exps)
     got = q.restore()
     assert got.shape == x.shape and got.dtype == x.dtype
     want = quant4ref.load(codes, exps, x.shape[-1])
@@ -73,14 +73,25 @@ def test_views():
     base = torch.randn(20, 500, device="cuda")
     for v in (base[:, 3:290], base.t(), base[::2, 1:], base.view(4, 5, 500), base[0]):
         a, b = tv_quantize4(v), tv_quantize4(v.contiguous())
-        rows = v.numel() // v.shape[-1]
-        assert torch.equal(a.codes, b.codes) and torch.equal(a.exps[:, :rows], b.exps[:, :rows]) and torch.equal(a.restore(), b.restore())
+        assert torch.equal(a.codes, b.codes) and torch.equal(a.exps, b.exps) and torch.equal(a.restore(), b.restore())
+
+
+def test_views_that_stand_for_the_negative_of_their_memory():
+    from paper_2204_03643_amd.quant4 import tv_linear4, tv_quantize4
+    for n in (1, 40):
+        z = torch.randn(3, n, dtype=torch.complex64, device="cuda")
+        v = z.conj().imag
+        assert v.is_neg() and torch.equal(tv_quantize4(v).restore(), tv_quantize4(v.resolve_neg().clone()).restore())
+        w = tv_quantize4(torch.randn(n, n, device="cuda"))
+        for m in (1, 3):
+            want = tv_linear4(v[:m].resolve_neg().clone(), w, v[0].resolve_neg().clone(), v[:m].resolve_neg().clone())
+            assert torch.equal(tv_linear4(v[:m], w, v[0], v[:m]), want)
 
 
 def test_many_rows_and_groups():
     """More rows and more groups than a launch's workgroups."""
     from paper_2204_03643_amd.quant4 import tv_quantize4
-    for rows, n in (((1 << 20) + 37, 24), (3, 64 * 128 * 3 + 5)):
+    for rows, n in (((1 << 20) + 37, 24), (3, 256 * 128 * 3 + 5)):
         x = torch.randn(rows, n, device="cuda")
         q = tv_quantize4(x)
         some = torch.tensor([0, 1, rows // 2, rows - 1], device="cuda")
