@@ -38,18 +38,15 @@ __device__ __forceinline__ uint32_t codes4_of(const float (&v)[8], float scale)
 }
 
 // 16 lanes a group of a row, eight values a lane; a workgroup has 16 rows at a time, so that their scale words leave side by
-// side, and four groups, whose loads are on their way together.
-constexpr int kGroupsAtOnce4 = 4;
-
-template <class T>
+// side, and U groups, whose loads are on their way together.  Workgroups next to each other have groups next to each other.
+template <class T, int U>
 __global__ __launch_bounds__(256) void mx4_save_kernel(const T *x, int64_t ldx, uint8_t *codes, uint32_t *exps, int64_t rows,
                                                        int n, int groups)
 {
-    constexpr int U = kGroupsAtOnce4;
     const int lane = threadIdx.x & 15;
     const int64_t pitch = rows4(rows);
-    for (int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); row < pitch; row += (int64_t)gridDim.x * 16)
-        for (int first = blockIdx.y * U; first < groups; first += gridDim.y * U) {
+    for (int64_t row = (int64_t)blockIdx.y * 16 + (threadIdx.x >> 4); row < pitch; row += (int64_t)gridDim.y * 16)
+        for (int first = blockIdx.x * U; first < groups; first += gridDim.x * U) {
             float v[U][8];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -83,8 +80,8 @@ __global__ __launch_bounds__(256) void mx4_load_kernel(const uint8_t *codes, con
 {
     const int lane = threadIdx.x & 15;
     const int64_t pitch = rows4(rows);
-    for (int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); row < rows; row += (int64_t)gridDim.x * 16)
-        for (int g = blockIdx.y; g < groups; g += gridDim.y) {
+    for (int64_t row = (int64_t)blockIdx.y * 16 + (threadIdx.x >> 4); row < rows; row += (int64_t)gridDim.y * 16)
+        for (int g = blockIdx.x; g < groups; g += gridDim.x) {
             const int k = g * kGroup4 + lane * 8, have = max(0, min(8, n - k));
             if (have == 0) continue;
             const uint32_t c = *(const uint32_t *)(codes + row * groups * 64 + g * 64 + lane * 4);
