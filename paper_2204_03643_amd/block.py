@@ -122,49 +122,45 @@ def _forward(x, f, weight, bias, gate, scale, next_weight, next_bias, border, se
     n = x.shape[-1]
     m = x.numel() // n
     rows, ldx = _rows(x)
-    y = h = stats = at_f = at_gate = at_y = at_h = at_stats = None
-    ldf = ldg = n
-    if f is not None:
-        frows, ldf = _rows(f)
-        y = x.new_empty(x.shape)
-        at_f, at_y = frows.data_ptr(), y.data_ptr()
-        if gate is not None:
-            grows, ldg = _rows(gate)
-            at_gate = grows.data_ptr()
+    h = stats = at_gate = at_h = at_stats = None
+    ldg = n
+    frows, ldf = _rows(f)
+    y = x.new_empty(x.shape)
+    if gate is not None:
+        grows, ldg = _rows(gate)
+        at_gate = grows.data_ptr()
     if border.next_norm:
         h = x.new_empty(x.shape)
         at_h = h.data_ptr()
     if hold:
         stats = x.new_empty((m, 4), dtype=torch.float32)
         at_stats = stats.data_ptr()
-    ins = _b.tv_block_in(rows.data_ptr(), at_f, _address(weight), _address(bias), at_gate, _address(scale), _address(next_weight),
-                         _address(next_bias))
-    _check(_b.lib().tv_block_fwd(ins, at_y, at_h, at_stats, _desc_of(m, n, ldx, ldf, ldg, _DTYPES[x.dtype], border, seed, seed_at),
+    ins = _b.tv_block_in(rows.data_ptr(), frows.data_ptr(), _address(weight), _address(bias), at_gate, _address(scale),
+                         _address(next_weight), _address(next_bias))
+    _check(_b.lib().tv_block_fwd(ins, y.data_ptr(), at_h, at_stats, _desc_of(m, n, ldx, ldf, ldg, _DTYPES[x.dtype], border, seed, seed_at),
                                  _b._stream(None)))
     return y, h, stats
 
 
 @_on_device
-def _backward(like, dy, dh, x, f, weight, bias, gate, scale, next_weight, stats, border, seed, seed_at, want):
+def _backward(like, dy, dh, y, f, weight, bias, gate, scale, next_weight, stats, border, seed, seed_at, want):
     """Gradients of x, f, weight, bias, gate, scale, next_weight, next_bias, None where not wanted."""
     shape, n = like.shape, like.shape[-1]
     m, dtype = like.numel() // n, _DTYPES[like.dtype]
-    at_x = at_f = at_gate = None
-    ldx = ldf = ldg = n
-    if x is not None:
-        x, ldx = _rows(x)
-        at_x = x.data_ptr()
-    if f is not None:
-        f, ldf = _rows(f)
-        at_f = f.data_ptr()
-        if gate is not None:
-            grows, ldg = _rows(gate)
-            at_gate = grows.data_ptr()
+    at_y = at_gate = None
+    ldx = ldg = n
+    if y is not None:
+        y, ldx = _rows(y)
+        at_y = y.data_ptr()
+    f, ldf = _rows(f)
+    if gate is not None:
+        grows, ldg = _rows(gate)
+        at_gate = grows.data_ptr()
     shapes = (shape, shape, n, n, None if gate is None else gate.shape, n, n, n)
     made = [like.new_empty(s) if w else None for s, w in zip(shapes, want)]
     dx, df, dweight, dbias, dgate, dscale, dnext_weight, dnext_bias = [None if t is None else t.data_ptr() for t in made]
-    ins = _b.tv_block_in(at_x, at_f, _address(weight), _address(bias), at_gate, _address(scale), _address(next_weight), None)
-    nbytes = _workspace_bytes(m, n, dtype, f is not None, gate is not None, border, want)
+    ins = _b.tv_block_in(at_y, f.data_ptr(), _address(weight), _address(bias), at_gate, _address(scale), _address(next_weight), None)
+    nbytes = _workspace_bytes(m, n, dtype, True, gate is not None, border, want)
     ws = like.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
     _check(_b.lib().tv_block_bwd(_address(dy), _address(dh), ins, _address(stats),
                                  _b.tv_block_grads(dx, df, dgate, dweight, dbias, dscale, dnext_weight, dnext_bias),
@@ -176,17 +172,16 @@ class _BorderFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, f, weight, bias, gate, scale, next_weight, next_bias, border, seed, seed_at):
         if _tangent_among(x, f, weight, bias, gate, scale, next_weight, next_bias):
-            raise NotImplementedError("tv_norm, tv_residual: no forward-mode derivative")
-        normed = border.next_norm or (f is not None and border.norm)
+            raise NotImplementedError("tv_residual: no forward-mode derivative")
+        normed = border.next_norm or border.norm
         y, h, stats = _forward(x, f, weight, bias, gate, scale, next_weight, next_bias, border, seed, seed_at, normed)
         # the next norm's gradient is taken at y as it was returned
-        at = (x if f is None else y) if border.next_norm else None
-        saved = (at, f, weight, bias, gate, scale, next_weight, stats, seed_at)
+        saved = (y if border.next_norm else None, f, weight, bias, gate, scale, next_weight, stats, seed_at)
         ctx.save_for_backward(*saved)
         ctx.saved_as = [None if t is None else (t.shape, t.dtype) for t in saved]
         ctx.border, ctx.seed = border, seed
         ctx.set_materialize_grads(False)
-        return h if y is None else y if h is None else (y, h)
+        return y if h is None else (y, h)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
@@ -197,16 +192,13 @@ class _BorderFunction(torch.autograd.Function):
         if like is None:
             return (None,) * 11
         if _tangent_among(*grads):
-            raise NotImplementedError("tv_norm, tv_residual: the gradients have no forward-mode derivative")
+            raise NotImplementedError("tv_residual: the gradients have no forward-mode derivative")
         # (hooks on saved tensors may bring back others, with the same values in strides of their own)
         for t, was in zip(saved, ctx.saved_as):
             if t is not None and (t.dtype is not was[1] or t.shape != was[0] or t.get_device() != like.get_device() or t.is_meta):
-                raise RuntimeError("tv_norm, tv_residual: a hook on saved tensors has brought back one of another shape, type or device")
-        at, f, weight, bias, gate, scale, next_weight, stats, seed_at = saved
-        if f is None:
-            dy, dh = None, grads[0]
-        else:
-            dy, dh = grads if border.next_norm else (grads[0], None)
+                raise RuntimeError("tv_residual: a hook on saved tensors has brought back one of another shape, type or device")
+        y, f, weight, bias, gate, scale, next_weight, stats, seed_at = saved
+        dy, dh = grads if border.next_norm else (grads[0], None)
         if dy is not None:
             dy = _dense(dy)
         if dh is not None:
@@ -220,12 +212,75 @@ class _BorderFunction(torch.autograd.Function):
             made = [like.new_zeros(s) if w else None for s, w in zip(shapes, need)]
         elif any(want):
             weight, bias, scale, next_weight, stats = [None if t is None else _dense(t) for t in (weight, bias, scale, next_weight, stats)]
-            made = _backward(like, dy, dh, at, f, weight, bias, gate, scale, next_weight, stats, border, ctx.seed, seed_at, want)
+            made = _backward(like, dy, dh, y, f, weight, bias, gate, scale, next_weight, stats, border, ctx.seed, seed_at, want)
         else:
             made = [None] * 8
         if need[0] and dh is None:
             made[0] = dy
         return (*made, None, None, None)
+
+
+@_on_device
+def _norm_forward(x, weight, bias, border, hold):
+    """(h, stats)"""
+    n = x.shape[-1]
+    m = x.numel() // n
+    rows, ldx = _rows(x)
+    h = x.new_empty(x.shape)
+    stats = x.new_empty((m, 4), dtype=torch.float32) if hold else None
+    ins = _b.tv_block_in(rows.data_ptr(), None, None, None, None, None, _address(weight), _address(bias))
+    _check(_b.lib().tv_block_fwd(ins, None, h.data_ptr(), _address(stats), _desc(m, n, ldx, n, n, _DTYPES[x.dtype], border), _b._stream(None)))
+    return h, stats
+
+
+@_on_device
+def _norm_backward(g, x, weight, stats, border, want):
+    """Gradients of x, weight and bias, None where not wanted."""
+    n = g.shape[-1]
+    m, dtype = g.numel() // n, _DTYPES[g.dtype]
+    x, ldx = _rows(x)
+    dx = g.new_empty(g.shape) if want[0] else None
+    dweight = g.new_empty(n) if want[1] else None
+    dbias = g.new_empty(n) if want[2] else None
+    ins = _b.tv_block_in(x.data_ptr(), None, None, None, None, None, _address(weight), None)
+    nbytes = _workspace_bytes(m, n, dtype, False, False, border, (want[0], False, False, False, False, False, want[1], want[2]))
+    ws = g.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+    _check(_b.lib().tv_block_bwd(None, g.data_ptr(), ins, stats.data_ptr(),
+                                 _b.tv_block_grads(_address(dx), None, None, None, None, None, _address(dweight), _address(dbias)),
+                                 _desc(m, n, ldx, n, n, dtype, border), _address(ws), nbytes, _b._stream(None)))
+    return dx, dweight, dbias
+
+
+class _Norm(torch.autograd.Function):
+    """A norm alone, which is called so often that it does without the border's other seven tensors."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, border):
+        if _tangent_among(x, weight, bias):
+            raise NotImplementedError("tv_norm: no forward-mode derivative")
+        h, stats = _norm_forward(x, weight, bias, border, True)
+        saved = (x, weight, stats)
+        ctx.save_for_backward(*saved)
+        ctx.saved_as = [None if t is None else (t.shape, t.dtype) for t in saved]
+        ctx.border = border
+        return h
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g):
+        if _tangent_among(g):
+            raise NotImplementedError("tv_norm: the gradients have no forward-mode derivative")
+        saved, where = ctx.saved_tensors, g.get_device()
+        for t, was in zip(saved, ctx.saved_as):
+            if t is not None and (t.dtype is not was[1] or t.shape != was[0] or t.get_device() != where or t.is_meta):
+                raise RuntimeError("tv_norm: a hook on saved tensors has brought back one of another shape, type or device")
+        x, weight, stats = saved
+        need = ctx.needs_input_grad
+        if g.numel() == 0:
+            n = g.shape[-1]
+            return (g if need[0] else None), (g.new_zeros(n) if need[1] else None), (g.new_zeros(n) if need[2] else None), None
+        dx, dweight, dbias = _norm_backward(_dense(g), x, None if weight is None else _dense(weight), _dense(stats), ctx.border, need)
+        return dx, dweight, dbias, None
 
 
 def _check_rows(x, what):
@@ -247,14 +302,13 @@ def _check_eps(eps, what):
 
 def _apply(x, f, weight, bias, gate, scale, next_weight, next_bias, border, seed, seed_at):
     grad = torch.is_grad_enabled() and (
-        x.requires_grad or (f is not None and (f.requires_grad or (weight is not None and weight.requires_grad)
-                                               or (bias is not None and bias.requires_grad) or (gate is not None and gate.requires_grad)
-                                               or (scale is not None and scale.requires_grad)))
-        or (next_weight is not None and next_weight.requires_grad) or (next_bias is not None and next_bias.requires_grad))
+        x.requires_grad or f.requires_grad or (weight is not None and weight.requires_grad)
+        or (bias is not None and bias.requires_grad) or (gate is not None and gate.requires_grad)
+        or (scale is not None and scale.requires_grad) or (next_weight is not None and next_weight.requires_grad) or (next_bias is not None and next_bias.requires_grad))
     if grad or _tangent_among(x, f, weight, bias, gate, scale, next_weight, next_bias):
         return _BorderFunction.apply(x, f, weight, bias, gate, scale, next_weight, next_bias, border, seed, seed_at)
     y, h, _ = _forward(x, f, weight, bias, gate, scale, next_weight, next_bias, border, seed, seed_at, False)
-    return h if y is None else y if h is None else (y, h)
+    return y if h is None else (y, h)
 
 
 def tv_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, kind: str = "rms",
@@ -267,7 +321,10 @@ def tv_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Ten
     weight = _check_channels(weight, n, "tv_norm (weight)", x)
     bias = _check_channels(bias, n, "tv_norm (bias)", x)
     border = _border(0, _NORMS[kind], 0, _check_eps(eps, "tv_norm"), 1, 0, 0)
-    return _apply(x, None, None, None, None, None, weight, bias, border, 0, None)
+    if (torch.is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad)
+                                     or (bias is not None and bias.requires_grad))) or _tangent_among(x, weight, bias):
+        return _Norm.apply(x, weight, bias, border)
+    return _norm_forward(x, weight, bias, border, False)[0]
 
 
 def tv_residual(x: torch.Tensor, f: torch.Tensor, norm: str = "none", weight: torch.Tensor | None = None,
@@ -307,7 +364,9 @@ def tv_residual(x: torch.Tensor, f: torch.Tensor, norm: str = "none", weight: to
 
 
 @_on_device
-def _drop(x, drop, seed, seed_at, offset):
+def _drop(x, how, seed_at):
+    """how: (drop, seed, offset)"""
+    drop, seed, offset = how
     n = x.shape[-1] if x.dim() else 1
     rows, ldx = _rows(x) if x.dim() else (x, 1)
     y = x.new_empty(x.shape)
@@ -318,20 +377,23 @@ def _drop(x, drop, seed, seed_at, offset):
 
 class _Dropout(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, drop, seed, seed_at, offset):
+    def forward(ctx, x, how, seed_at):
         if _tangent_among(x):
             raise NotImplementedError("tv_dropout: no forward-mode derivative")
-        ctx.how = drop, seed, offset
-        ctx.save_for_backward(seed_at)
-        return _drop(x, drop, seed, seed_at, offset)
+        ctx.how = how
+        if seed_at is not None:
+            ctx.save_for_backward(seed_at)
+        return _drop(x, how, seed_at)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, g):
         if _tangent_among(g):
             raise NotImplementedError("tv_dropout: the gradient has no forward-mode derivative")
-        drop, seed, offset = ctx.how
-        return _drop(g, drop, seed, ctx.saved_tensors[0], offset), None, None, None, None
+        saved = ctx.saved_tensors
+        if saved and (saved[0].dtype is not torch.int64 or saved[0].numel() != 1 or saved[0].device != g.device):
+            raise RuntimeError("tv_dropout: a hook on saved tensors has brought back one of another shape, type or device")
+        return _drop(g, ctx.how, saved[0] if saved else None), None, None
 
 
 def tv_dropout(x: torch.Tensor, p: float, seed, offset: int = 0) -> torch.Tensor:
@@ -347,8 +409,8 @@ def tv_dropout(x: torch.Tensor, p: float, seed, offset: int = 0) -> torch.Tensor
     if not drop or x.numel() == 0:
         return x
     if (torch.is_grad_enabled() and x.requires_grad) or _tangent_among(x):
-        return _Dropout.apply(x, drop, seed, seed_at, offset)
-    return _drop(x, drop, seed, seed_at, offset)
+        return _Dropout.apply(x, (drop, seed, offset), seed_at)
+    return _drop(x, (drop, seed, offset), seed_at)
 
 
 class TVNorm(torch.nn.Module):
