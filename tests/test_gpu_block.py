@@ -98,6 +98,56 @@ def test_many_rows(m, n, gate, dtype):
     assert all(torch.equal(got[k], again[k]) for k in got)
 
 
+@pytest.mark.parametrize("m,n", [(300001, 8), (8300, 8200), (8210, 2048)])
+def test_more_rows_than_a_launch_has_workgroups(m, n):
+    """A row's outputs and gradients are what they are among few others, to the bit; the vectors' gradients those of 64 bits."""
+    from paper_2204_03643_amd.block import tv_residual
+    gen = torch.Generator(device="cuda").manual_seed(m)
+    x, f, dy, dh = (torch.randn(m, n, generator=gen, device="cuda").bfloat16() for _ in range(4))
+    w = (1 + 0.1 * torch.randn(n, generator=gen, device="cuda")).bfloat16()
+
+    def call(*t):
+        x, f = (v.clone().requires_grad_() for v in t[:2])
+        y, h = tv_residual(x, f, norm="rms", weight=w, next_norm="layer", next_weight=w)
+        return [y.detach(), h.detach(), *torch.autograd.grad([y, h], [x, f], t[2:])]
+    some = torch.tensor([0, 1, m // 2, m - 2, m - 1], device="cuda")
+    for a, b in zip(call(x, f, dy, dh), call(*(v[some] for v in (x, f, dy, dh)))):
+        assert torch.equal(a[some], b)
+    leaf = w.clone().requires_grad_()
+    y, h = tv_residual(x, f, next_norm="rms", next_weight=leaf)
+    got = torch.autograd.grad(h, leaf, dh)[0].double()
+    for first in range(0, n, 1024):
+        cols = slice(first, first + 1024)
+        wide = x[:, cols].double() + f[:, cols].double()
+        r = ((x.float() + f.float()).square().mean(-1, keepdim=True) + 1e-6).rsqrt().double()
+        terms = dh[:, cols].double() * wide * r
+        # y is rounded to bf16 for the backward pass; the sum has m terms in 32 bits, and is rounded
+        off = terms.abs().sum(0) * (blockref.unit(torch.bfloat16) + (m + 48) * blockref.U32) + terms.sum(0).abs() * blockref.unit(torch.bfloat16)
+        assert bool(((got[cols] - terms.sum(0)).abs() <= off).all())
+
+
+def test_saved_tensors_that_come_back_as_others():
+    from paper_2204_03643_amd.block import tv_dropout, tv_norm, tv_residual
+    x, f = (torch.randn(6, 40, device="cuda", requires_grad=True) for _ in range(2))
+    seed = torch.tensor([4], device="cuda")
+
+    def call():
+        y, h = tv_residual(x, f, norm="layer", dropout=0.3, seed=seed, next_norm="rms")
+        return (y * h).sum() + tv_norm(f).sum() + tv_dropout(x, 0.5, seed, 1).square().sum()
+    want = torch.autograd.grad(call(), [x, f])
+    with torch.autograd.graph.save_on_cpu():
+        out = call()
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(out, [x, f]), want))
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: t.t().contiguous().t() if t.dim() == 2 else t):
+        out = call()
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(out, [x, f]), want))
+    for make in (lambda: tv_norm(f).sum(), lambda: tv_residual(x, f, norm="rms").sum()):
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: t[:1]):
+            out = make()
+        with pytest.raises(RuntimeError, match="hook"):
+            torch.autograd.grad(out, f)
+
+
 @pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
 @pytest.mark.parametrize("upstream", (("dy",), ("dh",)))
 def test_a_gradient_of_one_output_alone(upstream, dtype):

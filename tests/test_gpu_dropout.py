@@ -89,6 +89,15 @@ def test_rows_past_32_bits():
     assert torch.equal(tv_norm(x), tv_norm(dense))
 
 
+def test_more_rows_than_a_launch_has_workgroups():
+    from paper_2204_03643_amd.block import tv_dropout
+    rows, n = 300001, 12
+    y = tv_dropout(torch.ones(rows, n, device="cuda"), 0.4, 9)
+    some = [0, 1, 262143, 262144, 300000]
+    keep, _ = blockref.kept(some, n, 0.4, 9, 0)
+    assert torch.equal(y[some].cpu() != 0, keep)
+
+
 def test_shapes():
     from paper_2204_03643_amd.block import tv_dropout
     x = torch.randn(6, 50, device="cuda")
