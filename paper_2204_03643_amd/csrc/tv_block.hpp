@@ -213,6 +213,17 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_fwd_kernel(Blo
         for (int i = 0; i < 8; ++i) v[i] *= r;
         return float2{mean, r};
     };
+    // (the vectors' values for these channels, before anything waits)
+    Raw8<T> w, b, scale, nw, nb;
+    if constexpr (F) {
+        if (a.w) w = raw8<TAIL>((const T *)a.w + col, have);
+        if (a.b) b = raw8<TAIL>((const T *)a.b + col, have);
+        if (a.scale) scale = raw8<TAIL>((const T *)a.scale + col, have);
+    }
+    if constexpr (N) {
+        if (a.nw) nw = raw8<TAIL>((const T *)a.nw + col, have);
+        if (a.nb) nb = raw8<TAIL>((const T *)a.nb + col, have);
+    }
     int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES;
     if constexpr (LANES == 64) row = (int64_t)blockIdx.x * kRows + __builtin_amdgcn_readfirstlane(threadIdx.x / LANES);
     for (; row < a.m; row += (int64_t)gridDim.x * kRows) {
@@ -223,32 +234,26 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_fwd_kernel(Blo
             const Raw8<T> raw = raw8<TAIL>((const T *)a.f + row * a.ldf + col, have);
             Raw8<T> z;
             if (a.gate) z = raw8<TAIL>((const T *)a.gate + (int64_t)((uint32_t)row / (uint32_t)a.gate_div) * a.ldg + col, have);
-            float f[8], p[8];
+            float f[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = raw[i];
             if (a.norm != kNormNone) {
                 const float2 s = normalise(f, a.norm);
                 st.x = s.x;
                 st.y = s.y;
-                if (a.w) {
-                    vector8<TAIL, T>(p, a.w, col, have, 1.0f);
+                if (a.w)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) f[i] *= p[i];
-                }
-                if (a.b) {
-                    vector8<TAIL, T>(p, a.b, col, have, 0.0f);
+                    for (int i = 0; i < 8; ++i) f[i] *= w[i];
+                if (a.b)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) f[i] += p[i];
-                }
+                    for (int i = 0; i < 8; ++i) f[i] += b[i];
             }
             if (a.gate)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) f[i] *= gate_of<FAST>(z[i], a.act);
-            if (a.scale) {
-                vector8<TAIL, T>(p, a.scale, col, have, 1.0f);
+            if (a.scale)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] *= p[i];
-            }
+                for (int i = 0; i < 8; ++i) f[i] *= scale[i];
             if (drops) drop8(f, drop_numbers(key, (uint32_t)row, (uint32_t)col / 8), a.drop);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = x[i] + f[i];
@@ -261,17 +266,12 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_fwd_kernel(Blo
             const float2 s = normalise(v, a.next);
             st.z = s.x;
             st.w = s.y;
-            float p[8];
-            if (a.nw) {
-                vector8<TAIL, T>(p, a.nw, col, have, 1.0f);
+            if (a.nw)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] *= p[i];
-            }
-            if (a.nb) {
-                vector8<TAIL, T>(p, a.nb, col, have, 0.0f);
+                for (int i = 0; i < 8; ++i) v[i] *= nw[i];
+            if (a.nb)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] += p[i];
-            }
+                for (int i = 0; i < 8; ++i) v[i] += nb[i];
             if (live) store8(h + row * a.n + col, v, have);
         }
         if (stats && lane == 0) stats[row] = st;
