@@ -22,6 +22,17 @@ _GATE_ACTS = {"none": _b.TV_GATE_PLAIN, "sigmoid": _b.TV_GATE_SIGMOID, "silu": _
 _NO_DROP = _b.tv_drop(0, 0, None, 0)
 
 
+def _once_differentiable(backward):
+    """torch's decorator where a graph of the gradients is asked for (which refuses to differentiate it); without one the
+    function itself, which saves what the decorator costs in every step."""
+    refusing = torch.autograd.function.once_differentiable(backward)
+
+    @functools.wraps(backward)
+    def call(ctx, *grads):
+        return refusing(ctx, *grads) if torch.is_grad_enabled() else backward(ctx, *grads)
+    return call
+
+
 class _Border(typing.NamedTuple):
     """What a border does, beside its tensors."""
     norm: int
@@ -184,7 +195,7 @@ class _BorderFunction(torch.autograd.Function):
         return y if h is None else (y, h)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once_differentiable
     def backward(ctx, *grads):
         border, need = ctx.border, ctx.needs_input_grad
         saved = ctx.saved_tensors
@@ -266,7 +277,7 @@ class _Norm(torch.autograd.Function):
         return h
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once_differentiable
     def backward(ctx, g):
         if _tangent_among(g):
             raise NotImplementedError("tv_norm: the gradients have no forward-mode derivative")
@@ -386,7 +397,7 @@ class _Dropout(torch.autograd.Function):
         return _drop(x, how, seed_at)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once_differentiable
     def backward(ctx, g):
         if _tangent_among(g):
             raise NotImplementedError("tv_dropout: the gradient has no forward-mode derivative")

@@ -12,7 +12,7 @@ enum Vector : int { kDw = 0, kDb = 1, kDscale = 2, kDnw = 3, kDnb = 4 };
 inline int block_lanes(int64_t n)
 {
     const int64_t per = tiles(n, 8);
-    for (int lanes : {8, 32, 64, 128, 256, 512})
+    for (int lanes : {8, 16, 32, 64, 128, 256, 512})
         if (per <= lanes) return lanes;
     return 1024;
 }

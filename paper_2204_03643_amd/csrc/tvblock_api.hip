@@ -98,6 +98,7 @@ int block_fwd(const Block &a, void *y, void *h, float *stats, hipStream_t stream
 {
     switch (block_lanes(a.n)) {
     case 8: return launch_fwd<T, 8>(a, y, h, stats, stream);
+    case 16: return launch_fwd<T, 16>(a, y, h, stats, stream);
     case 32: return launch_fwd<T, 32>(a, y, h, stats, stream);
     case 64: return launch_fwd<T, 64>(a, y, h, stats, stream);
     case 128: return launch_fwd<T, 128>(a, y, h, stats, stream);
@@ -136,6 +137,7 @@ int block_bwd(const Block &a, BlockGrads o, const tv_block_grads &g, const Block
     switch (a.m > 0 ? block_lanes(a.n) : 0) {
     case 0: break;
     case 8: st = launch_bwd<T, 8>(a, o, stream); break;
+    case 16: st = launch_bwd<T, 16>(a, o, stream); break;
     case 32: st = launch_bwd<T, 32>(a, o, stream); break;
     case 64: st = launch_bwd<T, 64>(a, o, stream); break;
     case 128: st = launch_bwd<T, 128>(a, o, stream); break;
