@@ -373,6 +373,7 @@ struct BlockGrads {
     float2 *row_sums;        // [m] of the next norm, for the kernel that sums over rows by itself
     float *sums;             // [wanted ones][units][n]: the vectors', then the gate's where its rows are cut
     uint32_t want;           // a bit each
+    uint8_t slot[kSums];     // where the sums over rows lie in LDS (kNoSlot: not made), if they do
     Units units;
     __device__ __forceinline__ float *place(int k, int unit, int n) const
     {
@@ -442,8 +443,10 @@ __device__ __forceinline__ void branch_terms(float (&d)[8], float (&fh)[8], floa
     }
 }
 
-// A lane has the same eight channels of every row of its unit, the vectors' values for them and their sums over the rows in
-// registers, and the next row's values on their way while it works on one.  Without a TAIL the channels are a multiple
+// A lane has the same eight channels of every row of its unit.  Up to 4096 channels (SLOTS 0) it has the vectors' values for
+// them and their sums over the rows in registers, with the next row's values on their way while it works on one.  With more
+// (1024 lanes, 128 registers each) the sums lie in LDS, a slot of 8192 floats each, where a lane meets nobody else's, the vectors are
+// read again for every row, and only rows in bf16 come ahead of time.  Without a TAIL the channels are a multiple
 // of eight: a lane has eight or none, and one that has none goes along with the first lane's (in bounds, left out of
 // the row's sums and not stored).
 //
@@ -452,11 +455,12 @@ __device__ __forceinline__ void branch_terms(float (&d)[8], float (&fh)[8], floa
 //
 // Three waves to a SIMD, as the registers allow: 768 workgroups of 256 lanes (16384 x 2048: 86 us; 1024 workgroups without the
 // next row on its way, a third of them in a second round, masks at every value and sums by LDS permutes: 220).
-template <class T, int LANES, bool F, bool N, bool TAIL>
+template <class T, int LANES, bool F, bool N, bool TAIL, int SLOTS>
 __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Block a, BlockGrads o)
 {
-    constexpr bool FAST = sizeof(T) == 2;
+    constexpr bool FAST = sizeof(T) == 2, WIDE = SLOTS > 0, AHEAD = !WIDE || sizeof(T) == 2;
     __shared__ float2 lds[2][RowSum<LANES>::kWaves];
+    __shared__ f32x4 slots[WIDE ? SLOTS : 1][2][WIDE ? LANES : 1];
     RowSum<LANES> sum(lds);
     const int lane = threadIdx.x % LANES;
     const bool live = lane * 8 < a.n;
@@ -471,16 +475,50 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
     const bool own_gates = F && o.dgate && a.gate_div == 1, whole_gates = F && o.dgate && a.gate_div > 1 && o.units.cuts == 1;
     const DropKey key = drops ? drop_key(a.drop) : DropKey{};
 
-    float nw[8], w[8], b[8], scale[8];
-    if constexpr (N) vector8<TAIL, T>(nw, a.nw, col, have, 1.0f);
-    if constexpr (F) {
-        vector8<TAIL, T>(w, a.w, col, have, 1.0f);
-        vector8<TAIL, T>(b, a.b, col, have, 0.0f);
-        vector8<TAIL, T>(scale, a.scale, col, have, 1.0f);
+    // the vectors: once, or where they are used
+    constexpr int kOnce = WIDE ? 1 : 8;
+    float nw_[kOnce], w_[kOnce], b_[kOnce], scale_[kOnce];
+    if constexpr (!WIDE) {
+        if constexpr (N) vector8<TAIL, T>(nw_, a.nw, col, have, 1.0f);
+        if constexpr (F) {
+            vector8<TAIL, T>(w_, a.w, col, have, 1.0f);
+            vector8<TAIL, T>(b_, a.b, col, have, 0.0f);
+            vector8<TAIL, T>(scale_, a.scale, col, have, 1.0f);
+        }
     }
-    float A[8], B[8], dgate[8], dnw[8], dnb[8];
+    auto vector = [&](float (&v)[8], const float (&once)[kOnce], const void *p, float otherwise) __attribute__((always_inline)) {
+        if constexpr (WIDE) vector8<TAIL, T>(v, p, col, have, otherwise);
+        else
 #pragma unroll
-    for (int i = 0; i < 8; ++i) A[i] = B[i] = dgate[i] = dnw[i] = dnb[i] = 0.0f;
+            for (int i = 0; i < 8; ++i) v[i] = once[i];
+    };
+    // the sums over the rows: step(i, sum so far) for each channel
+    float sums_[WIDE ? 1 : kSums][8];
+    auto sum_of = [&](int k, auto step) __attribute__((always_inline)) {
+        if constexpr (WIDE) {
+            if (o.slot[k] < SLOTS) {
+                f32x4 v[2] = {slots[o.slot[k]][0][lane], slots[o.slot[k]][1][lane]};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = step(i, v[i >> 2][i & 3]);
+                slots[o.slot[k]][0][lane] = v[0];
+                slots[o.slot[k]][1][lane] = v[1];
+            }
+        } else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sums_[k][i] = step(i, sums_[k][i]);
+    };
+    auto take = [&](int k, float (&v)[8]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+        sum_of(k, [&](int i, float s) __attribute__((always_inline)) { v[i] = s; return s; });
+    };
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) {
+        if constexpr (WIDE) sum_of(k, [](int, float) __attribute__((always_inline)) { return 0.0f; });
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sums_[k][i] = 0.0f;
+    }
 
     struct Row {
         Raw8<T> dy, dh, y, f, z;
@@ -501,25 +539,29 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
         }
         return v;
     };
-    Row ahead = fetch(row);                          // (a unit has at least one row)
+    Row ahead;
+    if constexpr (AHEAD) ahead = fetch(row);         // (a unit has at least one row)
     for (; row < end; ++row) {
-        const Row v = ahead;
-        if (row + 1 < end) ahead = fetch(row + 1);
+        Row v;
+        if constexpr (AHEAD) {
+            v = ahead;
+            if (row + 1 < end) ahead = fetch(row + 1);
+        } else v = fetch(row);
         float d[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) d[i] = o.dy ? v.dy[i] : 0.0f;
         if (next) {
             float t[8], yh[8], s1 = 0.0f, s2 = 0.0f;
+            vector(t, nw_, a.nw, 1.0f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float g = v.dh[i];
                 yh[i] = a.next == kNormLayer ? (v.y[i] - v.st.z) * v.st.w : v.y[i] * v.st.w;
-                t[i] = g * nw[i];
+                t[i] *= v.dh[i];
                 s1 += t[i];
                 s2 = fmaf(t[i], yh[i], s2);
-                dnw[i] = fmaf(g, yh[i], dnw[i]);
-                dnb[i] += g;
             }
+            sum_of(kSumDnw, [&](int i, float s) __attribute__((always_inline)) { return fmaf(v.dh[i], yh[i], s); });
+            sum_of(kSumDnb, [&](int i, float s) __attribute__((always_inline)) { return s + v.dh[i]; });
             if (!TAIL && !live) s1 = s2 = 0.0f;
             const float2 c = sum(s1, s2);
             const float k1 = a.next == kNormLayer ? -v.st.w * c.x * a.inv_n : 0.0f, k2 = -v.st.w * c.y * a.inv_n;
@@ -531,32 +573,33 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
         }
         if (o.dx && live) store8((T *)o.dx + row * a.n + col, d, have);
         if constexpr (F) {
-            float fh[8], s1 = 0.0f, s2 = 0.0f;
+            float fh[8], w[8], scale[8], s1 = 0.0f, s2 = 0.0f;
+            vector(w, w_, a.w, 1.0f);
+            vector(scale, scale_, a.scale, 1.0f);
             if (drops) drop8(d, drop_numbers(key, (uint32_t)row, (uint32_t)col / 8), a.drop);
 #pragma unroll
             for (int i = 0; i < 8; ++i) fh[i] = !normed ? v.f[i] : a.norm == kNormLayer ? (v.f[i] - v.st.x) * v.st.y : v.f[i] * v.st.y;
             if (a.gate) {
-                float dg[8];
+                float dg[8], b[8];
+                vector(b, b_, a.b, 0.0f);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float z = v.z[i], p = d[i] * fmaf(fh[i], w[i], b[i]) * scale[i];
                     dg[i] = p * gate_slope<FAST>(z, a.act);
-                    dgate[i] += dg[i];
                     d[i] *= gate_of<FAST>(z, a.act);
                 }
+                sum_of(kSumGate, [&](int i, float s) __attribute__((always_inline)) { return s + dg[i]; });
                 if (own_gates && live) store8((T *)o.dgate + row * a.n + col, dg, have);
                 if (whole_gates && ((uint32_t)row + 1) % (uint32_t)a.gate_div == 0) {
-                    if (live) store8((T *)o.dgate + (int64_t)((uint32_t)row / (uint32_t)a.gate_div) * a.n + col, dgate, have);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) dgate[i] = 0.0f;
+                    take(kSumGate, dg);
+                    if (live) store8((T *)o.dgate + (int64_t)((uint32_t)row / (uint32_t)a.gate_div) * a.n + col, dg, have);
+                    sum_of(kSumGate, [](int, float) __attribute__((always_inline)) { return 0.0f; });
                 }
             }
+            sum_of(kSumA, [&](int i, float s) __attribute__((always_inline)) { return fmaf(d[i], fh[i], s); });
+            sum_of(kSumB, [&](int i, float s) __attribute__((always_inline)) { return s + d[i]; });
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                A[i] = fmaf(d[i], fh[i], A[i]);
-                B[i] += d[i];
-                d[i] *= scale[i];
-            }
+            for (int i = 0; i < 8; ++i) d[i] *= scale[i];
             if (normed) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -577,8 +620,14 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
     auto leave = [&](int k, const float (&v)[8]) __attribute__((always_inline)) {
         if (o.want >> k & 1) store8(o.place(k, unit, a.n) + col, v, have);
     };
+    float v[8];
     if constexpr (F) {
-        float v[8];
+        float A[8], B[8], w[8], b[8], scale[8];
+        take(kSumA, A);
+        take(kSumB, B);
+        vector(w, w_, a.w, 1.0f);
+        vector(b, b_, a.b, 0.0f);
+        vector(scale, scale_, a.scale, 1.0f);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = scale[i] * A[i];
         leave(kDw, v);
@@ -588,10 +637,13 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = fmaf(w[i], A[i], b[i] * B[i]);
         leave(kDscale, v);
-        leave(kVectors, dgate);
+        take(kSumGate, v);
+        leave(kVectors, v);
     }
-    leave(kDnw, dnw);
-    leave(kDnb, dnb);
+    take(kSumDnw, v);
+    leave(kDnw, v);
+    take(kSumDnb, v);
+    leave(kDnb, v);
 }
 
 // Rows of more channels: one row after the other, without sums over them.

@@ -7,6 +7,9 @@ namespace tvl {
 
 constexpr int kVectors = 5;                  // sums over rows, in this order; the gate's are the sixth
 enum Vector : int { kDw = 0, kDb = 1, kDscale = 2, kDnw = 3, kDnb = 4 };
+constexpr int kSums = 5;                     // what is summed over rows to make them: see block_bwd_kernel
+enum Sum : int { kSumA = 0, kSumB = 1, kSumDnw = 2, kSumDnb = 3, kSumGate = 4 };
+constexpr int kNoSlot = 255, kMostSlots = 4; // of 8192 floats each in LDS
 
 // Lanes side by side in a row of n channels, eight channels each (twice eight from 8193 channels on).
 inline int block_lanes(int64_t n)
@@ -16,7 +19,7 @@ inline int block_lanes(int64_t n)
         if (per <= lanes) return lanes;
     return 1024;
 }
-constexpr int kMostSumLanes = 512;           // with more, lanes keep no sums over rows
+constexpr int kMostSumLanes = 512;           // with more, lanes keep no sums over rows in registers
 
 // Units are runs of rows whose sums one group of lanes makes.  A gate's rows that are shared by several rows of x are either
 // cut into `cuts` units each, whose sums are joined afterwards, or lie whole within a unit (cuts 1).
@@ -64,6 +67,9 @@ inline Units block_units(int64_t m, int64_t n, bool shared_gate, int64_t gate_di
 struct BlockBwdPlan {
     Units units;
     uint32_t want;           // a bit a vector, and the gate's where its rows are cut
+    int slots;               // sums over rows in LDS; 0: in registers
+    uint8_t slot[kSums];
+    bool two_passes;         // the rows first, the sums over them in a pass of their own
     size_t row_sums, bytes;  // where the rows' own sums lie
 };
 
@@ -79,7 +85,16 @@ inline BlockBwdPlan block_bwd_plan(const tv_block_in &in, const tv_block_grads &
     if (shared && p.units.cuts > 1) p.want |= 1u << kVectors, ++wanted;
     p.row_sums = (size_t)up(wanted * p.units.count * d.n * 4, 256);
     p.bytes = p.row_sums;
-    if (block_lanes(d.n) > kMostSumLanes && (p.want || shared)) p.bytes += (size_t)up(d.m * 8, 256);
+    if (block_lanes(d.n) > kMostSumLanes) {
+        // Sums in LDS where its slots are enough: up to 8192 channels, and all but both norms' biases beside a shared gate
+        // (8192 bf16 channels of 4096 rows, two norms and a scale: 265 us in two passes, see block_bwd_kernel for one).
+        const bool bias = in.bias && d.norm != TV_NORM_NONE;
+        const bool made[kSums] = {in.f && (g.dweight || g.dscale), in.f && (g.dbias || (g.dscale && bias)), g.dnext_weight != nullptr,
+                                  g.dnext_bias != nullptr, shared};
+        for (int k = 0; k < kSums; ++k) p.slot[k] = made[k] ? (uint8_t)p.slots++ : (uint8_t)kNoSlot;
+        p.two_passes = p.slots > kMostSlots || d.n > 8192;
+        if (p.two_passes && (p.want || shared)) p.bytes += (size_t)up(d.m * 8, 256);
+    }
     return p;
 }
 

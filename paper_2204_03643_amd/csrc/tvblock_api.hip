@@ -108,15 +108,16 @@ int block_fwd(const Block &a, void *y, void *h, float *stats, hipStream_t stream
     }
 }
 
-template <class T, int LANES>
+template <class T, int LANES, int SLOTS>
 int launch_bwd(const Block &a, const BlockGrads &o, hipStream_t stream)
 {
     const int units = LANES > 64 ? 1 : 64 / LANES;
     const dim3 grid((uint32_t)tiles(o.units.count, units)), block(LANES > 64 ? LANES : 64);
     const bool tail = a.n % 8 != 0;
-    if (a.f && a.next) hipLaunchKernelGGL((tail ? block_bwd_kernel<T, LANES, true, true, true> : block_bwd_kernel<T, LANES, true, true, false>), grid, block, 0, stream, a, o);
-    else if (a.f) hipLaunchKernelGGL((tail ? block_bwd_kernel<T, LANES, true, false, true> : block_bwd_kernel<T, LANES, true, false, false>), grid, block, 0, stream, a, o);
-    else hipLaunchKernelGGL((tail ? block_bwd_kernel<T, LANES, false, true, true> : block_bwd_kernel<T, LANES, false, true, false>), grid, block, 0, stream, a, o);
+    if (a.f && a.next) hipLaunchKernelGGL((tail ? block_bwd_kernel<T, LANES, true, true, true, SLOTS> : block_bwd_kernel<T, LANES, true, true, false, SLOTS>), grid, block, 0, stream, a, o);
+    else if (a.f) hipLaunchKernelGGL((tail ? block_bwd_kernel<T, LANES, true, false, true, SLOTS> : block_bwd_kernel<T, LANES, true, false, false, SLOTS>), grid, block, 0, stream, a, o);
+    else if constexpr (SLOTS <= 2)                   // (two sums are all that a norm alone has)
+        hipLaunchKernelGGL((tail ? block_bwd_kernel<T, LANES, false, true, true, SLOTS> : block_bwd_kernel<T, LANES, false, true, false, SLOTS>), grid, block, 0, stream, a, o);
     return launched();
 }
 
@@ -136,14 +137,18 @@ int block_bwd(const Block &a, BlockGrads o, const tv_block_grads &g, const Block
     int st = TV_OK;
     switch (a.m > 0 ? block_lanes(a.n) : 0) {
     case 0: break;
-    case 8: st = launch_bwd<T, 8>(a, o, stream); break;
-    case 16: st = launch_bwd<T, 16>(a, o, stream); break;
-    case 32: st = launch_bwd<T, 32>(a, o, stream); break;
-    case 64: st = launch_bwd<T, 64>(a, o, stream); break;
-    case 128: st = launch_bwd<T, 128>(a, o, stream); break;
-    case 256: st = launch_bwd<T, 256>(a, o, stream); break;
-    case 512: st = launch_bwd<T, 512>(a, o, stream); break;
+    case 8: st = launch_bwd<T, 8, 0>(a, o, stream); break;
+    case 16: st = launch_bwd<T, 16, 0>(a, o, stream); break;
+    case 32: st = launch_bwd<T, 32, 0>(a, o, stream); break;
+    case 64: st = launch_bwd<T, 64, 0>(a, o, stream); break;
+    case 128: st = launch_bwd<T, 128, 0>(a, o, stream); break;
+    case 256: st = launch_bwd<T, 256, 0>(a, o, stream); break;
+    case 512: st = launch_bwd<T, 512, 0>(a, o, stream); break;
     default: {
+        if (!p.two_passes) {
+            st = p.slots <= 2 ? launch_bwd<T, 1024, 2>(a, o, stream) : launch_bwd<T, 1024, kMostSlots>(a, o, stream);
+            break;
+        }
         // rows first; then the sums over them
         st = a.n <= 8192 ? launch_rows<T, 1>(a, o, stream) : launch_rows<T, 2>(a, o, stream);
         if (st != TV_OK || !(p.want || (o.dgate && a.gate_div > 1))) break;
@@ -245,6 +250,7 @@ int tv_block_bwd(const void *dy, const void *dh, tv_block_in in, const float *st
     o.sums = (float *)ws;
     o.row_sums = p.bytes > p.row_sums ? (float2 *)((char *)ws + p.row_sums) : nullptr;
     o.want = p.want;
+    for (int k = 0; k < kSums; ++k) o.slot[k] = p.slot[k];
     o.units = p.units;
     return d.dtype == TV_BF16 ? block_bwd<bf16>(a, o, g, p, stream) : block_bwd<float>(a, o, g, p, stream);
 }

@@ -149,6 +149,17 @@ def test_saved_tensors_that_come_back_as_others():
 
 
 @pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("m,n,gate,norm,next_norm,bias", [(600, 4200, 6, "layer", "layer", True), (600, 8192, 600, "layer", "layer", True), (600, 8191, 2, "layer", "rms", True),
+                                                          (520, 5000, 0, "rms", "none", False), (520, 5000, 5, "none", "rms", False), (300, 6001, 0, "layer", "none", True)])
+def test_wide_rows(m, n, gate, norm, next_norm, bias, dtype):
+    """More than 4096 channels, with few sums over the rows, with many, and with more than fit beside each other."""
+    how = dict(norm=norm, next_norm=next_norm)
+    t = made(m, n, dtype, m + n, norm, next_norm, bias, gate, True)
+    got = run(t, (gate or 1, m // (gate or 1), n), (gate, 1, n), dropout=0.1, seed=3, **how)
+    check(t, dtype, got, p=0.1, seed=3, **how)
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
 @pytest.mark.parametrize("upstream", (("dy",), ("dh",)))
 def test_a_gradient_of_one_output_alone(upstream, dtype):
     how = dict(norm="rms", next_norm="layer")
