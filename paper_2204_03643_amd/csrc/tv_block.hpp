@@ -371,13 +371,14 @@ struct BlockGrads {
     const float4 *stats;
     void *dx, *df, *dgate;
     float2 *row_sums;        // [m] of the next norm, for the kernel that sums over rows by itself
-    float *sums;             // [wanted ones][units][n]: the vectors', then the gate's where its rows are cut
+    float *sums;             // [wanted ones][parts][n]: the vectors'; then [units][n], the gate's where its rows are cut
     uint32_t want;           // a bit each
     uint8_t slot[kSums];     // where the sums over rows lie in LDS (kNoSlot: not made), if they do
+    int32_t parts;           // how many sums of a vector's there are: one a workgroup, of all its units
     Units units;
-    __device__ __forceinline__ float *place(int k, int unit, int n) const
+    __device__ __forceinline__ float *place(int k, int part, int n) const
     {
-        return sums + ((int64_t)__popc(want & ((1u << k) - 1)) * units.count + unit) * n;
+        return sums + ((int64_t)__popc(want & ((1u << k) - 1)) * parts + part) * n;
     }
 };
 
@@ -468,9 +469,8 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
     constexpr int kUnits = LANES > 64 ? 1 : 64 / LANES;
     int unit = (int)blockIdx.x * kUnits + (LANES > 64 ? 0 : threadIdx.x / LANES);
     if constexpr (LANES == 64) unit = __builtin_amdgcn_readfirstlane(unit);
-    if (unit >= o.units.count) return;               // (whole rows of lanes; whole workgroups where there are barriers)
-    int64_t row, end;
-    range_of(o.units, unit, a.m, row, end);
+    int64_t row = 0, end = 0;                        // (a wave's last lanes may be without a unit)
+    if (unit < o.units.count) range_of(o.units, unit, a.m, row, end);
     const bool drops = F && a.drop.below != 0, next = N && o.dh, normed = F && a.norm != kNormNone;
     const bool own_gates = F && o.dgate && a.gate_div == 1, whole_gates = F && o.dgate && a.gate_div > 1 && o.units.cuts == 1;
     const DropKey key = drops ? drop_key(a.drop) : DropKey{};
@@ -540,7 +540,8 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
         return v;
     };
     Row ahead;
-    if constexpr (AHEAD) ahead = fetch(row);         // (a unit has at least one row)
+    if constexpr (AHEAD)
+        if (row < end) ahead = fetch(row);
     for (; row < end; ++row) {
         Row v;
         if constexpr (AHEAD) {
@@ -616,15 +617,22 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
             if (o.df && live) store8((T *)o.df + row * a.n + col, d, have);
         }
     }
-    if (!live) return;
+    // a workgroup's sums leave together: those of a wave's units are joined in it (a cut gate's are not, they stay apart)
+    auto joined = [&](int k, float (&v)[8]) __attribute__((always_inline)) {
+        take(k, v);
+#pragma unroll
+        for (int j = LANES; j < 64; j <<= 1)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += __shfl_xor(v[i], j);
+    };
     auto leave = [&](int k, const float (&v)[8]) __attribute__((always_inline)) {
-        if (o.want >> k & 1) store8(o.place(k, unit, a.n) + col, v, have);
+        if (live && threadIdx.x < LANES && (o.want >> k & 1)) store8(o.place(k, blockIdx.x, a.n) + col, v, have);
     };
     float v[8];
     if constexpr (F) {
         float A[8], B[8], w[8], b[8], scale[8];
-        take(kSumA, A);
-        take(kSumB, B);
+        joined(kSumA, A);
+        joined(kSumB, B);
         vector(w, w_, a.w, 1.0f);
         vector(b, b_, a.b, 0.0f);
         vector(scale, scale_, a.scale, 1.0f);
@@ -638,11 +646,11 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
         for (int i = 0; i < 8; ++i) v[i] = fmaf(w[i], A[i], b[i] * B[i]);
         leave(kDscale, v);
         take(kSumGate, v);
-        leave(kVectors, v);
+        if (live && unit < o.units.count && (o.want >> kVectors & 1)) store8(o.place(kVectors, unit, a.n) + col, v, have);
     }
-    take(kSumDnw, v);
+    joined(kSumDnw, v);
     leave(kDnw, v);
-    take(kSumDnb, v);
+    joined(kSumDnb, v);
     leave(kDnb, v);
 }
 
@@ -795,7 +803,7 @@ struct Joins {
     void *to[kVectors];
     const float *gate_from;
     void *gate_to;
-    int32_t vectors, units, cuts, n;
+    int32_t vectors, parts, cuts, n;
 };
 template <class T> __global__ __launch_bounds__(1024) void block_join_kernel(Joins j)
 {
@@ -804,7 +812,7 @@ template <class T> __global__ __launch_bounds__(1024) void block_join_kernel(Joi
     const int c = threadIdx.x & 31, g = threadIdx.x >> 5, col = (int)blockIdx.x * 32 + c, y = blockIdx.y;
     const float *from = y < j.vectors ? j.from[y] : j.gate_from + (int64_t)(y - j.vectors) * j.cuts * j.n;
     T *to = y < j.vectors ? (T *)j.to[y] : (T *)j.gate_to + (int64_t)(y - j.vectors) * j.n;
-    const int count = y < j.vectors ? j.units : j.cuts;
+    const int count = y < j.vectors ? j.parts : j.cuts;
     float s = 0.0f;
     if (col < j.n)
 #pragma unroll 8

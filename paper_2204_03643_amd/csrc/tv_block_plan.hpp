@@ -66,6 +66,7 @@ inline Units block_units(int64_t m, int64_t n, bool shared_gate, int64_t gate_di
 
 struct BlockBwdPlan {
     Units units;
+    int32_t parts;           // workgroups, each with sums of its units
     uint32_t want;           // a bit a vector, and the gate's where its rows are cut
     int slots;               // sums over rows in LDS; 0: in registers
     uint8_t slot[kSums];
@@ -79,11 +80,13 @@ inline BlockBwdPlan block_bwd_plan(const tv_block_in &in, const tv_block_grads &
     const bool shared = in.f && in.gate && g.dgate && d.gate_div > 1;
     p.units = block_units(d.m, d.n, shared, d.gate_div);
     const void *vectors[kVectors] = {in.f ? g.dweight : nullptr, in.f ? g.dbias : nullptr, in.f ? g.dscale : nullptr, g.dnext_weight, g.dnext_bias};
+    p.parts = (int32_t)(block_lanes(d.n) < 64 ? tiles(p.units.count, 64 / block_lanes(d.n)) : p.units.count);
     int64_t wanted = 0;
     for (int k = 0; k < kVectors; ++k)
         if (vectors[k]) p.want |= 1u << k, ++wanted;
-    if (shared && p.units.cuts > 1) p.want |= 1u << kVectors, ++wanted;
-    p.row_sums = (size_t)up(wanted * p.units.count * d.n * 4, 256);
+    const bool cut = shared && p.units.cuts > 1;
+    if (cut) p.want |= 1u << kVectors;
+    p.row_sums = (size_t)up((wanted * p.parts + (cut ? p.units.count : 0)) * d.n * 4, 256);
     p.bytes = p.row_sums;
     if (block_lanes(d.n) > kMostSumLanes) {
         // Sums in LDS where its slots are enough: up to 8192 channels, and all but both norms' biases beside a shared gate

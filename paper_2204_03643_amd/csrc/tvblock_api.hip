@@ -111,8 +111,7 @@ int block_fwd(const Block &a, void *y, void *h, float *stats, hipStream_t stream
 template <class T, int LANES, int SLOTS>
 int launch_bwd(const Block &a, const BlockGrads &o, hipStream_t stream)
 {
-    const int units = LANES > 64 ? 1 : 64 / LANES;
-    const dim3 grid((uint32_t)tiles(o.units.count, units)), block(LANES > 64 ? LANES : 64);
+    const dim3 grid((uint32_t)o.parts), block(LANES > 64 ? LANES : 64);
     const bool tail = a.n % 8 != 0;
     if (a.f && a.next) hipLaunchKernelGGL((tail ? block_bwd_kernel<T, LANES, true, true, true, SLOTS> : block_bwd_kernel<T, LANES, true, true, false, SLOTS>), grid, block, 0, stream, a, o);
     else if (a.f) hipLaunchKernelGGL((tail ? block_bwd_kernel<T, LANES, true, false, true, SLOTS> : block_bwd_kernel<T, LANES, true, false, false, SLOTS>), grid, block, 0, stream, a, o);
@@ -167,7 +166,7 @@ int block_bwd(const Block &a, BlockGrads o, const tv_block_grads &g, const Block
         if (p.want >> k & 1) {
             j.from[j.vectors] = from;
             j.to[j.vectors++] = to[k];
-            from += (int64_t)p.units.count * a.n;
+            from += (int64_t)p.parts * a.n;
         }
     int64_t sums = j.vectors;
     if (p.want >> kVectors & 1) {
@@ -175,7 +174,7 @@ int block_bwd(const Block &a, BlockGrads o, const tv_block_grads &g, const Block
         j.gate_to = g.dgate;
         sums += a.m / a.gate_div;
     }
-    j.units = p.units.count; j.cuts = p.units.cuts; j.n = a.n;
+    j.parts = p.parts; j.cuts = p.units.cuts; j.n = a.n;
     if (sums == 0) return TV_OK;
     hipLaunchKernelGGL((block_join_kernel<T>), dim3((uint32_t)tiles(a.n, 32), (uint32_t)sums), dim3(1024), 0, stream, j);
     return launched();
@@ -251,6 +250,7 @@ int tv_block_bwd(const void *dy, const void *dh, tv_block_in in, const float *st
     o.row_sums = p.bytes > p.row_sums ? (float2 *)((char *)ws + p.row_sums) : nullptr;
     o.want = p.want;
     for (int k = 0; k < kSums; ++k) o.slot[k] = p.slot[k];
+    o.parts = p.parts;
     o.units = p.units;
     return d.dtype == TV_BF16 ? block_bwd<bf16>(a, o, g, p, stream) : block_bwd<float>(a, o, g, p, stream);
 }

@@ -29,6 +29,18 @@ int main()
         const Units u = block_units(m, n, shared != 0, div);
         const char *wrong = units_wrong(u, m, shared != 0, div);
         if (!wrong && (int64_t)u.count * (block_lanes(n) > 64 ? block_lanes(n) : 64) >= (int64_t)1 << 32) wrong = "too many threads";
+        tv_block_in in{};
+        tv_block_grads g{};
+        tv_block_desc d{};
+        char there;
+        in.x = in.f = in.gate = in.bias = &there;
+        g.dweight = g.dbias = g.dscale = g.dgate = g.dnext_weight = g.dnext_bias = &there;
+        d.m = m; d.n = n; d.gate_div = shared ? div : 1; d.norm = d.next_norm = TV_NORM_LAYER;
+        const BlockBwdPlan p = block_bwd_plan(in, g, d);
+        const int64_t each = block_lanes(n) < 64 ? 64 / block_lanes(n) : 1;
+        if (!wrong && (p.parts * each < p.units.count || (p.parts - 1) * each >= p.units.count) && p.units.count) wrong = "units without a workgroup";
+        if (!wrong && p.bytes < (size_t)(5 * (int64_t)p.parts + (p.want >> kVectors & 1 ? p.units.count : 0)) * n * 4) wrong = "a workspace that is too small";
+        if (!wrong && block_lanes(n) > kMostSumLanes && p.two_passes != (p.slots > kMostSlots || n > 8192)) wrong = "the wrong passes";
         if (!wrong && u.cuts > 1 && m / div + kVectors > 65535) wrong = "too many sums to join in a launch";
         if (wrong) printf("%s\n", wrong);
         else printf("ok %d %d %d\n", u.count, u.rows, u.cuts);

@@ -60,7 +60,7 @@ def test_backward_refusals():
     assert bwd(desc(), ins(f=None), df=FAKE) == UNSUPPORTED and bwd(desc(), dgate=FAKE) == UNSUPPORTED
     assert bwd(desc(norm=0), dweight=FAKE) == UNSUPPORTED and bwd(desc(after=0), dh=None, dnext_bias=FAKE) == UNSUPPORTED
     need = tv.tv_block_bwd_workspace_bytes(ins(), tv.tv_block_grads(FAKE, FAKE, None, FAKE, None, FAKE, None, None), desc())
-    assert need >= 2 * 4 * 32 * 4                                                    # two sums of four units
+    assert need >= 2 * 32 * 4                                                        # two sums of one workgroup
     for ws, have in ((None, need), (FAKE + 8, need), (FAKE, need - 1)):
         assert bwd(desc(), dweight=FAKE, dscale=FAKE, ws=ws, nbytes=have) == WORKSPACE
     assert tv.tv_block_bwd_workspace_bytes(ins(), tv.tv_block_grads(FAKE, FAKE, None, None, None, None, None, None), desc()) == 0
