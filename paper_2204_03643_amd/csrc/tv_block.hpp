@@ -115,33 +115,74 @@ template <class T> struct Raw8 {
         else return __uint_as_float(v[i >> 2][i & 3]);
     }
 };
-// The first `have` values from p on and zeros; without a TAIL `have` is eight.
-template <bool TAIL, class T> __device__ __forceinline__ Raw8<T> raw8(const T *p, int have)
+// The channels of a lane: `have` from `col` on.  Without a TAIL that is eight.  A row's last lane may have fewer, and loads
+// the row's last eight, `back` before its own, to move them down: the same accesses as the other lanes', and none beyond the row
+// (16384 x 2047 bf16: 134 us with its last values one by one, BACK_US so).
+struct Cols {
+    int col, have, back;
+};
+template <bool TAIL> __device__ __forceinline__ Cols cols_of(int lane, int n)
+{
+    const bool live = lane * 8 < n;
+    Cols c{TAIL || live ? lane * 8 : 0, 8, 0};
+    if constexpr (TAIL) {
+        c.have = max(0, min(8, n - c.col));
+        c.back = c.have > 0 && n >= 8 ? 8 - c.have : 0;
+    }
+    return c;
+}
+
+// Asks for eight values of a row that starts at p; settle8 makes of them, once they are there, the lane's own and zeros for those
+// that do not exist.  (Apart, or whoever asks ahead of time would wait.)
+template <bool TAIL, class T> __device__ __forceinline__ Raw8<T> raw8(const T *p, Cols c)
 {
     Raw8<T> r;
-    if (!TAIL || have == 8) {
+    if (!TAIL || c.have == 8 || c.back) {
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.v[i] = get16(p + i * (16 / (int)sizeof(T)));
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.v[i] = get16(p + c.col - c.back + i * (16 / (int)sizeof(T)));
     } else {
-        constexpr int E = 16 / (int)sizeof(T);
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-            r.v[i] = u32x4{0, 0, 0, 0};
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.v[i] = u32x4{0, 0, 0, 0};
+        if (c.have)                                  // a row of fewer than eight
 #pragma unroll
-            for (int j = 0; j < E; ++j)
-                if (i * E + j < have) {
-                    if constexpr (sizeof(T) == 2) r.v[i][j >> 1] |= (uint32_t)((const uint16_t *)p)[j] << (16 * (j & 1));
-                    else r.v[i][j] = ((const uint32_t *)p)[i * E + j];
-                }
-        }
+            for (int i = 0; i < 8; ++i) {
+                const T v = p[min(i, c.have - 1)];
+                if constexpr (sizeof(T) == 2) r.v[0][i >> 1] |= i < c.have ? (uint32_t)__builtin_bit_cast(uint16_t, v) << (16 * (i & 1)) : 0u;
+                else r.v[i >> 2][i & 3] = i < c.have ? __float_as_uint(v) : 0u;
+            }
     }
     return r;
 }
+template <bool TAIL, class T> __device__ __forceinline__ void settle8(Raw8<T> &r, Cols c)
+{
+    if constexpr (TAIL)
+        if (c.back) {
+            constexpr int W = 2 * (int)sizeof(T);    // words
+            uint32_t w[W];
+#pragma unroll
+            for (int i = 0; i < W; ++i) w[i] = r.v[i >> 2][i & 3];
+            if (c.back & 4)
+#pragma unroll
+                for (int i = 0; i < W; ++i) w[i] = i + W / 2 < W ? w[i + W / 2] : 0u;
+            if (c.back & 2)
+#pragma unroll
+                for (int i = 0; i < W; ++i) w[i] = i + W / 4 < W ? w[i + W / 4] : 0u;
+            if (c.back & 1)
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    const uint32_t next = i + 1 < W ? w[i + 1] : 0u;
+                    w[i] = sizeof(T) == 4 ? next : __builtin_amdgcn_alignbit(next, w[i], 16);
+                }
+#pragma unroll
+            for (int i = 0; i < W; ++i) r.v[i >> 2][i & 3] = w[i];
+        }
+}
 // eight of a vector's values in 32 bits, or `otherwise` where there is none
-template <bool TAIL, class T> __device__ __forceinline__ void vector8(float (&v)[8], const void *p, int col, int have, float otherwise)
+template <bool TAIL, class T> __device__ __forceinline__ void vector8(float (&v)[8], const void *p, Cols c, float otherwise)
 {
     if (p) {
-        const Raw8<T> r = raw8<TAIL>((const T *)p + col, have);
+        Raw8<T> r = raw8<TAIL>((const T *)p, c);
+        settle8<TAIL>(r, c);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = r[i];
     } else
@@ -192,7 +233,8 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_fwd_kernel(Blo
     RowSum<LANES> sum(lds);
     const int lane = threadIdx.x % LANES;
     const bool live = lane * 8 < a.n;
-    const int col = TAIL || live ? lane * 8 : 0, have = TAIL ? max(0, min(8, a.n - col)) : 8;
+    const Cols at = cols_of<TAIL>(lane, a.n);
+    const int col = at.col, have = at.have;
     const bool drops = F && a.drop.below != 0;
     const DropKey key = drops ? drop_key(a.drop) : DropKey{};
     // (mean, r) of the values that the lanes hold, which become (v - mean) r; the variance is that of the differences
@@ -216,25 +258,26 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_fwd_kernel(Blo
     // (the vectors' values for these channels, before anything waits)
     Raw8<T> w, b, scale, nw, nb;
     if constexpr (F) {
-        if (a.w) w = raw8<TAIL>((const T *)a.w + col, have);
-        if (a.b) b = raw8<TAIL>((const T *)a.b + col, have);
-        if (a.scale) scale = raw8<TAIL>((const T *)a.scale + col, have);
+        if (a.w) w = raw8<TAIL>((const T *)a.w, at), settle8<TAIL>(w, at);
+        if (a.b) b = raw8<TAIL>((const T *)a.b, at), settle8<TAIL>(b, at);
+        if (a.scale) scale = raw8<TAIL>((const T *)a.scale, at), settle8<TAIL>(scale, at);
     }
     if constexpr (N) {
-        if (a.nw) nw = raw8<TAIL>((const T *)a.nw + col, have);
-        if (a.nb) nb = raw8<TAIL>((const T *)a.nb + col, have);
+        if (a.nw) nw = raw8<TAIL>((const T *)a.nw, at), settle8<TAIL>(nw, at);
+        if (a.nb) nb = raw8<TAIL>((const T *)a.nb, at), settle8<TAIL>(nb, at);
     }
     int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES;
     if constexpr (LANES == 64) row = (int64_t)blockIdx.x * kRows + __builtin_amdgcn_readfirstlane(threadIdx.x / LANES);
     for (; row < a.m; row += (int64_t)gridDim.x * kRows) {
         float v[8];
         float4 st = {0.0f, 0.0f, 0.0f, 0.0f};
-        const Raw8<T> x = raw8<TAIL>((const T *)a.x + row * a.ldx + col, have);
+        Raw8<T> x = raw8<TAIL>((const T *)a.x + row * a.ldx, at);
         if constexpr (F) {
-            const Raw8<T> raw = raw8<TAIL>((const T *)a.f + row * a.ldf + col, have);
+            Raw8<T> raw = raw8<TAIL>((const T *)a.f + row * a.ldf, at);
             Raw8<T> z;
-            if (a.gate) z = raw8<TAIL>((const T *)a.gate + (int64_t)((uint32_t)row / (uint32_t)a.gate_div) * a.ldg + col, have);
+            if (a.gate) z = raw8<TAIL>((const T *)a.gate + (int64_t)((uint32_t)row / (uint32_t)a.gate_div) * a.ldg, at);
             float f[8];
+            settle8<TAIL>(raw, at);
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = raw[i];
             if (a.norm != kNormNone) {
@@ -248,17 +291,21 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_fwd_kernel(Blo
 #pragma unroll
                     for (int i = 0; i < 8; ++i) f[i] += b[i];
             }
-            if (a.gate)
+            if (a.gate) {
+                settle8<TAIL>(z, at);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) f[i] *= gate_of<FAST>(z[i], a.act);
+            }
             if (a.scale)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) f[i] *= scale[i];
             if (drops) drop8(f, drop_numbers(key, (uint32_t)row, (uint32_t)col / 8), a.drop);
+            settle8<TAIL>(x, at);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = x[i] + f[i];
             if (y && live) store8(y + row * a.n + col, v, have);
         } else {
+            settle8<TAIL>(x, at);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = x[i];
         }
@@ -465,7 +512,8 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
     RowSum<LANES> sum(lds);
     const int lane = threadIdx.x % LANES;
     const bool live = lane * 8 < a.n;
-    const int col = TAIL || live ? lane * 8 : 0, have = TAIL ? max(0, min(8, a.n - col)) : 8;
+    const Cols at = cols_of<TAIL>(lane, a.n);
+    const int col = at.col, have = at.have;
     constexpr int kUnits = LANES > 64 ? 1 : 64 / LANES;
     int unit = (int)blockIdx.x * kUnits + (LANES > 64 ? 0 : threadIdx.x / LANES);
     if constexpr (LANES == 64) unit = __builtin_amdgcn_readfirstlane(unit);
@@ -479,15 +527,15 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
     constexpr int kOnce = WIDE ? 1 : 8;
     float nw_[kOnce], w_[kOnce], b_[kOnce], scale_[kOnce];
     if constexpr (!WIDE) {
-        if constexpr (N) vector8<TAIL, T>(nw_, a.nw, col, have, 1.0f);
+        if constexpr (N) vector8<TAIL, T>(nw_, a.nw, at, 1.0f);
         if constexpr (F) {
-            vector8<TAIL, T>(w_, a.w, col, have, 1.0f);
-            vector8<TAIL, T>(b_, a.b, col, have, 0.0f);
-            vector8<TAIL, T>(scale_, a.scale, col, have, 1.0f);
+            vector8<TAIL, T>(w_, a.w, at, 1.0f);
+            vector8<TAIL, T>(b_, a.b, at, 0.0f);
+            vector8<TAIL, T>(scale_, a.scale, at, 1.0f);
         }
     }
     auto vector = [&](float (&v)[8], const float (&once)[kOnce], const void *p, float otherwise) __attribute__((always_inline)) {
-        if constexpr (WIDE) vector8<TAIL, T>(v, p, col, have, otherwise);
+        if constexpr (WIDE) vector8<TAIL, T>(v, p, at, otherwise);
         else
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = once[i];
@@ -528,14 +576,14 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
         Row v;
         if (o.stats) v.st = o.stats[r];
         else v.st = float4{0.0f, 1.0f, 0.0f, 1.0f};
-        if (o.dy) v.dy = raw8<TAIL>((const T *)o.dy + r * a.n + col, have);
+        if (o.dy) v.dy = raw8<TAIL>((const T *)o.dy + r * a.n, at);
         if (next) {
-            v.dh = raw8<TAIL>((const T *)o.dh + r * a.n + col, have);
-            v.y = raw8<TAIL>((const T *)a.x + r * a.ldx + col, have);
+            v.dh = raw8<TAIL>((const T *)o.dh + r * a.n, at);
+            v.y = raw8<TAIL>((const T *)a.x + r * a.ldx, at);
         }
         if constexpr (F) {
-            v.f = raw8<TAIL>((const T *)a.f + r * a.ldf + col, have);
-            if (a.gate) v.z = raw8<TAIL>((const T *)a.gate + (int64_t)((uint32_t)r / (uint32_t)a.gate_div) * a.ldg + col, have);
+            v.f = raw8<TAIL>((const T *)a.f + r * a.ldf, at);
+            if (a.gate) v.z = raw8<TAIL>((const T *)a.gate + (int64_t)((uint32_t)r / (uint32_t)a.gate_div) * a.ldg, at);
         }
         return v;
     };
@@ -548,11 +596,14 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
             v = ahead;
             if (row + 1 < end) ahead = fetch(row + 1);
         } else v = fetch(row);
+        if (o.dy) settle8<TAIL>(v.dy, at);
         float d[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) d[i] = o.dy ? v.dy[i] : 0.0f;
         if (next) {
             float t[8], yh[8], s1 = 0.0f, s2 = 0.0f;
+            settle8<TAIL>(v.dh, at);
+            settle8<TAIL>(v.y, at);
             vector(t, nw_, a.nw, 1.0f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -575,6 +626,8 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
         if (o.dx && live) store8((T *)o.dx + row * a.n + col, d, have);
         if constexpr (F) {
             float fh[8], w[8], scale[8], s1 = 0.0f, s2 = 0.0f;
+            settle8<TAIL>(v.f, at);
+            if (a.gate) settle8<TAIL>(v.z, at);
             vector(w, w_, a.w, 1.0f);
             vector(scale, scale_, a.scale, 1.0f);
             if (drops) drop8(d, drop_numbers(key, (uint32_t)row, (uint32_t)col / 8), a.drop);
