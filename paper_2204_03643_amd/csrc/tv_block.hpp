@@ -2,8 +2,8 @@
 //
 // Reads and writes are all there is to it: a row is read once, its statistics are taken of what the lanes hold, and what
 // follows from them is written.  Lanes side by side in a row hold eight neighbouring channels each.  In bf16, microseconds
-// (GB/s read + written): norm of 8192 x 2048 13.5 (5000), its gradients 19.0 (5300) and the join of the weight's 4.8; border of 16384 x 2048
-// with norms, a gate a sequence, scale and dropout 58 (4600), its gradients 86 (4700) and the join 7.1.
+// (GB/s read + written): norm of 8192 x 2048 12.7 (5300), its gradients 19.3 (5200) and the join of the weight's 4.8; border of 16384 x 2048
+// with norms, a gate a sequence, scale and dropout 53.6 (5000), its gradients 86 (4700) and the join 7.1.
 #pragma once
 #include "tv_block_plan.hpp"
 #include "tv_drop.hpp"
@@ -117,7 +117,7 @@ template <class T> struct Raw8 {
 };
 // The channels of a lane: `have` from `col` on.  Without a TAIL that is eight.  A row's last lane may have fewer, and loads
 // the row's last eight, `back` before its own, to move them down: the same accesses as the other lanes', and none beyond the row
-// (16384 x 2047 bf16: 134 us with its last values one by one, BACK_US so).
+// (16384 x 2047 bf16: 134 us with its last values one by one, 73 so; 50 for 2040 channels, without a tail).
 struct Cols {
     int col, have, back;
 };
@@ -223,7 +223,8 @@ __device__ __forceinline__ float2 normalise(float (&v)[V][8], const int (&have)[
 
 // Eight channels of each row a lane, LANES lanes a row.  F: there is an f; N: there is a next norm.  TAIL as in the backward
 // kernel below: without one, lanes beyond the row's end go along with the first lane's channels, and no value needs a mask
-// (16384 x 2048 with gate and dropout: 70 us with masks and sums through LDS, 58 so).
+// (16384 x 2048 with gate and dropout: 70 us with masks and sums through LDS, 58 without, 53.6 with the vectors' values in
+// registers before anything waits).
 template <class T, int LANES, bool F, bool N, bool TAIL>
 __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_fwd_kernel(Block a, T *y, T *h, float4 *stats)
 {
@@ -502,7 +503,8 @@ __device__ __forceinline__ void branch_terms(float (&d)[8], float (&fh)[8], floa
 // dscale = w A + b B, dweight = scale A, dbias = scale B.
 //
 // Three waves to a SIMD, as the registers allow: 768 workgroups of 256 lanes (16384 x 2048: 86 us; 1024 workgroups without the
-// next row on its way, a third of them in a second round, masks at every value and sums by LDS permutes: 220).
+// next row on its way, a third of them in a second round, masks at every value and sums by LDS permutes: 220).  4096 rows of 8192
+// channels 99 us, with the sums in LDS; 260 in two passes.
 template <class T, int LANES, bool F, bool N, bool TAIL, int SLOTS>
 __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Block a, BlockGrads o)
 {
@@ -850,7 +852,7 @@ __global__ __launch_bounds__(256) void block_sums_kernel(Block a, BlockGrads o)
 }
 
 // The units' sums, joined in their order: workgroup (columns, y) has the y-th wanted sum.  Bound by the latency of its loads:
-// 32 of a column's units at a time 4.8 us for 745 units of 2048 channels, eight at a time 7.5.
+// 32 of a column's parts at a time 4.8 us for 745 parts of 2048 channels, eight at a time 7.5.
 struct Joins {
     const float *from[kVectors];
     void *to[kVectors];
