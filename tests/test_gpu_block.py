@@ -150,7 +150,8 @@ def test_saved_tensors_that_come_back_as_others():
 
 @pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
 @pytest.mark.parametrize("m,n,gate,norm,next_norm,bias", [(600, 4200, 6, "layer", "layer", True), (600, 8192, 600, "layer", "layer", True), (600, 8191, 2, "layer", "rms", True),
-                                                          (520, 5000, 0, "rms", "none", False), (520, 5000, 5, "none", "rms", False), (300, 6001, 0, "layer", "none", True)])
+                                                          (520, 5000, 0, "rms", "none", False), (520, 5000, 5, "none", "rms", False), (300, 6001, 0, "layer", "none", True),
+                                                          (600, 5000, 6, "layer", "none", True)])
 def test_wide_rows(m, n, gate, norm, next_norm, bias, dtype):
     """More than 4096 channels, with few sums over the rows, with many, and with more than fit beside each other."""
     how = dict(norm=norm, next_norm=next_norm)
@@ -170,7 +171,7 @@ def test_a_gradient_of_one_output_alone(upstream, dtype):
 
 @pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
 @pytest.mark.parametrize("kind", ("rms", "layer"))
-@pytest.mark.parametrize("m,n", [(1, 1), (1, 2048), (3, 7), (40, 64), (1500, 96), (5, 1001), (2, 16384), (300, 8200)])
+@pytest.mark.parametrize("m,n", [(1, 1), (1, 2048), (3, 7), (40, 64), (1500, 96), (5, 1001), (2, 16384), (300, 8200), (300, 5000), (20, 8191)])
 def test_norm_alone(m, n, kind, dtype):
     from paper_2204_03643_amd.block import tv_norm
     t = made(m, n, dtype, m + n, "none", kind, kind == "layer", 0, False)

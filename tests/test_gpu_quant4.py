@@ -136,6 +136,28 @@ def test_epilogues(act, dtype):
         product(70, 200, 90, dtype, act, bias, residual, seed=3)
 
 
+# products through each size of tile, with last tiles that are not whole, and split contractions that are joined
+LARGE = [(2049, 1100, 4100), (4097, 2304, 4104), (1500, 1300, 2100), (4100, 257, 4100), (300, 5000, 500), (70, 4100, 300), (129, 8200, 1001)]
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("M,K,N", LARGE)
+def test_large_products(M, K, N, dtype):
+    """Against products of the restored values in 64 bits on the GPU (restoring is held to its definition above)."""
+    from paper_2204_03643_amd.quant4 import tv_linear4, tv_quantize4
+    gen = torch.Generator(device="cuda").manual_seed(M + K + N)
+    x, w, r = (torch.randn(*s, generator=gen, device="cuda").to(dtype) for s in ((M, K), (N, K), (M, N)))
+    b = torch.randn(N, generator=gen, device="cuda").to(dtype)
+    x4, w4 = tv_quantize4(x * 2), tv_quantize4(w / K ** 0.5)
+    wide = x4.restore().double(), w4.restore().double(), b.double(), r.double()
+    for act, bias, residual in (("none", False, False), ("gelu", True, True), ("silu", True, False)):
+        got = tv_linear4(x4, w4, b if bias else None, r if residual else None, act=act)
+        _, y, _, off = linref.forward(*wide[:2], wide[2] if bias else None, wide[3] if residual else None, act, dtype)
+        assert bool(((got.double() - y).abs() <= off).all()), (act, float(((got.double() - y).abs() - off).max()))
+        if act == "none":
+            assert torch.equal(tv_linear4(x * 2, w4), got)
+
+
 @pytest.mark.parametrize("M", (1, 40, 300))
 def test_each_block_has_its_own_scale(M):
     """Scales that differ from block to block by many powers of two, of x and of W, so that a scale taken from a neighbour shows."""
