@@ -45,21 +45,30 @@ template <class T, bool OWN> struct RawPiece4 {
     {
         if constexpr (!OWN) return {raw[0], scale};
         else {
-            float v[4][8];
             uint32_t top = 0;
+            if constexpr (sizeof(T) == 2) {          // the largest of two at a time, as they lie
+                typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+                u16x2 most = {0, 0};
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < 16; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, raw[i >> 2][i & 3] & 0x7fff7fffu));
+                top = (uint32_t)max(most[0], most[1]) << 16;
+            } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    if constexpr (sizeof(T) == 2) v[i][j] = __uint_as_float(j & 1 ? raw[i][j >> 1] & 0xffff0000u : raw[i][j >> 1] << 16);
-                    else v[i][j] = __uint_as_float(raw[2 * i + (j >> 2)][j & 3]);
-                    top = max(top, __float_as_uint(v[i][j]) & 0x7fffffffu);
-                }
+                for (int i = 0; i < 32; ++i) top = max(top, raw[i >> 2][i & 3] & 0x7fffffffu);
+            }
             const uint32_t byte = scale4_byte(top);
             Piece4 o{{0, 0, 0, 0}, (int)byte};
             if (byte != 255u)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o.codes[i] = codes4_of(v[i], __uint_as_float(byte << 23));
+                for (int i = 0; i < 4; ++i) {
+                    float v[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        if constexpr (sizeof(T) == 2) v[j] = __uint_as_float(j & 1 ? raw[i][j >> 1] & 0xffff0000u : raw[i][j >> 1] << 16);
+                        else v[j] = __uint_as_float(raw[2 * i + (j >> 2)][j & 3]);
+                    }
+                    o.codes[i] = codes4_of(v, __uint_as_float(byte << 23));
+                }
             return o;
         }
     }
