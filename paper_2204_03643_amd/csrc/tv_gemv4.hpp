@@ -85,6 +85,12 @@ __global__ __launch_bounds__(512) void gemv4_kernel(Product g, Rows4 x, const ui
     const int64_t pitch = g.ldb / 32;                // groups of a row
     const char *pw = (const char *)g.b + (int64_t)n * pitch * 64 + block * 16;
     const uint32_t *ps = w_scales + n;
+    // two threads a row finish it, eight columns each: bias and residual are on their way before anything else
+    const int m = threadIdx.x / 2, column = n0 + threadIdx.x % 2 * 8;
+    const int have = m < min(MT * 16, g.M) ? max(0, min(8, g.N - column)) : 0;
+    float bias[8], res[8];
+    if (e.bias) load8(bias, (const T *)e.bias + column, have);
+    if (e.res) load8(res, (const T *)e.res + (int64_t)m * e.ldr + column, have);
     f32x4 acc[MT];
 #pragma unroll
     for (int j = 0; j < MT; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -117,17 +123,23 @@ __global__ __launch_bounds__(512) void gemv4_kernel(Product g, Rows4 x, const ui
 #pragma unroll
     for (int j = 0; j < MT; ++j) *(f32x4 *)&sums[wave][(16 * j + row) * kPitch + block * 4] = acc[j];
     __syncthreads();
-    // two threads a row, eight columns each
-    const int m = threadIdx.x / 2, c = threadIdx.x % 2 * 8;
-    if (m < MT * 16) {
+    if (have) {
+        const float *from = sums[0] + m * kPitch + threadIdx.x % 2 * 8;
         f32x4 a = {0.0f, 0.0f, 0.0f, 0.0f}, b = a;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            a += *(const f32x4 *)&sums[w][m * kPitch + c];
-            b += *(const f32x4 *)&sums[w][m * kPitch + c + 4];
+            a += *(const f32x4 *)(from + w * (MT * 16 * kPitch));
+            b += *(const f32x4 *)(from + w * (MT * 16 * kPitch) + 4);
         }
         float p[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-        finish8<T>(p, m, n0 + c, g.N, m < g.M, e);
+        if (e.bias)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] += bias[i];
+        act8<sizeof(T) == 2>(p, e.act);
+        if (e.res)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] += res[i];
+        store8((T *)e.y + (int64_t)m * e.ldy + column, p, have);
     }
 }
 
