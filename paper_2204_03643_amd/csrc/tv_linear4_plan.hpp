@@ -25,18 +25,18 @@ inline Choice4 cut4(Kind4 kind, bool own, int64_t s, int64_t groups, int64_t uni
     return {kind, own, (int)tiles(groups, per), (int)per * 32, 0.0};
 }
 
-constexpr int64_t kFewRows4 = 32, kOwnValues4 = 16384;
+constexpr int64_t kFewRows4 = 32, kOwnValues4 = 16384, kOwnLength4 = 8192;
 
 // Sizes alone decide.  Up to 32 rows stream the weight (2048 -> 8192, x taken to 4 bits included: 32 rows 7.6 us streamed, 8.1
-// through tiles; 64 rows 9.8 and 8.4), few values of x in the same launch (one row 5.6 us in one, 5.9 in two and a launch's time on the
-// host; 16 rows, 32768 values, 7.5 and 6.6).  Otherwise the cheapest by a model of the time in microseconds, fitted to
+// through tiles; 64 rows 9.8 and 8.4), few values of x in the same launch (one row of 2048 -> 8192 5.1 us in one, 6.2 in two; 16 rows,
+// 32768 values, 7.5 and 6.6; one row of 8192 -> 2048 8.3 and 7.9, of 16384 -> 4096 16.1 and 13.1).  Otherwise the cheapest by a model of the time in microseconds, fitted to
 // sweeps of tiles and splits over outputs of 64 x 1024 to 8192 x 8192 and contractions of 1024 to 8192: a launch; rounds of
 // workgroups over 256 compute units, in each a start and an end and so much a step of 256; for split contractions the second launch
 // and the sums' trip through memory.
 inline Choice4 choose4(bool codes, int64_t M, int64_t N, int64_t K, int64_t groups)
 {
     // (as long as a launch of 512 threads for every 16 columns has fewer than 2^32)
-    if (M <= kFewRows4 && N <= ((int64_t)1 << 26)) return cut4(kFew4, !codes && M <= 16 && M * K <= kOwnValues4, 1, groups, 8);
+    if (M <= kFewRows4 && N <= ((int64_t)1 << 26)) return cut4(kFew4, !codes && M <= 16 && K <= kOwnLength4 && M * K <= kOwnValues4, 1, groups, 8);
     struct Cost { Kind4 kind; int m, n; double round, step; };
     constexpr Cost costs[] = {{kTile64x4, 64, 128, 1.5, 0.30}, {kTile128x4, 128, 128, 2.4, 0.60}, {kTile256x4, 256, 256, 6.0, 1.75}};
     Choice4 best{};

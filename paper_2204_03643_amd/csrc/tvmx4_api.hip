@@ -56,13 +56,13 @@ void launch_tiles(Product g, const Scales &scales, const Epilogue &e, hipStream_
     hipLaunchKernelGGL((gemm4_kernel<T, BM, BN, WM, WN, BUF, G>), dim3(g.tiles_m * g.tiles_n, g.splits), dim3(WM * WN * 64), 0, stream, g, scales, e);
 }
 
-template <class T>
+template <class T, int NT>
 void launch_few(const Product &g, const Rows4 &x, bool own, const Scales &s, const Epilogue &e, hipStream_t stream)
 {
-    const dim3 grid((uint32_t)tiles(g.N, 16)), block(512);
-    if (own) hipLaunchKernelGGL((gemv4_kernel<T, 1, 2, true>), grid, block, 0, stream, g, x, s.w, s.w_rows, e);
-    else if (g.M <= 16) hipLaunchKernelGGL((gemv4_kernel<T, 1, 4, false>), grid, block, 0, stream, g, x, s.w, s.w_rows, e);
-    else hipLaunchKernelGGL((gemv4_kernel<T, 2, 4, false>), grid, block, 0, stream, g, x, s.w, s.w_rows, e);
+    const dim3 grid((uint32_t)tiles(g.N, 16 * NT)), block(512);
+    if (own) hipLaunchKernelGGL((gemv4_kernel<T, 1, NT, 2, true>), grid, block, 0, stream, g, x, s.w, s.w_rows, e);
+    else if (g.M <= 16) hipLaunchKernelGGL((gemv4_kernel<T, 1, NT, 4, false>), grid, block, 0, stream, g, x, s.w, s.w_rows, e);
+    else hipLaunchKernelGGL((gemv4_kernel<T, 2, NT, 4, false>), grid, block, 0, stream, g, x, s.w, s.w_rows, e);
 }
 
 template <class T>
@@ -82,7 +82,11 @@ int linear4(const void *x, const uint8_t *x_exps, const uint8_t *w, const uint8_
     if (p.c.kind == kTile64x4) launch_tiles<T, 64, 128, 2, 2, 4, 2>(g, s, e, stream);
     if (p.c.kind == kFew4) {
         const Rows4 rows{g.a, s.x, d.ldx, s.x_rows, (int32_t)d.k};
-        launch_few<T>(g, rows, p.c.own, s, e, stream);
+        // so many columns a workgroup as leave one for each compute unit (one row of 4096: -> 4096 5.7, 6.2 and 7.7 us with
+        // 16, 32 and 64; 2048 -> 8192 6.2, 5.1 and 5.7; 4096 -> 16384 15.5, 10.9 and 8.6)
+        if (d.n > 8192) launch_few<T, 4>(g, rows, p.c.own, s, e, stream);
+        else if (d.n > 4096) launch_few<T, 2>(g, rows, p.c.own, s, e, stream);
+        else launch_few<T, 1>(g, rows, p.c.own, s, e, stream);
     }
     if (p.c.splits > 1) {
         if (launched() != TV_OK) return TV_ERR_HIP;

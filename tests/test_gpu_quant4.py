@@ -119,7 +119,8 @@ def product(M, K, N, dtype, act, bias, residual, seed=0, lead=None):
 
 
 SHAPES = [(1, 1, 1), (1, 32, 16), (1, 2048, 512), (2, 100, 33), (7, 1001, 777), (16, 128, 64), (17, 129, 65), (31, 300, 100), (33, 4096, 48),
-          (64, 640, 200), (65, 256, 128), (100, 512, 130), (129, 1000, 257), (200, 64, 300), (256, 2048, 256), (257, 384, 515), (600, 896, 1030)]
+          (64, 640, 200), (65, 256, 128), (100, 512, 130), (129, 1000, 257), (200, 64, 300), (256, 2048, 256), (257, 384, 515), (600, 896, 1030), (3, 130, 4104), (16, 2048, 4100), (29, 257, 8192), (1, 1000, 8200),
+          (17, 300, 8200), (2, 8200, 100)]
 
 
 @pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
