@@ -76,9 +76,9 @@ def _check_drop(p, seed, offset, like, what):
 def _check_channels(t, n, what, like):
     if t is None:
         return None
-    if t.dtype is not like.dtype or t.device != like.device:
+    if t.dtype is not like.dtype or t.get_device() != like.get_device():
         _check_tensor(t, what, like)
-    if t.shape != (n,):
+    if t.numel() != n or t.dim() != 1:
         raise ValueError("%s: shape (%d,) expected, got %r" % (what, n, tuple(t.shape)))
     return _dense(t)
 
@@ -94,6 +94,8 @@ def _rows(t):
 
 def _gate_div(x, gate, what):
     """How many rows of x share a row of the gate: x's shape, with ones in its last leading axes where they do."""
+    if gate.shape == x.shape:
+        return 1
     lead = tuple(x.shape[:-1])
     rows = tuple(gate.shape[:-1]) if gate.dim() > 1 or x.dim() == 1 else (1,) * len(lead)
     k = len(rows)
@@ -351,7 +353,8 @@ def tv_residual(x: torch.Tensor, f: torch.Tensor, norm: str = "none", weight: to
     """
     what = "tv_residual"
     n = _check_rows(x, what)
-    _check_tensor(f, what + " (f)", x)
+    if f.dtype is not x.dtype or f.get_device() != x.get_device():
+        _check_tensor(f, "tv_residual (f)", x)
     if f.shape != x.shape:
         raise ValueError("tv_residual: f of shape %r expected, got %r" % (tuple(x.shape), tuple(f.shape)))
     if norm not in _NORMS or next_norm not in _NORMS:
@@ -367,7 +370,8 @@ def tv_residual(x: torch.Tensor, f: torch.Tensor, norm: str = "none", weight: to
     next_bias = _check_channels(next_bias, n, "tv_residual (next_bias)", x)
     div = 1
     if gate is not None:
-        _check_tensor(gate, "tv_residual (gate)", x)
+        if gate.dtype is not x.dtype or gate.get_device() != x.get_device():
+            _check_tensor(gate, "tv_residual (gate)", x)
         div = _gate_div(x, gate, what)
     drop, seed, seed_at, offset = _check_drop(dropout, seed, offset, x, what)
     border = _border(_NORMS[norm], _NORMS[next_norm], _GATE_ACTS[gate_act], _check_eps(eps, what), div, drop, offset)

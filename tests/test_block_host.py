@@ -147,3 +147,15 @@ def test_probabilities_and_seeds():
                                    (0.5, 1.0, 0, TypeError), (0.5, 0, "1", TypeError), (0.5, True, 0, TypeError)):
         with pytest.raises(error):
             block._check_drop(p, seed, offset, x, "")
+
+
+def test_a_mixer_as_it_was_and_with_borders():
+    from paper_2204_03643_amd.linear import TVMixer
+    names = ["raw_lambda", "expand.weight", "expand.bias", "reduce.weight", "reduce.bias"]
+    assert list(TVMixer(8, 16).state_dict()) == names
+    full = TVMixer(8, 16, norm="layer", post_norm="rms", init_scale=0.1, dropout=0.1, gate_act="silu")
+    assert list(full.state_dict()) == names + ["norm.weight", "norm.bias", "residual.scale", "residual.norm.weight"]
+    assert full.residual.scale.tolist() == [pytest.approx(0.1)] * 8
+    for kwargs in (dict(norm="l2"), dict(post_norm="l2"), dict(dropout=-0.1), dict(gate_act="relu")):
+        with pytest.raises(ValueError):
+            TVMixer(8, 16, **kwargs)

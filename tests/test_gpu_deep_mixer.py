@@ -81,3 +81,17 @@ def test_a_stack_in_training_and_in_4_bits():
         # h's rounding may fall on either side and then on either side of a border of 4 bits: about a percent of its norm
         assert (got.double() - want).norm() <= 0.01 * want.norm()
         y = got
+
+
+@pytest.mark.parametrize("more", ((), ("--norm", "rms", "--dropout", "0.1")))
+def test_the_example_runs(more, monkeypatch, capsys):
+    import importlib.util
+    import os
+    import sys
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "denoise_tokens.py")
+    spec = importlib.util.spec_from_file_location("denoise_tokens", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    monkeypatch.setattr(sys, "argv", [path, "--steps", "3", "--tokens", "64", "--channels", "16", *more])
+    example.main()
+    assert "in 4 bits" in capsys.readouterr().out
