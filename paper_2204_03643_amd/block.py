@@ -107,10 +107,11 @@ def _gate_div(x, gate, what):
     return max(1, math.prod(lead[k:]))
 
 
-# How much workspace a backward call needs, which its sizes and what is given and wanted say in full.
+# How much workspace a backward call needs, which its sizes, whether there is an f, a bias and a gate, and what is wanted say in
+# full (a bias adds a sum over the rows to dscale's).
 @functools.lru_cache(maxsize=4096)
-def _workspace_bytes(m, n, dtype, has_f, has_gate, border, want):
-    ins = _b.tv_block_in(16, 16 if has_f else None, None, None, 16 if has_gate else None, None, None, None)
+def _workspace_bytes(m, n, dtype, has_f, has_bias, has_gate, border, want):
+    ins = _b.tv_block_in(16, 16 if has_f else None, None, 16 if has_bias else None, 16 if has_gate else None, None, None, None)
     dx, df, dweight, dbias, dgate, dscale, dnext_weight, dnext_bias = (16 if w else None for w in want)
     return _b.tv_block_bwd_workspace_bytes(ins, _b.tv_block_grads(dx, df, dgate, dweight, dbias, dscale, dnext_weight, dnext_bias),
                                            _desc(m, n, n, n, n, dtype, border))
@@ -173,7 +174,7 @@ def _backward(like, dy, dh, y, f, weight, bias, gate, scale, next_weight, stats,
     made = [like.new_empty(s) if w else None for s, w in zip(shapes, want)]
     dx, df, dweight, dbias, dgate, dscale, dnext_weight, dnext_bias = [None if t is None else t.data_ptr() for t in made]
     ins = _b.tv_block_in(at_y, f.data_ptr(), _address(weight), _address(bias), at_gate, _address(scale), _address(next_weight), None)
-    nbytes = _workspace_bytes(m, n, dtype, True, gate is not None, border, want)
+    nbytes = _workspace_bytes(m, n, dtype, True, bias is not None, gate is not None, border, want)
     ws = like.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
     _check(_b.lib().tv_block_bwd(_address(dy), _address(dh), ins, _address(stats),
                                  _b.tv_block_grads(dx, df, dgate, dweight, dbias, dscale, dnext_weight, dnext_bias),
@@ -256,7 +257,7 @@ def _norm_backward(g, x, weight, stats, border, want):
     dweight = g.new_empty(n) if want[1] else None
     dbias = g.new_empty(n) if want[2] else None
     ins = _b.tv_block_in(x.data_ptr(), None, None, None, None, None, _address(weight), None)
-    nbytes = _workspace_bytes(m, n, dtype, False, False, border, (want[0], False, False, False, False, False, want[1], want[2]))
+    nbytes = _workspace_bytes(m, n, dtype, False, False, False, border, (want[0], False, False, False, False, False, want[1], want[2]))
     ws = g.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
     _check(_b.lib().tv_block_bwd(None, g.data_ptr(), ins, stats.data_ptr(),
                                  _b.tv_block_grads(_address(dx), None, None, None, None, None, _address(dweight), _address(dbias)),

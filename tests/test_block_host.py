@@ -159,3 +159,34 @@ def test_a_mixer_as_it_was_and_with_borders():
     for kwargs in (dict(norm="l2"), dict(post_norm="l2"), dict(dropout=-0.1), dict(gate_act="relu")):
         with pytest.raises(ValueError):
             TVMixer(8, 16, **kwargs)
+
+
+@pytest.mark.parametrize("n", (64, 4096, 4097, 8192, 8193))
+@pytest.mark.parametrize("has_bias", (False, True))
+def test_workspaces_are_as_large_as_the_call_asks_for(n, has_bias, monkeypatch):
+    """A backward call's workspace against the size that its own operands need, for each set of gradients that are wanted."""
+    real = tv.lib()
+    asked = []
+
+    class Library:
+        def __getattr__(self, name):
+            return getattr(real, name)
+
+        def tv_block_bwd(self, dy, dh, i, stats, grads, d, ws, nbytes, stream):
+            asked.append((nbytes, tv.tv_block_bwd_workspace_bytes(i, grads, d)))
+            return OK
+    library = Library()
+    monkeypatch.setattr(block._b, "lib", lambda: library)
+    monkeypatch.setattr(block._b, "_stream", lambda stream: None)
+    x, gate, v = torch.zeros(6, n), torch.zeros(2, n), torch.zeros(n)
+    stats = torch.zeros(6, 4)
+    bias = v if has_bias else None
+    for norm, after in ((2, 2), (1, 0)):
+        border = block._border(norm, after, 0, 1e-6, 3, 0, 0)
+        for bits in range(256):
+            want = tuple(bool(bits >> k & 1) for k in range(8))
+            if (want[3] and not has_bias) or (not after and (want[6] or want[7])):
+                continue
+            block._backward.__wrapped__(x, x, x if after else None, x if after else None, x, v, bias, gate, v, v if after else None, stats, border, 0,
+                                        None, want)
+    assert len(asked) == (320 if has_bias else 160) and [a for a in asked if a[0] != a[1]] == []
