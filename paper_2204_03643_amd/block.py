@@ -454,8 +454,9 @@ class TVResidual(torch.nn.Module):
     """``tv_residual`` with the norm after a block, the scale (init_scale, no scale where it is None) and the norm before the
     next block as parameters.
 
-    ``forward(x, f, gate=None, seed=None)`` is y, or (y, h) with a next norm.  Dropout acts in training alone; without a seed one is
-    drawn from torch's CPU generator (which a captured graph would repeat: hand it a seed tensor there).
+    ``forward(x, f, gate=None, seed=None, offset=0)`` is y, or (y, h) with a next norm.  Dropout acts in training alone; without a
+    seed one is drawn from torch's CPU generator (which a captured graph would repeat: hand it a seed tensor there).  Borders that
+    are handed one seed, as those of a stack are, drop the same places unless each has an offset of its own.
     """
 
     def __init__(self, channels: int, norm: str = "none", next_norm: str = "none", gate_act: str = "none",
@@ -475,14 +476,14 @@ class TVResidual(torch.nn.Module):
         if init_scale is not None:
             self.scale = torch.nn.Parameter(torch.full((channels,), float(init_scale), device=device, dtype=dtype))
 
-    def forward(self, x: torch.Tensor, f: torch.Tensor, gate: torch.Tensor | None = None, seed=None):
+    def forward(self, x: torch.Tensor, f: torch.Tensor, gate: torch.Tensor | None = None, seed=None, offset: int = 0):
         p = self.dropout if self.training else 0.0
         if p and seed is None:
             seed = int(torch.randint(0, (1 << 63) - 1, ()))
         norm, after = self.norm, self.next
         return tv_residual(x, f, "none" if norm is None else norm.kind, None if norm is None else norm.weight,
                            None if norm is None else norm.bias, gate, self.gate_act if gate is not None else "none", self.scale, p,
-                           seed, 0, "none" if after is None else after.kind, None if after is None else after.weight,
+                           seed, offset, "none" if after is None else after.kind, None if after is None else after.weight,
                            None if after is None else after.bias, self.eps)
 
     def extra_repr(self) -> str:

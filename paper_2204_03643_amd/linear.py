@@ -385,7 +385,8 @@ class TVMixer(torch.nn.Module):
 
     For deep stacks: `norm` ("rms", "layer") is a norm before the TV pass, `post_norm` one of the block's output before it is
     added, `init_scale` a trainable scale a channel of it, `dropout` acts on it in training, and forward's gate, of x's shape
-    or [B, 1, C], multiplies it through `gate_act` (see ``block.tv_residual``; its dropout takes forward's seed).
+    or [B, 1, C], multiplies it through `gate_act` (see ``block.tv_residual``; its dropout takes forward's seed and offset: blocks
+    that are handed one seed are told apart by their offsets).
     ``quantized4()`` is the block for serving.
     """
 
@@ -405,7 +406,7 @@ class TVMixer(torch.nn.Module):
         # (none of it: the residual is added by the second product)
         self.residual = _block.TVResidual(channels, post_norm, "none", gate_act, init_scale, dropout, **like)
 
-    def forward(self, x: torch.Tensor, gate: torch.Tensor | None = None, seed=None) -> torch.Tensor:
+    def forward(self, x: torch.Tensor, gate: torch.Tensor | None = None, seed=None, offset: int = 0) -> torch.Tensor:
         if x.dim() != 3 or x.shape[-1] != self.raw_lambda.numel():
             raise ValueError("TVMixer: [B, T, %d] expected, got %r" % (self.raw_lambda.numel(), tuple(x.shape)))
         lam = torch.nn.functional.softplus(self.raw_lambda)
@@ -414,7 +415,7 @@ class TVMixer(torch.nn.Module):
         border = self.residual
         if gate is None and border.norm is None and border.scale is None and not (border.dropout and self.training):
             return self.reduce(self.expand(smooth), residual=x)
-        return border(x, self.reduce(self.expand(smooth)), gate, seed)
+        return border(x, self.reduce(self.expand(smooth)), gate, seed, offset)
 
     def quantized4(self) -> "TVMixer":
         """A copy whose products run in 4 bits, for serving: it has no gradients."""
