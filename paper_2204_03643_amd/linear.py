@@ -413,7 +413,7 @@ class TVMixer(torch.nn.Module):
         before = x if self.norm is None else self.norm(x)
         smooth = tv_prox_1d(before.float(), lam, axis=1).to(x.dtype)
         border = self.residual
-        if gate is None and border.norm is None and border.scale is None and not (border.dropout and self.training):
+        if gate is None and border.norm is None and border.scale is None and not (border.dropout and border.training):
             return self.reduce(self.expand(smooth), residual=x)
         return border(x, self.reduce(self.expand(smooth)), gate, seed, offset)
 

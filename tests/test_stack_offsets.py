@@ -17,6 +17,28 @@ def test_modules_hand_their_offset_on(monkeypatch):
     assert seen == [(4, 0), (4, 7), (4, 1 << 40)]
 
 
+def test_a_border_in_training_within_a_block_that_is_not(monkeypatch):
+    """Dropout goes by the border's own mode, whichever else the border does."""
+    from paper_2204_03643_amd import linear
+
+    class Product(torch.nn.Module):
+        def forward(self, x, residual=None):
+            return x if residual is None else x + residual
+    seen = []
+    monkeypatch.setattr(linear, "tv_prox_1d", lambda x, lam, axis: x)
+    monkeypatch.setattr(block, "tv_residual", lambda *a: seen.append(a[8]) or a[0])
+    x = torch.zeros(1, 2, 8)
+    for init_scale in (None, 1.0):
+        mixer = TVMixer(8, 16, dropout=0.5, init_scale=init_scale)
+        mixer.expand = mixer.reduce = Product()
+        seen.clear()
+        mixer(x)
+        mixer.eval()
+        mixer.residual.train()
+        mixer(x)
+        assert seen == [0.5, 0.5]
+
+
 @pytest.mark.gpu
 def test_masks_of_a_stack_with_one_seed_tensor():
     seed = torch.tensor([11], device="cuda")
