@@ -383,8 +383,8 @@ def tv_residual(x: torch.Tensor, f: torch.Tensor, norm: str = "none", weight: to
 def _drop(x, how, seed_at):
     """how: (drop, seed, offset)"""
     drop, seed, offset = how
-    n = x.shape[-1] if x.dim() else 1
-    rows, ldx = _rows(x) if x.dim() else (x, 1)
+    rows, ldx = _rows(x if x.dim() else x.view(1))
+    n = rows.shape[-1]
     y = x.new_empty(x.shape)
     _check(_b.lib().tv_drop_apply(rows.data_ptr(), y.data_ptr(), x.numel() // n, n, ldx, _DTYPES[x.dtype],
                                   _b.tv_drop(seed, offset, _address(seed_at), drop), _b._stream(None)))
