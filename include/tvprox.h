@@ -454,7 +454,8 @@ int tv_block_fwd(tv_block_in in, void *y, void *h, float *stats, tv_block_desc d
  *   dscale = sum_i t act(gate) norm(f),  dgate = t scale act'(gate) norm(f), summed over the rows that share it
  *   dweight, dbias = sum_i dP (f - mu) r, sum_i dP;  dnext_weight, dnext_bias = sum_i dh (y - mu) r, sum_i dh
  *
- * Each output is packed and may be NULL where it is not wanted.  Sums over rows are fp32, in an order that depends on
+ * A place that dropout took out has no part in any gradient of gate, scale and f: its gate, and without a norm its f, may be
+ * infinite or a NaN.  Each output is packed and may be NULL where it is not wanted.  Sums over rows are fp32, in an order that depends on
  * the sizes alone: results do not change from run to run.  m = 0 sets the vectors to zero.  ws: as in tv_linear_bwd.
  */
 typedef struct {

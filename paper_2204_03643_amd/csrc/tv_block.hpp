@@ -453,8 +453,13 @@ __device__ __forceinline__ void branch_terms(float (&d)[8], float (&fh)[8], floa
 {
     constexpr bool FAST = sizeof(T) == 2;
     float p[8], P[8];
-    if (drops) drop8(d, drop_numbers(key, (uint32_t)row, (uint32_t)col / 8), a.drop);
+    u32x4 numbers;
     get8(fh, (const T *)a.f + row * a.ldf + col, have);
+    if (drops) {
+        numbers = drop_numbers(key, (uint32_t)row, (uint32_t)col / 8);
+        drop8(d, numbers, a.drop);
+        if (a.norm == kNormNone) clear8(fh, numbers, a.drop);        // (a norm takes in the whole row)
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) P[i] = fh[i];
     if (a.norm != kNormNone) {
@@ -475,6 +480,7 @@ __device__ __forceinline__ void branch_terms(float (&d)[8], float (&fh)[8], floa
     if (a.gate) {
         float z[8];
         get8(z, (const T *)a.gate + (int64_t)((uint32_t)row / (uint32_t)a.gate_div) * a.ldg + col, have);
+        if (drops) clear8(z, numbers, a.drop);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float G = gate_of<FAST>(z[i], a.act), q = d[i] * p[i];
@@ -498,6 +504,9 @@ __device__ __forceinline__ void branch_terms(float (&d)[8], float (&fh)[8], floa
 // read again for every row, and only rows in bf16 come ahead of time.  Without a TAIL the channels are a multiple
 // of eight: a lane has eight or none, and one that has none goes along with the first lane's (in bounds, left out of
 // the row's sums and not stored).
+//
+// What dropout has taken out has no part in any gradient, whatever it was: beside a gradient of 0 the gate, and f where no norm takes
+// in its row, count as 0 (1 % of the time: 16384 x 2047 with gate and dropout, both ways, 268 -> 272 us).
 //
 // With s = t act(gate), A = sum s (f - mu) r and B = sum s two sums over rows give three gradients:
 // dscale = w A + b B, dweight = scale A, dbias = scale B.
@@ -632,15 +641,23 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
             if (a.gate) settle8<TAIL>(v.z, at);
             vector(w, w_, a.w, 1.0f);
             vector(scale, scale_, a.scale, 1.0f);
-            if (drops) drop8(d, drop_numbers(key, (uint32_t)row, (uint32_t)col / 8), a.drop);
+            u32x4 numbers;
+            if (drops) {
+                numbers = drop_numbers(key, (uint32_t)row, (uint32_t)col / 8);
+                drop8(d, numbers, a.drop);
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) fh[i] = !normed ? v.f[i] : a.norm == kNormLayer ? (v.f[i] - v.st.x) * v.st.y : v.f[i] * v.st.y;
+            if (drops && !normed) clear8(fh, numbers, a.drop);       // (a norm takes in the whole row)
             if (a.gate) {
-                float dg[8], b[8];
+                float dg[8], b[8], z8[8];
                 vector(b, b_, a.b, 0.0f);
 #pragma unroll
+                for (int i = 0; i < 8; ++i) z8[i] = v.z[i];
+                if (drops) clear8(z8, numbers, a.drop);
+#pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float z = v.z[i], p = d[i] * fmaf(fh[i], w[i], b[i]) * scale[i];
+                    const float z = z8[i], p = d[i] * fmaf(fh[i], w[i], b[i]) * scale[i];
                     dg[i] = p * gate_slope<FAST>(z, a.act);
                     d[i] *= gate_of<FAST>(z, a.act);
                 }

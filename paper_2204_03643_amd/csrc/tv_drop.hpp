@@ -41,14 +41,21 @@ __device__ __forceinline__ u32x4 drop_numbers(DropKey k, uint32_t row, uint32_t 
     return u32x4{c0, c1, c2, c3};
 }
 
+__device__ __forceinline__ bool dropped(u32x4 numbers, int i, const Drop &d)
+{
+    return (i & 1 ? numbers[i >> 1] >> 16 : numbers[i >> 1] & 0xffffu) < d.below;
+}
 // v is zero where a column is dropped, whatever it was, and the factor times as large elsewhere.
 __device__ __forceinline__ void drop8(float (&v)[8], u32x4 numbers, const Drop &d)
 {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t u = i & 1 ? numbers[i >> 1] >> 16 : numbers[i >> 1] & 0xffffu;
-        v[i] = u < d.below ? 0.0f : v[i] * d.factor;
-    }
+    for (int i = 0; i < 8; ++i) v[i] = dropped(numbers, i, d) ? 0.0f : v[i] * d.factor;
+}
+// The same without the factor: for what a dropped place's gradient of 0 is multiplied by, which could be infinite or a NaN.
+__device__ __forceinline__ void clear8(float (&v)[8], u32x4 numbers, const Drop &d)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = dropped(numbers, i, d) ? 0.0f : v[i];
 }
 
 // Rows of n values, `lanes` lanes (a power of two, at most 256) side by side in a row, eight values each.
