@@ -438,6 +438,7 @@ typedef struct {
     int32_t dtype, norm, next_norm, gate_act;
     float eps;
     tv_drop drop;
+    int32_t remake_y;                       /* backward call with f, bf16: see there; 0 or 1 */
 } tv_block_desc;
 
 typedef struct {
@@ -448,7 +449,9 @@ int tv_block_fwd(tv_block_in in, void *y, void *h, float *stats, tv_block_desc d
 
 /*
  * The gradients, from dy and dh (packed; either may be NULL: zero), the forward call's `stats` and, as in.x, its y (rows
- * of ldx elements; x where f is NULL; may be NULL without next_norm), all else as in the forward call:
+ * of ldx elements; x where f is NULL; may be NULL without next_norm), all else as in the forward call.  A y in bf16 was
+ * rounded, h was not made of that: with remake_y in.x is the forward call's x, and y is made again of it, in fp32
+ * (TV_ERR_UNSUPPORTED with f in fp32, whose y is not rounded):
  *
  *   g = dy + next_norm'(dh),  dx = g,  t = d g,  dP = t scale act(gate),  df = norm'(dP)
  *   dscale = sum_i t act(gate) norm(f),  dgate = t scale act'(gate) norm(f), summed over the rows that share it
@@ -456,7 +459,7 @@ int tv_block_fwd(tv_block_in in, void *y, void *h, float *stats, tv_block_desc d
  *
  * A place that dropout took out has no part in any gradient of gate, scale and f: its gate, and without a norm its f, may be
  * infinite or a NaN.  Each output is packed and may be NULL where it is not wanted.  Sums over rows are fp32, in an order that depends on
- * the sizes alone: results do not change from run to run.  m = 0 sets the vectors to zero.  ws: as in tv_linear_bwd.
+ * the sizes and on what is given and wanted alone, as the workspace does: results do not change from run to run.  m = 0 sets the vectors to zero.  ws: as in tv_linear_bwd.
  */
 typedef struct {
     void *dx, *df, *dgate, *dweight, *dbias, *dscale, *dnext_weight, *dnext_bias;

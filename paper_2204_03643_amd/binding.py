@@ -39,7 +39,7 @@ class tv_drop(ctypes.Structure):
 class tv_block_desc(ctypes.Structure):
     _fields_ = [("m", _i64), ("n", _i64), ("ldx", _i64), ("ldf", _i64), ("ldg", _i64), ("gate_div", _i64),
                 ("dtype", ctypes.c_int32), ("norm", ctypes.c_int32), ("next_norm", ctypes.c_int32),
-                ("gate_act", ctypes.c_int32), ("eps", ctypes.c_float), ("drop", tv_drop)]
+                ("gate_act", ctypes.c_int32), ("eps", ctypes.c_float), ("drop", tv_drop), ("remake_y", ctypes.c_int32)]
 
 
 class tv_block_in(ctypes.Structure):

@@ -118,16 +118,21 @@ def _workspace_bytes(m, n, dtype, has_f, has_bias, has_gate, border, want):
 
 
 @functools.lru_cache(maxsize=4096)
-def _desc(m, n, ldx, ldf, ldg, dtype, border):
+def _desc(m, n, ldx, ldf, ldg, dtype, border, remake_y=0):
     return _b.tv_block_desc(m, n, ldx, ldf, ldg, border.gate_div, dtype, border.norm, border.next_norm, border.act, border.eps,
-                            _NO_DROP)
+                            _NO_DROP, remake_y)
 
 
-def _desc_of(m, n, ldx, ldf, ldg, dtype, border, seed, seed_at):
+def _desc_of(m, n, ldx, ldf, ldg, dtype, border, seed, seed_at, remake_y=0):
     if not border.drop:
-        return _desc(m, n, ldx, ldf, ldg, dtype, border)
+        return _desc(m, n, ldx, ldf, ldg, dtype, border, remake_y)
     return _b.tv_block_desc(m, n, ldx, ldf, ldg, border.gate_div, dtype, border.norm, border.next_norm, border.act, border.eps,
-                            _b.tv_drop(seed, border.offset, _address(seed_at), border.drop))
+                            _b.tv_drop(seed, border.offset, _address(seed_at), border.drop), remake_y)
+
+
+def _remakes_y(dtype):
+    """Whether the next norm's gradient makes y again of x and f: where y was rounded when it was returned."""
+    return int(dtype is torch.bfloat16)
 
 
 @_on_device
@@ -157,15 +162,16 @@ def _forward(x, f, weight, bias, gate, scale, next_weight, next_bias, border, se
 
 
 @_on_device
-def _backward(like, dy, dh, y, f, weight, bias, gate, scale, next_weight, stats, border, seed, seed_at, want):
-    """Gradients of x, f, weight, bias, gate, scale, next_weight, next_bias, None where not wanted."""
+def _backward(like, dy, dh, after, f, weight, bias, gate, scale, next_weight, stats, border, seed, seed_at, want):
+    """Gradients of x, f, weight, bias, gate, scale, next_weight, next_bias, None where not wanted.  after: with a next norm y,
+    or x where y is made again."""
     shape, n = like.shape, like.shape[-1]
     m, dtype = like.numel() // n, _DTYPES[like.dtype]
-    at_y = at_gate = None
+    at_after = at_gate = None
     ldx = ldg = n
-    if y is not None:
-        y, ldx = _rows(y)
-        at_y = y.data_ptr()
+    if after is not None:
+        after, ldx = _rows(after)
+        at_after = after.data_ptr()
     f, ldf = _rows(f)
     if gate is not None:
         grows, ldg = _rows(gate)
@@ -173,12 +179,12 @@ def _backward(like, dy, dh, y, f, weight, bias, gate, scale, next_weight, stats,
     shapes = (shape, shape, n, n, None if gate is None else gate.shape, n, n, n)
     made = [like.new_empty(s) if w else None for s, w in zip(shapes, want)]
     dx, df, dweight, dbias, dgate, dscale, dnext_weight, dnext_bias = [None if t is None else t.data_ptr() for t in made]
-    ins = _b.tv_block_in(at_y, f.data_ptr(), _address(weight), _address(bias), at_gate, _address(scale), _address(next_weight), None)
+    ins = _b.tv_block_in(at_after, f.data_ptr(), _address(weight), _address(bias), at_gate, _address(scale), _address(next_weight), None)
     nbytes = _workspace_bytes(m, n, dtype, True, bias is not None, gate is not None, border, want)
     ws = like.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
     _check(_b.lib().tv_block_bwd(_address(dy), _address(dh), ins, _address(stats),
                                  _b.tv_block_grads(dx, df, dgate, dweight, dbias, dscale, dnext_weight, dnext_bias),
-                                 _desc_of(m, n, ldx, ldf, ldg, dtype, border, seed, seed_at), _address(ws), nbytes, _b._stream(None)))
+                                 _desc_of(m, n, ldx, ldf, ldg, dtype, border, seed, seed_at, _remakes_y(like.dtype)), _address(ws), nbytes, _b._stream(None)))
     return made
 
 
@@ -189,8 +195,8 @@ class _BorderFunction(torch.autograd.Function):
             raise NotImplementedError("tv_residual: no forward-mode derivative")
         normed = border.next_norm or border.norm
         y, h, stats = _forward(x, f, weight, bias, gate, scale, next_weight, next_bias, border, seed, seed_at, normed)
-        # the next norm's gradient is taken at y as it was returned
-        saved = (y if border.next_norm else None, f, weight, bias, gate, scale, next_weight, stats, seed_at)
+        after = (x if _remakes_y(x.dtype) else y) if border.next_norm else None
+        saved = (after, f, weight, bias, gate, scale, next_weight, stats, seed_at)
         ctx.save_for_backward(*saved)
         ctx.saved_as = [None if t is None else (t.shape, t.dtype) for t in saved]
         ctx.border, ctx.seed = border, seed
@@ -211,7 +217,7 @@ class _BorderFunction(torch.autograd.Function):
         for t, was in zip(saved, ctx.saved_as):
             if t is not None and (t.dtype is not was[1] or t.shape != was[0] or t.get_device() != like.get_device() or t.is_meta):
                 raise RuntimeError("tv_residual: a hook on saved tensors has brought back one of another shape, type or device")
-        y, f, weight, bias, gate, scale, next_weight, stats, seed_at = saved
+        after, f, weight, bias, gate, scale, next_weight, stats, seed_at = saved
         dy, dh = grads if border.next_norm else (grads[0], None)
         if dy is not None:
             dy = _dense(dy)
@@ -226,7 +232,7 @@ class _BorderFunction(torch.autograd.Function):
             made = [like.new_zeros(s) if w else None for s, w in zip(shapes, need)]
         elif any(want):
             weight, bias, scale, next_weight, stats = [None if t is None else _dense(t) for t in (weight, bias, scale, next_weight, stats)]
-            made = _backward(like, dy, dh, y, f, weight, bias, gate, scale, next_weight, stats, border, ctx.seed, seed_at, want)
+            made = _backward(like, dy, dh, after, f, weight, bias, gate, scale, next_weight, stats, border, ctx.seed, seed_at, want)
         else:
             made = [None] * 8
         if need[0] and dh is None:
@@ -346,7 +352,7 @@ def tv_residual(x: torch.Tensor, f: torch.Tensor, norm: str = "none", weight: to
                 scale: torch.Tensor | None = None, dropout: float = 0.0, seed=None, offset: int = 0, next_norm: str = "none",
                 next_weight: torch.Tensor | None = None, next_bias: torch.Tensor | None = None, eps: float = 1e-6):
     """Differentiable ``y = x + dropout(scale * act(gate) * norm(f))`` over the last axis; with a next norm ``(y, h)``, h the
-    next norm of y (before y is rounded).
+    next norm of y (before y is rounded, in its gradients too: in bfloat16 they take y from x and f again).
 
     x, f [..., n]; norm and next_norm "none", "rms" or "layer" with weights and biases [n] or None (see ``tv_norm``);
     gate of x's shape, or with ones in its last leading axes (one row for all rows that share it), gate_act "none", "sigmoid" or

@@ -17,6 +17,7 @@ struct Block {
     const void *x, *f, *w, *b, *gate, *scale, *nw, *nb;
     int64_t m, ldx, ldf, ldg;
     int32_t n, gate_div, norm, next, act;
+    bool    again;           // backward: y is made again of x and f (bf16)
     float   eps, inv_n;
     Drop    drop;
 };
@@ -43,6 +44,9 @@ template <int LANES> __device__ __forceinline__ float wave_sum(float v)
     }
     return v;
 }
+
+// A value that is the same in all lanes of a wave, out of the vector registers.
+__device__ __forceinline__ float of_wave(float v) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))); }
 
 // Sums over the LANES lanes of a row.  More than a wave: through LDS, in two places in turn, so that one barrier a sum is
 // enough (between the read of a place and its next write lies the barrier of the sum in between).
@@ -84,18 +88,42 @@ template <int LANES> struct RowSum {
     }
 };
 
-// act(z) and, where it is asked for, its slope.
+// act(z).
 template <bool FAST> __device__ __forceinline__ float gate_of(float z, int act)
 {
     if (act == kGateSigmoid) return logistic<FAST>(z);
     if (act == kGateSilu) return z * logistic<FAST>(z);
     return z;
 }
-template <bool FAST> __device__ __forceinline__ float gate_slope(float z, int act)
+// act(z) in place of eight z, which one is asked once for all of them.
+template <bool FAST> __device__ __forceinline__ void gate8(float (&z)[8], int act)
 {
-    if (act == kGatePlain) return 1.0f;
-    const float s = logistic<FAST>(z);
-    return act == kGateSigmoid ? s * (1.0f - s) : s * (1.0f + z * (1.0f - s));
+    if (act == kGateSigmoid)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = logistic<FAST>(z[i]);
+    else if (act == kGateSilu)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] *= logistic<FAST>(z[i]);
+}
+// The same, and the eight values of v times act's slope; four at a time, which takes fewer registers.
+template <bool FAST> __device__ __forceinline__ void gate8(float (&z)[8], float (&v)[8], int act)
+{
+    if (act == kGateSigmoid)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float s = logistic<FAST>(z[i]);
+            v[i] *= s * (1.0f - s);
+            z[i] = s;
+            if (i == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+    else if (act == kGateSilu)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float s = logistic<FAST>(z[i]);
+            v[i] *= s * (1.0f + z[i] * (1.0f - s));
+            z[i] *= s;
+            if (i == 3) __builtin_amdgcn_sched_barrier(0);
+        }
 }
 
 template <class T> __device__ __forceinline__ void load_or(float (&v)[8], const void *p, int col, int have, float otherwise)
@@ -430,71 +458,107 @@ struct BlockGrads {
     }
 };
 
-// One row's gradients.  D: gradient of y on entry of the second half.
-template <class T, bool N>
+// Of eight channels of a row: f normalised and w f^ + b.  Where a column is dropped, the gate and an f that no norm has taken in
+// count as 0.
+template <class T, bool F = true> struct Branch8 {
+    static constexpr bool FAST = sizeof(T) == 2;
+    const Block &a;
+    const bool drops;
+    const u32x4 numbers;
+    const int64_t row;
+    const int col, have;
+    float fh[8], P[8];
+
+    __device__ __forceinline__ Branch8(const Block &block, float4 st, bool d, u32x4 n, int64_t r, int c, int h)
+        : a(block), drops(d), numbers(n), row(r), col(c), have(h)
+    {
+        if constexpr (!F) return;
+        float p[8];
+        get8(fh, (const T *)a.f + row * a.ldf + col, have);
+        if (drops && a.norm == kNormNone) clear8(fh, numbers, a.drop);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) P[i] = fh[i];
+        if (a.norm != kNormNone) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) P[i] = fh[i] = i < have ? (fh[i] - st.x) * st.y : 0.0f;
+            if (a.w) {
+                get8(p, (const T *)a.w + col, have);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) P[i] *= p[i];
+            }
+            if (a.b) {
+                get8(p, (const T *)a.b + col, have);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) P[i] += p[i];
+            }
+        }
+    }
+    __device__ __forceinline__ void gates(float (&z)[8]) const
+    {
+        get8(z, (const T *)a.gate + (int64_t)((uint32_t)row / (uint32_t)a.gate_div) * a.ldg + col, have);
+        if (drops) clear8(z, numbers, a.drop);
+    }
+    // y += what the forward call added to x
+    __device__ __forceinline__ void add_to(float (&y)[8]) const
+    {
+        float f[8], p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = P[i];
+        if (a.gate) {
+            gates(p);
+            gate8<FAST>(p, a.act);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] *= p[i];
+        }
+        if (a.scale) {
+            get8(p, (const T *)a.scale + col, have);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] *= p[i];
+        }
+        if (drops) drop8(f, numbers, a.drop);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] += f[i];
+    }
+    // From the gradient d of y: dP, and what goes to dscale and dgate.
+    __device__ __forceinline__ void terms(float (&d)[8], float (&dscale)[8], float (&dgate)[8]) const
+    {
+        float s[8];
+        if (drops) drop8(d, numbers, a.drop);
+        load_or<T>(s, a.scale, col, have, 1.0f);
+        if (a.gate) {
+            float z[8];
+            gates(z);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dgate[i] = d[i] * s[i] * P[i];
+            gate8<FAST>(z, dgate, a.act);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] *= z[i];
+        } else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dgate[i] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            dscale[i] = d[i] * P[i];
+            d[i] *= s[i];
+        }
+    }
+};
+
+// The next norm's part in a row's gradients: t = dh w, y normalised, g = dh.  add: of y from x, where that is to be done.
+template <class T, bool F, class Add>
 __device__ __forceinline__ void next_norm_terms(float (&t)[8], float (&yh)[8], float (&g)[8], const Block &a, const BlockGrads &o,
-                                                float4 st, int64_t row, int col, int have)
+                                                float4 st, int64_t row, int col, int have, Add add)
 {
     float p[8];
     get8(g, (const T *)o.dh + row * a.n + col, have);
     get8(yh, (const T *)a.x + row * a.ldx + col, have);
+    if constexpr (F && sizeof(T) == 2)
+        if (a.again) add(yh);
     load_or<T>(p, a.nw, col, have, 1.0f);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         yh[i] = (yh[i] - st.z) * st.w;
         t[i] = g[i] * p[i];
-    }
-}
-
-// From the gradient d of y: dP, the normalised f, and what goes to dscale and dgate, each for eight channels.
-template <class T>
-__device__ __forceinline__ void branch_terms(float (&d)[8], float (&fh)[8], float (&dscale)[8], float (&dgate)[8], const Block &a,
-                                             float4 st, bool drops, DropKey key, int64_t row, int col, int have)
-{
-    constexpr bool FAST = sizeof(T) == 2;
-    float p[8], P[8];
-    u32x4 numbers;
-    get8(fh, (const T *)a.f + row * a.ldf + col, have);
-    if (drops) {
-        numbers = drop_numbers(key, (uint32_t)row, (uint32_t)col / 8);
-        drop8(d, numbers, a.drop);
-        if (a.norm == kNormNone) clear8(fh, numbers, a.drop);        // (a norm takes in the whole row)
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) P[i] = fh[i];
-    if (a.norm != kNormNone) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) P[i] = fh[i] = i < have ? (fh[i] - st.x) * st.y : 0.0f;
-        if (a.w) {
-            get8(p, (const T *)a.w + col, have);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) P[i] *= p[i];
-        }
-        if (a.b) {
-            get8(p, (const T *)a.b + col, have);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) P[i] += p[i];
-        }
-    }
-    load_or<T>(p, a.scale, col, have, 1.0f);
-    if (a.gate) {
-        float z[8];
-        get8(z, (const T *)a.gate + (int64_t)((uint32_t)row / (uint32_t)a.gate_div) * a.ldg + col, have);
-        if (drops) clear8(z, numbers, a.drop);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float G = gate_of<FAST>(z[i], a.act), q = d[i] * p[i];
-            dscale[i] = d[i] * G * P[i];
-            dgate[i] = q * P[i] * gate_slope<FAST>(z[i], a.act);
-            d[i] = q * G;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            dscale[i] = d[i] * P[i];
-            dgate[i] = 0.0f;
-            d[i] *= p[i];
-        }
     }
 }
 
@@ -505,8 +569,16 @@ __device__ __forceinline__ void branch_terms(float (&d)[8], float (&fh)[8], floa
 // of eight: a lane has eight or none, and one that has none goes along with the first lane's (in bounds, left out of
 // the row's sums and not stored).
 //
+// y in bf16 was rounded, and h is not made of that: y is made again of x and f, the same bytes and a tenth more instructions
+// (16384 x 2048 with gate and dropout, forward and gradients, 149 -> 152 us, 4096 x 8192 with norms and scale 168 -> 177; the
+// gradients of the next norm are off by bf16's rounding of themselves, 1.7e-3 of their norm, where a rounded y makes that 2.3e-3, and
+// anything where y's mean is large beside what a layer norm is made of).
+//
 // What dropout has taken out has no part in any gradient, whatever it was: beside a gradient of 0 the gate, and f where no norm takes
-// in its row, count as 0 (1 % of the time: 16384 x 2047 with gate and dropout, both ways, 268 -> 272 us).
+// in its row, count as 0 (1 % of the time).
+//
+// Which norm and gate is asked once for a row's eight channels, not for each (4096 x 4096 in f32 with layer norms, a sigmoid gate and
+// dropout, both ways, 195 -> 175 us); what is the same in all lanes of a wave lies in scalar registers.
 //
 // With s = t act(gate), A = sum s (f - mu) r and B = sum s two sums over rows give three gradients:
 // dscale = w A + b B, dweight = scale A, dbias = scale B.
@@ -517,7 +589,7 @@ __device__ __forceinline__ void branch_terms(float (&d)[8], float (&fh)[8], floa
 template <class T, int LANES, bool F, bool N, bool TAIL, int SLOTS>
 __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Block a, BlockGrads o)
 {
-    constexpr bool FAST = sizeof(T) == 2, WIDE = SLOTS > 0, AHEAD = !WIDE || sizeof(T) == 2;
+    constexpr bool FAST = sizeof(T) == 2, WIDE = SLOTS > 0, AHEAD = !WIDE || sizeof(T) == 2, AGAIN = F && N && sizeof(T) == 2;
     __shared__ float2 lds[2][RowSum<LANES>::kWaves];
     __shared__ f32x4 slots[WIDE ? SLOTS : 1][2][WIDE ? LANES : 1];
     RowSum<LANES> sum(lds);
@@ -534,20 +606,28 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
     const bool own_gates = F && o.dgate && a.gate_div == 1, whole_gates = F && o.dgate && a.gate_div > 1 && o.units.cuts == 1;
     const DropKey key = drops ? drop_key(a.drop) : DropKey{};
 
-    // the vectors: once, or where they are used
+    // the vectors: once, or where they are used; of the branch, w and b times scale and what dropout multiplies by
     constexpr int kOnce = WIDE ? 1 : 8;
-    float nw_[kOnce], w_[kOnce], b_[kOnce], scale_[kOnce];
+    const float factor = drops ? a.drop.factor : 1.0f;
+    float nw_[kOnce], ws_[kOnce], bs_[kOnce];
+    auto scaled = [&](float (&ws)[8], float (&bs)[8]) __attribute__((always_inline)) {
+        float s[8];
+        vector8<TAIL, T>(s, a.scale, at, 1.0f);
+        vector8<TAIL, T>(ws, a.w, at, 1.0f);
+        vector8<TAIL, T>(bs, a.b, at, 0.0f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            s[i] *= factor;
+            ws[i] *= s[i];
+            if (a.b) bs[i] *= s[i];
+        }
+    };
     if constexpr (!WIDE) {
         if constexpr (N) vector8<TAIL, T>(nw_, a.nw, at, 1.0f);
-        if constexpr (F) {
-            vector8<TAIL, T>(w_, a.w, at, 1.0f);
-            vector8<TAIL, T>(b_, a.b, at, 0.0f);
-            vector8<TAIL, T>(scale_, a.scale, at, 1.0f);
-        }
+        if constexpr (F) scaled(ws_, bs_);
     }
-    auto vector = [&](float (&v)[8], const float (&once)[kOnce], const void *p, float otherwise) __attribute__((always_inline)) {
-        if constexpr (WIDE) vector8<TAIL, T>(v, p, at, otherwise);
-        else
+    auto kept_or = [&](float (&v)[8], const float (&once)[kOnce]) __attribute__((always_inline)) {
+        if constexpr (!WIDE)
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = once[i];
     };
@@ -607,18 +687,64 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
             v = ahead;
             if (row + 1 < end) ahead = fetch(row + 1);
         } else v = fetch(row);
+        if constexpr (LANES >= 64) v.st = float4{of_wave(v.st.x), of_wave(v.st.y), of_wave(v.st.z), of_wave(v.st.w)};
         if (o.dy) settle8<TAIL>(v.dy, at);
         float d[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) d[i] = o.dy ? v.dy[i] : 0.0f;
+        // f normalised, w scale times dropout's factor, and d scale (w f^ + b), d dropout's factor or 0
+        float fh[8], ws[8], e[8];
+        const float mu = normed && a.norm == kNormLayer ? v.st.x : 0.0f, r = normed ? v.st.y : 1.0f;
+        u32x4 numbers;
+        auto branch = [&](bool whole) __attribute__((always_inline)) {
+            float bs[8];
+            if constexpr (WIDE) scaled(ws, bs);
+            kept_or(ws, ws_);
+            kept_or(bs, bs_);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) fh[i] = (v.f[i] - mu) * r;
+            if (drops && !normed) clear8(fh, numbers, a.drop);       // (a norm takes in the whole row)
+            if (whole) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[i] = fmaf(fh[i], ws[i], bs[i]);
+                if (drops) clear8(e, numbers, a.drop);
+            }
+        };
+        auto gates = [&](float (&z)[8]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = v.z[i];
+            if (drops) clear8(z, numbers, a.drop);
+        };
+        if constexpr (F) {
+            if (drops) numbers = drop_numbers(key, (uint32_t)row, (uint32_t)col / 8);
+            settle8<TAIL>(v.f, at);
+            if (a.gate) settle8<TAIL>(v.z, at);
+            if constexpr (AGAIN) branch(a.gate || (next && a.again));
+        }
         if (next) {
             float t[8], yh[8], s1 = 0.0f, s2 = 0.0f;
             settle8<TAIL>(v.dh, at);
             settle8<TAIL>(v.y, at);
-            vector(t, nw_, a.nw, 1.0f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) yh[i] = v.y[i];
+            if constexpr (AGAIN)
+                if (a.again) {
+                    if (a.gate) {
+                        float z[8];
+                        gates(z);
+                        gate8<FAST>(z, a.act);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) yh[i] = fmaf(e[i], z[i], yh[i]);
+                    } else
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) yh[i] += e[i];
+                }
+            if constexpr (WIDE) vector8<TAIL, T>(t, a.nw, at, 1.0f);
+            kept_or(t, nw_);
+            const float next_mu = a.next == kNormLayer ? v.st.z : 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                yh[i] = a.next == kNormLayer ? (v.y[i] - v.st.z) * v.st.w : v.y[i] * v.st.w;
+                yh[i] = (yh[i] - next_mu) * v.st.w;
                 t[i] *= v.dh[i];
                 s1 += t[i];
                 s2 = fmaf(t[i], yh[i], s2);
@@ -636,31 +762,17 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
         }
         if (o.dx && live) store8((T *)o.dx + row * a.n + col, d, have);
         if constexpr (F) {
-            float fh[8], w[8], scale[8], s1 = 0.0f, s2 = 0.0f;
-            settle8<TAIL>(v.f, at);
-            if (a.gate) settle8<TAIL>(v.z, at);
-            vector(w, w_, a.w, 1.0f);
-            vector(scale, scale_, a.scale, 1.0f);
-            u32x4 numbers;
-            if (drops) {
-                numbers = drop_numbers(key, (uint32_t)row, (uint32_t)col / 8);
-                drop8(d, numbers, a.drop);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) fh[i] = !normed ? v.f[i] : a.norm == kNormLayer ? (v.f[i] - v.st.x) * v.st.y : v.f[i] * v.st.y;
-            if (drops && !normed) clear8(fh, numbers, a.drop);       // (a norm takes in the whole row)
+            float s1 = 0.0f, s2 = 0.0f;
+            if constexpr (!AGAIN || WIDE) branch(a.gate);   // (wide: once more, in place of registers that there are not)
+            if (drops) clear8(d, numbers, a.drop);
             if (a.gate) {
-                float dg[8], b[8], z8[8];
-                vector(b, b_, a.b, 0.0f);
+                float dg[8], z[8];
+                gates(z);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) z8[i] = v.z[i];
-                if (drops) clear8(z8, numbers, a.drop);
+                for (int i = 0; i < 8; ++i) dg[i] = d[i] * e[i];
+                gate8<FAST>(z, dg, a.act);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float z = z8[i], p = d[i] * fmaf(fh[i], w[i], b[i]) * scale[i];
-                    dg[i] = p * gate_slope<FAST>(z, a.act);
-                    d[i] *= gate_of<FAST>(z, a.act);
-                }
+                for (int i = 0; i < 8; ++i) d[i] *= z[i];
                 sum_of(kSumGate, [&](int i, float s) __attribute__((always_inline)) { return s + dg[i]; });
                 if (own_gates && live) store8((T *)o.dgate + row * a.n + col, dg, have);
                 if (whole_gates && ((uint32_t)row + 1) % (uint32_t)a.gate_div == 0) {
@@ -672,11 +784,10 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
             sum_of(kSumA, [&](int i, float s) __attribute__((always_inline)) { return fmaf(d[i], fh[i], s); });
             sum_of(kSumB, [&](int i, float s) __attribute__((always_inline)) { return s + d[i]; });
 #pragma unroll
-            for (int i = 0; i < 8; ++i) d[i] *= scale[i];
+            for (int i = 0; i < 8; ++i) d[i] *= ws[i];
             if (normed) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    d[i] *= w[i];
                     s1 += d[i];
                     s2 = fmaf(d[i], fh[i], s2);
                 }
@@ -705,9 +816,11 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Bloc
         float A[8], B[8], w[8], b[8], scale[8];
         joined(kSumA, A);
         joined(kSumB, B);
-        vector(w, w_, a.w, 1.0f);
-        vector(b, b_, a.b, 0.0f);
-        vector(scale, scale_, a.scale, 1.0f);
+        vector8<TAIL, T>(w, a.w, at, 1.0f);
+        vector8<TAIL, T>(b, a.b, at, 0.0f);
+        vector8<TAIL, T>(scale, a.scale, at, 1.0f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) A[i] *= factor, B[i] *= factor;
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = scale[i] * A[i];
         leave(kDw, v);
@@ -745,8 +858,10 @@ __global__ __launch_bounds__(LANES) void block_rows_kernel(Block a, BlockGrads o
     for (int64_t row = blockIdx.x; row < a.m; row += gridDim.x) {
         const float4 st = (N || F) && o.stats ? o.stats[row] : float4{0.0f, 1.0f, 0.0f, 1.0f};
         float d[V][8];
+        u32x4 numbers[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) {
+            numbers[j] = drops ? drop_numbers(key, (uint32_t)row, (uint32_t)col[j] / 8) : u32x4{0, 0, 0, 0};
             if (o.dy) get8(d[j], (const T *)o.dy + row * a.n + col[j], have[j]);
             else
 #pragma unroll
@@ -757,7 +872,9 @@ __global__ __launch_bounds__(LANES) void block_rows_kernel(Block a, BlockGrads o
                 float t[V][8], yh[V][8], g[8], s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    next_norm_terms<T, N>(t[j], yh[j], g, a, o, st, row, col[j], have[j]);
+                    next_norm_terms<T, F>(t[j], yh[j], g, a, o, st, row, col[j], have[j], [&](float (&y)[8]) __attribute__((always_inline)) {
+                        Branch8<T>(a, st, drops, numbers[j], row, col[j], have[j]).add_to(y);
+                    });
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         s1 += t[j][i];
@@ -782,7 +899,11 @@ __global__ __launch_bounds__(LANES) void block_rows_kernel(Block a, BlockGrads o
             float fh[V][8], dscale[8], dgate[8], s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                branch_terms<T>(d[j], fh[j], dscale, dgate, a, st, drops, key, row, col[j], have[j]);
+                // (once more, in place of registers that there are not)
+                const Branch8<T> branch(a, st, drops, numbers[j], row, col[j], have[j]);
+                branch.terms(d[j], dscale, dgate);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) fh[j][i] = branch.fh[i];
                 if (o.dgate && a.gate_div == 1) store8((T *)o.dgate + row * a.n + col[j], dgate, have[j]);
                 if (a.norm != kNormNone) {
                     float p[8];
@@ -829,6 +950,8 @@ __global__ __launch_bounds__(256) void block_sums_kernel(Block a, BlockGrads o)
         for (int i = 0; i < 8; ++i) acc[k][i] = 0.0f;
     for (; row < end; ++row) {
         const float4 st = o.stats ? o.stats[row] : float4{0.0f, 1.0f, 0.0f, 1.0f};
+        const u32x4 numbers = drops ? drop_numbers(key, (uint32_t)row, (uint32_t)col / 8) : u32x4{0, 0, 0, 0};
+        const Branch8<T, F> branch(a, st, drops, numbers, row, col, have);
         float d[8];
         if (o.dy) get8(d, (const T *)o.dy + row * a.n + col, have);
         else
@@ -837,7 +960,8 @@ __global__ __launch_bounds__(256) void block_sums_kernel(Block a, BlockGrads o)
         if constexpr (N)
             if (o.dh) {
                 float t[8], yh[8], g[8];
-                next_norm_terms<T, N>(t, yh, g, a, o, st, row, col, have);
+                next_norm_terms<T, F>(t, yh, g, a, o, st, row, col, have,
+                                      [&](float (&y)[8]) __attribute__((always_inline)) { branch.add_to(y); });
                 const float2 c = o.row_sums[row];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -847,13 +971,13 @@ __global__ __launch_bounds__(256) void block_sums_kernel(Block a, BlockGrads o)
                 }
             }
         if constexpr (F) {
-            float fh[8], dscale[8], dgate[8];
-            branch_terms<T>(d, fh, dscale, dgate, a, st, drops, key, row, col, have);
+            float dscale[8], dgate[8];
+            branch.terms(d, dscale, dgate);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 acc[kDscale][i] += dscale[i];
                 acc[kVectors][i] += dgate[i];
-                acc[kDw][i] = fmaf(d[i], fh[i], acc[kDw][i]);
+                acc[kDw][i] = fmaf(d[i], branch.fh[i], acc[kDw][i]);
                 acc[kDb][i] += d[i];
             }
             if (o.dgate && a.gate_div > 1 && o.units.cuts == 1 && ((uint32_t)row + 1) % (uint32_t)a.gate_div == 0) {

@@ -33,6 +33,7 @@ int check_sizes(const tv_block_in &in, const tv_block_desc &d)
         if (d.norm < TV_NORM_NONE || d.norm > TV_NORM_LAYER || d.gate_act < TV_GATE_PLAIN || d.gate_act > TV_GATE_SILU) return TV_ERR_UNSUPPORTED;
         if (d.ldf < d.n || d.ldf >= kMostStride) return TV_ERR_STRIDE;
         if (in.gate && (d.ldg < d.n || d.ldg >= kMostStride)) return TV_ERR_STRIDE;
+        if (d.remake_y && (d.remake_y != 1 || d.dtype != TV_BF16)) return TV_ERR_UNSUPPORTED;
         return check_drop(d.drop);
     }
     return TV_OK;
@@ -65,6 +66,7 @@ Block block_of(const tv_block_in &in, const tv_block_desc &d)
         a.ldf = d.ldf;
         if (in.gate) a.ldg = d.ldg, a.gate_div = (int32_t)d.gate_div;
         a.norm = d.norm; a.act = d.gate_act;
+        a.again = d.remake_y != 0;
         a.drop = drop_of(d.drop);
     }
     return a;

@@ -190,3 +190,14 @@ def test_workspaces_are_as_large_as_the_call_asks_for(n, has_bias, monkeypatch):
             block._backward.__wrapped__(x, x, x if after else None, x if after else None, x, v, bias, gate, v, v if after else None, stats, border, 0,
                                         None, want)
     assert len(asked) == (320 if has_bias else 160) and [a for a in asked if a[0] != a[1]] == []
+
+
+def test_remaking_y_is_for_sums_that_were_rounded():
+    def d(**more):
+        r = desc(**more)
+        r.remake_y = remake
+        return r
+    for remake, status in ((1, OK), (2, UNSUPPORTED), (-1, UNSUPPORTED)):
+        assert bwd(d(m=0, dtype=tv.TV_BF16)) == status
+        assert bwd(d(m=0, dtype=tv.TV_BF16), ins(f=None)) == OK      # (in.x is x in either case)
+        assert bwd(d(m=0)) == UNSUPPORTED and fwd(d(m=0)) == UNSUPPORTED

@@ -1,0 +1,76 @@
+"""The next norm's gradients are those of the y that it was made of, not of y as it was rounded."""
+import blockref
+import pytest
+import torch
+from test_gpu_block import NAMES, made, run, wide
+
+pytestmark = pytest.mark.gpu
+
+
+def exact(t, **how):
+    """blockref's values and bounds of a border in f32 (its allowance for a rounded y is then f32's), rounded to bf16."""
+    ref = wide(t)
+    want = blockref.border(torch.float32, **{k: ref[k] for k in ("x", "f", "dy", "dh") + NAMES}, **how)
+    u = blockref.unit(torch.bfloat16)
+    return {k: (v, e * (1 + u) + u * v.abs()) for k, (v, e) in want.items()}
+
+
+@pytest.mark.parametrize("m,n,gate,p,norm,next_norm", [
+    (9, 200, 0, 0.0, "none", "layer"), (12, 201, 3, 0.2, "rms", "rms"), (40, 2048, 4, 0.1, "layer", "layer"), (3, 1, 0, 0.0, "none", "rms"),
+    (5, 4096, 0, 0.3, "none", "rms"), (30, 5000, 5, 0.1, "rms", "layer"), (20, 8191, 0, 0.1, "layer", "layer"), (6, 4104, 2, 0.0, "layer", "layer"),
+    (7, 9000, 0, 0.2, "rms", "layer"), (8, 16384, 4, 0.0, "layer", "rms"), (6, 8200, 6, 0.1, "none", "layer")])
+def test_gradients_of_the_sum_before_it_is_rounded(m, n, gate, p, norm, next_norm):
+    dtype = torch.bfloat16
+    t = made(m, n, dtype, m * n, norm, next_norm, True, gate, True)
+    how = dict(norm=norm, next_norm=next_norm)
+    got = run(t, (gate or 1, m // (gate or 1), n), (gate, 1, n), dropout=p, seed=3, **how)
+    want = exact(t, p=p, seed=3, **how)
+    for k, v in got.items():
+        blockref.within(v, want[k], k)
+
+
+def test_a_sum_whose_steps_are_larger_than_what_is_added():
+    """y near 128 has steps of 1: rounded, it would have lost f, of which the norm is made."""
+    from paper_2204_03643_amd.block import tv_residual
+    gen = torch.Generator().manual_seed(5)
+    m, n = 64, 512
+    f, dh = (torch.randn(m, n, generator=gen).bfloat16() for _ in range(2))
+    x = torch.full((m, n), 128.0).bfloat16()
+    w = torch.ones(n).bfloat16()
+    leaves = [v.cuda().requires_grad_() for v in (x, f * 0.125, w)]
+    y, h = tv_residual(leaves[0], leaves[1], next_norm="layer", next_weight=leaves[2])
+    got = torch.autograd.grad(h, leaves, dh.cuda())
+    v = [a.detach().double().cpu().requires_grad_() for a in leaves]
+    s = v[0] + v[1]
+    want = torch.autograd.grad(torch.nn.functional.layer_norm(s, (n,), v[2], None, 1e-6), v, dh.double())
+    assert float((y.detach().double().cpu() - s.detach()).abs().max()) > 0.2
+    # each is rounded to bf16, 2^-8 of itself at most.  A mean of 512 values near 128 (8 in a lane, 6 steps over a wave) is off by
+    # 16 2^-24 128 at most, 1e-3 of f's deviation of 1/8, which all of a row's normalised values share; a sum x + f by a sixteenth of that
+    for a, b in zip(got, want):
+        off = (a.double().cpu() - b).norm() / b.norm()
+        assert off <= 2.0 ** -8 + 2e-3, float(off)
+
+
+@pytest.mark.parametrize("m,n", [(6, 200), (9, 2047), (5, 4104), (4, 9000)])
+def test_the_library_takes_either(m, n):
+    """tv_block_bwd with y as it was returned, and with x of which it makes y again."""
+    import paper_2204_03643_amd as tv
+    dtype = torch.bfloat16
+    t = made(m, n, dtype, n, "layer", "layer", False, 0, False)
+    c = {k: v.cuda() for k, v in t.items() if v is not None}
+    y, h, dx, df = (torch.empty_like(c["x"]) for _ in range(4))
+    stats = torch.empty(m, 4, device="cuda")
+    ref = wide(t)
+    for remake in (0, 1):
+        d = tv.tv_block_desc(m, n, n, n, n, 1, tv.TV_BF16, tv.TV_NORM_LAYER, tv.TV_NORM_LAYER, tv.TV_GATE_PLAIN, 1e-6, tv.tv_drop(0, 0, None, 0), remake)
+
+        def ins(x):
+            return tv.tv_block_in(x.data_ptr(), c["f"].data_ptr(), c["weight"].data_ptr(), None, None, None, c["next_weight"].data_ptr(), None)
+        grads = tv.tv_block_grads(dx.data_ptr(), df.data_ptr(), None, None, None, None, None, None)
+        tv.tv_block_fwd(ins(c["x"]), y, h, stats, d)
+        assert tv.tv_block_bwd_workspace_bytes(ins(y), grads, d) == 0
+        tv.tv_block_bwd(c["dy"], c["dh"], ins(c["x"] if remake else y), stats, grads, d)
+        how = dict(norm="layer", next_norm="layer")
+        want = exact(t, **how) if remake else blockref.border(dtype, **{k: ref[k] for k in ("x", "f", "dy", "dh") + NAMES}, **how)
+        for k, v in (("y", y), ("h", h), ("dx", dx), ("df", df)):
+            blockref.within(v, want[k], k)
