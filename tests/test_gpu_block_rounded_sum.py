@@ -74,3 +74,24 @@ def test_the_library_takes_either(m, n):
         want = exact(t, **how) if remake else blockref.border(dtype, **{k: ref[k] for k in ("x", "f", "dy", "dh") + NAMES}, **how)
         for k, v in (("y", y), ("h", h), ("dx", dx), ("df", df)):
             blockref.within(v, want[k], k)
+
+
+def test_what_is_changed_in_place_afterwards():
+    """In bfloat16 the sum may be changed (its gradients are made of x and f); x and f may not, and that is noticed."""
+    from paper_2204_03643_amd.block import tv_residual
+    x, f, dh = (torch.randn(4, 40, device="cuda").bfloat16() for _ in range(3))
+
+    def call():
+        leaves = [x.clone().requires_grad_(), f.clone().requires_grad_()]
+        parts = [leaf * 1 for leaf in leaves]
+        return leaves, parts, tv_residual(*parts, next_norm="rms")
+    leaves, _, (y, h) = call()
+    want = torch.autograd.grad(h, leaves, dh)
+    leaves, _, (y, h) = call()
+    y.mul_(3)
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(h, leaves, dh), want))
+    for which in (0, 1):
+        leaves, parts, (y, h) = call()
+        parts[which].mul_(2)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            torch.autograd.grad(h, leaves, dh)
