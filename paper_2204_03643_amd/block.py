@@ -5,6 +5,9 @@ on request, the norm before the next block of the sum; one pass over the rows ea
 (``tv_block_fwd`` / ``tv_block_bwd`` of ``include/tvprox.h``).  ``tv_dropout`` takes its numbers from a counter-based
 generator: no mask is stored, and the same seed and offset always mean the same mask.  ``TVNorm`` and ``TVResidual`` are the
 modules.  float32 and bfloat16, CUDA tensors only: there is no CPU path.
+
+A step that is captured into a graph starts from leaves of which no eager step's graph is alive any more: torch's engine would
+otherwise wait for the eager step's stream within the capture.
 """
 from __future__ import annotations
 

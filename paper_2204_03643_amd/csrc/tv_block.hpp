@@ -3,7 +3,7 @@
 // Reads and writes are all there is to it: a row is read once, its statistics are taken of what the lanes hold, and what
 // follows from them is written.  Lanes side by side in a row hold eight neighbouring channels each.  In bf16, microseconds
 // (GB/s read + written): norm of 8192 x 2048 12.7 (5300), its gradients 19.3 (5200) and the join of the weight's 4.8; border of 16384 x 2048
-// with norms, a gate a sequence, scale and dropout 53.6 (5000), its gradients 86 (4700) and the join 7.1.
+// with norms, a gate a sequence, scale and dropout 52 (5100), its gradients 92 (4400) and the join 7.1.
 #pragma once
 #include "tv_block_plan.hpp"
 #include "tv_drop.hpp"
@@ -583,9 +583,9 @@ __device__ __forceinline__ void next_norm_terms(float (&t)[8], float (&yh)[8], f
 // With s = t act(gate), A = sum s (f - mu) r and B = sum s two sums over rows give three gradients:
 // dscale = w A + b B, dweight = scale A, dbias = scale B.
 //
-// Three waves to a SIMD, as the registers allow: 768 workgroups of 256 lanes (16384 x 2048: 86 us; 1024 workgroups without the
+// Three waves to a SIMD, as the registers allow: 768 workgroups of 256 lanes (16384 x 2048: 92 us; 1024 workgroups without the
 // next row on its way, a third of them in a second round, masks at every value and sums by LDS permutes: 220).  4096 rows of 8192
-// channels 99 us, with the sums in LDS; 260 in two passes.
+// channels 107 us, with the sums in LDS; 260 and more in two passes.
 template <class T, int LANES, bool F, bool N, bool TAIL, int SLOTS>
 __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void block_bwd_kernel(Block a, BlockGrads o)
 {

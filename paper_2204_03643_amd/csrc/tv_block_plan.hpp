@@ -90,7 +90,7 @@ inline BlockBwdPlan block_bwd_plan(const tv_block_in &in, const tv_block_grads &
     p.bytes = p.row_sums;
     if (block_lanes(d.n) > kMostSumLanes) {
         // Sums in LDS where its slots are enough: up to 8192 channels, and all but both norms' biases beside a shared gate
-        // (4096 rows of 8192 bf16 channels, two norms and a scale: 99 us, and 260 in two passes).
+        // (4096 rows of 8192 bf16 channels, two norms and a scale: 107 us, and more than 260 in two passes).
         const bool bias = in.bias && d.norm != TV_NORM_NONE;
         const bool made[kSums] = {in.f && (g.dweight || g.dscale), in.f && (g.dbias || (g.dscale && bias)), g.dnext_weight != nullptr,
                                   g.dnext_bias != nullptr, shared};

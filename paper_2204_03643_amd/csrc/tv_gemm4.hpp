@@ -8,7 +8,8 @@
 // bytes come out of L2 at 10 TB/s, whose channels are busy for 0.70 of the cycles, the matrix units for 0.55, at the 1.8 GHz that a full
 // card keeps (64 workgroups on an otherwise idle card: 0.77 us a step).  Smaller tiles read more: 128 x 256 on two workgroups
 // a compute unit, whose epilogues run behind each other's products, took 305 us for 8192 x 8192 -> 8192 in place of 257, and 98
-// in place of 92 for 8192 x 2048 -> 8192.  Of those 92, 26 are the outputs' bytes; gelu adds 20.  Four waves of 128 x 128, four buffers of
+// in place of 92 for 8192 x 2048 -> 8192.  Of those 92, 26 are the outputs' bytes; gelu adds 28, and outputs in f32 24 (with
+// gelu 63).  Four waves of 128 x 128, four buffers of
 // half a step and streaming stores changed times by -3 to +5 %.
 #pragma once
 #include "tv_gemm16.hpp"

@@ -82,8 +82,10 @@ int linear4(const void *x, const uint8_t *x_exps, const uint8_t *w, const uint8_
     if (p.c.kind == kTile64x4) launch_tiles<T, 64, 128, 2, 2, 4, 2>(g, s, e, stream);
     if (p.c.kind == kFew4) {
         const Rows4 rows{g.a, s.x, d.ldx, s.x_rows, (int32_t)d.k};
-        // so many columns a workgroup as leave one for each compute unit (one row of 4096: -> 4096 5.7, 6.2 and 7.7 us with
-        // 16, 32 and 64; 2048 -> 8192 6.2, 5.1 and 5.7; 4096 -> 16384 15.5, 10.9 and 8.6)
+        // The fewest columns a workgroup with which no compute unit has two of them, 64 at most.  One row of 4096 in bf16 with 16, 32
+        // and 64, us in a graph: -> 4096 5.3, 5.6, 7.5; 4104 6.9, 5.5, 7.4; 8192 7.6, 5.6, 7.6; 8200 9.3, 8.0, 7.7; 16384 13.7, 9.5,
+        // 7.9.  With codes there is nothing of x to share, and the same rule loses at most 2: 4104 4.2, 4.7, 6.4; 8200 5.5, 6.0,
+        // 7.4; 16384 8.5, 7.5, 7.9; 32 rows of them 7.5, 6.3, 8.4; 10.4, 9.2, 9.2; 14.5, 10.5, 9.5.
         if (d.n > 8192) launch_few<T, 4>(g, rows, p.c.own, s, e, stream);
         else if (d.n > 4096) launch_few<T, 2>(g, rows, p.c.own, s, e, stream);
         else launch_few<T, 1>(g, rows, p.c.own, s, e, stream);
